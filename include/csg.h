@@ -56,7 +56,8 @@ typedef enum {
     CSG_ERR_STATE = 6         /* call not allowed in the object's current state */
 } csg_status;
 
-typedef enum { CSG_BF16 = 0, CSG_F32 = 1 } csg_dtype;
+/* CSG_F16 (IEEE binary16 bit patterns): attention over documents and over a cache only. */
+typedef enum { CSG_BF16 = 0, CSG_F32 = 1, CSG_F16 = 2 } csg_dtype;
 
 typedef enum {
     CSG_AG_GEMM = 0,        /* AllGather(A) + GEMM: tiles consume arriving A row chunks */
@@ -477,6 +478,125 @@ csg_status csg_attn_plan_create(int32_t n_heads, int32_t n_kv_heads, int32_t hea
 csg_status csg_ring_attn(csg_plan* p, const void* q, void* k_landing, void* v_landing,
                          const void* k_staging, const void* v_staging, void* o, void* lse,
                          csg_mode mode, void* compute_stream, void* copy_stream);
+
+/* ---- attention over packed documents, its gradient, and over a paged cache ---------
+ *
+ * One definition of a score for all of them: for query row i of head h and key j of the
+ * same document or sequence (key/value head h / (n_heads / n_kv_heads)),
+ *   s = scale q_i . k_j;  softcap c > 0: s = c tanh(s / c);  slopes: s -= slopes[h] |p_i - j|
+ * with p_i the key that row i stands at: rows are the last ones of their document or
+ * sequence (p_i = i + keys - rows). The output is sum_j exp(s_ij - lse_i) v_j over the keys
+ * that row i sees, lse_i = log sum_j exp(s_ij), natural logarithm; a row that sees none has
+ * output 0 and lse -inf. Partial results over disjoint keys (ring attention's among them)
+ * join by their lse.
+ *
+ * These calls own nothing: no plan, no allocation, no host wait, and no copy. They queue
+ * their kernels on `stream` (a hipStream_t of `device`; the device current before is
+ * restored), so they may be captured into a graph. Lengths, document bounds, page tables
+ * and slopes are device arrays that the kernels read, so that a replayed graph follows
+ * them. Calls on different streams may overlap unless they share a workspace or write
+ * what the other reads: two graphs that may run at once need a workspace each.
+ * dtype is CSG_BF16 or CSG_F16, head_dim 64 or 128, n_heads a multiple of n_kv_heads.
+ * Buffers are 16-byte aligned. Tensors of heads are rows of n_heads (n_kv_heads) heads of
+ * head_dim elements; a stride is the number of elements between rows (0 = dense), a
+ * multiple of 8 and at most 2^23, so that q, k and v may be parts of one projection's
+ * output. Statistics and sums are fp32; weights are rounded to dtype before they are
+ * multiplied with the values. Every sum has a fixed order: equal calls give equal bits.
+ * CSG_ERR_INVALID for a malformed request, CSG_ERR_UNSUPPORTED for another type, head
+ * dimension or device, or sizes that a launch cannot hold; nothing is queued then. */
+
+typedef struct {
+    int32_t n_heads, n_kv_heads, head_dim;
+    int32_t dtype;                /* csg_dtype of every tensor of heads */
+    int32_t causal;               /* 1: row i sees key j if j <= p_i or j < the document's prefix */
+    int32_t n_docs;
+    float scale;                  /* > 0; 0 = 1 / sqrt(head_dim) */
+    float softcap;                /* c; 0 = none */
+    int64_t q_rows, k_rows;       /* rows of q (o, gradients of either) and of k and v */
+    int64_t q_stride, k_stride, v_stride;
+    int64_t dq_stride, dk_stride, dv_stride;
+} csg_doc_attn_cfg;
+
+/* Attention over packed documents: document t's rows are q_ptr[t] .. q_ptr[t+1] - 1, its
+ * keys k_ptr[t] .. k_ptr[t+1] - 1 (int32[n_docs + 1] each, ascending; they may be the same
+ * array). Rows see keys of their own document: all of them, or, with causal, those up to
+ * their own and the first prefix[t] (int32[n_docs], NULL = 0 for every document). Lengths
+ * may be 0 and differ between rows and keys; with more rows than keys a causal document's
+ * first rows see nothing. slopes: float[n_heads] or NULL. o: [q_rows][n_heads][head_dim],
+ * lse: float[n_heads][q_rows]. Rows of no document (behind the last one, say) are left as
+ * they are. Values of one document never reach another's results; within a document the
+ * values of a masked key are multiplied with weights of 0, as in a product of matrices, so
+ * they must be finite (masked keys may be anything).
+ * Bounds that do not ascend or leave 0 .. rows select fewer rows, never memory outside. */
+csg_status csg_doc_attn(const csg_doc_attn_cfg* cfg, const void* q, const void* k, const void* v,
+                        const int32_t* q_ptr, const int32_t* k_ptr, const int32_t* prefix,
+                        const float* slopes, void* o, void* lse, int device, void* stream);
+
+/* Bytes of workspace that csg_doc_attn_grad needs for cfg. */
+csg_status csg_doc_attn_grad_workspace(const csg_doc_attn_cfg* cfg, size_t* bytes);
+
+/* The gradient: from d_o (layout of o) and the forward call's o and lse to dq, dk, dv (rows
+ * as q, k, v, strides dq_stride ...), overwritten for every row and key of a document,
+ * others left as they are. dk and dv are summed over the heads that share a key/value
+ * head. The slopes are constants. workspace: csg_doc_attn_grad_workspace bytes, any
+ * content. dq, dk and dv may not overlap the inputs. */
+csg_status csg_doc_attn_grad(const csg_doc_attn_cfg* cfg, const void* q, const void* k, const void* v,
+                             const int32_t* q_ptr, const int32_t* k_ptr, const int32_t* prefix,
+                             const float* slopes, const void* o, const void* lse, const void* d_o,
+                             void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes,
+                             int device, void* stream);
+
+typedef struct {
+    int32_t n_heads, n_kv_heads, head_dim;
+    int32_t dtype;
+    int32_t n_pages;              /* pages of the cache */
+    int32_t page_size;            /* tokens per page: 16, 32, 64, 128 or 256 */
+    int32_t batch, max_pages;     /* sequences; pages per row of the page table */
+    int32_t n_groups;             /* groups of sequences that share a prefix (0: none) */
+    int32_t rot_dim;              /* csg_cache_append: elements of a head that are rotated, a
+                                     multiple of 16 (0: none) */
+    int32_t interleaved;          /* pairs are elements 2 i, 2 i + 1 (1) or i, i + rot_dim / 2 (0) */
+    float scale, softcap;         /* csg_cache_attn, as in csg_doc_attn_cfg */
+    int64_t tokens;               /* rows of q, k, v: at least q_ptr[batch] */
+    int64_t q_stride, k_stride, v_stride;
+} csg_cache_cfg;
+
+/* A paged cache: k_pages and v_pages are [n_pages][n_kv_heads][page_size][head_dim]; token x
+ * of sequence b lies in page page_table[b * max_pages + x / page_size], row x % page_size.
+ * lens[b] is the sequence's length, its new tokens included: rows q_ptr[b] .. q_ptr[b+1] - 1
+ * of q, k and v (int32[batch + 1], ascending; a sequence may have none), which are its last.
+ * status: int32 on the device or NULL; a call sets bit 0 if it met a page number outside 0 ..
+ * n_pages - 1 where a token lies, bit 1 for a length beyond max_pages pages or a new token
+ * before position 0; it never clears them. Such tokens are not written, their keys count as
+ * zeros, and the outputs of the sequence mean nothing; no memory outside is touched. */
+
+/* Puts the new tokens' keys and values into the cache, the keys (and queries) rotated by
+ * their position: pair (x, y) number i of a head becomes (x cos a - y sin a, y cos a + x sin a),
+ * a = position * inv_freq[i] (double[rot_dim / 2] on the device; the product is reduced in
+ * 64 bits, so that far positions keep their angle). q, q_out ([tokens][n_heads][head_dim],
+ * may be q if that is dense) may both be NULL. Rows of no sequence are left as they are. Two
+ * new tokens may not fall on one row of one page. */
+csg_status csg_cache_append(const csg_cache_cfg* cfg, void* k_pages, void* v_pages, const void* k,
+                            const void* v, const void* q, void* q_out, const int32_t* q_ptr,
+                            const int32_t* lens, const int32_t* page_table, const double* inv_freq,
+                            int32_t* status, int device, void* stream);
+
+/* Bytes of workspace that csg_cache_attn needs for cfg on device. */
+csg_status csg_cache_attn_workspace(const csg_cache_cfg* cfg, int device, size_t* bytes);
+
+/* Attention of the new tokens (one per sequence in a decode step; more for drafts or a
+ * prompt's part) over the cache; each sees the keys up to its own position. Sequences
+ * group_ptr[g] .. group_ptr[g+1] - 1 (int32[n_groups + 1], ascending; sequences outside every
+ * group share nothing) have the same first prefix[g] tokens: their keys and values are read
+ * once for the group, from the pages of its first sequence. A sequence shorter than that
+ * shares what it has. o: [tokens][n_heads][head_dim]; lse: float[n_heads][tokens], or NULL.
+ * Rows of no sequence are left as they are. workspace: csg_cache_attn_workspace bytes, any
+ * content. At most 2048 sequences and groups. */
+csg_status csg_cache_attn(const csg_cache_cfg* cfg, const void* q, const void* k_pages,
+                          const void* v_pages, const int32_t* q_ptr, const int32_t* lens,
+                          const int32_t* page_table, const int32_t* group_ptr, const int32_t* prefix,
+                          const float* slopes, void* o, void* lse, void* workspace,
+                          size_t workspace_bytes, int32_t* status, int device, void* stream);
 
 /* Waits for the plan's last call to complete (its kernel and every copy it issued)
  * and reports its diagnostics.

@@ -24,7 +24,7 @@ LIB_PATH = os.path.join(_HERE, "libcsg.so")
 # csg_status
 CSG_OK, CSG_ERR_INVALID, CSG_ERR_UNSUPPORTED, CSG_ERR_HIP, CSG_ERR_NOMEM, CSG_ERR_TIMEOUT, CSG_ERR_STATE = range(7)
 # csg_dtype
-CSG_BF16, CSG_F32 = 0, 1
+CSG_BF16, CSG_F32, CSG_F16 = 0, 1, 2
 # csg_op
 CSG_AG_GEMM, CSG_GEMM_RS, CSG_GROUPED_GEMM, CSG_GEMM_AR = 0, 1, 2, 3
 # csg_order
@@ -37,7 +37,7 @@ CSG_COPY_SDMA, CSG_COPY_KERNEL = 0, 1
 ORDERS = {"ring": CSG_ORDER_RING, "swizzle1d": CSG_ORDER_SWIZZLE1D, "permutation": CSG_ORDER_PERMUTATION,
           "rs_ring": CSG_ORDER_RS_RING}
 MODES = {"overlap": CSG_MODE_OVERLAP, "compute_only": CSG_MODE_COMPUTE_ONLY, "copy_only": CSG_MODE_COPY_ONLY}
-DTYPES = {"bf16": CSG_BF16, "f32": CSG_F32}
+DTYPES = {"bf16": CSG_BF16, "f32": CSG_F32, "f16": CSG_F16}
 OPS = {"ag": CSG_AG_GEMM, "rs": CSG_GEMM_RS, "grouped": CSG_GROUPED_GEMM, "ar": CSG_GEMM_AR}
 COPY_BACKENDS = {"sdma": CSG_COPY_SDMA, "kernel": CSG_COPY_KERNEL}
 
@@ -50,6 +50,8 @@ ABI_FUNCTIONS = (
     "csg_ag_gemm", "csg_gemm_rs", "csg_gemm_ar", "csg_grouped_gemm", "csg_plan_check", "csg_plan_kernel_times",
     "csg_plan_trace", "csg_plan_destroy", "csg_attn_plan_create", "csg_ring_attn", "csg_plan_join",
     "csg_measure_mfma_peak", "csg_ag_gemm_noalloc",
+    "csg_doc_attn", "csg_doc_attn_grad", "csg_doc_attn_grad_workspace", "csg_cache_append", "csg_cache_attn",
+    "csg_cache_attn_workspace",
 )
 
 
@@ -89,6 +91,24 @@ class csg_trace_unit(ctypes.Structure):
                 ("xcd", ctypes.c_int32), ("workgroup", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("t_take", ctypes.c_uint64), ("t_start", ctypes.c_uint64), ("t_end", ctypes.c_uint64),
                 ("cycles", ctypes.c_uint64)]
+
+
+class csg_doc_attn_cfg(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32), ("n_docs", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("q_rows", ctypes.c_int64),
+                ("k_rows", ctypes.c_int64), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("dq_stride", ctypes.c_int64), ("dk_stride", ctypes.c_int64),
+                ("dv_stride", ctypes.c_int64)]
+
+
+class csg_cache_cfg(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_groups", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("softcap", ctypes.c_float), ("tokens", ctypes.c_int64), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
 class csg_diag(ctypes.Structure):
@@ -136,6 +156,12 @@ def _lib():
         "csg_plan_destroy": ([vp], None),
         "csg_plan_join": ([vp, vp], st),
         "csg_ag_gemm_noalloc": ([vp, i64, i64, i64, st, st, vp, vp, vp, vp, st, i32, ctypes.c_int, vp], st),
+        "csg_doc_attn": ([P(csg_doc_attn_cfg)] + [vp] * 9 + [ctypes.c_int, vp], st),
+        "csg_doc_attn_grad_workspace": ([P(csg_doc_attn_cfg), P(ctypes.c_size_t)], st),
+        "csg_doc_attn_grad": ([P(csg_doc_attn_cfg)] + [vp] * 14 + [ctypes.c_size_t, ctypes.c_int, vp], st),
+        "csg_cache_append": ([P(csg_cache_cfg)] + [vp] * 11 + [ctypes.c_int, vp], st),
+        "csg_cache_attn_workspace": ([P(csg_cache_cfg), ctypes.c_int, P(ctypes.c_size_t)], st),
+        "csg_cache_attn": ([P(csg_cache_cfg)] + [vp] * 12 + [ctypes.c_size_t, vp, ctypes.c_int, vp], st),
         "csg_measure_mfma_peak": ([ctypes.c_int, i32, P(ctypes.c_double), P(ctypes.c_double), P(ctypes.c_double)],
                                   st),
     }
@@ -396,6 +422,44 @@ def csg_ag_gemm_noalloc(schedule, M, N, K, in_dtype, out_dtype, a_landing, a_sta
                                       copy_workgroups, device, _stream(stream)), "csg_ag_gemm_noalloc")
 
 
+def csg_doc_attn(cfg: csg_doc_attn_cfg, q, k, v, q_ptr, k_ptr, prefix, slopes, o, lse, device=0, stream=None) -> None:
+    _check(_lib().csg_doc_attn(cfg, _ptr(q), _ptr(k), _ptr(v), _ptr(q_ptr), _ptr(k_ptr), _ptr(prefix), _ptr(slopes),
+                               _ptr(o), _ptr(lse), device, _stream(stream)), "csg_doc_attn")
+
+
+def csg_doc_attn_grad_workspace(cfg: csg_doc_attn_cfg) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib().csg_doc_attn_grad_workspace(cfg, ctypes.byref(n)), "csg_doc_attn_grad_workspace")
+    return n.value
+
+
+def csg_doc_attn_grad(cfg: csg_doc_attn_cfg, q, k, v, q_ptr, k_ptr, prefix, slopes, o, lse, d_o, dq, dk, dv, workspace,
+                      workspace_bytes: int, device=0, stream=None) -> None:
+    _check(_lib().csg_doc_attn_grad(cfg, _ptr(q), _ptr(k), _ptr(v), _ptr(q_ptr), _ptr(k_ptr), _ptr(prefix), _ptr(slopes),
+                                    _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
+                                    workspace_bytes, device, _stream(stream)), "csg_doc_attn_grad")
+
+
+def csg_cache_append(cfg: csg_cache_cfg, k_pages, v_pages, k, v, q, q_out, q_ptr, lens, page_table, inv_freq, status=None,
+                     device=0, stream=None) -> None:
+    _check(_lib().csg_cache_append(cfg, _ptr(k_pages), _ptr(v_pages), _ptr(k), _ptr(v), _ptr(q), _ptr(q_out), _ptr(q_ptr),
+                                   _ptr(lens), _ptr(page_table), _ptr(inv_freq), _ptr(status), device, _stream(stream)),
+           "csg_cache_append")
+
+
+def csg_cache_attn_workspace(cfg: csg_cache_cfg, device=0) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib().csg_cache_attn_workspace(cfg, device, ctypes.byref(n)), "csg_cache_attn_workspace")
+    return n.value
+
+
+def csg_cache_attn(cfg: csg_cache_cfg, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse,
+                   workspace, workspace_bytes: int, status=None, device=0, stream=None) -> None:
+    _check(_lib().csg_cache_attn(cfg, _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(q_ptr), _ptr(lens), _ptr(page_table),
+                                 _ptr(group_ptr), _ptr(prefix), _ptr(slopes), _ptr(o), _ptr(lse), _ptr(workspace),
+                                 workspace_bytes, _ptr(status), device, _stream(stream)), "csg_cache_attn")
+
+
 def csg_plan_join(plan: int, stream) -> None:
     """Queues on `stream` a wait, on the device, for every copy of the plan's last call."""
     _check(_lib().csg_plan_join(plan, _stream(stream)), "csg_plan_join")
@@ -572,3 +636,147 @@ class AttnPlan(Plan):
             _buf(t, n, what)
         csg_ring_attn(self.handle, q, k_landing, v_landing, k_staging, v_staging, o, lse, mode, compute_stream,
                       copy_stream)
+
+
+def _tensor(t, need: int, what: str, device: int) -> None:
+    """_buf's checks, and that the tensor lives on the calls' device."""
+    _buf(t, need, what)
+    if t is not None and not isinstance(t, int) and t.device.index != device:
+        raise ValueError("%s must be on GPU %d" % (what, device))
+
+
+def _heads(t, rows: Optional[int], heads: int, head_dim: int, what: str, device: int) -> int:
+    """Checks a tensor of rows of heads, which may be part of a wider one, and returns its
+    row stride in elements."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim or (rows is not None and t.shape[0] != rows):
+        raise ValueError("%s must be (%s, %d, %d); it is %s"
+                         % (what, "rows" if rows is None else rows, heads, head_dim, tuple(t.shape)))
+    if t.element_size() != 2:
+        raise ValueError("%s must have 2-byte elements" % what)
+    row, head, one = t.stride()
+    if one != 1 or (heads > 1 and head != head_dim):
+        raise ValueError("%s: the heads of a row must lie behind each other" % what)
+    if t.device.type != "cuda" or t.device.index != device:
+        raise ValueError("%s must be on GPU %d" % (what, device))
+    return row if t.shape[0] > 1 else heads * head_dim
+
+
+class DocAttn:
+    """Attention over packed documents and its gradient (csg_doc_attn, csg_doc_attn_grad).
+
+    Keeps the shape of the heads and the scores; owns no device memory. Tensors of heads are
+    (rows, heads, head_dim); q, k, v and their gradients may be slices of a wider tensor.
+    q_ptr and k_ptr are int32 (documents + 1), prefix int32 (documents), slopes float32 (heads)."""
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, dtype, causal=True, scale=0.0, softcap=0.0, device: int = 0):
+        self.device = device
+        self._cfg = csg_doc_attn_cfg(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
+                                     dtype=DTYPES[dtype] if isinstance(dtype, str) else int(dtype), causal=int(causal),
+                                     scale=scale, softcap=softcap)
+        csg_doc_attn_grad_workspace(self._cfg)  # checks the configuration
+
+    def workspace_bytes(self, q_rows: int, k_rows: int) -> int:
+        """Bytes of the workspace that backward needs."""
+        c = csg_doc_attn_cfg.from_buffer_copy(self._cfg)
+        c.q_rows, c.k_rows = q_rows, k_rows
+        c.q_stride = c.k_stride = c.v_stride = c.dq_stride = c.dk_stride = c.dv_stride = 0
+        return csg_doc_attn_grad_workspace(c)
+
+    def _set(self, q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes):
+        c, dev = self._cfg, self.device
+        h, hkv, d = c.n_heads, c.n_kv_heads, c.head_dim
+        c.q_stride = _heads(q, None, h, d, "q", dev)
+        c.k_stride = _heads(k, None, hkv, d, "k", dev)
+        c.v_stride = _heads(v, k.shape[0], hkv, d, "v", dev)
+        c.q_rows, c.k_rows = n, m = q.shape[0], k.shape[0]
+        c.n_docs = docs = q_ptr.numel() - 1
+        _tensor(q_ptr, 4 * (docs + 1), "q_ptr", dev)
+        _tensor(k_ptr, 4 * (docs + 1), "k_ptr", dev)
+        _tensor(prefix, 4 * docs, "prefix", dev)
+        _tensor(slopes, 4 * h, "slopes", dev)
+        _tensor(o, 2 * n * h * d, "o", dev)
+        _tensor(lse, 4 * n * h, "lse", dev)
+
+    def forward(self, q, k, v, q_ptr, k_ptr, o, lse, prefix=None, slopes=None, stream=None):
+        self._set(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
+        csg_doc_attn(self._cfg, q, k, v, q_ptr, k_ptr, prefix, slopes, o, lse, self.device, stream)
+
+    def backward(self, q, k, v, q_ptr, k_ptr, o, lse, d_o, dq, dk, dv, workspace, prefix=None, slopes=None, stream=None):
+        self._set(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
+        c, dev = self._cfg, self.device
+        c.dq_stride = _heads(dq, q.shape[0], c.n_heads, c.head_dim, "dq", dev)
+        c.dk_stride = _heads(dk, k.shape[0], c.n_kv_heads, c.head_dim, "dk", dev)
+        c.dv_stride = _heads(dv, k.shape[0], c.n_kv_heads, c.head_dim, "dv", dev)
+        _tensor(d_o, 2 * q.shape[0] * c.n_heads * c.head_dim, "d_o", dev)
+        _tensor(workspace, 1, "workspace", dev)
+        csg_doc_attn_grad(c, q, k, v, q_ptr, k_ptr, prefix, slopes, o, lse, d_o, dq, dk, dv, workspace,
+                          workspace.numel() * workspace.element_size(), dev, stream)
+
+
+class PagedCache:
+    """A paged key/value cache: append and attn (csg_cache_append, csg_cache_attn).
+
+    Keeps the cache's geometry; the pages, (n_pages, n_kv_heads, page_size, head_dim) for keys
+    and for values, are the caller's. q_ptr is int32 (batch + 1), lens int32 (batch), page_table
+    int32 (batch, max_pages); k, v and q are (tokens, heads, head_dim) and may be slices of a
+    wider tensor; status, if given, is one int32."""
+
+    def __init__(self, n_heads, n_kv_heads, head_dim, dtype, n_pages, page_size, batch, max_pages, device: int = 0):
+        self.device = device
+        self._cfg = csg_cache_cfg(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
+                                  dtype=DTYPES[dtype] if isinstance(dtype, str) else int(dtype), n_pages=n_pages,
+                                  page_size=page_size, batch=batch, max_pages=max_pages)
+        csg_cache_attn_workspace(self._cfg, -1)  # checks the configuration
+
+    def workspace_bytes(self, tokens: int, n_groups: int = 0) -> int:
+        """Bytes of the workspace that attn needs for up to that many new tokens and groups."""
+        c = csg_cache_cfg.from_buffer_copy(self._cfg)
+        c.tokens, c.n_groups, c.q_stride = tokens, n_groups, 0
+        return csg_cache_attn_workspace(c, self.device)
+
+    def _set(self, k_pages, v_pages, q_ptr, lens, page_table, status):
+        c, dev = self._cfg, self.device
+        pages = 2 * c.n_pages * c.n_kv_heads * c.page_size * c.head_dim
+        _tensor(k_pages, pages, "k_pages", dev)
+        _tensor(v_pages, pages, "v_pages", dev)
+        _tensor(q_ptr, 4 * (c.batch + 1), "q_ptr", dev)
+        _tensor(lens, 4 * c.batch, "lens", dev)
+        _tensor(page_table, 4 * c.batch * c.max_pages, "page_table", dev)
+        _tensor(status, 4, "status", dev)
+
+    def append(self, k_pages, v_pages, k, v, q_ptr, lens, page_table, inv_freq=None, interleaved=False, q=None, q_out=None,
+               status=None, stream=None):
+        """Keys are rotated in their first 2 * inv_freq.numel() elements (float64), and so are
+        the queries q, into q_out."""
+        self._set(k_pages, v_pages, q_ptr, lens, page_table, status)
+        c, dev = self._cfg, self.device
+        c.tokens = n = k.shape[0]
+        c.k_stride = _heads(k, None, c.n_kv_heads, c.head_dim, "k", dev)
+        c.v_stride = _heads(v, n, c.n_kv_heads, c.head_dim, "v", dev)
+        c.q_stride = 0
+        if q is not None:
+            c.q_stride = _heads(q, n, c.n_heads, c.head_dim, "q", dev)
+            _tensor(q_out, 2 * n * c.n_heads * c.head_dim, "q_out", dev)
+        c.rot_dim = 0 if inv_freq is None else 2 * inv_freq.numel()
+        _tensor(inv_freq, 4 * c.rot_dim, "inv_freq", dev)
+        c.interleaved = int(interleaved)
+        csg_cache_append(c, k_pages, v_pages, k, v, q, q_out, q_ptr, lens, page_table, inv_freq, status, dev, stream)
+
+    def attn(self, q, k_pages, v_pages, q_ptr, lens, page_table, o, lse, workspace, group_ptr=None, prefix=None, scale=0.0,
+             softcap=0.0, slopes=None, status=None, stream=None):
+        """group_ptr int32 (groups + 1) and prefix int32 (groups): sequences that share their
+        first tokens; lse may be None."""
+        self._set(k_pages, v_pages, q_ptr, lens, page_table, status)
+        c, dev = self._cfg, self.device
+        c.q_stride = _heads(q, None, c.n_heads, c.head_dim, "q", dev)
+        c.tokens = n = q.shape[0]
+        c.n_groups = 0 if group_ptr is None else group_ptr.numel() - 1
+        c.scale, c.softcap = scale, softcap
+        _tensor(group_ptr, 4 * (c.n_groups + 1), "group_ptr", dev)
+        _tensor(prefix, 4 * c.n_groups, "prefix", dev)
+        _tensor(slopes, 4 * c.n_heads, "slopes", dev)
+        _tensor(o, 2 * n * c.n_heads * c.head_dim, "o", dev)
+        _tensor(lse, 4 * n * c.n_heads, "lse", dev)
+        _tensor(workspace, 1, "workspace", dev)
+        csg_cache_attn(c, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse, workspace,
+                       workspace.numel() * workspace.element_size(), status, dev, stream)

@@ -44,13 +44,14 @@
 
 #include "csg.h"
 #include "attn.hpp"
+#include "errors.hpp"
 #include "exec_tables.hpp"
 #include "noalloc.hpp"
 #include "kernels.hpp"
 #include "planner.hpp"
 #include "sdma.hpp"
 
-namespace {
+namespace csg {
 
 thread_local std::string g_last_error;
 
@@ -64,30 +65,15 @@ csg_status fail(csg_status s, const char* fmt, ...) {
   return s;
 }
 
-csg_status hip_fail(hipError_t e, const char* what) {
-  return fail(e == hipErrorOutOfMemory ? CSG_ERR_NOMEM : CSG_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
+}  // namespace csg
 
-#define CSG_HIP(expr)                                      \
-  do {                                                     \
-    hipError_t e_ = (expr);                                \
-    if (e_ != hipSuccess) return hip_fail(e_, #expr);      \
-  } while (0)
+namespace {
 
-// Restores the caller's current device on scope exit.
-struct DeviceGuard {
-  int prev = -1;
-  hipError_t err = hipSuccess;
-  explicit DeviceGuard(int dev) {
-    err = hipGetDevice(&prev);
-    if (err == hipSuccess && prev != dev) err = hipSetDevice(dev);
-  }
-  ~DeviceGuard() {
-    if (prev >= 0) (void)hipSetDevice(prev);
-  }
-};
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+using csg::aligned16;
+using csg::DeviceGuard;
+using csg::fail;
+using csg::g_last_error;
+using csg::hip_fail;
 
 // Epochs run 1 .. kEpochWrap - 1; on reaching it the emitted-flag words are cleared.
 constexpr uint32_t kEpochWrap = 1u << 30;

@@ -1,0 +1,481 @@
+// Attention over packed documents, and its gradient, for gfx950 (CDNA4).
+//
+// Rows (queries) and keys of document t are rows q_ptr[t] .. q_ptr[t+1] - 1 and k_ptr[t] ..
+// k_ptr[t+1] - 1. Row i of a document stands at its key p = i + keys - rows (the last row at
+// the last key). It sees key j of its document if the mask is not causal, or j <= p, or
+// j < prefix[t]: always the first hi(i) keys, and hi grows with i, so a tile of rows walks
+// the blocks of keys below its last row's hi, and only blocks above its first row's hi look
+// at the mask at all. With s the scores (scaled, capped, less the distance bias),
+//   lse_i = log sum_j exp(s_ij),  P_ij = exp(s_ij - lse_i),  o_i = sum_j P_ij v_j,
+//   D_i = do_i . o_i,  dS_ij = P_ij (do_i . v_j - D_i) (1 - tanh^2),
+//   dQ_i = scale sum_j dS_ij k_j,  dK_j = scale sum_i dS_ij q_i,  dV_j = sum_i P_ij do_i.
+//
+// Tiles never hold rows of two documents, so no document's values reach another's results.
+// A tile is 128 (row, head) pairs, one wave per 32 rows of a head; where heads share keys,
+// 2 or 4 of them share the tile: then it spans 64 or 32 rows, which leaves less of it unused
+// on short documents and computes fewer masked pairs. The tiles of a launch are bounded by
+// the host, which does not know the documents: document t's first tile is q_ptr[t] / rows a
+// tile + t, which leaves room for its last, part-filled one; a workgroup without rows ends.
+#include <hip/hip_runtime.h>
+
+#include "attn_tile.hpp"
+#include "doc_attn.hpp"
+
+namespace csg {
+namespace {
+
+using namespace tile;
+
+constexpr int kThreads = 256;
+static_assert(kDocTileRows == 32 * (kThreads / 64), "one wave per 32 rows");
+
+// A document and the part of it that a tile holds.
+struct Place {
+  int q0, q_len, k0, k_len, prefix;
+  int first;  // the tile's first row (key) in the document
+  bool any;
+};
+
+// The document of tile `slot` of `step` rows each; `by_keys`: the tile holds keys.
+__device__ __forceinline__ Place find_place(const DocAttnArgs& a, int slot, int step, bool by_keys) {
+  Place p;
+  const int32_t* ptr = by_keys ? a.k_ptr : a.q_ptr;
+  const int rows = by_keys ? a.k_rows : a.q_rows;
+  const int d = last_below(a.n_docs, [&](int i) { return clamped(ptr[i], 0, rows) / step + i <= slot; });
+  p.q0 = clamped(a.q_ptr[d], 0, a.q_rows);
+  p.q_len = clamped(a.q_ptr[d + 1], p.q0, a.q_rows) - p.q0;
+  p.k0 = clamped(a.k_ptr[d], 0, a.k_rows);
+  p.k_len = clamped(a.k_ptr[d + 1], p.k0, a.k_rows) - p.k0;
+  p.prefix = a.prefix ? clamped(a.prefix[d], 0, p.k_len) : 0;
+  const int t = slot - ((by_keys ? p.k0 : p.q0) / step + d);
+  p.any = t >= 0 && static_cast<int64_t>(t) * step < (by_keys ? p.k_len : p.q_len);
+  p.first = p.any ? t * step : 0;
+  return p;
+}
+
+// Keys that row i of the document sees.
+__device__ __forceinline__ int visible(const DocAttnArgs& a, const Place& p, int i) {
+  return a.causal ? clamped(max(p.prefix, i + p.k_len - p.q_len + 1), 0, p.k_len) : p.k_len;
+}
+
+// This wave's share of the loads of 64 rows (fewer at the end: rows past `rows` read zero) of
+// one head into a tile at LDS byte `lds`. src: the head's part of the first row.
+template <int D>
+__device__ __forceinline__ void load_tile(const uint16_t* src, int64_t stride, int rows, uint32_t lds, int wave,
+                                          const LoadLane<D>& ll) {
+  const int n = rows < kDocBlock ? rows : kDocBlock;
+  const __amdgpu_buffer_rsrc_t rs = make_rsrc(src, n > 0 ? static_cast<int>(((n - 1) * stride + D) * 2) : 0);
+  constexpr int kPer = kDocBlock / kLoadRows<D> / 4;
+  const int stride2 = static_cast<int>(2 * stride);
+#pragma unroll
+  for (int q = 0; q < kPer; ++q) {
+    // loads 4 q' of a wave: the turn of the pieces depends on q alone
+    const int i = wave * kPer + q;
+    constexpr int kTurns = 16 / kLoadRows<D>;
+    const int turn = swz<D>(kLoadRows<D> * (q % kTurns));
+    static_assert(kPer % kTurns == 0, "every wave starts at a multiple of 16 rows");
+    const int voff = (kLoadRows<D> * i + ll.row) * stride2 + 16 * (ll.piece ^ turn);
+    load_to_lds(rs, __builtin_amdgcn_readfirstlane(lds + 1024u * i), voff);
+  }
+}
+
+// A wave's 32 rows of one head as second operand: lane row `row`, zero if it is not `ok`.
+template <class T, int D>
+__device__ __forceinline__ void load_rows(const uint16_t* head, int64_t stride, int row, bool ok, int hlf,
+                                          typename T::x8 (&f)[D / 16]) {
+  const uint16_t* p = head + (ok ? row : 0) * stride + 8 * hlf;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const u32x4_t raw = ok ? *reinterpret_cast<const u32x4_t*>(p + 16 * s) : u32x4_t{0u, 0u, 0u, 0u};
+    f[s] = __builtin_bit_cast(typename T::x8, raw);
+  }
+}
+
+// A result transposed (lane: one row, 16 elements per 32 in runs of four) times f, rounded.
+template <class T, int D>
+__device__ __forceinline__ void store_rows(uint16_t* head, int64_t stride, int row, int hlf, const f32x16_t (&acc)[D / 32],
+                                           float f) {
+  uint16_t* p = head + row * stride + 4 * hlf;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const f32x4_t v{acc[db][4 * b] * f, acc[db][4 * b + 1] * f, acc[db][4 * b + 2] * f, acc[db][4 * b + 3] * f};
+      *reinterpret_cast<u32x2_t*>(p + 32 * db + 8 * b) = __builtin_bit_cast(u32x2_t, __builtin_convertvector(v, typename T::x4));
+    }
+}
+
+// Products of 64 keys with the wave's rows: lane (l32, hlf) has those of row l32.
+template <class T, int D>
+__device__ __forceinline__ void products(const unsigned char* t, const Frags<D>& f, const typename T::x8 (&qf)[D / 16],
+                                         f32x16_t (&sc)[2]) {
+  sc[0] = f32x16_t{};
+  sc[1] = f32x16_t{};
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) sc[kb] = T::mfma(row_frag<T, D>(t, f, s, 32 * kb), qf[s], sc[kb]);
+}
+
+// ---- forward -----------------------------------------------------------------------------
+template <class T, int D, bool kPlain>
+__global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
+  constexpr int kTile = kDocBlock * D * 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char sK[2 * kTile];
+  __shared__ __attribute__((aligned(1024))) unsigned char sV[2 * kTile];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, hlf = lane >> 5;
+  const int span = kDocTileRows / a.tile_heads, groups = a.H / a.tile_heads;
+  // a die runs every 8th workgroup: with the head fastest, it keeps to few key/value heads;
+  // the last rows of a causal document, which see the most keys, come first
+  const int hg = blockIdx.x % groups;
+  const Place p = find_place(a, gridDim.x / groups - 1 - blockIdx.x / groups, span, false);
+  if (!p.any) return;
+  const int G = a.H / a.Hkv, per_kv = G / a.tile_heads;
+  const int kvh = hg / per_kv;
+  const int h = kvh * G + (hg - kvh * per_kv) * a.tile_heads + wave % a.tile_heads;
+  const int first = p.first + wave / a.tile_heads * 32;
+  const int row = first + l32;
+  const bool ok = row < p.q_len;
+  const int hi = visible(a, p, min(row, p.q_len - 1));
+  const int wave_lo = visible(a, p, min(first, p.q_len - 1));  // seen by every row of the wave
+  const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kDocBlock - 1) / kDocBlock;
+  const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[h] : 0.0f;
+  const int at = row + p.k_len - p.q_len;  // the row's own key
+
+  const LoadLane<D> ll(lane);
+  const Frags<D> fr(lane);
+  const uint32_t sK_addr = lds_address(sK), sV_addr = lds_address(sV);
+  const lds_u8_t* sV_lds = (const lds_u8_t*)sV;
+  const uint16_t* kh = a.K + p.k0 * a.k_stride + kvh * D;
+  const uint16_t* vh = a.V + p.k0 * a.v_stride + kvh * D;
+  auto load = [&](int j) {
+    load_tile<D>(kh + static_cast<int64_t>(j) * kDocBlock * a.k_stride, a.k_stride, p.k_len - j * kDocBlock,
+                 sK_addr + (j & 1) * kTile, wave, ll);
+    load_tile<D>(vh + static_cast<int64_t>(j) * kDocBlock * a.v_stride, a.v_stride, p.k_len - j * kDocBlock,
+                 sV_addr + (j & 1) * kTile, wave, ll);
+  };
+  if (nb > 0) load(0);
+
+  typename T::x8 qf[D / 16];
+  load_rows<T, D>(a.Q + p.q0 * a.q_stride + h * D, a.q_stride, row, ok, hlf, qf);
+  f32x16_t acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
+  RowSoftmax sm;
+  const float c = kPlain ? a.scale * kLog2e : kLog2e;
+
+  for (int j = 0; j < nb; ++j) {
+    wait_vm<0>();
+    __syncthreads();  // block j is there, and everyone is done with block j - 1
+    if (j + 1 < nb) load(j + 1);
+    const int buf = (j & 1) * kTile;
+    const int key0 = j * kDocBlock;
+    f32x16_t sc[2];
+    products<T, D>(sK + buf, fr, qf, sc);
+    if constexpr (!kPlain) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          sc[kb][r] = score_of(sc[kb][r], a.scoring, slope, at - (key0 + 32 * kb + result_row(r, hlf))).value;
+    }
+    if (key0 + kDocBlock > wave_lo) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (key0 + 32 * kb + result_row(r, hlf) >= hi) sc[kb][r] = -__builtin_inff();
+    }
+    typename T::x8 pb[4];
+    bool moved;
+    const float alpha = sm.block<T, 2>(sc, c, pb, moved);
+    if (moved) {
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        acc[db] = T::mfma(col_frag<T, D>(sV_lds + buf, fr, db, 16 * t), pb[t], acc[db]);
+  }
+  if (!ok) return;
+  const float total = sum_halves(sm.l);
+  if (total == 0.0f) {  // nothing visible
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
+  }
+  store_rows<T, D>(a.O + (static_cast<int64_t>(p.q0) * a.H + h) * D, static_cast<int64_t>(a.H) * D, row, hlf, acc,
+                   total == 0.0f ? 0.0f : 1.0f / total);
+  if (hlf == 0)
+    a.LSE[static_cast<int64_t>(h) * a.q_rows + p.q0 + row] = fmaf(log2f(total), kLn2, kPlain ? sm.m * a.scale : sm.m);
+}
+
+// ---- gradient of the queries --------------------------------------------------------------
+// The forward's tiles; also leaves each row's statistics to the kernel of the keys' gradient.
+template <class T, int D, bool kPlain>
+__global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
+  constexpr int kTile = kDocBlock * D * 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char sK[2 * kTile];
+  __shared__ __attribute__((aligned(1024))) unsigned char sV[2 * kTile];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, hlf = lane >> 5;
+  const int span = kDocTileRows / a.tile_heads, groups = a.H / a.tile_heads;
+  const int hg = blockIdx.x % groups;
+  const Place p = find_place(a, gridDim.x / groups - 1 - blockIdx.x / groups, span, false);
+  if (!p.any) return;
+  const int G = a.H / a.Hkv, per_kv = G / a.tile_heads;
+  const int kvh = hg / per_kv;
+  const int h = kvh * G + (hg - kvh * per_kv) * a.tile_heads + wave % a.tile_heads;
+  const int first = p.first + wave / a.tile_heads * 32;
+  const int row = first + l32;
+  const bool ok = row < p.q_len;
+  const int hi = visible(a, p, min(row, p.q_len - 1));
+  const int wave_lo = visible(a, p, min(first, p.q_len - 1));
+  const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kDocBlock - 1) / kDocBlock;
+  const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[h] : 0.0f;
+  const int at = row + p.k_len - p.q_len;
+
+  const LoadLane<D> ll(lane);
+  const Frags<D> fr(lane);
+  const uint32_t sK_addr = lds_address(sK), sV_addr = lds_address(sV);
+  const lds_u8_t* sK_lds = (const lds_u8_t*)sK;
+  const uint16_t* kh = a.K + p.k0 * a.k_stride + kvh * D;
+  const uint16_t* vh = a.V + p.k0 * a.v_stride + kvh * D;
+  auto load = [&](int j) {
+    load_tile<D>(kh + static_cast<int64_t>(j) * kDocBlock * a.k_stride, a.k_stride, p.k_len - j * kDocBlock,
+                 sK_addr + (j & 1) * kTile, wave, ll);
+    load_tile<D>(vh + static_cast<int64_t>(j) * kDocBlock * a.v_stride, a.v_stride, p.k_len - j * kDocBlock,
+                 sV_addr + (j & 1) * kTile, wave, ll);
+  };
+  if (nb > 0) load(0);
+
+  typename T::x8 qf[D / 16], gf[D / 16];
+  load_rows<T, D>(a.Q + p.q0 * a.q_stride + h * D, a.q_stride, row, ok, hlf, qf);
+  const int64_t o_stride = static_cast<int64_t>(a.H) * D, o_head = p.q0 * o_stride + h * D;
+  load_rows<T, D>(a.dO + o_head, o_stride, row, ok, hlf, gf);
+  const float c = kPlain ? a.scale * kLog2e : kLog2e;
+  float delta = 0.0f, lse2 = 0.0f;
+  {
+    typename T::x8 of[D / 16];
+    load_rows<T, D>(a.O + o_head, o_stride, row, ok, hlf, of);
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf(static_cast<float>(gf[s][e]), static_cast<float>(of[s][e]), delta);
+    delta = sum_halves(delta);
+    if (ok) {
+      const float lse = a.LSE[static_cast<int64_t>(h) * a.q_rows + p.q0 + row];
+      // a row that sees nothing: against +inf every weight is 0
+      lse2 = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+      if (hlf == 0) {
+        const int64_t pitch = a.q_rows + kStatPad;
+        float* st = a.stats + h * pitch + p.q0 + row;
+        st[0] = lse2;
+        st[a.H * pitch] = delta;
+      }
+    }
+  }
+  f32x16_t acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
+
+  for (int j = 0; j < nb; ++j) {
+    wait_vm<0>();
+    __syncthreads();  // block j is there, and everyone is done with block j - 1
+    if (j + 1 < nb) load(j + 1);
+    const int buf = (j & 1) * kTile;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      f32x16_t sc{}, dp{};
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) {
+        sc = T::mfma(row_frag<T, D>(sK + buf, fr, s, 32 * kb), qf[s], sc);
+        dp = T::mfma(row_frag<T, D>(sV + buf, fr, s, 32 * kb), gf[s], dp);
+      }
+      const int key0 = j * kDocBlock + 32 * kb;
+      f32x16_t ds;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if constexpr (kPlain) {
+          ds[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -lse2)) * (dp[r] - delta);
+        } else {
+          const Score s = score_of(sc[r], a.scoring, slope, at - (key0 + result_row(r, hlf)));
+          ds[r] = __builtin_amdgcn_exp2f(fmaf(s.value, c, -lse2)) * (dp[r] - delta) * s.slip;
+        }
+      }
+      if (key0 + 32 > wave_lo) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (key0 + result_row(r, hlf) >= hi) ds[r] = 0.0f;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const typename T::x8 w = pack<T>(ds, t);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+          acc[db] = T::mfma(col_frag<T, D>(sK_lds + buf, fr, db, 32 * kb + 16 * t), w, acc[db]);
+      }
+    }
+  }
+  if (ok) store_rows<T, D>(a.dQ + p.q0 * a.dq_stride + h * D, a.dq_stride, row, hlf, acc, a.scale);
+}
+
+// ---- gradients of the keys and values ------------------------------------------------------
+// A tile is 128 keys of one key/value head, 32 a wave, whose gradients stay in registers while
+// the rows that see them pass, head by head of the group: a sum over shared heads is no more
+// than a longer loop, in a fixed order.
+template <class T, int D, bool kPlain>
+__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttnArgs a) {
+  constexpr int kTile = kDocBlock * D * 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char sQ[2 * kTile];
+  __shared__ __attribute__((aligned(1024))) unsigned char sG[2 * kTile];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, hlf = lane >> 5;
+  const int kvh = blockIdx.x % a.Hkv;
+  const Place p = find_place(a, blockIdx.x / a.Hkv, kDocTileRows, true);  // (the first keys have the most rows)
+  if (!p.any) return;
+  const int G = a.H / a.Hkv;
+  const int shift = p.k_len - p.q_len;
+  // the first row that sees key j
+  auto first_row = [&](int j) { return a.causal && j >= p.prefix ? max(0, j - shift) : 0; };
+  const int first = p.first + wave * 32;
+  const int key = first + l32;
+  const bool ok = key < p.k_len;
+  const int lo = first_row(key);
+  const int wave_hi = first_row(first + 31);  // rows from here on see every key of the wave
+  const int r0 = min(first_row(p.first), p.q_len);
+  const int nb = (p.q_len - r0 + kDocBlock - 1) / kDocBlock;
+  const int steps = nb * G;
+
+  const LoadLane<D> ll(lane);
+  const Frags<D> fr(lane);
+  const uint32_t sQ_addr = lds_address(sQ), sG_addr = lds_address(sG);
+  const lds_u8_t* sQ_lds = (const lds_u8_t*)sQ;
+  const lds_u8_t* sG_lds = (const lds_u8_t*)sG;
+  const int64_t o_stride = static_cast<int64_t>(a.H) * D;
+  const uint16_t* qh = a.Q + p.q0 * a.q_stride + kvh * G * D;
+  const uint16_t* gh = a.dO + p.q0 * o_stride + kvh * G * D;
+  auto load = [&](int i, int g, int j) {  // step i: block j of head g of the group
+    const int64_t r = r0 + j * kDocBlock;
+    load_tile<D>(qh + r * a.q_stride + g * D, a.q_stride, p.q_len - static_cast<int>(r), sQ_addr + (i & 1) * kTile, wave, ll);
+    load_tile<D>(gh + r * o_stride + g * D, o_stride, p.q_len - static_cast<int>(r), sG_addr + (i & 1) * kTile, wave, ll);
+  };
+  if (steps > 0) load(0, 0, 0);
+
+  typename T::x8 kf[D / 16], vf[D / 16];
+  load_rows<T, D>(a.K + p.k0 * a.k_stride + kvh * D, a.k_stride, key, ok, hlf, kf);
+  load_rows<T, D>(a.V + p.k0 * a.v_stride + kvh * D, a.v_stride, key, ok, hlf, vf);
+  f32x16_t dk[D / 32], dv[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    dk[db] = f32x16_t{};
+    dv[db] = f32x16_t{};
+  }
+  const float c = kPlain ? a.scale * kLog2e : kLog2e;
+  const int64_t pitch = a.q_rows + kStatPad;
+  typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
+
+  for (int i = 0, g = 0, j = 0; i < steps; ++i) {
+    wait_vm<0>();
+    __syncthreads();
+    const int gn = j + 1 < nb ? g : g + 1, jn = j + 1 < nb ? j + 1 : 0;
+    if (i + 1 < steps) load(i + 1, gn, jn);
+    const int buf = (i & 1) * kTile;
+    const int h = kvh * G + g;
+    const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[h] : 0.0f;
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      const int row0 = r0 + j * kDocBlock + 32 * rb;
+      // (rows up to 63 behind the document's last: other rows' statistics, or the padding)
+      const float* st = a.stats + h * pitch + p.q0 + row0 + 4 * hlf;
+      f32x4_t lse2[4], delta[4];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        lse2[b] = *reinterpret_cast<const f32x4u_t*>(st + 8 * b);
+        delta[b] = *reinterpret_cast<const f32x4u_t*>(st + a.H * pitch + 8 * b);
+      }
+      f32x16_t sc{}, dp{};
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) {
+        sc = T::mfma(row_frag<T, D>(sQ + buf, fr, s, 32 * rb), kf[s], sc);
+        dp = T::mfma(row_frag<T, D>(sG + buf, fr, s, 32 * rb), vf[s], dp);
+      }
+      f32x16_t w, ds;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float l2 = lse2[r >> 2][r & 3], dl = delta[r >> 2][r & 3];
+        if constexpr (kPlain) {
+          w[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -l2));
+          ds[r] = w[r] * (dp[r] - dl);
+        } else {
+          const Score s = score_of(sc[r], a.scoring, slope, row0 + result_row(r, hlf) + shift - key);
+          w[r] = __builtin_amdgcn_exp2f(fmaf(s.value, c, -l2));
+          ds[r] = w[r] * (dp[r] - dl) * s.slip;
+        }
+      }
+      if (row0 < wave_hi || row0 + 32 > p.q_len) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = row0 + result_row(r, hlf);
+          if (row < lo || row >= p.q_len) w[r] = ds[r] = 0.0f;
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const typename T::x8 wt = pack<T>(w, t), dt = pack<T>(ds, t);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+          dv[db] = T::mfma(col_frag<T, D>(sG_lds + buf, fr, db, 32 * rb + 16 * t), wt, dv[db]);
+          dk[db] = T::mfma(col_frag<T, D>(sQ_lds + buf, fr, db, 32 * rb + 16 * t), dt, dk[db]);
+        }
+      }
+    }
+    g = gn;
+    j = jn;
+  }
+  if (!ok) return;
+  store_rows<T, D>(a.dK + p.k0 * a.dk_stride + kvh * D, a.dk_stride, key, hlf, dk, a.scale);
+  store_rows<T, D>(a.dV + p.k0 * a.dv_stride + kvh * D, a.dv_stride, key, hlf, dv, 1.0f);
+}
+
+template <class T, int D, bool kPlain>
+hipError_t forward(const DocAttnArgs& a, hipStream_t stream) {
+  const int64_t slots = a.q_rows / (kDocTileRows / a.tile_heads) + a.n_docs;
+  hipLaunchKernelGGL((doc_forward<T, D, kPlain>), dim3(slots * (a.H / a.tile_heads)), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <class T, int D, bool kPlain>
+hipError_t grad(const DocAttnArgs& a, hipStream_t stream) {
+  const int64_t slots = a.q_rows / (kDocTileRows / a.tile_heads) + a.n_docs;
+  hipLaunchKernelGGL((doc_grad_q<T, D, kPlain>), dim3(slots * (a.H / a.tile_heads)), dim3(kThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t k_slots = a.k_rows / kDocTileRows + a.n_docs;
+  hipLaunchKernelGGL((doc_grad_kv<T, D, kPlain>), dim3(k_slots * a.Hkv), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <class T, int D>
+hipError_t dispatch(const DocAttnArgs& a, bool gradient, hipStream_t s) {
+  if (a.scoring.plain()) return gradient ? grad<T, D, true>(a, s) : forward<T, D, true>(a, s);
+  return gradient ? grad<T, D, false>(a, s) : forward<T, D, false>(a, s);
+}
+
+hipError_t dispatch(const DocAttnArgs& a, bool f16, int head_dim, bool gradient, hipStream_t s) {
+  if (head_dim == 128) return f16 ? dispatch<F16, 128>(a, gradient, s) : dispatch<Bf16, 128>(a, gradient, s);
+  return f16 ? dispatch<F16, 64>(a, gradient, s) : dispatch<Bf16, 64>(a, gradient, s);
+}
+
+}  // namespace
+
+hipError_t launch_doc_forward(const DocAttnArgs& a, bool f16, int head_dim, hipStream_t stream) {
+  return dispatch(a, f16, head_dim, false, stream);
+}
+hipError_t launch_doc_grad(const DocAttnArgs& a, bool f16, int head_dim, hipStream_t stream) {
+  return dispatch(a, f16, head_dim, true, stream);
+}
+
+}  // namespace csg
