@@ -638,27 +638,34 @@ class AttnPlan(Plan):
                       copy_stream)
 
 
-def _tensor(t, need: int, what: str, device: int) -> None:
-    """_buf's checks, and that the tensor lives on the calls' device."""
+def _arg(t, need: int, what: str, device: int) -> int:
+    """_buf's checks, and that the tensor lives on the calls' device; its address. (A few
+    queries of the tensor: a decode step's kernels take less time than careful ones.)"""
+    if t is None:
+        return 0
+    if type(t) is int:
+        return t
+    if t.is_contiguous() and t.nbytes >= need and t.get_device() == device:
+        return t.data_ptr()
     _buf(t, need, what)
-    if t is not None and not isinstance(t, int) and t.device.index != device:
-        raise ValueError("%s must be on GPU %d" % (what, device))
+    raise ValueError("%s must be on GPU %d" % (what, device))
 
 
-def _heads(t, rows: Optional[int], heads: int, head_dim: int, what: str, device: int) -> int:
-    """Checks a tensor of rows of heads, which may be part of a wider one, and returns its
-    row stride in elements."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim or (rows is not None and t.shape[0] != rows):
+def _heads(t, rows: Optional[int], heads: int, head_dim: int, what: str, device: int):
+    """Checks a tensor of rows of heads, which may be part of a wider one: (address, rows, row
+    stride in elements)."""
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim or (rows is not None and shape[0] != rows):
         raise ValueError("%s must be (%s, %d, %d); it is %s"
-                         % (what, "rows" if rows is None else rows, heads, head_dim, tuple(t.shape)))
-    if t.element_size() != 2:
+                         % (what, "rows" if rows is None else rows, heads, head_dim, tuple(shape)))
+    if t.itemsize != 2:
         raise ValueError("%s must have 2-byte elements" % what)
     row, head, one = t.stride()
     if one != 1 or (heads > 1 and head != head_dim):
         raise ValueError("%s: the heads of a row must lie behind each other" % what)
-    if t.device.type != "cuda" or t.device.index != device:
+    if t.get_device() != device:
         raise ValueError("%s must be on GPU %d" % (what, device))
-    return row if t.shape[0] > 1 else heads * head_dim
+    return t.data_ptr(), shape[0], (row if shape[0] > 1 else heads * head_dim)
 
 
 class DocAttn:
@@ -666,7 +673,8 @@ class DocAttn:
 
     Keeps the shape of the heads and the scores; owns no device memory. Tensors of heads are
     (rows, heads, head_dim); q, k, v and their gradients may be slices of a wider tensor.
-    q_ptr and k_ptr are int32 (documents + 1), prefix int32 (documents), slopes float32 (heads)."""
+    q_ptr and k_ptr are int32 (documents + 1), prefix int32 (documents), slopes float32 (heads).
+    Not thread-safe: threads take an object each."""
 
     def __init__(self, n_heads, n_kv_heads, head_dim, dtype, causal=True, scale=0.0, softcap=0.0, device: int = 0):
         self.device = device
@@ -674,6 +682,7 @@ class DocAttn:
                                      dtype=DTYPES[dtype] if isinstance(dtype, str) else int(dtype), causal=int(causal),
                                      scale=scale, softcap=softcap)
         csg_doc_attn_grad_workspace(self._cfg)  # checks the configuration
+        self._shape = n_heads, n_kv_heads, head_dim
 
     def workspace_bytes(self, q_rows: int, k_rows: int) -> int:
         """Bytes of the workspace that backward needs."""
@@ -682,35 +691,33 @@ class DocAttn:
         c.q_stride = c.k_stride = c.v_stride = c.dq_stride = c.dk_stride = c.dv_stride = 0
         return csg_doc_attn_grad_workspace(c)
 
-    def _set(self, q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes):
+    def _inputs(self, q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes):
+        """Checks what both calls take and sets the configuration: rows, keys, addresses."""
         c, dev = self._cfg, self.device
-        h, hkv, d = c.n_heads, c.n_kv_heads, c.head_dim
-        c.q_stride = _heads(q, None, h, d, "q", dev)
-        c.k_stride = _heads(k, None, hkv, d, "k", dev)
-        c.v_stride = _heads(v, k.shape[0], hkv, d, "v", dev)
-        c.q_rows, c.k_rows = n, m = q.shape[0], k.shape[0]
+        h, hkv, d = self._shape
+        qa, n, c.q_stride = _heads(q, None, h, d, "q", dev)
+        ka, m, c.k_stride = _heads(k, None, hkv, d, "k", dev)
+        va, _, c.v_stride = _heads(v, m, hkv, d, "v", dev)
+        c.q_rows, c.k_rows = n, m
         c.n_docs = docs = q_ptr.numel() - 1
-        _tensor(q_ptr, 4 * (docs + 1), "q_ptr", dev)
-        _tensor(k_ptr, 4 * (docs + 1), "k_ptr", dev)
-        _tensor(prefix, 4 * docs, "prefix", dev)
-        _tensor(slopes, 4 * h, "slopes", dev)
-        _tensor(o, 2 * n * h * d, "o", dev)
-        _tensor(lse, 4 * n * h, "lse", dev)
+        return n, m, (qa, ka, va, _arg(q_ptr, 4 * (docs + 1), "q_ptr", dev), _arg(k_ptr, 4 * (docs + 1), "k_ptr", dev),
+                      _arg(prefix, 4 * docs, "prefix", dev), _arg(slopes, 4 * h, "slopes", dev),
+                      _arg(o, 2 * n * h * d, "o", dev), _arg(lse, 4 * n * h, "lse", dev))
 
     def forward(self, q, k, v, q_ptr, k_ptr, o, lse, prefix=None, slopes=None, stream=None):
-        self._set(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
-        csg_doc_attn(self._cfg, q, k, v, q_ptr, k_ptr, prefix, slopes, o, lse, self.device, stream)
+        _, _, args = self._inputs(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
+        _check(_lib().csg_doc_attn(self._cfg, *args, self.device, _stream(stream)), "csg_doc_attn")
 
     def backward(self, q, k, v, q_ptr, k_ptr, o, lse, d_o, dq, dk, dv, workspace, prefix=None, slopes=None, stream=None):
-        self._set(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
+        n, m, args = self._inputs(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
         c, dev = self._cfg, self.device
-        c.dq_stride = _heads(dq, q.shape[0], c.n_heads, c.head_dim, "dq", dev)
-        c.dk_stride = _heads(dk, k.shape[0], c.n_kv_heads, c.head_dim, "dk", dev)
-        c.dv_stride = _heads(dv, k.shape[0], c.n_kv_heads, c.head_dim, "dv", dev)
-        _tensor(d_o, 2 * q.shape[0] * c.n_heads * c.head_dim, "d_o", dev)
-        _tensor(workspace, 1, "workspace", dev)
-        csg_doc_attn_grad(c, q, k, v, q_ptr, k_ptr, prefix, slopes, o, lse, d_o, dq, dk, dv, workspace,
-                          workspace.numel() * workspace.element_size(), dev, stream)
+        h, hkv, d = self._shape
+        dqa, _, c.dq_stride = _heads(dq, n, h, d, "dq", dev)
+        dka, _, c.dk_stride = _heads(dk, m, hkv, d, "dk", dev)
+        dva, _, c.dv_stride = _heads(dv, m, hkv, d, "dv", dev)
+        _check(_lib().csg_doc_attn_grad(c, *args, _arg(d_o, 2 * n * h * d, "d_o", dev), dqa, dka, dva,
+                                        _arg(workspace, 1, "workspace", dev), workspace.nbytes, dev, _stream(stream)),
+               "csg_doc_attn_grad")
 
 
 class PagedCache:
@@ -719,7 +726,7 @@ class PagedCache:
     Keeps the cache's geometry; the pages, (n_pages, n_kv_heads, page_size, head_dim) for keys
     and for values, are the caller's. q_ptr is int32 (batch + 1), lens int32 (batch), page_table
     int32 (batch, max_pages); k, v and q are (tokens, heads, head_dim) and may be slices of a
-    wider tensor; status, if given, is one int32."""
+    wider tensor; status, if given, is one int32. Not thread-safe: threads take an object each."""
 
     def __init__(self, n_heads, n_kv_heads, head_dim, dtype, n_pages, page_size, batch, max_pages, device: int = 0):
         self.device = device
@@ -727,6 +734,10 @@ class PagedCache:
                                   dtype=DTYPES[dtype] if isinstance(dtype, str) else int(dtype), n_pages=n_pages,
                                   page_size=page_size, batch=batch, max_pages=max_pages)
         csg_cache_attn_workspace(self._cfg, -1)  # checks the configuration
+        self._shape = n_heads, n_kv_heads, head_dim
+        self._batch = batch
+        self._page_bytes = 2 * n_pages * n_kv_heads * page_size * head_dim
+        self._table_bytes = 4 * batch * max_pages
 
     def workspace_bytes(self, tokens: int, n_groups: int = 0) -> int:
         """Bytes of the workspace that attn needs for up to that many new tokens and groups."""
@@ -734,49 +745,41 @@ class PagedCache:
         c.tokens, c.n_groups, c.q_stride = tokens, n_groups, 0
         return csg_cache_attn_workspace(c, self.device)
 
-    def _set(self, k_pages, v_pages, q_ptr, lens, page_table, status):
-        c, dev = self._cfg, self.device
-        pages = 2 * c.n_pages * c.n_kv_heads * c.page_size * c.head_dim
-        _tensor(k_pages, pages, "k_pages", dev)
-        _tensor(v_pages, pages, "v_pages", dev)
-        _tensor(q_ptr, 4 * (c.batch + 1), "q_ptr", dev)
-        _tensor(lens, 4 * c.batch, "lens", dev)
-        _tensor(page_table, 4 * c.batch * c.max_pages, "page_table", dev)
-        _tensor(status, 4, "status", dev)
-
     def append(self, k_pages, v_pages, k, v, q_ptr, lens, page_table, inv_freq=None, interleaved=False, q=None, q_out=None,
                status=None, stream=None):
         """Keys are rotated in their first 2 * inv_freq.numel() elements (float64), and so are
         the queries q, into q_out."""
-        self._set(k_pages, v_pages, q_ptr, lens, page_table, status)
-        c, dev = self._cfg, self.device
-        c.tokens = n = k.shape[0]
-        c.k_stride = _heads(k, None, c.n_kv_heads, c.head_dim, "k", dev)
-        c.v_stride = _heads(v, n, c.n_kv_heads, c.head_dim, "v", dev)
-        c.q_stride = 0
+        c, dev, batch = self._cfg, self.device, self._batch
+        h, hkv, d = self._shape
+        ka, n, c.k_stride = _heads(k, None, hkv, d, "k", dev)
+        va, _, c.v_stride = _heads(v, n, hkv, d, "v", dev)
+        c.tokens = n
+        qa = qo = c.q_stride = 0
         if q is not None:
-            c.q_stride = _heads(q, n, c.n_heads, c.head_dim, "q", dev)
-            _tensor(q_out, 2 * n * c.n_heads * c.head_dim, "q_out", dev)
-        c.rot_dim = 0 if inv_freq is None else 2 * inv_freq.numel()
-        _tensor(inv_freq, 4 * c.rot_dim, "inv_freq", dev)
-        c.interleaved = int(interleaved)
-        csg_cache_append(c, k_pages, v_pages, k, v, q, q_out, q_ptr, lens, page_table, inv_freq, status, dev, stream)
+            qa, _, c.q_stride = _heads(q, n, h, d, "q", dev)
+            qo = _arg(q_out, 2 * n * h * d, "q_out", dev)
+        c.rot_dim = rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        c.interleaved = interleaved
+        _check(_lib().csg_cache_append(
+            c, _arg(k_pages, self._page_bytes, "k_pages", dev), _arg(v_pages, self._page_bytes, "v_pages", dev), ka, va, qa, qo,
+            _arg(q_ptr, 4 * batch + 4, "q_ptr", dev), _arg(lens, 4 * batch, "lens", dev),
+            _arg(page_table, self._table_bytes, "page_table", dev), _arg(inv_freq, 4 * rot, "inv_freq", dev),
+            _arg(status, 4, "status", dev), dev, _stream(stream)), "csg_cache_append")
 
     def attn(self, q, k_pages, v_pages, q_ptr, lens, page_table, o, lse, workspace, group_ptr=None, prefix=None, scale=0.0,
              softcap=0.0, slopes=None, status=None, stream=None):
         """group_ptr int32 (groups + 1) and prefix int32 (groups): sequences that share their
         first tokens; lse may be None."""
-        self._set(k_pages, v_pages, q_ptr, lens, page_table, status)
-        c, dev = self._cfg, self.device
-        c.q_stride = _heads(q, None, c.n_heads, c.head_dim, "q", dev)
-        c.tokens = n = q.shape[0]
-        c.n_groups = 0 if group_ptr is None else group_ptr.numel() - 1
+        c, dev, batch = self._cfg, self.device, self._batch
+        h, hkv, d = self._shape
+        qa, n, c.q_stride = _heads(q, None, h, d, "q", dev)
+        c.tokens = n
+        c.n_groups = groups = 0 if group_ptr is None else group_ptr.numel() - 1
         c.scale, c.softcap = scale, softcap
-        _tensor(group_ptr, 4 * (c.n_groups + 1), "group_ptr", dev)
-        _tensor(prefix, 4 * c.n_groups, "prefix", dev)
-        _tensor(slopes, 4 * c.n_heads, "slopes", dev)
-        _tensor(o, 2 * n * c.n_heads * c.head_dim, "o", dev)
-        _tensor(lse, 4 * n * c.n_heads, "lse", dev)
-        _tensor(workspace, 1, "workspace", dev)
-        csg_cache_attn(c, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse, workspace,
-                       workspace.numel() * workspace.element_size(), status, dev, stream)
+        _check(_lib().csg_cache_attn(
+            c, qa, _arg(k_pages, self._page_bytes, "k_pages", dev), _arg(v_pages, self._page_bytes, "v_pages", dev),
+            _arg(q_ptr, 4 * batch + 4, "q_ptr", dev), _arg(lens, 4 * batch, "lens", dev),
+            _arg(page_table, self._table_bytes, "page_table", dev), _arg(group_ptr, 4 * groups + 4, "group_ptr", dev),
+            _arg(prefix, 4 * groups, "prefix", dev), _arg(slopes, 4 * h, "slopes", dev), _arg(o, 2 * n * h * d, "o", dev),
+            _arg(lse, 4 * n * h, "lse", dev), _arg(workspace, 1, "workspace", dev), workspace.nbytes,
+            _arg(status, 4, "status", dev), dev, _stream(stream)), "csg_cache_attn")

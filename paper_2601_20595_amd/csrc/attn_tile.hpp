@@ -108,6 +108,8 @@ __device__ __forceinline__ void wait_vm() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
 }
 
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // Rows one load_to_lds fills (1 KiB), and the loads of a tile of `rows` rows.
 template <int D>
 constexpr int kLoadRows = 512 / D;

@@ -119,19 +119,25 @@ __global__ __launch_bounds__(kThreads) void cache_append(AppendArgs a) {
 // ---- attention over the cache ---------------------------------------------------------------
 // Work: entry e < n_groups is the shared keys of a group, for the rows of all its sequences;
 // entry n_groups + b is the other keys of sequence b, for its own rows. A row is a new token and
-// a head of the key/value head's group, tokens first; 32 rows make a tile; an entry, a tile and
-// a key/value head make a task. A task is its blocks of 32 keys, and all tasks' blocks stand in
-// one row (by key/value head, entry, tile, block) that is cut into equal runs, one a workgroup:
-// every workgroup reads the same number of keys, whatever the lengths are. What a workgroup has
-// of a task is a part: its weights' sums and products against its own reference, which
-// cache_merge joins. Task t and workgroup w meet in at most one part, and parts in their order
-// never go back in t or w: t + w numbers them.
+// a head of the key/value head's group, tokens first. Up to 32 rows of an entry are a narrow
+// task: the four waves take different blocks of 32 keys for the same rows, each at its own
+// pace. More rows make wide tasks of 128, 32 a wave, whose waves share the keys. Every key/value
+// head has the same number of workgroups. All tasks' blocks of 32 keys stand in one row (by
+// entry, task, block) that is cut into equal runs, one a workgroup of the head: every workgroup
+// reads the same number of keys, whatever the lengths are. What a workgroup has of a task is a
+// part: for each tile of 32 rows, its weights' sums and products against its own reference,
+// which cache_merge joins. With the tiles counted through, tile t of run w is in place t + 4 w:
+// of two parts one after the other, the second has a later tile, or the next run and at most
+// the three tiles before.
 struct Entry {
   int token0, rows;    // first token, (token, head) rows
   int b0, b1;          // its sequences; the first one's pages are read
   int lo, end;         // keys
+  bool own;            // the keys of one sequence, up to its end
   int block0, blocks;  // blocks of keys that hold them
   __device__ __forceinline__ int tiles() const { return (rows + kCacheTileRows - 1) / kCacheTileRows; }
+  __device__ __forceinline__ bool wide() const { return rows > kCacheTileRows; }
+  __device__ __forceinline__ int tasks() const { return wide() ? (rows + kCacheWideRows - 1) / kCacheWideRows : 1; }
 };
 
 // The group of sequence b, -1 if it has none.
@@ -158,7 +164,8 @@ __device__ __forceinline__ int prefix_of(const CacheAttnArgs& a, int g) {
 __device__ __forceinline__ Entry entry_of(const CacheAttnArgs& a, int e) {
   const CacheArgs& c = a.c;
   Entry x;
-  if (e < a.n_groups) {
+  x.own = e >= a.n_groups;
+  if (!x.own) {
     x.b0 = clamped(a.group_ptr[e], 0, c.batch);
     x.b1 = clamped(a.group_ptr[e + 1], x.b0, c.batch);
     x.lo = 0;
@@ -177,291 +184,428 @@ __device__ __forceinline__ Entry entry_of(const CacheAttnArgs& a, int e) {
   return x;
 }
 
-// The plan of a call in the workspace: blocks of one key/value head, tasks of one, blocks a
-// workgroup takes; then blocks and tasks before each entry.
-struct Plan {
-  int64_t* blocks;  // [0]: all, [1]: a run; [2 + e]
-  int32_t* tasks;   // [0]: all; [1 + e]
+// The plan of a call in the workspace, for cache_merge: an entry's blocks and tiles before it,
+// its own blocks, rows and first token; of a sequence, its group's entry too (-1: none).
+struct PlanEntry {
+  int32_t before, tiles, blocks, rows, token0, group, unused[2];
 };
-__device__ __forceinline__ Plan plan_in(unsigned char* ws) {
-  Plan p;
-  p.blocks = reinterpret_cast<int64_t*>(ws);
-  p.tasks = reinterpret_cast<int32_t*>(ws + 16 + 8 * kMaxCacheEntries);
-  return p;
-}
+struct Plan {
+  int32_t run;    // blocks of a run
+  int32_t tiles;  // tiles of one key/value head
+  int32_t unused[6];
+};
+__device__ __forceinline__ Plan* plan_in(unsigned char* ws) { return reinterpret_cast<Plan*>(ws); }
+__device__ __forceinline__ PlanEntry* entries_in(unsigned char* ws) { return reinterpret_cast<PlanEntry*>(ws + sizeof(Plan)); }
+static_assert(sizeof(Plan) + kMaxCacheEntries * sizeof(PlanEntry) <= cache_plan_bytes(), "the plan fits");
 
 // What sums against reference m count against reference top; nothing if they saw no key.
 __device__ __forceinline__ float factor(float m, float top, float c) {
   return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - top) * c);
 }
 
-// A wave reads its own blocks of keys: into its own part of LDS, a block ahead, so that it
-// waits for no other wave; their results meet at the part's end.
+// A workgroup's part of a task, and this lane's row of it.
+struct Part {
+  int kvh, tile;       // key/value head; the wave's tile of 32 rows in the entry
+  int key0, end;       // keys of the part (those below the entry's lo are masked)
+  int lo;
+  const int32_t* table;
+  bool ok;             // the lane has a row
+  int token, h, pos;   // its token, head, position
+  int hi;              // it sees keys below this (lanes without a row, whose queries are 0: all)
+  int all_hi;          // every row of the wave sees keys below this
+};
+
+template <int D>
+__device__ __forceinline__ void locate_row(const CacheAttnArgs& a, const Entry& x, int l32, Part& p) {
+  const CacheArgs& c = a.c;
+  const int G = c.H / c.Hkv;
+  const int r = p.tile * kCacheTileRows + l32;
+  p.ok = r < x.rows;
+  p.token = x.token0 + (p.ok ? r / G : 0);
+  p.h = p.kvh * G + (p.ok ? r % G : 0);
+  if (x.own) {
+    p.pos = x.end - (x.token0 + x.rows / G - p.token);
+  } else {
+    int b = x.b0;
+    for (int n = x.b1 - x.b0; n > 1;) {  // the last of the group's sequences that starts by then
+      const int half = n / 2;
+      const bool up = c.q_ptr[b + half] <= p.token;
+      b = up ? b + half : b;
+      n = up ? n - half : half;
+    }
+    p.pos = length_of(c, b) - (first_token(c, b + 1) - p.token);
+  }
+  p.hi = p.ok ? min(p.pos + 1, p.end) : p.end;
+  int all_hi = p.hi;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) all_hi = min(all_hi, __shfl_xor(all_hi, d));
+  p.all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+}
+
+template <class T, int D>
+__device__ __forceinline__ void load_queries(const CacheAttnArgs& a, const Part& p, int hlf, typename T::x8 (&qf)[D / 16]) {
+  const uint16_t* q = a.c.Q + p.token * a.c.q_stride + p.h * D + 8 * hlf;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const u32x4_t raw = p.ok ? *reinterpret_cast<const u32x4_t*>(q + 16 * s) : u32x4_t{0u, 0u, 0u, 0u};
+    qf[s] = __builtin_bit_cast(typename T::x8, raw);
+  }
+}
+
+// The page of a key, -1 if it has none to read.
+__device__ __forceinline__ int page_of(const CacheArgs& c, const Part& p, int key) {
+  if (key >= p.end) return -1;
+  const int page = p.table[key >> c.page_shift];
+  if (page >= 0 && page < c.n_pages) return page;
+  tell(c, kCacheBadPage);
+  return -1;
+}
+
+// Keys (or values) key .. key + 15, which lie in one page, into LDS; what is behind the part's
+// end reads zero.
+template <int D>
+__device__ __forceinline__ void load_16(const CacheArgs& c, const uint16_t* pages, const Part& p, int page, int key, uint32_t lds,
+                                        const LoadLane<D>& ll) {
+  const int rows = page < 0 ? 0 : clamped(p.end - key, 0, 16);
+  const int64_t row = ((static_cast<int64_t>(max(page, 0)) * c.Hkv + p.kvh) << c.page_shift) + (key & ((1 << c.page_shift) - 1));
+  const __amdgpu_buffer_rsrc_t rs = make_rsrc(pages + row * D, rows * 2 * D);
+#pragma unroll
+  for (int i = 0; i < 16 / kLoadRows<D>; ++i) load_to_lds(rs, lds + 1024u * i, ll.offset(i, 2 * D));
+}
+
+// Scores of a block of 32 N keys from its products: cap, bias, mask.
+template <int N, bool kPlain>
+__device__ __forceinline__ void finish_scores(const CacheAttnArgs& a, const Part& p, float slope, int key0, int hlf, f32x16_t (&sc)[N]) {
+  if constexpr (!kPlain) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        sc[n][i] = score_of(sc[n][i], a.scoring, slope, p.pos - (key0 + 32 * n + result_row(i, hlf))).value;
+  }
+  if (key0 + 32 * N > p.all_hi || key0 < p.lo) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = key0 + 32 * n + result_row(i, hlf);
+        if (key >= p.hi || key < p.lo) sc[n][i] = -__builtin_inff();
+      }
+  }
+}
+
+// A narrow part: each wave takes every fourth block, through 16 KiB (D = 128) of LDS of its own:
+// the next keys load once the products have read the last, the next values once the sums have.
+// Two workgroups a CU keep 128 KiB in flight, and one streams while the other begins or ends
+// a part.
 template <class T, int D, bool kPlain>
-__global__ __launch_bounds__(kThreads, 1) void cache_attn(CacheAttnArgs a) {
-  constexpr int kRowBytes = 2 * D;
-  constexpr int kTile = kCacheBlock * kRowBytes;     // keys or values of a block
-  constexpr int kStage = 2 * kTile;
-  constexpr int kLoads = kCacheBlock / kLoadRows<D>; // loads of a tile
-  constexpr int kHalfLoads = kLoads / 2;             // of 16 rows, which lie in one page
-  __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * 2 * kStage];
-  __shared__ int64_t s_blocks[kMaxCacheEntries + 1];
-  __shared__ int32_t s_tasks[kMaxCacheEntries + 1];
-  __shared__ int64_t s_wave_blocks[4];
-  __shared__ int32_t s_wave_tasks[4];
+__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, Part& p, unsigned char* stage, float (&s_ref)[4][32],
+                                            float (&s_sum)[4][32], float* out, int lane, int wave) {
+  constexpr int kTile = kCacheBlock * 2 * D, kLoads = kCacheBlock / kLoadRows<D>;
+  const CacheArgs& c = a.c;
+  const int l32 = lane & 31, hlf = lane >> 5;
+  const LoadLane<D> ll(lane);
+  unsigned char* mine = stage + wave * 2 * kTile;
+  const uint32_t k_lds = lds_address(mine), v_lds = k_lds + kTile;
+  const int count = (p.end - p.key0 + kCacheBlock - 1) / kCacheBlock;
+  const int mine_n = count > wave ? (count - wave + 3) / 4 : 0;
+
+  // lane n holds the page of the 16 keys n % 2 of the wave's block n / 2 (32 blocks at a time)
+  int pages = -1;
+  auto key_of = [&](int n) { return p.key0 + (wave + 4 * n) * kCacheBlock; };
+  auto fetch = [&](int n) { pages = page_of(c, p, key_of(n + (lane >> 1)) + 16 * (lane & 1)); };
+  auto load = [&](int n, const uint16_t* from, uint32_t lds) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+      load_16<D>(c, from, p, __builtin_amdgcn_readlane(pages, 2 * (n & 31) + half), key_of(n) + 16 * half, lds + half * (kTile / 2), ll);
+  };
+  if (mine_n > 0) fetch(0);
+  locate_row<D>(a, x, l32, p);
+  typename T::x8 qf[D / 16];
+  load_queries<T, D>(a, p, hlf, qf);
+  if (mine_n > 0) {
+    load(0, c.k_pages, k_lds);
+    load(0, c.v_pages, v_lds);
+  }
+  const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[p.h] : 0.0f;
+  const float cexp = kPlain ? a.scoring.scale * kLog2e : kLog2e;
+  const Frags<D> fr(lane);
+  f32x16_t acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
+  RowSoftmax sm;
+  for (int n = 0; n < mine_n; ++n) {
+    const bool more = n + 1 < mine_n;
+    wait_vm<kLoads>();  // the keys are there; the values may be on their way
+    f32x16_t sc[1] = {f32x16_t{}};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) sc[0] = T::mfma(row_frag<T, D>(mine, fr, s, 0), qf[s], sc[0]);
+    wait_lds();  // the keys have been read
+    if (more) {
+      if (((n + 1) & 31) == 0) fetch(n + 1);
+      load(n + 1, c.k_pages, k_lds);
+    }
+    finish_scores<1, kPlain>(a, p, slope, key_of(n), hlf, sc);
+    typename T::x8 pb[2];
+    bool moved;
+    const float alpha = sm.block<T, 1>(sc, cexp, pb, moved);
+    if (moved) {
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
+    }
+    if (more)
+      wait_vm<kLoads>();
+    else
+      wait_vm<0>();
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        acc[db] = T::mfma(col_frag<T, D>((const lds_u8_t*)(mine + kTile), fr, db, 16 * t), pb[t], acc[db]);
+    wait_lds();
+    if (more) load(n + 1, c.v_pages, v_lds);
+  }
+
+  // the waves' results against their common reference, summed in the order of the waves; the
+  // 16-byte pieces of a row are turned by its number, against bank conflicts
+  const float l = sum_halves(sm.l);
+  if (hlf == 0) {
+    s_ref[wave][l32] = sm.m;
+    s_sum[wave][l32] = l;
+  }
+  __syncthreads();  // (also: every wave has read its stage)
+  const float top = fmaxf(fmaxf(s_ref[0][l32], s_ref[1][l32]), fmaxf(s_ref[2][l32], s_ref[3][l32]));
+  const int live = min(kCacheTileRows, x.rows - p.tile * kCacheTileRows);
+  constexpr int kPieces = D / 4;
+  if (l32 < live) {
+    const float f = factor(sm.m, top, cexp);
+    f32x4_t* to = reinterpret_cast<f32x4_t*>(stage) + (wave * 32 + l32) * kPieces;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        to[(8 * db + 2 * q + hlf) ^ (l32 & 7)] =
+            f32x4_t{acc[db][4 * q] * f, acc[db][4 * q + 1] * f, acc[db][4 * q + 2] * f, acc[db][4 * q + 3] * f};
+  }
+  __syncthreads();
+  if (out) {
+    const f32x4_t* in = reinterpret_cast<const f32x4_t*>(stage);
+    const int tid = wave * 64 + lane;
+    for (int i = tid; i < live * kPieces; i += kThreads) {
+      const int row = i / kPieces, at = row * kPieces + ((i % kPieces) ^ (row & 7));
+      f32x4_t v = in[at];
+#pragma unroll
+      for (int k = 1; k < 4; ++k) v += in[k * 32 * kPieces + at];
+      *reinterpret_cast<f32x4_t*>(out + 4 * i) = v;
+    }
+    if (tid < live) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum = fmaf(s_sum[k][l32], factor(s_ref[k][l32], top, cexp), sum);
+      out[32 * D + l32] = top;
+      out[32 * D + 32 + l32] = sum;
+    }
+  }
+  __syncthreads();  // the stages are free again
+}
+
+// A wide part: blocks of 64 keys in two buffers, which all waves read.
+template <class T, int D, bool kPlain>
+__device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, Part& p, unsigned char* stage, float* out, int lane,
+                                          int wave) {
+  constexpr int kTile = kCacheWideBlock * 2 * D;
+  const CacheArgs& c = a.c;
+  const int l32 = lane & 31, hlf = lane >> 5;
+  const LoadLane<D> ll(lane);
+  const uint32_t lds = lds_address(stage) + static_cast<uint32_t>(wave * 16 * 2 * D);
+  const int nb = (p.end - p.key0 + kCacheWideBlock - 1) / kCacheWideBlock;
+  // a wave brings 16 keys and values of each block; lane n holds the page of those of block n
+  // (64 blocks at a time)
+  int pages = -1;
+  auto fetch = [&](int n) { pages = page_of(c, p, p.key0 + (n + lane) * kCacheWideBlock + 16 * wave); };
+  auto load = [&](int n) {
+    if (n > 0 && (n & 63) == 0) fetch(n);
+    const int page = __builtin_amdgcn_readlane(pages, n & 63), key = p.key0 + n * kCacheWideBlock + 16 * wave;
+    const uint32_t to = lds + (n & 1) * 2 * kTile;
+    load_16<D>(c, c.k_pages, p, page, key, to, ll);
+    load_16<D>(c, c.v_pages, p, page, key, to + kTile, ll);
+  };
+  fetch(0);
+  locate_row<D>(a, x, l32, p);
+  typename T::x8 qf[D / 16];
+  load_queries<T, D>(a, p, hlf, qf);
+  load(0);
+  const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[p.h] : 0.0f;
+  const float cexp = kPlain ? a.scoring.scale * kLog2e : kLog2e;
+  const Frags<D> fr(lane);
+  f32x16_t acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
+  RowSoftmax sm;
+  const bool idle = p.tile * kCacheTileRows >= x.rows;  // no row in this wave
+  for (int n = 0; n < nb; ++n) {
+    wait_vm<0>();
+    __syncthreads();  // block n is there, and everyone is done with block n - 1
+    if (n + 1 < nb) load(n + 1);
+    if (idle) continue;
+    const unsigned char* kt = stage + (n & 1) * 2 * kTile;
+    f32x16_t sc[2] = {f32x16_t{}, f32x16_t{}};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) sc[kb] = T::mfma(row_frag<T, D>(kt, fr, s, 32 * kb), qf[s], sc[kb]);
+    finish_scores<2, kPlain>(a, p, slope, p.key0 + n * kCacheWideBlock, hlf, sc);
+    typename T::x8 pb[4];
+    bool moved;
+    const float alpha = sm.block<T, 2>(sc, cexp, pb, moved);
+    if (moved) {
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        acc[db] = T::mfma(col_frag<T, D>((const lds_u8_t*)(kt + kTile), fr, db, 16 * t), pb[t], acc[db]);
+  }
+  const float l = sum_halves(sm.l);
+  if (out && p.ok) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4_t*>(out + l32 * D + 32 * db + 8 * q + 4 * hlf) =
+            f32x4_t{acc[db][4 * q], acc[db][4 * q + 1], acc[db][4 * q + 2], acc[db][4 * q + 3]};
+    if (hlf == 0) {
+      out[32 * D + l32] = sm.m;
+      out[32 * D + 32 + l32] = l;
+    }
+  }
+  __syncthreads();  // the buffers are free again
+}
+
+template <class T, int D, bool kPlain>
+__global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * 2 * kCacheBlock * 2 * D];
   __shared__ float s_ref[4][32], s_sum[4][32];
-  static_assert(4 * kTile <= sizeof(stage) / 2, "the waves' results fit the stages");
+  __shared__ int s_wave_blocks[4], s_wave_tiles[4], s_entry, s_first, s_tiles;
+  static_assert(sizeof(stage) == 2 * 2 * kCacheWideBlock * 2 * D, "the same memory holds the wide parts' buffers");
+  static_assert(sizeof(stage) >= 4 * 32 * D * 4, "and the waves' results");
 
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, hlf = lane >> 5;
-  const int G = c.H / c.Hkv;
   const int n_entries = a.n_groups + c.batch;
+  // a die runs every 8th workgroup: with the head fastest, it has few heads, and runs that follow
+  // each other, whose tasks may read the same keys
+  const int kvh = blockIdx.x % c.Hkv;
+  int w = blockIdx.x / c.Hkv;
+  if (a.head_workers % a.dies == 0) w = w % a.dies * (a.head_workers / a.dies) + w / a.dies;
 
-  // blocks and tasks before each entry
-  {
-    const int per = (n_entries + kThreads - 1) / kThreads;
-    int64_t blocks = 0;
-    int32_t tasks = 0;
+  // Each thread counts some entries; blocks and tiles before each of them by a scan.
+  const int per = (n_entries + kThreads - 1) / kThreads;
+  int blocks = 0, tiles = 0;
+  for (int i = 0; i < per; ++i) {
+    const int e = tid * per + i;
+    if (e >= n_entries) break;
+    const Entry x = entry_of(a, e);
+    blocks += x.tasks() * x.blocks;
+    tiles += x.tiles();
+  }
+  const int own_blocks = blocks, own_tiles = tiles;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int ub = __shfl_up(blocks, d), ut = __shfl_up(tiles, d);
+    if (lane >= d) {
+      blocks += ub;
+      tiles += ut;
+    }
+  }
+  if (lane == 63) {
+    s_wave_blocks[wave] = blocks;
+    s_wave_tiles[wave] = tiles;
+  }
+  __syncthreads();
+  blocks -= own_blocks;
+  tiles -= own_tiles;
+  for (int i = 0; i < wave; ++i) {
+    blocks += s_wave_blocks[i];
+    tiles += s_wave_tiles[i];
+  }
+  const int all = __builtin_amdgcn_readfirstlane(s_wave_blocks[0] + s_wave_blocks[1] + s_wave_blocks[2] + s_wave_blocks[3]);
+  const int all_tiles = __builtin_amdgcn_readfirstlane(s_wave_tiles[0] + s_wave_tiles[1] + s_wave_tiles[2] + s_wave_tiles[3]);
+  const int run = max(kCacheMinRun, (all + a.head_workers - 1) / a.head_workers);
+  if (blockIdx.x == 0) {  // for cache_merge
+    int before = blocks, tiles_before = tiles;
     for (int i = 0; i < per; ++i) {
       const int e = tid * per + i;
       if (e >= n_entries) break;
       const Entry x = entry_of(a, e);
-      s_blocks[e] = blocks;  // before the thread's own
-      s_tasks[e] = tasks;
-      blocks += static_cast<int64_t>(x.tiles()) * x.blocks;
-      tasks += x.tiles();
-      if (blockIdx.x == 0 && e >= a.n_groups && length_of(c, x.b0) != c.lens[x.b0]) tell(c, kCacheBadLength);
+      entries_in(a.ws)[e] = {before, tiles_before, x.blocks, x.rows, x.token0, x.own ? group_of(a, x.b0) : -1, {0, 0}};
+      before += x.tasks() * x.blocks;
+      tiles_before += x.tiles();
+      if (x.own && length_of(c, x.b0) != c.lens[x.b0]) tell(c, kCacheBadLength);
     }
-    const int64_t own_blocks = blocks;
-    const int32_t own_tasks = tasks;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int64_t ub = __shfl_up(blocks, d);
-      const int32_t ut = __shfl_up(tasks, d);
-      if (lane >= d) {
-        blocks += ub;
-        tasks += ut;
-      }
-    }
-    if (lane == 63) {
-      s_wave_blocks[wave] = blocks;
-      s_wave_tasks[wave] = tasks;
-    }
-    __syncthreads();
-    blocks -= own_blocks;
-    tasks -= own_tasks;
-    for (int w = 0; w < wave; ++w) {
-      blocks += s_wave_blocks[w];
-      tasks += s_wave_tasks[w];
-    }
+    if (tid == 0) *plan_in(a.ws) = {run, all_tiles, {0, 0, 0, 0, 0, 0}};
+  }
+  const int begin = w * run;
+  if (begin >= all) return;
+  int left = min(run, all - begin);
+  // the entry where the run begins
+  if (blocks <= begin && begin < blocks + own_blocks) {
     for (int i = 0; i < per; ++i) {
       const int e = tid * per + i;
-      if (e >= n_entries) break;
-      s_blocks[e] += blocks;
-      s_tasks[e] += tasks;
+      const Entry x = entry_of(a, e);
+      const int n = x.tasks() * x.blocks;
+      if (begin < blocks + n) {
+        s_entry = e;
+        s_first = begin - blocks;
+        s_tiles = tiles;
+        break;
+      }
+      blocks += n;
+      tiles += x.tiles();
     }
   }
-  const int64_t all = s_wave_blocks[0] + s_wave_blocks[1] + s_wave_blocks[2] + s_wave_blocks[3];
-  const int32_t all_tasks = s_wave_tasks[0] + s_wave_tasks[1] + s_wave_tasks[2] + s_wave_tasks[3];
-  const int64_t total = all * c.Hkv;
-  const int64_t run = max(int64_t{1}, (total + a.workers - 1) / a.workers);
   __syncthreads();
-  if (blockIdx.x == 0) {  // for cache_merge
-    const Plan p = plan_in(a.ws);
-    for (int e = tid; e < n_entries; e += kThreads) {
-      p.blocks[2 + e] = s_blocks[e];
-      p.tasks[1 + e] = s_tasks[e];
-    }
-    if (tid == 0) {
-      p.blocks[0] = all;
-      p.blocks[1] = run;
-      p.tasks[0] = all_tasks;
-    }
-  }
-
-  // a die runs every 8th workgroup: its runs follow each other, so that the tiles of a group,
-  // which read the same keys, share its cache
-  const int w = a.workers % 8 == 0 ? blockIdx.x % 8 * (a.workers / 8) + blockIdx.x / 8 : blockIdx.x;
-  const LoadLane<D> ll(lane);
-  const Frags<D> fr(lane);
-  unsigned char* mine = stage + wave * 2 * kStage;
-  const uint32_t mine_addr = lds_address(mine);
-  const float cexp = kPlain ? a.scoring.scale * kLog2e : kLog2e;
-  const int page_mask = (1 << c.page_shift) - 1;
-
-  int64_t at = w * run;
-  const int64_t stop = min(total, at + run);
-  while (at < stop) {
-    const int kvh = __builtin_amdgcn_readfirstlane(static_cast<int>(at / all));
-    const int64_t in_head = at - kvh * all;
-    const int e = last_below(n_entries, [&](int i) { return s_blocks[i] <= in_head; });
+  int e = __builtin_amdgcn_readfirstlane(s_entry), in_entry = __builtin_amdgcn_readfirstlane(s_first);
+  int tiles_before = __builtin_amdgcn_readfirstlane(s_tiles);
+  const int64_t places = static_cast<int64_t>(kvh) * (all_tiles + 4 * a.head_workers) + 4 * w;
+  while (left > 0) {
     const Entry x = entry_of(a, e);
-    const int64_t in_entry = in_head - s_blocks[e];
-    const int tile = __builtin_amdgcn_readfirstlane(static_cast<int>(in_entry / x.blocks));
-    const int first = __builtin_amdgcn_readfirstlane(static_cast<int>(in_entry - static_cast<int64_t>(tile) * x.blocks));
-    const int count = __builtin_amdgcn_readfirstlane(static_cast<int>(min<int64_t>(x.blocks - first, stop - at)));
-    const int64_t part = static_cast<int64_t>(kvh) * all_tasks + s_tasks[e] + tile + w;
-
-    // the lane's row: its token, the keys that it sees
-    const int r = tile * kCacheTileRows + l32;
-    const bool ok = r < x.rows;
-    const int token = x.token0 + (ok ? r / G : 0);
-    const int h = kvh * G + (ok ? r % G : 0);
-    int b = x.b0;
-    for (int n = x.b1 - x.b0; n > 1;) {  // the last of the entry's sequences that starts by then
-      const int half = n / 2;
-      const bool up = c.q_ptr[b + half] <= token;
-      b = up ? b + half : b;
-      n = up ? n - half : half;
+    const int n = x.tasks() * x.blocks;
+    if (in_entry < n) {
+      Part p;
+      p.kvh = kvh;
+      const bool wide = x.wide();
+      const int task = wide ? __builtin_amdgcn_readfirstlane(in_entry / x.blocks) : 0;
+      const int first = in_entry - task * x.blocks;
+      const int count = min(x.blocks - first, left);
+      p.table = c.table + static_cast<int64_t>(x.b0) * c.max_pages;
+      p.lo = x.lo;
+      p.key0 = (x.block0 + first) * kCacheBlock;
+      p.end = min(x.end, p.key0 + count * kCacheBlock);
+      p.tile = wide ? 4 * task + wave : 0;
+      const int64_t place = places + tiles_before + p.tile;
+      float* out = place < a.max_parts ? reinterpret_cast<float*>(a.ws + cache_plan_bytes() + place * cache_part_bytes(D)) : nullptr;
+      if (wide)
+        wide_part<T, D, kPlain>(a, x, p, stage, out, lane, wave);
+      else
+        narrow_part<T, D, kPlain>(a, x, p, stage, s_ref, s_sum, out, lane, wave);
+      left -= count;
+      in_entry += count;
+    } else {
+      in_entry = 0;
+      tiles_before += x.tiles();
+      ++e;
     }
-    const int pos = length_of(c, b) - (first_token(c, b + 1) - token);
-    const int hi = ok ? min(pos + 1, x.end) : x.end;  // (rows that are none: their queries are 0)
-    const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[h] : 0.0f;
-    typename T::x8 qf[D / 16];
-    {
-      const uint16_t* q = c.Q + token * c.q_stride + h * D + 8 * hlf;
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        const u32x4_t raw = ok ? *reinterpret_cast<const u32x4_t*>(q + 16 * s) : u32x4_t{0u, 0u, 0u, 0u};
-        qf[s] = __builtin_bit_cast(typename T::x8, raw);
-      }
-    }
-    // every row sees keys below this
-    int all_hi = hi;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) all_hi = min(all_hi, __shfl_xor(all_hi, d));
-    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-
-    f32x16_t acc[D / 32];
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
-    RowSoftmax sm;
-
-    // The wave's blocks are first + wave, first + wave + 4, ...; lane n holds the page of the
-    // 16 keys n % 2 of its block n / 2 (32 blocks at a time): a table entry is there long
-    // before its block is asked for.
-    const int mine_n = count > wave ? (count - wave + 3) / 4 : 0;
-    const int32_t* table = c.table + static_cast<int64_t>(x.b0) * c.max_pages;
-    int pages = -1;
-    auto fetch_pages = [&](int n) {
-      const int key = (x.block0 + first + wave + 4 * (n + (lane >> 1))) * kCacheBlock + 16 * (lane & 1);
-      pages = -1;
-      if (key < x.end) {
-        pages = table[key >> c.page_shift];
-        if (pages < 0 || pages >= c.n_pages) {
-          tell(c, kCacheBadPage);
-          pages = -1;
-        }
-      }
-    };
-    auto load = [&](int n) {
-      const int key0 = (x.block0 + first + wave + 4 * n) * kCacheBlock;
-      const uint32_t lds = mine_addr + (n & 1) * kStage;
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int page = __builtin_amdgcn_readlane(pages, 2 * (n & 31) + half);
-        const int key = key0 + 16 * half;
-        const int rows = page < 0 ? 0 : clamped(x.end - key, 0, 16);  // what is behind reads zero
-        const int64_t off = ((static_cast<int64_t>(max(page, 0)) * c.Hkv + kvh) << c.page_shift) + (key & page_mask);
-        const __amdgpu_buffer_rsrc_t rk = make_rsrc(c.k_pages + off * D, rows * kRowBytes);
-        const __amdgpu_buffer_rsrc_t rv = make_rsrc(c.v_pages + off * D, rows * kRowBytes);
-#pragma unroll
-        for (int i = 0; i < kHalfLoads; ++i) {
-          load_to_lds(rk, lds + 1024u * (half * kHalfLoads + i), ll.offset(i, kRowBytes));
-          load_to_lds(rv, lds + kTile + 1024u * (half * kHalfLoads + i), ll.offset(i, kRowBytes));
-        }
-      }
-    };
-    if (mine_n > 0) {
-      fetch_pages(0);
-      load(0);
-    }
-    for (int n = 0; n < mine_n; ++n) {
-      if (n + 1 < mine_n) {
-        if (((n + 1) & 31) == 0) fetch_pages(n + 1);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // block n - 1 has been read from LDS
-        load(n + 1);
-        wait_vm<2 * kLoads>();
-      } else {
-        wait_vm<0>();
-      }
-      const unsigned char* kt = mine + (n & 1) * kStage;
-      const lds_u8_t* vt = (const lds_u8_t*)(kt + kTile);
-      const int key0 = (x.block0 + first + wave + 4 * n) * kCacheBlock;
-      f32x16_t sc[1] = {f32x16_t{}};
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) sc[0] = T::mfma(row_frag<T, D>(kt, fr, s, 0), qf[s], sc[0]);
-      if constexpr (!kPlain) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sc[0][i] = score_of(sc[0][i], a.scoring, slope, pos - (key0 + result_row(i, hlf))).value;
-      }
-      if (key0 + kCacheBlock > all_hi || key0 < x.lo) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = key0 + result_row(i, hlf);
-          if (key >= hi || key < x.lo) sc[0][i] = -__builtin_inff();
-        }
-      }
-      typename T::x8 pb[2];
-      bool moved;
-      const float alpha = sm.block<T, 1>(sc, cexp, pb, moved);
-      if (moved) {
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) acc[db] = T::mfma(col_frag<T, D>(vt, fr, db, 16 * t), pb[t], acc[db]);
-    }
-
-    // the waves' results against their common reference, in the order of the waves
-    const float l = sum_halves(sm.l);
-    if (hlf == 0) {
-      s_ref[wave][l32] = sm.m;
-      s_sum[wave][l32] = l;
-    }
-    __syncthreads();  // (also: every wave has read its stages)
-    const float top = fmaxf(fmaxf(s_ref[0][l32], s_ref[1][l32]), fmaxf(s_ref[2][l32], s_ref[3][l32]));
-    {
-      const float f = factor(sm.m, top, cexp);
-      float* out = reinterpret_cast<float*>(stage) + (wave * 32 + l32) * D;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4_t v{acc[db][4 * q] * f, acc[db][4 * q + 1] * f, acc[db][4 * q + 2] * f, acc[db][4 * q + 3] * f};
-          *reinterpret_cast<f32x4_t*>(out + 32 * db + 8 * q + 4 * hlf) = v;
-        }
-    }
-    __syncthreads();
-    if (part < a.max_parts) {
-      float* out = reinterpret_cast<float*>(a.ws + cache_plan_bytes() + part * cache_part_bytes(D));
-      const float* in = reinterpret_cast<const float*>(stage);
-      for (int i = tid; i < 32 * D / 4; i += kThreads) {
-        f32x4_t v = *reinterpret_cast<const f32x4_t*>(in + 4 * i);
-#pragma unroll
-        for (int k = 1; k < 4; ++k) v += *reinterpret_cast<const f32x4_t*>(in + k * 32 * D + 4 * i);
-        *reinterpret_cast<f32x4_t*>(out + 4 * i) = v;
-      }
-      if (tid < 32) {
-        float sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sum = fmaf(s_sum[k][l32], factor(s_ref[k][l32], top, cexp), sum);
-        out[32 * D + l32] = top;
-        out[32 * D + 32 + l32] = sum;
-      }
-    }
-    __syncthreads();  // the stages are free again
-    at += count;
   }
 }
 
-// One wave joins the parts of one row, in order.
+// One wave joins the parts of one row. D / 4 lanes hold the row's products of one part, so that
+// 256 / D parts stand side by side in the wave; each of them sums every (256 / D)th part.
 template <class T, int D, bool kPlain>
 __global__ __launch_bounds__(kThreads) void cache_merge(CacheAttnArgs a) {
+  constexpr int kSide = 256 / D;
   const CacheArgs& c = a.c;
   const int lane = threadIdx.x & 63;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -469,44 +613,71 @@ __global__ __launch_bounds__(kThreads) void cache_merge(CacheAttnArgs a) {
   if (token >= first_token(c, c.batch)) return;
   const int G = c.H / c.Hkv, kvh = h / G;
   const int b = last_below(c.batch, [&](int i) { return c.q_ptr[i] <= token; });
-  const Plan p = plan_in(a.ws);
+  const Plan plan = *plan_in(a.ws);
+  const PlanEntry own = entries_in(a.ws)[a.n_groups + b];
   const float cexp = kPlain ? a.scoring.scale * kLog2e : kLog2e;
-  const int64_t all = p.blocks[0], run = p.blocks[1];
-  const int32_t all_tasks = p.tasks[0];
-  constexpr int kPer = D / 64;
-  float acc[kPer] = {}, m = -__builtin_inff(), l = 0.0f;
-  const int g = group_of(a, b);
-  for (int i = 0; i < 2; ++i) {
-    const int e = i == 0 ? g : a.n_groups + b;
-    if (e < 0) continue;
-    const Entry x = entry_of(a, e);
-    if (x.blocks == 0 || token < x.token0) continue;
+  f32x4_t acc{};
+  float m = -__builtin_inff(), l = 0.0f;
+  const int side = lane / (D / 4), col = 4 * (lane % (D / 4));
+  for (int i = own.group < 0; i < 2; ++i) {
+    const PlanEntry x = i == 0 ? entries_in(a.ws)[own.group] : own;
     const int r = (token - x.token0) * G + (h - kvh * G);
+    if (x.blocks == 0 || r < 0 || r >= x.rows) continue;
     const int tile = r / kCacheTileRows, in_tile = r % kCacheTileRows;
-    if (tile >= x.tiles()) continue;
-    const int64_t start = kvh * all + p.blocks[2 + e] + static_cast<int64_t>(tile) * x.blocks;
-    const int64_t task = static_cast<int64_t>(kvh) * all_tasks + p.tasks[1 + e] + tile;
-    for (int64_t w = start / run; w <= (start + x.blocks - 1) / run; ++w) {
-      if (task + w >= a.max_parts) break;
-      const float* in = reinterpret_cast<const float*>(a.ws + cache_plan_bytes() + (task + w) * cache_part_bytes(D));
-      const float pm = in[32 * D + in_tile], pl = in[32 * D + 32 + in_tile];
-      const float top = fmaxf(m, pm);
-      const float f = factor(m, top, cexp), pf = factor(pm, top, cexp);
-      l = fmaf(l, f, pl * pf);
+    const int start = x.before + (x.rows > kCacheTileRows ? r / kCacheWideRows : 0) * x.blocks;
+    const int w0 = start / plan.run, w1 = (start + x.blocks - 1) / plan.run;
+    const int64_t first = static_cast<int64_t>(kvh) * (plan.tiles + 4 * a.head_workers) + x.tiles + tile + 4 * w0;
+    const int parts = static_cast<int>(min<int64_t>(w1 - w0 + 1, (a.max_parts - first + 3) / 4));
+    const unsigned char* base = a.ws + cache_plan_bytes() + first * cache_part_bytes(D);
+    auto part = [&](int q) { return reinterpret_cast<const float*>(base + int64_t{4} * q * cache_part_bytes(D)); };
+    // 64 parts at a time: their references and sums by the lanes, then their products
+    for (int p0 = 0; p0 < parts; p0 += 64) {
+      const int n = min(64, parts - p0);
+      float pm = -__builtin_inff(), pl = 0.0f;
+      if (lane < n) {
+        pm = part(p0 + lane)[32 * D + in_tile];
+        pl = part(p0 + lane)[32 * D + 32 + in_tile];
+      }
+      constexpr int kAtOnce = 4;
+      f32x4_t in[kAtOnce];
+      auto load = [&](int q0) {  // (behind the end the last one again, which weighs 0 there)
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) acc[k] = fmaf(acc[k], f, in[in_tile * D + lane * kPer + k] * pf);
+        for (int q = 0; q < kAtOnce; ++q)
+          in[q] = *reinterpret_cast<const f32x4_t*>(part(p0 + min(q0 + kSide * q + side, n - 1)) + in_tile * D + col);
+      };
+      load(0);
+      float top = pm;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+      top = fmaxf(top, m);
+      const float f = factor(m, top, cexp), pf = factor(pm, top, cexp);
+      float sum = pl * pf;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+      l = fmaf(l, f, sum);
+      acc *= f;
       m = top;
+      for (int q0 = 0; q0 < n; q0 += kSide * kAtOnce) {
+        if (q0) load(q0);
+#pragma unroll
+        for (int q = 0; q < kAtOnce; ++q) {
+          const int at = q0 + kSide * q + side;
+          const float wt = __shfl(pf, min(at, 63));
+          if (at < n) acc += in[q] * wt;
+        }
+      }
     }
   }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int d = D / 4; d < 64; d *= 2)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[k] += __shfl_xor(acc[k], d);
   const bool none = l == 0.0f;  // nothing visible (its products may hold what masked keys have)
-  const f32x4_t v{none ? 0.0f : acc[0] * inv, none ? 0.0f : acc[kPer - 1] * inv, 0.0f, 0.0f};
-  const uint32_t bits = __builtin_bit_cast(u32x2_t, __builtin_convertvector(v, typename T::x4))[0];
-  uint16_t* out = a.O + row * D + lane * kPer;
-  if constexpr (kPer == 2)
-    *reinterpret_cast<uint32_t*>(out) = bits;
-  else
-    *out = static_cast<uint16_t>(bits);
+  const float inv = none ? 0.0f : 1.0f / l;
+  if (side == 0) {
+    const f32x4_t v = none ? f32x4_t{} : acc * inv;
+    *reinterpret_cast<u32x2_t*>(a.O + row * D + col) = __builtin_bit_cast(u32x2_t, __builtin_convertvector(v, typename T::x4));
+  }
   if (lane == 0 && a.LSE)
     a.LSE[static_cast<int64_t>(h) * c.tokens + token] =
         none ? -__builtin_inff() : fmaf(log2f(l), kLn2, kPlain ? m * a.scoring.scale : m);
@@ -520,7 +691,7 @@ hipError_t append(const AppendArgs& a, hipStream_t s) {
 
 template <class T, int D, bool kPlain>
 hipError_t attend(const CacheAttnArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((cache_attn<T, D, kPlain>), dim3(a.workers), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((cache_attn<T, D, kPlain>), dim3(a.head_workers * a.c.Hkv), dim3(kThreads), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = static_cast<int64_t>(a.c.tokens) * a.c.H;

@@ -9,8 +9,11 @@
 
 namespace csg {
 
-constexpr int kCacheTileRows = 32;     // (token, head) rows of a tile
-constexpr int kCacheBlock = 32;        // keys per inner step of a wave
+constexpr int kCacheTileRows = 32;     // (token, head) rows of a tile, one wave's
+constexpr int kCacheWideRows = 128;    // rows of a wide task: a tile for each of four waves
+constexpr int kCacheBlock = 32;        // keys per inner step of a wave, and unit of work
+constexpr int kCacheWideBlock = 64;    // keys per inner step of a wide task
+constexpr int kCacheMinRun = 4;        // blocks a workgroup takes at least: one for each wave
 constexpr int kMaxCacheEntries = 2048; // sequences and groups of one call
 
 // status bits
@@ -48,20 +51,23 @@ struct CacheAttnArgs {
   const int32_t* group_ptr;  // [n_groups + 1]
   const int32_t* prefix;     // [n_groups]
   int32_t n_groups;
-  int32_t workers;   // workgroups that share the blocks of keys
-  int32_t max_parts; // partial results the workspace holds
+  int32_t head_workers;  // workgroups that share the blocks of keys of a key/value head
+  int32_t dies;          // dies that its workgroups are on
+  int64_t max_parts;     // places of partial results in the workspace
   unsigned char* ws;
   Scoring scoring;
 };
 
 // Workspace: the plan of a call, then partial results of 32 rows each.
-constexpr int64_t cache_plan_bytes() { return 16 + kMaxCacheEntries * 16 + 240; }
+constexpr int64_t cache_plan_bytes() { return 256 + kMaxCacheEntries * 32; }
 constexpr int64_t cache_part_bytes(int head_dim) { return kCacheTileRows * (head_dim + 2) * 4; }
-// Every task (a key/value head, one tile of rows, the keys of a sequence or the shared ones of
-// a group) is cut where the work of one workgroup ends: no more parts than tasks and cuts.
-inline int64_t cache_max_parts(int32_t H, int32_t Hkv, int64_t tokens, int32_t batch, int32_t n_groups, int32_t workers) {
+// Workgroups for each key/value head, all of them as many as are on the device at once (two a
+// CU, by their registers and, for 128 elements a head, 64 KiB of LDS).
+constexpr int32_t cache_head_workers(int32_t cus, int32_t Hkv) { return 2 * cus > Hkv ? 2 * cus / Hkv : 1; }
+// Places of parts: the tiles and four for each workgroup.
+inline int64_t cache_max_parts(int32_t H, int32_t Hkv, int64_t tokens, int32_t batch, int32_t n_groups, int32_t head_workers) {
   const int64_t tiles = tokens * (H / Hkv) / kCacheTileRows * (n_groups > 0 ? 2 : 1) + batch + n_groups;
-  return tiles * Hkv + workers;
+  return (tiles + int64_t{4} * head_workers) * Hkv;
 }
 
 hipError_t launch_cache_append(const AppendArgs& a, bool f16, int head_dim, hipStream_t stream);
