@@ -62,11 +62,8 @@ csg_status check_scores(float* scale, float softcap, int32_t head_dim) {
 csg::Scoring scoring(float scale, float softcap, const float* slopes) {
   constexpr float kLog2e = 1.4426950408889634f;
   csg::Scoring s{};
-  s.scale = scale;
-  if (softcap > 0.0f) {
-    s.cap_in = 2.0f * scale * kLog2e / softcap;
-    s.cap = softcap;
-  }
+  s.unit = softcap > 0.0f ? softcap : scale;
+  if (softcap > 0.0f) s.cap_in = 2.0f * scale * kLog2e / softcap;
   s.slopes = slopes;
   return s;
 }
@@ -136,7 +133,7 @@ csg::DocAttnArgs doc_args(const csg_doc_attn_cfg& c, const void* q, const void* 
   return a;
 }
 
-int64_t grad_workspace(const csg_doc_attn_cfg& c) { return 2 * (c.q_rows + csg::kStatPad) * c.n_heads * 4; }
+int64_t grad_workspace(const csg_doc_attn_cfg& c) { return 2 * c.q_rows * c.n_heads * 4; }
 
 csg_status check_cache(csg_cache_cfg* c) {
   CSG_CHECK(check_heads(c->n_heads, c->n_kv_heads, c->head_dim, c->dtype));
@@ -237,7 +234,7 @@ csg_status csg_doc_attn_grad(const csg_doc_attn_cfg* cfg, const void* q, const v
   csg_doc_attn_cfg c = *cfg;
   CSG_CHECK(check_docs(&c, true));
   if (c.n_docs == 0 || (c.q_rows == 0 && c.k_rows == 0)) return CSG_OK;
-  if (!q_ptr || !k_ptr || !workspace || (c.q_rows > 0 && (!q || !o || !lse || !d_o || !dq)) ||
+  if (!q_ptr || !k_ptr || (c.q_rows > 0 && (!q || !o || !lse || !d_o || !dq || !workspace)) ||
       (c.k_rows > 0 && (!k || !v || !dk || !dv)))
     return fail(CSG_ERR_INVALID, "NULL buffer");
   if (!all_aligned({q, k, v, o, lse, d_o, dq, dk, dv, workspace}))

@@ -3,12 +3,14 @@
 
 namespace csg {
 
+// A score is unit times x, where x is the product less a distance's share, or with a cap (unit
+// is the cap) tanh of the product's share less that of the distance. Kernels keep x: the unit
+// goes into the factor of the exponent.
 struct Scoring {
-  float scale;          // no cap: products to scores
-  float cap_in;         // cap c: products to twice tanh's argument in base 2: 2 scale log2 e / c
-  float cap;            // c; 0: no cap
+  float unit;           // softmax scale; cap c: c
+  float cap_in;         // cap: products to twice tanh's argument in base 2: 2 scale log2 e / c; 0: no cap
   const float* slopes;  // [n_heads], or null
-  bool plain() const { return cap == 0.0f && !slopes; }
+  bool plain() const { return cap_in == 0.0f && !slopes; }
 };
 
 }  // namespace csg

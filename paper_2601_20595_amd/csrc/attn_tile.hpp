@@ -103,6 +103,19 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rs, uint32_t 
       : "memory");
 }
 
+// The same with 4 bytes per lane.
+__device__ __forceinline__ void load_dword_to_lds(__amdgpu_buffer_rsrc_t rs, uint32_t lds, int voff) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\t"
+      "s_mov_b32 m0, %1\n\t"
+      "buffer_load_dword %2, %3, 0 offen lds\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "s"(lds), "v"(voff), "s"(rs)
+      : "memory");
+}
+
 template <int n>
 __device__ __forceinline__ void wait_vm() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory");
@@ -200,25 +213,32 @@ __device__ __forceinline__ float tanh_from_log2(float y) {
   return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y));
 }
 
-// Product of a query and a key to score. distance: between the row's place and the key's.
-// slip: the cap's derivative, 1 - tanh^2.
-struct Score {
-  float value, slip;
-};
-__device__ __forceinline__ Score score_of(float product, const Scoring& p, float slope, int distance) {
-  Score s{product * p.scale, 1.0f};
-  if (p.cap != 0.0f) {
-    const float t = tanh_from_log2(product * p.cap_in);
-    s.value = t * p.cap;
-    s.slip = fmaf(-t, t, 1.0f);
-  }
-  s.value = fmaf(-slope, fabsf(static_cast<float>(distance)), s.value);
-  return s;
+// A head's slope in units of x.
+__device__ __forceinline__ float slope_of(const Scoring& p, int h) { return p.slopes ? p.slopes[h] / p.unit : 0.0f; }
+
+// Products of N tiles to x, where the scores are not plain. `at`: what stands at the tile's row
+// (or column) of register 0, lane hlf 0, less the other side's place; `sign`: it counts down
+// (-1: keys in the registers) or up (1: rows) with the tile's rows.
+template <int N>
+__device__ __forceinline__ void cap_scores(const Scoring& p, f32x16_t (&x)[N]) {
+  if (p.cap_in == 0.0f) return;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[n][r] = tanh_from_log2(x[n][r] * p.cap_in);
+}
+template <int N, int sign>
+__device__ __forceinline__ void bias_scores(const Scoring& p, float slope, int at, int hlf, f32x16_t (&x)[N]) {
+  if (!p.slopes) return;
+  const float from = static_cast<float>(at + sign * 4 * hlf);
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[n][r] = fmaf(-slope, fabsf(from + sign * static_cast<float>(32 * n + result_row(r, 0))), x[n][r]);
 }
 
-// A row's softmax so far, over blocks of N tiles of 32 keys each. Scores x weigh 2^(c (x - m));
-// plain scores stay products (c = scale log2 e), others are in natural units (c = log2 e). The
-// reference m moves to the row's largest x only where a block's weights would leave their
+// A row's softmax so far, over blocks of N tiles of 32 keys each. x weighs 2^(c (x - m)), c =
+// unit log2 e. The reference m moves to the row's largest x only where a block's weights would leave their
 // range; on the first block, where it is -inf, and as long as every score is -inf, always.
 // Both lanes of a row see the same sums and maxima, so they keep the same reference.
 struct RowSoftmax {

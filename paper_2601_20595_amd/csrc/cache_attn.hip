@@ -277,11 +277,8 @@ __device__ __forceinline__ void load_16(const CacheArgs& c, const uint16_t* page
 template <int N, bool kPlain>
 __device__ __forceinline__ void finish_scores(const CacheAttnArgs& a, const Part& p, float slope, int key0, int hlf, f32x16_t (&sc)[N]) {
   if constexpr (!kPlain) {
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        sc[n][i] = score_of(sc[n][i], a.scoring, slope, p.pos - (key0 + 32 * n + result_row(i, hlf))).value;
+    cap_scores<N>(a.scoring, sc);
+    bias_scores<N, -1>(a.scoring, slope, p.pos - key0, hlf, sc);
   }
   if (key0 + 32 * N > p.all_hi || key0 < p.lo) {
 #pragma unroll
@@ -327,8 +324,8 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
     load(0, c.k_pages, k_lds);
     load(0, c.v_pages, v_lds);
   }
-  const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[p.h] : 0.0f;
-  const float cexp = kPlain ? a.scoring.scale * kLog2e : kLog2e;
+  const float slope = kPlain ? 0.0f : slope_of(a.scoring, p.h);
+  const float cexp = a.scoring.unit * kLog2e;
   const Frags<D> fr(lane);
   f32x16_t acc[D / 32];
 #pragma unroll
@@ -435,8 +432,8 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
   typename T::x8 qf[D / 16];
   load_queries<T, D>(a, p, hlf, qf);
   load(0);
-  const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[p.h] : 0.0f;
-  const float cexp = kPlain ? a.scoring.scale * kLog2e : kLog2e;
+  const float slope = kPlain ? 0.0f : slope_of(a.scoring, p.h);
+  const float cexp = a.scoring.unit * kLog2e;
   const Frags<D> fr(lane);
   f32x16_t acc[D / 32];
 #pragma unroll
@@ -603,7 +600,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
 
 // One wave joins the parts of one row. D / 4 lanes hold the row's products of one part, so that
 // 256 / D parts stand side by side in the wave; each of them sums every (256 / D)th part.
-template <class T, int D, bool kPlain>
+template <class T, int D>
 __global__ __launch_bounds__(kThreads) void cache_merge(CacheAttnArgs a) {
   constexpr int kSide = 256 / D;
   const CacheArgs& c = a.c;
@@ -615,7 +612,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge(CacheAttnArgs a) {
   const int b = last_below(c.batch, [&](int i) { return c.q_ptr[i] <= token; });
   const Plan plan = *plan_in(a.ws);
   const PlanEntry own = entries_in(a.ws)[a.n_groups + b];
-  const float cexp = kPlain ? a.scoring.scale * kLog2e : kLog2e;
+  const float cexp = a.scoring.unit * kLog2e;
   f32x4_t acc{};
   float m = -__builtin_inff(), l = 0.0f;
   const int side = lane / (D / 4), col = 4 * (lane % (D / 4));
@@ -680,7 +677,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge(CacheAttnArgs a) {
   }
   if (lane == 0 && a.LSE)
     a.LSE[static_cast<int64_t>(h) * c.tokens + token] =
-        none ? -__builtin_inff() : fmaf(log2f(l), kLn2, kPlain ? m * a.scoring.scale : m);
+        none ? -__builtin_inff() : fmaf(log2f(l), kLn2, m * a.scoring.unit);
 }
 
 template <class T, int D>
@@ -695,7 +692,7 @@ hipError_t attend(const CacheAttnArgs& a, hipStream_t s) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t rows = static_cast<int64_t>(a.c.tokens) * a.c.H;
-  hipLaunchKernelGGL((cache_merge<T, D, kPlain>), dim3((rows + 3) / 4), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((cache_merge<T, D>), dim3((rows + 3) / 4), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
   const int hi = visible(a, p, min(row, p.q_len - 1));
   const int wave_lo = visible(a, p, min(first, p.q_len - 1));  // seen by every row of the wave
   const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kDocBlock - 1) / kDocBlock;
-  const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[h] : 0.0f;
+  const float slope = kPlain ? 0.0f : slope_of(a.scoring, h);
   const int at = row + p.k_len - p.q_len;  // the row's own key
 
   const LoadLane<D> ll(lane);
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
   RowSoftmax sm;
-  const float c = kPlain ? a.scale * kLog2e : kLog2e;
+  const float c = a.scoring.unit * kLog2e;
 
   for (int j = 0; j < nb; ++j) {
     wait_vm<0>();
@@ -174,11 +174,8 @@ __global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
     f32x16_t sc[2];
     products<T, D>(sK + buf, fr, qf, sc);
     if constexpr (!kPlain) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          sc[kb][r] = score_of(sc[kb][r], a.scoring, slope, at - (key0 + 32 * kb + result_row(r, hlf))).value;
+      cap_scores<2>(a.scoring, sc);
+      bias_scores<2, -1>(a.scoring, slope, at - key0, hlf, sc);
     }
     if (key0 + kDocBlock > wave_lo) {
 #pragma unroll
@@ -209,7 +206,7 @@ __global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
   store_rows<T, D>(a.O + (static_cast<int64_t>(p.q0) * a.H + h) * D, static_cast<int64_t>(a.H) * D, row, hlf, acc,
                    total == 0.0f ? 0.0f : 1.0f / total);
   if (hlf == 0)
-    a.LSE[static_cast<int64_t>(h) * a.q_rows + p.q0 + row] = fmaf(log2f(total), kLn2, kPlain ? sm.m * a.scale : sm.m);
+    a.LSE[static_cast<int64_t>(h) * a.q_rows + p.q0 + row] = fmaf(log2f(total), kLn2, sm.m * a.scoring.unit);
 }
 
 // ---- gradient of the queries --------------------------------------------------------------
@@ -234,7 +231,7 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
   const int hi = visible(a, p, min(row, p.q_len - 1));
   const int wave_lo = visible(a, p, min(first, p.q_len - 1));
   const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kDocBlock - 1) / kDocBlock;
-  const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[h] : 0.0f;
+  const float slope = kPlain ? 0.0f : slope_of(a.scoring, h);
   const int at = row + p.k_len - p.q_len;
 
   const LoadLane<D> ll(lane);
@@ -243,19 +240,19 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
   const lds_u8_t* sK_lds = (const lds_u8_t*)sK;
   const uint16_t* kh = a.K + p.k0 * a.k_stride + kvh * D;
   const uint16_t* vh = a.V + p.k0 * a.v_stride + kvh * D;
-  auto load = [&](int j) {
+  auto load = [&](int i, int j) {  // block j into buffer i % 2
     load_tile<D>(kh + static_cast<int64_t>(j) * kDocBlock * a.k_stride, a.k_stride, p.k_len - j * kDocBlock,
-                 sK_addr + (j & 1) * kTile, wave, ll);
+                 sK_addr + (i & 1) * kTile, wave, ll);
     load_tile<D>(vh + static_cast<int64_t>(j) * kDocBlock * a.v_stride, a.v_stride, p.k_len - j * kDocBlock,
-                 sV_addr + (j & 1) * kTile, wave, ll);
+                 sV_addr + (i & 1) * kTile, wave, ll);
   };
-  if (nb > 0) load(0);
+  if (nb > 0) load(0, 0);
 
   typename T::x8 qf[D / 16], gf[D / 16];
   load_rows<T, D>(a.Q + p.q0 * a.q_stride + h * D, a.q_stride, row, ok, hlf, qf);
   const int64_t o_stride = static_cast<int64_t>(a.H) * D, o_head = p.q0 * o_stride + h * D;
   load_rows<T, D>(a.dO + o_head, o_stride, row, ok, hlf, gf);
-  const float c = kPlain ? a.scale * kLog2e : kLog2e;
+  const float c = a.scoring.unit * kLog2e;
   float delta = 0.0f, lse2 = 0.0f;
   {
     typename T::x8 of[D / 16];
@@ -269,47 +266,77 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
       const float lse = a.LSE[static_cast<int64_t>(h) * a.q_rows + p.q0 + row];
       // a row that sees nothing: against +inf every weight is 0
       lse2 = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
-      if (hlf == 0) {
-        const int64_t pitch = a.q_rows + kStatPad;
-        float* st = a.stats + h * pitch + p.q0 + row;
-        st[0] = lse2;
-        st[a.H * pitch] = delta;
-      }
     }
+  }
+  // Block j, whose loads have been issued, is there, and everyone is done with the one before;
+  // the next one's loads are issued (behind the last block the first one's, for the second pass).
+  auto turn = [&](int i, int j, bool more) {
+    wait_vm<0>();
+    __syncthreads();
+    if (more) load(i + 1, j + 1 < nb ? j + 1 : 0);
+    return (i & 1) * kTile;
+  };
+  // P (do . v - delta) of keys key0 .. key0 + 31, times the cap's slip in the second pass; 0 where
+  // masked.
+  auto gradients = [&](int buf, int kb, int key0, bool second, f32x16_t& ds) {
+    f32x16_t sc[1] = {f32x16_t{}}, dp{};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      sc[0] = T::mfma(row_frag<T, D>(sK + buf, fr, s, 32 * kb), qf[s], sc[0]);
+      dp = T::mfma(row_frag<T, D>(sV + buf, fr, s, 32 * kb), gf[s], dp);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dp[r] -= delta;
+    if constexpr (!kPlain) {
+      cap_scores<1>(a.scoring, sc);
+      if (second && a.scoring.cap_in != 0.0f) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= fmaf(-sc[0][r], sc[0][r], 1.0f);
+      }
+      bias_scores<1, -1>(a.scoring, slope, at - key0, hlf, sc);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(sc[0][r], c, -lse2)) * dp[r];
+    if (key0 + 32 > wave_lo) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (key0 + result_row(r, hlf) >= hi) ds[r] = 0.0f;
+    }
+  };
+  // First pass: sum_j P_ij (do_i . v_j) itself. do_i . o_i equals it, but for the rounding of o
+  // (and of the weights that made it), which a row with few large weights cannot afford: there
+  // do . v_j - D cancels. With it alone, gradients of 20 short documents were off by 3.7e-4 of
+  // their norm in fp16, not by 2.9e-4, and of sharp scores in bf16 by 4.6e-3. It still serves
+  // to sum small terms.
+  float more = 0.0f;
+  int i = 0;
+  for (int j = 0; j < nb; ++j, ++i) {
+    const int buf = turn(i, j, true);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      f32x16_t ds;
+      gradients(buf, kb, j * kDocBlock + 32 * kb, false, ds);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) more += ds[r];
+    }
+  }
+  delta += sum_halves(more);
+  if (ok && hlf == 0) {
+    const int64_t pitch = a.q_rows;
+    float* st = a.stats + h * pitch + p.q0 + row;
+    st[0] = lse2;
+    st[a.H * pitch] = -delta;
   }
   f32x16_t acc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
 
-  for (int j = 0; j < nb; ++j) {
-    wait_vm<0>();
-    __syncthreads();  // block j is there, and everyone is done with block j - 1
-    if (j + 1 < nb) load(j + 1);
-    const int buf = (j & 1) * kTile;
+  for (int j = 0; j < nb; ++j, ++i) {
+    const int buf = turn(i, j, j + 1 < nb);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      f32x16_t sc{}, dp{};
-#pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        sc = T::mfma(row_frag<T, D>(sK + buf, fr, s, 32 * kb), qf[s], sc);
-        dp = T::mfma(row_frag<T, D>(sV + buf, fr, s, 32 * kb), gf[s], dp);
-      }
-      const int key0 = j * kDocBlock + 32 * kb;
       f32x16_t ds;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if constexpr (kPlain) {
-          ds[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -lse2)) * (dp[r] - delta);
-        } else {
-          const Score s = score_of(sc[r], a.scoring, slope, at - (key0 + result_row(r, hlf)));
-          ds[r] = __builtin_amdgcn_exp2f(fmaf(s.value, c, -lse2)) * (dp[r] - delta) * s.slip;
-        }
-      }
-      if (key0 + 32 > wave_lo) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key0 + result_row(r, hlf) >= hi) ds[r] = 0.0f;
-      }
+      gradients(buf, kb, j * kDocBlock + 32 * kb, true, ds);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const typename T::x8 w = pack<T>(ds, t);
@@ -325,12 +352,17 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
 // ---- gradients of the keys and values ------------------------------------------------------
 // A tile is 128 keys of one key/value head, 32 a wave, whose gradients stay in registers while
 // the rows that see them pass, head by head of the group: a sum over shared heads is no more
-// than a longer loop, in a fixed order.
+// than a longer loop, in a fixed order. The accumulators leave room for one wave per SIMD (D =
+// 128), which has to keep its own loads ahead of their use.
 template <class T, int D, bool kPlain>
 __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttnArgs a) {
   constexpr int kTile = kDocBlock * D * 2;
-  __shared__ __attribute__((aligned(1024))) unsigned char sQ[2 * kTile];
-  __shared__ __attribute__((aligned(1024))) unsigned char sG[2 * kTile];
+  constexpr bool kAhead = D == 128;
+  constexpr int kRing = kAhead ? 3 : 2;  // steps in LDS: the one at work, the next (kAhead: whose first rows it
+                                         // reads), and one loading
+  __shared__ __attribute__((aligned(1024))) unsigned char sQ[kRing * kTile];
+  __shared__ __attribute__((aligned(1024))) unsigned char sG[kRing * kTile];
+  __shared__ __attribute__((aligned(256))) float s_stats[kRing][2][kDocBlock];  // log-sum-exp, delta
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, hlf = lane >> 5;
   const int kvh = blockIdx.x % a.Hkv;
@@ -351,18 +383,29 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
 
   const LoadLane<D> ll(lane);
   const Frags<D> fr(lane);
-  const uint32_t sQ_addr = lds_address(sQ), sG_addr = lds_address(sG);
-  const lds_u8_t* sQ_lds = (const lds_u8_t*)sQ;
-  const lds_u8_t* sG_lds = (const lds_u8_t*)sG;
+  const uint32_t sQ_addr = lds_address(sQ), sG_addr = lds_address(sG), st_addr = lds_address(s_stats);
   const int64_t o_stride = static_cast<int64_t>(a.H) * D;
+  const int64_t pitch = a.q_rows;
   const uint16_t* qh = a.Q + p.q0 * a.q_stride + kvh * G * D;
   const uint16_t* gh = a.dO + p.q0 * o_stride + kvh * G * D;
-  auto load = [&](int i, int g, int j) {  // step i: block j of head g of the group
-    const int64_t r = r0 + j * kDocBlock;
-    load_tile<D>(qh + r * a.q_stride + g * D, a.q_stride, p.q_len - static_cast<int>(r), sQ_addr + (i & 1) * kTile, wave, ll);
-    load_tile<D>(gh + r * o_stride + g * D, o_stride, p.q_len - static_cast<int>(r), sG_addr + (i & 1) * kTile, wave, ll);
+  int load_g = 0, load_j = 0, load_at = 0;  // the next step to load: block load_j of head load_g, place in the ring
+  auto load = [&]() {
+    const int64_t r = r0 + load_j * kDocBlock;
+    const int rows = p.q_len - static_cast<int>(r);
+    load_tile<D>(qh + r * a.q_stride + load_g * D, a.q_stride, rows, sQ_addr + load_at * kTile, wave, ll);
+    load_tile<D>(gh + r * o_stride + load_g * D, o_stride, rows, sG_addr + load_at * kTile, wave, ll);
+    if (wave < 2) {  // (as loads of the tile, or waiting for them would wait for the tile)
+      const float* st = a.stats + (wave * a.H + kvh * G + load_g) * pitch + p.q0 + r;
+      load_dword_to_lds(make_rsrc(st, 4 * min(kDocBlock, rows)), st_addr + 4 * kDocBlock * (load_at * 2 + wave), 4 * lane);
+    }
+    load_at = load_at + 1 < kRing ? load_at + 1 : 0;
+    if (++load_j == nb) {
+      load_j = 0;
+      ++load_g;
+    }
   };
-  if (steps > 0) load(0, 0, 0);
+  if (steps > 0) load();
+  if (kAhead && steps > 1) load();
 
   typename T::x8 kf[D / 16], vf[D / 16];
   load_rows<T, D>(a.K + p.k0 * a.k_stride + kvh * D, a.k_stride, key, ok, hlf, kf);
@@ -373,67 +416,132 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
     dk[db] = f32x16_t{};
     dv[db] = f32x16_t{};
   }
-  const float c = kPlain ? a.scale * kLog2e : kLog2e;
-  const int64_t pitch = a.q_rows + kStatPad;
-  typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
+  const float c = a.scoring.unit * kLog2e;
 
-  for (int i = 0, g = 0, j = 0; i < steps; ++i) {
-    wait_vm<0>();
-    __syncthreads();
-    const int gn = j + 1 < nb ? g : g + 1, jn = j + 1 < nb ? j + 1 : 0;
-    if (i + 1 < steps) load(i + 1, gn, jn);
-    const int buf = (i & 1) * kTile;
-    const int h = kvh * G + g;
-    const float slope = !kPlain && a.scoring.slopes ? a.scoring.slopes[h] : 0.0f;
+  // kAhead: fragments are read from LDS a phase before they are multiplied: the rows of the next
+  // 32 while the last 32 are summed up, their columns while the products are formed.
+  typename T::x8 rq[D / 16], rg[D / 16], cq[2][D / 32], cg[2][D / 32];
+  f32x4_t lse2[4], delta[4];
+  auto read_stats = [&](int at, int rb) {
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-      const int row0 = r0 + j * kDocBlock + 32 * rb;
-      // (rows up to 63 behind the document's last: other rows' statistics, or the padding)
-      const float* st = a.stats + h * pitch + p.q0 + row0 + 4 * hlf;
-      f32x4_t lse2[4], delta[4];
+    for (int b = 0; b < 4; ++b) {
+      lse2[b] = *reinterpret_cast<const f32x4_t*>(&s_stats[at][0][32 * rb + 8 * b + 4 * hlf]);
+      delta[b] = *reinterpret_cast<const f32x4_t*>(&s_stats[at][1][32 * rb + 8 * b + 4 * hlf]);
+    }
+  };
+  auto row_q = [&](int at, int rb, int s) { return row_frag<T, D>(sQ + at * kTile, fr, s, 32 * rb); };
+  auto row_g = [&](int at, int rb, int s) { return row_frag<T, D>(sG + at * kTile, fr, s, 32 * rb); };
+  auto col_q = [&](int at, int rb, int t, int db) {
+    return col_frag<T, D>((const lds_u8_t*)(sQ + at * kTile), fr, db, 32 * rb + 16 * t);
+  };
+  auto col_g = [&](int at, int rb, int t, int db) {
+    return col_frag<T, D>((const lds_u8_t*)(sG + at * kTile), fr, db, 32 * rb + 16 * t);
+  };
+  auto read_rows = [&](int at, int rb) {
+    read_stats(at, rb);
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        lse2[b] = *reinterpret_cast<const f32x4u_t*>(st + 8 * b);
-        delta[b] = *reinterpret_cast<const f32x4u_t*>(st + a.H * pitch + 8 * b);
-      }
-      f32x16_t sc{}, dp{};
+    for (int s = 0; s < D / 16; ++s) {
+      rq[s] = row_q(at, rb, s);
+      rg[s] = row_g(at, rb, s);
+    }
+  };
+  // q . k and do . v - delta of 32 rows (half rb of the step in place `at`) and the wave's keys
+  auto products = [&](int at, int rb, f32x16_t& sc, f32x16_t& dp) {
+    if constexpr (!kAhead) read_stats(at, rb);
+    sc = f32x16_t{};
 #pragma unroll
-      for (int s = 0; s < D / 16; ++s) {
-        sc = T::mfma(row_frag<T, D>(sQ + buf, fr, s, 32 * rb), kf[s], sc);
-        dp = T::mfma(row_frag<T, D>(sG + buf, fr, s, 32 * rb), vf[s], dp);
-      }
-      f32x16_t w, ds;
+    for (int r = 0; r < 16; ++r) dp[r] = delta[r >> 2][r & 3];  // (negative)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float l2 = lse2[r >> 2][r & 3], dl = delta[r >> 2][r & 3];
-        if constexpr (kPlain) {
-          w[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], c, -l2));
-          ds[r] = w[r] * (dp[r] - dl);
-        } else {
-          const Score s = score_of(sc[r], a.scoring, slope, row0 + result_row(r, hlf) + shift - key);
-          w[r] = __builtin_amdgcn_exp2f(fmaf(s.value, c, -l2));
-          ds[r] = w[r] * (dp[r] - dl) * s.slip;
-        }
-      }
-      if (row0 < wave_hi || row0 + 32 > p.q_len) {
+    for (int s = 0; s < D / 16; ++s) {
+      sc = T::mfma(kAhead ? rq[s] : row_q(at, rb, s), kf[s], sc);
+      dp = T::mfma(kAhead ? rg[s] : row_g(at, rb, s), vf[s], dp);
+    }
+    if constexpr (kAhead) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int row = row0 + result_row(r, hlf);
-          if (row < lo || row >= p.q_len) w[r] = ds[r] = 0.0f;
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const typename T::x8 wt = pack<T>(w, t), dt = pack<T>(ds, t);
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) {
-          dv[db] = T::mfma(col_frag<T, D>(sG_lds + buf, fr, db, 32 * rb + 16 * t), wt, dv[db]);
-          dk[db] = T::mfma(col_frag<T, D>(sQ_lds + buf, fr, db, 32 * rb + 16 * t), dt, dk[db]);
+          cg[t][db] = col_g(at, rb, t, db);
+          cq[t][db] = col_q(at, rb, t, db);
         }
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);    // a product
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);  // reads from LDS
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // them to weights and gradients of scores
+  auto weigh = [&](int row0, float slope, bool masked, f32x16_t& x, f32x16_t& dp) {
+    f32x16_t sc[1] = {x};
+    if constexpr (!kPlain) {
+      cap_scores<1>(a.scoring, sc);
+      if (a.scoring.cap_in != 0.0f) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] *= fmaf(-sc[0][r], sc[0][r], 1.0f);
+      }
+      bias_scores<1, 1>(a.scoring, slope, row0 + shift - key, hlf, sc);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r] = __builtin_amdgcn_exp2f(fmaf(sc[0][r], c, -lse2[r >> 2][r & 3]));
+      dp[r] *= x[r];
+    }
+    if (masked) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = row0 + result_row(r, hlf);
+        const bool out = row < lo || row >= p.q_len;
+        x[r] = out ? 0.0f : x[r];
+        dp[r] = out ? 0.0f : dp[r];
       }
     }
-    g = gn;
-    j = jn;
+  };
+  auto accumulate = [&](int at, int rb, int next_at, int next_rb, const f32x16_t& w, const f32x16_t& ds) {
+    if constexpr (kAhead) {
+      __builtin_amdgcn_sched_barrier(0);
+      read_rows(next_at, next_rb);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const typename T::x8 wt = pack<T>(w, t), dt = pack<T>(ds, t);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        dv[db] = T::mfma(kAhead ? cg[t][db] : col_g(at, rb, t, db), wt, dv[db]);
+        dk[db] = T::mfma(kAhead ? cq[t][db] : col_q(at, rb, t, db), dt, dk[db]);
+      }
+    }
+    if constexpr (kAhead) {
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  for (int i = 0, g = 0, j = 0, at = 0; i < steps; ++i) {
+    wait_vm<0>();
+    __syncthreads();  // step i (kAhead: i + 1 too) is there, and everyone is done with step i - 1
+    if (i + kRing - 1 < steps) load();
+    if (kAhead && i == 0) read_rows(0, 0);
+    const int next = at + 1 < kRing ? at + 1 : 0;
+    const int row0 = r0 + j * kDocBlock;
+    const float slope = kPlain ? 0.0f : slope_of(a.scoring, kvh * G + g);
+    const bool masked = row0 < wave_hi || row0 + kDocBlock > p.q_len;
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      f32x16_t sc, dp;
+      products(at, rb, sc, dp);
+      weigh(row0 + 32 * rb, slope, masked, sc, dp);
+      accumulate(at, rb, rb == 0 ? at : next, rb ^ 1, sc, dp);  // (behind the last step: old rows, unused)
+    }
+    at = next;
+    if (++j == nb) {
+      j = 0;
+      ++g;
+    }
   }
   if (!ok) return;
   store_rows<T, D>(a.dK + p.k0 * a.dk_stride + kvh * D, a.dk_stride, key, hlf, dk, a.scale);

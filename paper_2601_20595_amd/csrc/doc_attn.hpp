@@ -11,7 +11,6 @@ namespace csg {
 
 constexpr int kDocTileRows = 128;  // (row, head) pairs of a tile: 4 waves of 32
 constexpr int kDocBlock = 64;      // keys (gradient of keys and values: rows) per inner step
-constexpr int kStatPad = 64;       // rows behind the last that a step may read statistics of
 
 struct DocAttnArgs {
   const uint16_t* Q;   // rows of H heads of D elements, q_stride elements apart; K, V: Hkv heads
@@ -23,7 +22,7 @@ struct DocAttnArgs {
   uint16_t* dQ;
   uint16_t* dK;
   uint16_t* dV;
-  float* stats;        // [2][H][q_rows + kStatPad]: log-sum-exp in base 2, then sum(dO . O)
+  float* stats;        // [2][H][q_rows]: log-sum-exp in base 2, then less sum_j P_ij (dO_i . V_j)
   const int32_t* q_ptr;   // [n_docs + 1]
   const int32_t* k_ptr;   // [n_docs + 1]
   const int32_t* prefix;  // [n_docs], or null

@@ -64,7 +64,7 @@ def test_gradients_refuse(change, status):
 
 def test_documents_refuse_buffers():
     need = csg.csg_doc_attn_grad_workspace(_docs())
-    assert need == 2 * 8 * (100 + 64) * 4
+    assert need == 2 * 8 * 100 * 4
     for i in (0, 1, 2, 3, 4, 7, 8):
         args = [P, P, P, P, P, 0, 0, P, P]
         args[i] = 0
