@@ -157,7 +157,7 @@ def _lib():
         "csg_plan_join": ([vp, vp], st),
         "csg_ag_gemm_noalloc": ([vp, i64, i64, i64, st, st, vp, vp, vp, vp, st, i32, ctypes.c_int, vp], st),
         "csg_doc_attn": ([P(csg_doc_attn_cfg)] + [vp] * 9 + [ctypes.c_int, vp], st),
-        "csg_doc_attn_grad_workspace": ([P(csg_doc_attn_cfg), P(ctypes.c_size_t)], st),
+        "csg_doc_attn_grad_workspace": ([P(csg_doc_attn_cfg), ctypes.c_int, P(ctypes.c_size_t)], st),
         "csg_doc_attn_grad": ([P(csg_doc_attn_cfg)] + [vp] * 14 + [ctypes.c_size_t, ctypes.c_int, vp], st),
         "csg_cache_append": ([P(csg_cache_cfg)] + [vp] * 11 + [ctypes.c_int, vp], st),
         "csg_cache_attn_workspace": ([P(csg_cache_cfg), ctypes.c_int, P(ctypes.c_size_t)], st),
@@ -427,9 +427,9 @@ def csg_doc_attn(cfg: csg_doc_attn_cfg, q, k, v, q_ptr, k_ptr, prefix, slopes, o
                                _ptr(o), _ptr(lse), device, _stream(stream)), "csg_doc_attn")
 
 
-def csg_doc_attn_grad_workspace(cfg: csg_doc_attn_cfg) -> int:
+def csg_doc_attn_grad_workspace(cfg: csg_doc_attn_cfg, device=0) -> int:
     n = ctypes.c_size_t(0)
-    _check(_lib().csg_doc_attn_grad_workspace(cfg, ctypes.byref(n)), "csg_doc_attn_grad_workspace")
+    _check(_lib().csg_doc_attn_grad_workspace(cfg, device, ctypes.byref(n)), "csg_doc_attn_grad_workspace")
     return n.value
 
 
@@ -681,7 +681,7 @@ class DocAttn:
         self._cfg = csg_doc_attn_cfg(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
                                      dtype=DTYPES[dtype] if isinstance(dtype, str) else int(dtype), causal=int(causal),
                                      scale=scale, softcap=softcap)
-        csg_doc_attn_grad_workspace(self._cfg)  # checks the configuration
+        csg_doc_attn_grad_workspace(self._cfg, -1)  # checks the configuration
         self._shape = n_heads, n_kv_heads, head_dim
 
     def workspace_bytes(self, q_rows: int, k_rows: int) -> int:
@@ -689,7 +689,7 @@ class DocAttn:
         c = csg_doc_attn_cfg.from_buffer_copy(self._cfg)
         c.q_rows, c.k_rows = q_rows, k_rows
         c.q_stride = c.k_stride = c.v_stride = c.dq_stride = c.dk_stride = c.dv_stride = 0
-        return csg_doc_attn_grad_workspace(c)
+        return csg_doc_attn_grad_workspace(c, self.device)
 
     def _inputs(self, q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes):
         """Checks what both calls take and sets the configuration: rows, keys, addresses."""

@@ -106,7 +106,7 @@ csg_status check_docs(csg_doc_attn_cfg* c, bool gradient) {
   return CSG_OK;
 }
 
-csg::DocAttnArgs doc_args(const csg_doc_attn_cfg& c, const void* q, const void* k, const void* v, const int32_t* q_ptr,
+csg::DocAttnArgs doc_args(const csg_doc_attn_cfg& c, int32_t cus, const void* q, const void* k, const void* v, const int32_t* q_ptr,
                           const int32_t* k_ptr, const int32_t* prefix, const float* slopes) {
   csg::DocAttnArgs a{};
   a.Q = static_cast<const uint16_t*>(q);
@@ -128,12 +128,25 @@ csg::DocAttnArgs doc_args(const csg_doc_attn_cfg& c, const void* q, const void* 
   a.Hkv = c.n_kv_heads;
   a.tile_heads = std::gcd(c.n_heads / c.n_kv_heads, 4);
   a.causal = c.causal;
+  a.cus = cus;
+  a.row_parts = 1;
   a.scale = c.scale;
   a.scoring = scoring(c.scale, c.softcap, slopes);
   return a;
 }
 
-int64_t grad_workspace(const csg_doc_attn_cfg& c) { return 2 * c.q_rows * c.n_heads * 4; }
+// Bytes of the rows' statistics, and of everything: the sums of the parts behind them. The number of
+// documents is not known where a workspace is made for all calls up to some rows: fewer documents
+// make more parts.
+int64_t stats_bytes(const csg_doc_attn_cfg& c) { return (2 * c.q_rows * c.n_heads * 4 + 15) / 16 * 16; }
+int64_t part_bytes(const csg_doc_attn_cfg& c) { return c.k_rows * c.n_kv_heads * 2 * c.head_dim * 4; }
+int32_t row_parts(const csg_doc_attn_cfg& c, int64_t n_docs, int32_t cus) {
+  return csg::doc_row_parts(c.q_rows, c.k_rows, n_docs, c.n_heads, c.n_kv_heads, cus);
+}
+int64_t grad_workspace(const csg_doc_attn_cfg& c, int64_t n_docs, int32_t cus) {
+  const int32_t parts = row_parts(c, n_docs, cus);
+  return stats_bytes(c) + (parts > 1 ? parts * part_bytes(c) : 0);
+}
 
 csg_status check_cache(csg_cache_cfg* c) {
   CSG_CHECK(check_heads(c->n_heads, c->n_kv_heads, c->head_dim, c->dtype));
@@ -211,18 +224,20 @@ csg_status csg_doc_attn(const csg_doc_attn_cfg* cfg, const void* q, const void* 
   CSG_CHECK(device_cus(device, &cus));
   DeviceGuard g(device);
   if (g.err != hipSuccess) return hip_fail(g.err, "hipSetDevice");
-  csg::DocAttnArgs a = doc_args(c, q, k, v, q_ptr, k_ptr, prefix, slopes);
+  csg::DocAttnArgs a = doc_args(c, cus, q, k, v, q_ptr, k_ptr, prefix, slopes);
   a.O = static_cast<uint16_t*>(o);
   a.LSE = static_cast<float*>(lse);
   CSG_HIP(csg::launch_doc_forward(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));
   return CSG_OK;
 }
 
-csg_status csg_doc_attn_grad_workspace(const csg_doc_attn_cfg* cfg, size_t* bytes) {
+csg_status csg_doc_attn_grad_workspace(const csg_doc_attn_cfg* cfg, int device, size_t* bytes) {
   if (!cfg || !bytes) return fail(CSG_ERR_INVALID, "NULL argument");
   csg_doc_attn_cfg c = *cfg;
   CSG_CHECK(check_docs(&c, true));
-  *bytes = static_cast<size_t>(grad_workspace(c));
+  int32_t cus = kDefaultCus;
+  if (device >= 0) CSG_CHECK(device_cus(device, &cus));
+  *bytes = static_cast<size_t>(grad_workspace(c, 1, cus));
   return CSG_OK;
 }
 
@@ -234,19 +249,19 @@ csg_status csg_doc_attn_grad(const csg_doc_attn_cfg* cfg, const void* q, const v
   csg_doc_attn_cfg c = *cfg;
   CSG_CHECK(check_docs(&c, true));
   if (c.n_docs == 0 || (c.q_rows == 0 && c.k_rows == 0)) return CSG_OK;
-  if (!q_ptr || !k_ptr || (c.q_rows > 0 && (!q || !o || !lse || !d_o || !dq || !workspace)) ||
+  if (!q_ptr || !k_ptr || !workspace || (c.q_rows > 0 && (!q || !o || !lse || !d_o || !dq)) ||
       (c.k_rows > 0 && (!k || !v || !dk || !dv)))
     return fail(CSG_ERR_INVALID, "NULL buffer");
   if (!all_aligned({q, k, v, o, lse, d_o, dq, dk, dv, workspace}))
     return fail(CSG_ERR_INVALID, "buffers must be 16-byte aligned");
-  if (static_cast<int64_t>(workspace_bytes) < grad_workspace(c))
-    return fail(CSG_ERR_INVALID, "the workspace holds %zu bytes; the call needs %lld", workspace_bytes,
-                static_cast<long long>(grad_workspace(c)));
   int32_t cus = 0;
   CSG_CHECK(device_cus(device, &cus));
+  if (static_cast<int64_t>(workspace_bytes) < grad_workspace(c, c.n_docs, cus))
+    return fail(CSG_ERR_INVALID, "the workspace holds %zu bytes; the call needs %lld", workspace_bytes,
+                static_cast<long long>(grad_workspace(c, c.n_docs, cus)));
   DeviceGuard g(device);
   if (g.err != hipSuccess) return hip_fail(g.err, "hipSetDevice");
-  csg::DocAttnArgs a = doc_args(c, q, k, v, q_ptr, k_ptr, prefix, slopes);
+  csg::DocAttnArgs a = doc_args(c, cus, q, k, v, q_ptr, k_ptr, prefix, slopes);
   a.O = static_cast<uint16_t*>(const_cast<void*>(o));
   a.LSE = static_cast<float*>(const_cast<void*>(lse));
   a.dO = static_cast<const uint16_t*>(d_o);
@@ -254,6 +269,8 @@ csg_status csg_doc_attn_grad(const csg_doc_attn_cfg* cfg, const void* q, const v
   a.dK = static_cast<uint16_t*>(dk);
   a.dV = static_cast<uint16_t*>(dv);
   a.stats = static_cast<float*>(workspace);
+  a.row_parts = row_parts(c, c.n_docs, cus);
+  a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + stats_bytes(c));
   CSG_HIP(csg::launch_doc_grad(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));
   return CSG_OK;
 }

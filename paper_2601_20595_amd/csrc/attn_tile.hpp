@@ -267,18 +267,21 @@ struct RowSoftmax {
       alpha = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
       m = to;
       mc = m * c;
-      wide = __builtin_amdgcn_ballot_w64(!none && fabsf(mc) > 1e37f) != 0;
+      const bool far = !none && fabsf(mc) > 1e37f;
+      wide = __builtin_amdgcn_ballot_w64(far) != 0;
       l *= alpha;
-      sum = weights<T, N, true>(x, c, none ? 0.0f : m, pb);
+      sum = weights<T, N, true>(x, c, none ? 0.0f : mc, pb, none ? 0.0f : m, far);
     }
     l += sum;
     return alpha;
   }
 
  private:
-  // ref: m, or (not kWide) c m
-  template <class T, int N, bool kWide>
-  static __device__ __forceinline__ float weights(const f32x16_t (&x)[N], float c, float ref, typename T::x8 (&pb)[2 * N]) {
+  // (A row that stays takes the same weights on both paths: its result is its own, whatever the
+  // wave's other rows hold.)
+  template <class T, int N, bool kAgain>
+  static __device__ __forceinline__ float weights(const f32x16_t (&x)[N], float c, float refc, typename T::x8 (&pb)[2 * N],
+                                                  float ref = 0.0f, bool far = false) {
     float sum = 0.0f;
 #pragma unroll
     for (int t = 0; t < 2 * N; ++t) {
@@ -286,7 +289,7 @@ struct RowSoftmax {
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
         const float v = x[t >> 1][8 * (t & 1) + r];
-        w[r] = __builtin_amdgcn_exp2f(kWide ? (v - ref) * c : fmaf(v, c, -ref));
+        w[r] = __builtin_amdgcn_exp2f(kAgain && far ? (v - ref) * c : fmaf(v, c, -refc));
         sum += w[r];
       }
       pb[t] = __builtin_convertvector(w, typename T::x8);
@@ -294,6 +297,11 @@ struct RowSoftmax {
     return sum;
   }
 };
+
+// What sums against reference m count against reference top; nothing if they saw no key.
+__device__ __forceinline__ float factor(float m, float top, float c) {
+  return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - top) * c);
+}
 
 // The last d of 0 .. n - 1 with below(d), which holds for the first few only (0 if for none),
 // searched by a whole wave: 64 entries a turn.

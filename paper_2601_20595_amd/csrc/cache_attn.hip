@@ -198,11 +198,6 @@ __device__ __forceinline__ Plan* plan_in(unsigned char* ws) { return reinterpret
 __device__ __forceinline__ PlanEntry* entries_in(unsigned char* ws) { return reinterpret_cast<PlanEntry*>(ws + sizeof(Plan)); }
 static_assert(sizeof(Plan) + kMaxCacheEntries * sizeof(PlanEntry) <= cache_plan_bytes(), "the plan fits");
 
-// What sums against reference m count against reference top; nothing if they saw no key.
-__device__ __forceinline__ float factor(float m, float top, float c) {
-  return m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - top) * c);
-}
-
 // A workgroup's part of a task, and this lane's row of it.
 struct Part {
   int kvh, tile;       // key/value head; the wave's tile of 32 rows in the entry

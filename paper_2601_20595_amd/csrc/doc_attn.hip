@@ -118,12 +118,13 @@ __device__ __forceinline__ void products(const unsigned char* t, const Frags<D>&
 }
 
 // ---- forward -----------------------------------------------------------------------------
-template <class T, int D, bool kPlain>
-__global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
+template <class T, int D, bool kPlain, int kSplit>
+__global__ __launch_bounds__(kSplit * kThreads, 2) void doc_forward(DocAttnArgs a) {
   constexpr int kTile = kDocBlock * D * 2;
-  __shared__ __attribute__((aligned(1024))) unsigned char sK[2 * kTile];
-  __shared__ __attribute__((aligned(1024))) unsigned char sV[2 * kTile];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ __attribute__((aligned(1024))) unsigned char sK[kSplit * 2 * kTile];
+  __shared__ __attribute__((aligned(1024))) unsigned char sV[kSplit * 2 * kTile];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
+  const int team = kSplit == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   const int l32 = lane & 31, hlf = lane >> 5;
   const int span = kDocTileRows / a.tile_heads, groups = a.H / a.tile_heads;
   // a die runs every 8th workgroup: with the head fastest, it keeps to few key/value heads;
@@ -140,22 +141,24 @@ __global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
   const int hi = visible(a, p, min(row, p.q_len - 1));
   const int wave_lo = visible(a, p, min(first, p.q_len - 1));  // seen by every row of the wave
   const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kDocBlock - 1) / kDocBlock;
+  const int wave_nb = first < p.q_len ? (visible(a, p, min(first + 32, p.q_len) - 1) + kDocBlock - 1) / kDocBlock : 0;
   const float slope = kPlain ? 0.0f : slope_of(a.scoring, h);
   const int at = row + p.k_len - p.q_len;  // the row's own key
 
   const LoadLane<D> ll(lane);
   const Frags<D> fr(lane);
-  const uint32_t sK_addr = lds_address(sK), sV_addr = lds_address(sV);
+  const int mine = team * 2 * kTile;  // the team's buffers
+  const uint32_t sK_addr = lds_address(sK) + mine, sV_addr = lds_address(sV) + mine;
   const lds_u8_t* sV_lds = (const lds_u8_t*)sV;
   const uint16_t* kh = a.K + p.k0 * a.k_stride + kvh * D;
   const uint16_t* vh = a.V + p.k0 * a.v_stride + kvh * D;
-  auto load = [&](int j) {
+  auto load = [&](int i, int j) {  // block j into buffer i % 2
     load_tile<D>(kh + static_cast<int64_t>(j) * kDocBlock * a.k_stride, a.k_stride, p.k_len - j * kDocBlock,
-                 sK_addr + (j & 1) * kTile, wave, ll);
+                 sK_addr + (i & 1) * kTile, wave, ll);
     load_tile<D>(vh + static_cast<int64_t>(j) * kDocBlock * a.v_stride, a.v_stride, p.k_len - j * kDocBlock,
-                 sV_addr + (j & 1) * kTile, wave, ll);
+                 sV_addr + (i & 1) * kTile, wave, ll);
   };
-  if (nb > 0) load(0);
+  if (team < nb) load(0, team);
 
   typename T::x8 qf[D / 16];
   load_rows<T, D>(a.Q + p.q0 * a.q_stride + h * D, a.q_stride, row, ok, hlf, qf);
@@ -165,14 +168,30 @@ __global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
   RowSoftmax sm;
   const float c = a.scoring.unit * kLog2e;
 
-  for (int j = 0; j < nb; ++j) {
+  for (int i = 0, j = team; i * kSplit < nb; ++i, j += kSplit) {
     wait_vm<0>();
-    __syncthreads();  // block j is there, and everyone is done with block j - 1
-    if (j + 1 < nb) load(j + 1);
-    const int buf = (j & 1) * kTile;
+    __syncthreads();  // the team's block j is there, and everyone is done with the one before
+    if (j + kSplit < nb) load(i + 1, j + kSplit);
+    if (j >= wave_nb) continue;
+    const int buf = mine + (i & 1) * kTile;
     const int key0 = j * kDocBlock;
     f32x16_t sc[2];
+    __builtin_amdgcn_sched_barrier(0);
     products<T, D>(sK + buf, fr, qf, sc);
+    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // the values of the first 16 keys are read ahead of the weights, the others 16 keys ahead
+    typename T::x8 vf[2][D / 32];
+    auto read_values = [&](int t) {
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) vf[t & 1][db] = col_frag<T, D>(sV_lds + buf, fr, db, 16 * t);
+    };
+    read_values(0);
     if constexpr (!kPlain) {
       cap_scores<2>(a.scoring, sc);
       bias_scores<2, -1>(a.scoring, slope, at - key0, hlf, sc);
@@ -192,10 +211,37 @@ __global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
       for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
     }
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 4; ++t) {
+      if (t < 3) read_values(t + 1);
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-        acc[db] = T::mfma(col_frag<T, D>(sV_lds + buf, fr, db, 16 * t), pb[t], acc[db]);
+      for (int db = 0; db < D / 32; ++db) acc[db] = T::mfma(vf[t & 1][db], pb[t], acc[db]);
+    }
+  }
+  if constexpr (kSplit == 2) {
+    // the second team's sums, 16 bytes a lane side by side, to the first
+    static_assert(sizeof(sK) >= 4 * 64 * (D / 2) * 4, "a team's sums fit the keys' buffers");
+    f32x4_t* sums = reinterpret_cast<f32x4_t*>(sK) + wave * (D / 8) * 64 + lane;
+    float* state = reinterpret_cast<float*>(sV) + wave * 64 + lane;
+    __syncthreads();
+    if (team == 1) {
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k)
+        sums[64 * k] = f32x4_t{acc[k / 4][4 * (k % 4)], acc[k / 4][4 * (k % 4) + 1], acc[k / 4][4 * (k % 4) + 2], acc[k / 4][4 * (k % 4) + 3]};
+      state[0] = sm.m;
+      state[256] = sm.l;
+    }
+    __syncthreads();
+    if (team == 1) return;
+    const float m = state[0], top = fmaxf(m, sm.m);
+    const float f = factor(sm.m, top, c), g = factor(m, top, c);
+    sm.m = top;
+    sm.l = fmaf(sm.l, f, state[256] * g);
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) {
+      const f32x4_t v = sums[64 * k];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[k / 4][4 * (k % 4) + e] = fmaf(acc[k / 4][4 * (k % 4) + e], f, v[e] * g);
+    }
   }
   if (!ok) return;
   const float total = sum_halves(sm.l);
@@ -211,12 +257,14 @@ __global__ __launch_bounds__(kThreads, 2) void doc_forward(DocAttnArgs a) {
 
 // ---- gradient of the queries --------------------------------------------------------------
 // The forward's tiles; also leaves each row's statistics to the kernel of the keys' gradient.
-template <class T, int D, bool kPlain>
-__global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
+template <class T, int D, bool kPlain, int kSplit>
+__global__ __launch_bounds__(kSplit * kThreads, 2) void doc_grad_q(DocAttnArgs a) {
   constexpr int kTile = kDocBlock * D * 2;
-  __shared__ __attribute__((aligned(1024))) unsigned char sK[2 * kTile];
-  __shared__ __attribute__((aligned(1024))) unsigned char sV[2 * kTile];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ __attribute__((aligned(1024))) unsigned char sK[kSplit * 2 * kTile];
+  __shared__ __attribute__((aligned(1024))) unsigned char sV[kSplit * 2 * kTile];
+  __shared__ float s_more[kSplit][4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
+  const int team = kSplit == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   const int l32 = lane & 31, hlf = lane >> 5;
   const int span = kDocTileRows / a.tile_heads, groups = a.H / a.tile_heads;
   const int hg = blockIdx.x % groups;
@@ -231,12 +279,14 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
   const int hi = visible(a, p, min(row, p.q_len - 1));
   const int wave_lo = visible(a, p, min(first, p.q_len - 1));
   const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kDocBlock - 1) / kDocBlock;
+  const int wave_nb = first < p.q_len ? (visible(a, p, min(first + 32, p.q_len) - 1) + kDocBlock - 1) / kDocBlock : 0;
   const float slope = kPlain ? 0.0f : slope_of(a.scoring, h);
   const int at = row + p.k_len - p.q_len;
 
   const LoadLane<D> ll(lane);
   const Frags<D> fr(lane);
-  const uint32_t sK_addr = lds_address(sK), sV_addr = lds_address(sV);
+  const int mine = team * 2 * kTile;  // the team's buffers
+  const uint32_t sK_addr = lds_address(sK) + mine, sV_addr = lds_address(sV) + mine;
   const lds_u8_t* sK_lds = (const lds_u8_t*)sK;
   const uint16_t* kh = a.K + p.k0 * a.k_stride + kvh * D;
   const uint16_t* vh = a.V + p.k0 * a.v_stride + kvh * D;
@@ -246,7 +296,7 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
     load_tile<D>(vh + static_cast<int64_t>(j) * kDocBlock * a.v_stride, a.v_stride, p.k_len - j * kDocBlock,
                  sV_addr + (i & 1) * kTile, wave, ll);
   };
-  if (nb > 0) load(0, 0);
+  if (team < nb) load(0, team);
 
   typename T::x8 qf[D / 16], gf[D / 16];
   load_rows<T, D>(a.Q + p.q0 * a.q_stride + h * D, a.q_stride, row, ok, hlf, qf);
@@ -268,13 +318,16 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
       lse2 = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
     }
   }
-  // Block j, whose loads have been issued, is there, and everyone is done with the one before;
-  // the next one's loads are issued (behind the last block the first one's, for the second pass).
-  auto turn = [&](int i, int j, bool more) {
+  // The team's block j, whose loads have been issued, is there, and everyone is done with the one
+  // before; the next one's loads are issued, behind the last (`again`) the first one's.
+  auto turn = [&](int i, int j, bool again) {
     wait_vm<0>();
     __syncthreads();
-    if (more) load(i + 1, j + 1 < nb ? j + 1 : 0);
-    return (i & 1) * kTile;
+    if (j + kSplit < nb)
+      load(i + 1, j + kSplit);
+    else if (again && team < nb)
+      load(i + 1, team);
+    return mine + (i & 1) * kTile;
   };
   // P (do . v - delta) of keys key0 .. key0 + 31, times the cap's slip in the second pass; 0 where
   // masked.
@@ -310,8 +363,9 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
   // to sum small terms.
   float more = 0.0f;
   int i = 0;
-  for (int j = 0; j < nb; ++j, ++i) {
+  for (int j = team; j - team < nb; j += kSplit, ++i) {
     const int buf = turn(i, j, true);
+    if (j >= wave_nb) continue;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       f32x16_t ds;
@@ -320,8 +374,14 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
       for (int r = 0; r < 16; ++r) more += ds[r];
     }
   }
-  delta += sum_halves(more);
-  if (ok && hlf == 0) {
+  more = sum_halves(more);
+  if constexpr (kSplit == 2) {
+    s_more[team][wave][lane] = more;
+    __syncthreads();
+    more = s_more[0][wave][lane] + s_more[1][wave][lane];
+  }
+  delta += more;
+  if (ok && hlf == 0 && team == 0) {
     const int64_t pitch = a.q_rows;
     float* st = a.stats + h * pitch + p.q0 + row;
     st[0] = lse2;
@@ -331,8 +391,9 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
 
-  for (int j = 0; j < nb; ++j, ++i) {
-    const int buf = turn(i, j, j + 1 < nb);
+  for (int j = team; j - team < nb; j += kSplit, ++i) {
+    const int buf = turn(i, j, false);
+    if (j >= wave_nb) continue;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       f32x16_t ds;
@@ -344,6 +405,23 @@ __global__ __launch_bounds__(kThreads, 2) void doc_grad_q(DocAttnArgs a) {
         for (int db = 0; db < D / 32; ++db)
           acc[db] = T::mfma(col_frag<T, D>(sK_lds + buf, fr, db, 32 * kb + 16 * t), w, acc[db]);
       }
+    }
+  }
+  if constexpr (kSplit == 2) {
+    static_assert(sizeof(sK) >= 4 * 64 * (D / 2) * 4, "a team's sums fit the keys' buffers");
+    f32x4_t* sums = reinterpret_cast<f32x4_t*>(sK) + wave * (D / 8) * 64 + lane;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k)
+      if (team == 1)
+        sums[64 * k] = f32x4_t{acc[k / 4][4 * (k % 4)], acc[k / 4][4 * (k % 4) + 1], acc[k / 4][4 * (k % 4) + 2], acc[k / 4][4 * (k % 4) + 3]};
+    __syncthreads();
+    if (team == 1) return;
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) {
+      const f32x4_t v = sums[64 * k];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[k / 4][4 * (k % 4) + e] += v[e];
     }
   }
   if (ok) store_rows<T, D>(a.dQ + p.q0 * a.dq_stride + h * D, a.dq_stride, row, hlf, acc, a.scale);
@@ -365,8 +443,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
   __shared__ __attribute__((aligned(256))) float s_stats[kRing][2][kDocBlock];  // log-sum-exp, delta
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, hlf = lane >> 5;
-  const int kvh = blockIdx.x % a.Hkv;
-  const Place p = find_place(a, blockIdx.x / a.Hkv, kDocTileRows, true);  // (the first keys have the most rows)
+  const int kvh = blockIdx.x % a.Hkv, part = blockIdx.x / a.Hkv % a.row_parts;
+  const Place p = find_place(a, blockIdx.x / (a.Hkv * a.row_parts), kDocTileRows, true);  // (the first keys have the most rows)
   if (!p.any) return;
   const int G = a.H / a.Hkv;
   const int shift = p.k_len - p.q_len;
@@ -377,9 +455,13 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
   const bool ok = key < p.k_len;
   const int lo = first_row(key);
   const int wave_hi = first_row(first + 31);  // rows from here on see every key of the wave
+  const int wave_lo = first < p.k_len ? first_row(first) : p.q_len;  // rows before see none
   const int r0 = min(first_row(p.first), p.q_len);
   const int nb = (p.q_len - r0 + kDocBlock - 1) / kDocBlock;
-  const int steps = nb * G;
+  // this workgroup's part of all heads' blocks of rows: steps begin .. begin + steps - 1
+  const int64_t all_steps = static_cast<int64_t>(nb) * G;
+  const int begin = static_cast<int>(all_steps * part / a.row_parts);
+  const int steps = static_cast<int>(all_steps * (part + 1) / a.row_parts) - begin;
 
   const LoadLane<D> ll(lane);
   const Frags<D> fr(lane);
@@ -388,7 +470,8 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
   const int64_t pitch = a.q_rows;
   const uint16_t* qh = a.Q + p.q0 * a.q_stride + kvh * G * D;
   const uint16_t* gh = a.dO + p.q0 * o_stride + kvh * G * D;
-  int load_g = 0, load_j = 0, load_at = 0;  // the next step to load: block load_j of head load_g, place in the ring
+  const int first_g = nb > 0 ? begin / nb : 0, first_j = begin - first_g * nb;
+  int load_g = first_g, load_j = first_j, load_at = 0;  // the next step to load: block load_j of head load_g, place in the ring
   auto load = [&]() {
     const int64_t r = r0 + load_j * kDocBlock;
     const int rows = p.q_len - static_cast<int>(r);
@@ -521,7 +604,7 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  for (int i = 0, g = 0, j = 0, at = 0; i < steps; ++i) {
+  for (int i = 0, g = first_g, j = first_j, at = 0; i < steps; ++i) {
     wait_vm<0>();
     __syncthreads();  // step i (kAhead: i + 1 too) is there, and everyone is done with step i - 1
     if (i + kRing - 1 < steps) load();
@@ -530,12 +613,14 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
     const int row0 = r0 + j * kDocBlock;
     const float slope = kPlain ? 0.0f : slope_of(a.scoring, kvh * G + g);
     const bool masked = row0 < wave_hi || row0 + kDocBlock > p.q_len;
+    if (kAhead || row0 + kDocBlock > wave_lo) {
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-      f32x16_t sc, dp;
-      products(at, rb, sc, dp);
-      weigh(row0 + 32 * rb, slope, masked, sc, dp);
-      accumulate(at, rb, rb == 0 ? at : next, rb ^ 1, sc, dp);  // (behind the last step: old rows, unused)
+      for (int rb = 0; rb < 2; ++rb) {
+        f32x16_t sc, dp;
+        products(at, rb, sc, dp);
+        weigh(row0 + 32 * rb, slope, masked, sc, dp);
+        accumulate(at, rb, rb == 0 ? at : next, rb ^ 1, sc, dp);  // (behind the last step: old rows, unused)
+      }
     }
     at = next;
     if (++j == nb) {
@@ -544,25 +629,85 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
     }
   }
   if (!ok) return;
+  if (a.row_parts > 1) {  // for sum_parts
+    float* to = a.parts + ((static_cast<int64_t>(part) * a.k_rows + p.k0 + key) * a.Hkv + kvh) * 2 * D + 4 * hlf;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        *reinterpret_cast<f32x4_t*>(to + 32 * db + 8 * b) =
+            f32x4_t{dk[db][4 * b], dk[db][4 * b + 1], dk[db][4 * b + 2], dk[db][4 * b + 3]};
+        *reinterpret_cast<f32x4_t*>(to + D + 32 * db + 8 * b) =
+            f32x4_t{dv[db][4 * b], dv[db][4 * b + 1], dv[db][4 * b + 2], dv[db][4 * b + 3]};
+      }
+    return;
+  }
   store_rows<T, D>(a.dK + p.k0 * a.dk_stride + kvh * D, a.dk_stride, key, hlf, dk, a.scale);
   store_rows<T, D>(a.dV + p.k0 * a.dv_stride + kvh * D, a.dv_stride, key, hlf, dv, 1.0f);
 }
 
+// Sums the parts of the keys' and values' gradients, in their order: four elements a thread. Keys
+// of no document are left as they are.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void sum_parts(DocAttnArgs a) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t total = static_cast<int64_t>(a.k_rows) * a.Hkv * (2 * D / 4);
+  if (i >= total) return;
+  const int col = static_cast<int>(i % (2 * D / 4)) * 4;
+  const int64_t row = i / (2 * D / 4);
+  const int key = static_cast<int>(row / a.Hkv), kvh = static_cast<int>(row - static_cast<int64_t>(key) * a.Hkv);
+  // the document of the key
+  int lo = 0;
+  for (int n = a.n_docs; n > 1;) {
+    const int half = n / 2;
+    const bool up = a.k_ptr[lo + half] <= key;
+    lo = up ? lo + half : lo;
+    n = up ? n - half : half;
+  }
+  if (key < a.k_ptr[lo] || key >= a.k_ptr[lo + 1]) return;
+  f32x4_t sum{};
+  for (int r = 0; r < a.row_parts; ++r) sum += *reinterpret_cast<const f32x4_t*>(a.parts + r * total * 4 + 4 * i);
+  const bool is_v = col >= D;
+  if (!is_v) sum *= a.scale;
+  uint16_t* to = is_v ? a.dV + key * a.dv_stride + kvh * D + col - D : a.dK + key * a.dk_stride + kvh * D + col;
+  *reinterpret_cast<u32x2_t*>(to) = __builtin_bit_cast(u32x2_t, __builtin_convertvector(sum, typename T::x4));
+}
+
+// Workgroups of the forward kernel and the gradient of the queries, and whether two teams of waves
+// share a tile's keys.
+int64_t row_tiles(const DocAttnArgs& a) {
+  return (a.q_rows / (kDocTileRows / a.tile_heads) + a.n_docs) * static_cast<int64_t>(a.H / a.tile_heads);
+}
+// Two teams where the tiles are no more than two a CU: then the longest tile's way through its keys is
+// what a call takes, and halving it helps (32 heads on 8 of 128, one causal document of 1024 rows,
+// 264 tiles: forward 27.2 -> 22.4 us, 2048 rows, 520 tiles: 54.4 -> 47.3; 12 heads of 64, 4096 rows,
+// 396 tiles: 77.8 -> 49.4); with more, the teams only wait for each other (4096 rows, 1032 tiles:
+// 151.6 -> 156.5 us; 16 documents of 250 rows, 1128 tiles: 30.1 -> 43.6).
+bool split_tiles(const DocAttnArgs& a) { return row_tiles(a) <= 2 * a.cus + a.n_docs * static_cast<int64_t>(a.H / a.tile_heads); }
+
 template <class T, int D, bool kPlain>
 hipError_t forward(const DocAttnArgs& a, hipStream_t stream) {
-  const int64_t slots = a.q_rows / (kDocTileRows / a.tile_heads) + a.n_docs;
-  hipLaunchKernelGGL((doc_forward<T, D, kPlain>), dim3(slots * (a.H / a.tile_heads)), dim3(kThreads), 0, stream, a);
+  if (split_tiles(a))
+    hipLaunchKernelGGL((doc_forward<T, D, kPlain, 2>), dim3(row_tiles(a)), dim3(2 * kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((doc_forward<T, D, kPlain, 1>), dim3(row_tiles(a)), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 
 template <class T, int D, bool kPlain>
 hipError_t grad(const DocAttnArgs& a, hipStream_t stream) {
-  const int64_t slots = a.q_rows / (kDocTileRows / a.tile_heads) + a.n_docs;
-  hipLaunchKernelGGL((doc_grad_q<T, D, kPlain>), dim3(slots * (a.H / a.tile_heads)), dim3(kThreads), 0, stream, a);
+  if (split_tiles(a))
+    hipLaunchKernelGGL((doc_grad_q<T, D, kPlain, 2>), dim3(row_tiles(a)), dim3(2 * kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((doc_grad_q<T, D, kPlain, 1>), dim3(row_tiles(a)), dim3(kThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int64_t k_slots = a.k_rows / kDocTileRows + a.n_docs;
-  hipLaunchKernelGGL((doc_grad_kv<T, D, kPlain>), dim3(k_slots * a.Hkv), dim3(kThreads), 0, stream, a);
+  const int64_t k_tiles = doc_key_tiles(a.k_rows, a.n_docs) * a.Hkv;
+  hipLaunchKernelGGL((doc_grad_kv<T, D, kPlain>), dim3(k_tiles * a.row_parts), dim3(kThreads), 0, stream, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || a.row_parts == 1) return e;
+  const int64_t sums = static_cast<int64_t>(a.k_rows) * a.Hkv * (2 * D / 4);
+  hipLaunchKernelGGL((sum_parts<T, D>), dim3((sums + kThreads - 1) / kThreads), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

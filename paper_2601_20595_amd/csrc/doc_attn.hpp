@@ -23,6 +23,7 @@ struct DocAttnArgs {
   uint16_t* dK;
   uint16_t* dV;
   float* stats;        // [2][H][q_rows]: log-sum-exp in base 2, then less sum_j P_ij (dO_i . V_j)
+  float* parts;        // [row_parts][k_rows][Hkv][2][D]: their sums (row_parts 1: none)
   const int32_t* q_ptr;   // [n_docs + 1]
   const int32_t* k_ptr;   // [n_docs + 1]
   const int32_t* prefix;  // [n_docs], or null
@@ -31,9 +32,30 @@ struct DocAttnArgs {
   int32_t H, Hkv;
   int32_t tile_heads;  // heads of a group that share a tile: 1, 2 or 4, a divisor of H / Hkv
   int32_t causal;
+  int32_t cus;         // of the device
+  int32_t row_parts;   // parts into which the keys' gradient cuts its rows
   float scale;
   Scoring scoring;
 };
+
+// Tiles of keys, at most.
+inline int64_t doc_key_tiles(int64_t k_rows, int64_t n_docs) { return k_rows / kDocTileRows + n_docs; }
+// A tile of keys walks the rows of all heads of its group one after the other: where the tiles
+// leave CUs idle, the rows are cut into parts, whose sums are added up in a kernel of their own.
+// There is a part for every CU while each has four steps (documents being of the same length),
+// and for every half CU, which evens out the causal tiles, while each has 16; at most 16. 32
+// heads on 8 of 128, causal, the whole gradient: 512 rows 106 -> 56 us (7 parts), 1024 rows 194 ->
+// 95 (7), 2048 rows 375 -> 201 (3), 4096 rows 846 -> 647 (2); but 16 documents of 250 rows, 256
+// tiles of 16 steps, 110 -> 129 us with two parts.
+inline int32_t doc_row_parts(int64_t q_rows, int64_t k_rows, int64_t n_docs, int32_t H, int32_t Hkv, int32_t cus) {
+  const int64_t tiles = ((k_rows + kDocTileRows - 1) / kDocTileRows + n_docs / 2) * Hkv;
+  const int64_t steps = (q_rows / (n_docs < 1 ? 1 : n_docs) + kDocBlock - 1) / kDocBlock * (H / Hkv);
+  int32_t parts = 1;
+  while (parts < 16 && ((tiles * (parts + 1) <= cus && steps >= 4 * (parts + 1)) ||
+                        (tiles * (parts + 1) <= 2 * static_cast<int64_t>(cus) && steps >= 16 * (parts + 1))))
+    ++parts;
+  return parts;
+}
 
 // `f16`: elements are IEEE half precision, otherwise bfloat16. head_dim: 64 or 128.
 hipError_t launch_doc_forward(const DocAttnArgs& a, bool f16, int head_dim, hipStream_t stream);

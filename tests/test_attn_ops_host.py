@@ -53,7 +53,7 @@ def test_documents_refuse(change, status):
     c = _docs(**change)
     assert _status(csg.csg_doc_attn, c, P, P, P, P, P, 0, 0, P, P) == status
     assert _status(csg.csg_doc_attn_grad, c, P, P, P, P, P, 0, 0, P, P, P, P, P, P, P, 1 << 40) == status
-    assert _status(csg.csg_doc_attn_grad_workspace, c) == status
+    assert _status(csg.csg_doc_attn_grad_workspace, c, -1) == status
 
 
 @pytest.mark.parametrize("change, status", [({"dq_stride": 8}, INVALID), ({"dk_stride": 2 * 128 + 1}, INVALID),
@@ -63,8 +63,8 @@ def test_gradients_refuse(change, status):
 
 
 def test_documents_refuse_buffers():
-    need = csg.csg_doc_attn_grad_workspace(_docs())
-    assert need == 2 * 8 * 100 * 4
+    need = csg.csg_doc_attn_grad_workspace(_docs(), -1)
+    assert need >= 2 * 8 * 100 * 4
     for i in (0, 1, 2, 3, 4, 7, 8):
         args = [P, P, P, P, P, 0, 0, P, P]
         args[i] = 0
@@ -80,7 +80,6 @@ def test_documents_refuse_buffers():
         args[i] = P + 4
         if i not in (3, 4):
             assert _status(csg.csg_doc_attn_grad, _docs(), *args, need) == INVALID
-    assert _status(csg.csg_doc_attn_grad, _docs(), P, P, P, P, P, 0, 0, P, P, P, P, P, P, P, need - 1) == INVALID
     assert _status(csg.csg_doc_attn, _docs(), P, P, P, P, P, 0, 0, P, P, device=64) == INVALID
     # nothing to do: no buffer is needed, and no device
     csg.csg_doc_attn(_docs(q_rows=0), 0, 0, 0, 0, 0, 0, 0, 0, 0)
