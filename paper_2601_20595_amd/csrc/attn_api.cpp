@@ -171,7 +171,7 @@ csg_status check_cache_attn(csg_cache_cfg* c) {
   // blocks of keys times tasks that read them, at most; they are counted in 32 bits
   const int64_t tasks = 2 * (c->tokens * (c->n_heads / c->n_kv_heads) / csg::kCacheWideRows) + c->batch + c->n_groups;
   const int64_t blocks = static_cast<int64_t>(c->max_pages) * c->page_size / csg::kCacheBlock + 1;
-  if (tasks > 0 && blocks > 0x7fffffff / tasks)
+  if (tasks > 0 && blocks + csg::kCacheTaskCost > 0x7fffffff / tasks)
     return fail(CSG_ERR_UNSUPPORTED, "max_pages pages for every sequence are too many keys for one launch");
   return CSG_OK;
 }

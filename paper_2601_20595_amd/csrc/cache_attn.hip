@@ -123,8 +123,9 @@ __global__ __launch_bounds__(kThreads) void cache_append(AppendArgs a) {
 // task: the four waves take different blocks of 32 keys for the same rows, each at its own
 // pace. More rows make wide tasks of 128, 32 a wave, whose waves share the keys. Every key/value
 // head has the same number of workgroups. All tasks' blocks of 32 keys stand in one row (by
-// entry, task, block) that is cut into equal runs, one a workgroup of the head: every workgroup
-// reads the same number of keys, whatever the lengths are. What a workgroup has of a task is a
+// entry, task, block), each task's behind kCacheTaskCost empty ones, and the row is cut into equal
+// runs, one a workgroup of the head: every workgroup has the same to do, whatever the lengths
+// are. What a workgroup has of a task is a
 // part: for each tile of 32 rows, its weights' sums and products against its own reference,
 // which cache_merge joins. With the tiles counted through, tile t of run w is in place t + 4 w:
 // of two parts one after the other, the second has a later tile, or the next run and at most
@@ -133,20 +134,41 @@ struct Entry {
   int token0, rows;    // first token, (token, head) rows
   int b0, b1;          // its sequences; the first one's pages are read
   int lo, end;         // keys
-  bool own;            // the keys of one sequence, up to its end
+  int own;             // the keys of one sequence, up to its end
+  int group;           // its group, -1: none
   int block0, blocks;  // blocks of keys that hold them
   __device__ __forceinline__ int tiles() const { return (rows + kCacheTileRows - 1) / kCacheTileRows; }
   __device__ __forceinline__ bool wide() const { return rows > kCacheTileRows; }
   __device__ __forceinline__ int tasks() const { return wide() ? (rows + kCacheWideRows - 1) / kCacheWideRows : 1; }
+  // a task's units of work: its blocks, behind what beginning and ending it costs
+  __device__ __forceinline__ int span() const { return blocks > 0 ? kCacheTaskCost + blocks : 0; }
+};
+
+// The groups of a call where they are given.
+struct GlobalGroups {
+  const CacheAttnArgs& a;
+  __device__ __forceinline__ int first(int g) const { return clamped(a.group_ptr[g], 0, a.c.batch); }
+  __device__ __forceinline__ int prefix(int g) const {  // no longer than the first sequence
+    const int b = first(g);
+    return b < a.c.batch ? clamped(a.prefix[g], 0, length_of(a.c, b)) : 0;
+  }
+};
+// The same, copied into LDS.
+struct LocalGroups {
+  const int32_t* firsts;
+  const int32_t* prefixes;
+  __device__ __forceinline__ int first(int g) const { return firsts[g]; }
+  __device__ __forceinline__ int prefix(int g) const { return prefixes[g]; }
 };
 
 // The group of sequence b, -1 if it has none.
-__device__ __forceinline__ int group_of(const CacheAttnArgs& a, int b) {
-  if (a.n_groups == 0 || b < a.group_ptr[0] || b >= a.group_ptr[a.n_groups]) return -1;
+template <class Groups>
+__device__ __forceinline__ int group_of(const CacheAttnArgs& a, const Groups& groups, int b) {
+  if (a.n_groups == 0 || b < groups.first(0) || b >= groups.first(a.n_groups)) return -1;
   int lo = 0, n = a.n_groups;
   while (n > 1) {
     const int half = n / 2;
-    if (a.group_ptr[lo + half] <= b) {
+    if (groups.first(lo + half) <= b) {
       lo += half;
       n -= half;
     } else {
@@ -156,26 +178,24 @@ __device__ __forceinline__ int group_of(const CacheAttnArgs& a, int b) {
   return lo;
 }
 
-__device__ __forceinline__ int prefix_of(const CacheAttnArgs& a, int g) {
-  const int b = clamped(a.group_ptr[g], 0, a.c.batch);
-  return b < a.c.batch ? clamped(a.prefix[g], 0, length_of(a.c, b)) : 0;
-}
-
-__device__ __forceinline__ Entry entry_of(const CacheAttnArgs& a, int e) {
+template <class Groups>
+__device__ __forceinline__ Entry entry_of(const CacheAttnArgs& a, const Groups& groups, int e) {
   const CacheArgs& c = a.c;
   Entry x;
-  x.own = e >= a.n_groups;
-  if (!x.own) {
-    x.b0 = clamped(a.group_ptr[e], 0, c.batch);
-    x.b1 = clamped(a.group_ptr[e + 1], x.b0, c.batch);
+  x.group = -1;
+  if (e < a.n_groups) {
+    x.own = 0;
+    x.b0 = groups.first(e);
+    x.b1 = max(x.b0, groups.first(e + 1));
     x.lo = 0;
-    x.end = x.b1 > x.b0 ? prefix_of(a, e) : 0;
+    x.end = x.b1 > x.b0 ? groups.prefix(e) : 0;
   } else {
+    x.own = 1;
     x.b0 = e - a.n_groups;
     x.b1 = x.b0 + 1;
     x.end = length_of(c, x.b0);
-    const int g = group_of(a, x.b0);
-    x.lo = g < 0 ? 0 : min(prefix_of(a, g), x.end);
+    x.group = group_of(a, groups, x.b0);
+    x.lo = x.group < 0 ? 0 : min(groups.prefix(x.group), x.end);
   }
   x.token0 = first_token(c, x.b0);
   x.rows = x.b1 > x.b0 ? max(0, first_token(c, x.b1) - x.token0) * (c.H / c.Hkv) : 0;
@@ -184,13 +204,13 @@ __device__ __forceinline__ Entry entry_of(const CacheAttnArgs& a, int e) {
   return x;
 }
 
-// The plan of a call in the workspace, for cache_merge: an entry's blocks and tiles before it,
+// The plan of a call in the workspace, for cache_merge: an entry's units and tiles before it,
 // its own blocks, rows and first token; of a sequence, its group's entry too (-1: none).
 struct PlanEntry {
   int32_t before, tiles, blocks, rows, token0, group, unused[2];
 };
 struct Plan {
-  int32_t run;    // blocks of a run
+  int32_t run;    // units of a run
   int32_t tiles;  // tiles of one key/value head
   int32_t unused[6];
 };
@@ -210,8 +230,8 @@ struct Part {
   int all_hi;          // every row of the wave sees keys below this
 };
 
-template <int D>
-__device__ __forceinline__ void locate_row(const CacheAttnArgs& a, const Entry& x, int l32, Part& p) {
+// `local`: the sequences' entries, where they are in LDS.
+__device__ __forceinline__ void locate_row(const CacheAttnArgs& a, const Entry& x, const Entry* local, int l32, Part& p) {
   const CacheArgs& c = a.c;
   const int G = c.H / c.Hkv;
   const int r = p.tile * kCacheTileRows + l32;
@@ -224,11 +244,14 @@ __device__ __forceinline__ void locate_row(const CacheAttnArgs& a, const Entry& 
     int b = x.b0;
     for (int n = x.b1 - x.b0; n > 1;) {  // the last of the group's sequences that starts by then
       const int half = n / 2;
-      const bool up = c.q_ptr[b + half] <= p.token;
+      const bool up = (local ? local[b + half].token0 : first_token(c, b + half)) <= p.token;
       b = up ? b + half : b;
       n = up ? n - half : half;
     }
-    p.pos = length_of(c, b) - (first_token(c, b + 1) - p.token);
+    if (local)
+      p.pos = local[b].end - (local[b].token0 + local[b].rows / G - p.token);
+    else
+      p.pos = length_of(c, b) - (first_token(c, b + 1) - p.token);
   }
   p.hi = p.ok ? min(p.pos + 1, p.end) : p.end;
   int all_hi = p.hi;
@@ -291,7 +314,7 @@ __device__ __forceinline__ void finish_scores(const CacheAttnArgs& a, const Part
 // Two workgroups a CU keep 128 KiB in flight, and one streams while the other begins or ends
 // a part.
 template <class T, int D, bool kPlain>
-__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, Part& p, unsigned char* stage, float (&s_ref)[4][32],
+__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, Part& p, unsigned char* stage, float (&s_ref)[4][32],
                                             float (&s_sum)[4][32], float* out, int lane, int wave) {
   constexpr int kTile = kCacheBlock * 2 * D, kLoads = kCacheBlock / kLoadRows<D>;
   const CacheArgs& c = a.c;
@@ -311,14 +334,14 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
     for (int half = 0; half < 2; ++half)
       load_16<D>(c, from, p, __builtin_amdgcn_readlane(pages, 2 * (n & 31) + half), key_of(n) + 16 * half, lds + half * (kTile / 2), ll);
   };
-  if (mine_n > 0) fetch(0);
-  locate_row<D>(a, x, l32, p);
-  typename T::x8 qf[D / 16];
-  load_queries<T, D>(a, p, hlf, qf);
   if (mine_n > 0) {
+    fetch(0);
     load(0, c.k_pages, k_lds);
     load(0, c.v_pages, v_lds);
   }
+  locate_row(a, x, local, l32, p);
+  typename T::x8 qf[D / 16];
+  load_queries<T, D>(a, p, hlf, qf);
   const float slope = kPlain ? 0.0f : slope_of(a.scoring, p.h);
   const float cexp = a.scoring.unit * kLog2e;
   const Frags<D> fr(lane);
@@ -403,7 +426,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 
 // A wide part: blocks of 64 keys in two buffers, which all waves read.
 template <class T, int D, bool kPlain>
-__device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, Part& p, unsigned char* stage, float* out, int lane,
+__device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, Part& p, unsigned char* stage, float* out, int lane,
                                           int wave) {
   constexpr int kTile = kCacheWideBlock * 2 * D;
   const CacheArgs& c = a.c;
@@ -423,10 +446,10 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
     load_16<D>(c, c.v_pages, p, page, key, to + kTile, ll);
   };
   fetch(0);
-  locate_row<D>(a, x, l32, p);
+  load(0);
+  locate_row(a, x, local, l32, p);
   typename T::x8 qf[D / 16];
   load_queries<T, D>(a, p, hlf, qf);
-  load(0);
   const float slope = kPlain ? 0.0f : slope_of(a.scoring, p.h);
   const float cexp = a.scoring.unit * kLog2e;
   const Frags<D> fr(lane);
@@ -480,9 +503,11 @@ template <class T, int D, bool kPlain>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * 2 * kCacheBlock * 2 * D];
   __shared__ float s_ref[4][32], s_sum[4][32];
-  __shared__ int s_wave_blocks[4], s_wave_tiles[4], s_entry, s_first, s_tiles;
+  __shared__ int s_wave_units[4], s_wave_tiles[4], s_entry, s_first, s_tiles;
+  __shared__ Entry s_entries[kThreads];
   static_assert(sizeof(stage) == 2 * 2 * kCacheWideBlock * 2 * D, "the same memory holds the wide parts' buffers");
   static_assert(sizeof(stage) >= 4 * 32 * D * 4, "and the waves' results");
+  static_assert(sizeof(stage) >= (2 * kMaxCacheEntries + 1) * 4, "and, before, the groups");
 
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -493,85 +518,108 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
   int w = blockIdx.x / c.Hkv;
   if (a.head_workers % a.dies == 0) w = w % a.dies * (a.head_workers / a.dies) + w / a.dies;
 
-  // Each thread counts some entries; blocks and tiles before each of them by a scan.
+  int32_t* firsts = reinterpret_cast<int32_t*>(stage);
+  const LocalGroups local{firsts, firsts + a.n_groups + 1};
+  if (a.n_groups > 0) {
+    const GlobalGroups global{a};
+    for (int g = tid; g <= a.n_groups; g += kThreads) {
+      firsts[g] = global.first(g);
+      if (g < a.n_groups) firsts[a.n_groups + 1 + g] = global.prefix(g);
+    }
+    __syncthreads();
+  }
+  // Each thread counts some entries; units and tiles before each of them by a scan. Where a thread
+  // has one entry, everyone finds it in LDS.
   const int per = (n_entries + kThreads - 1) / kThreads;
-  int blocks = 0, tiles = 0;
+  int units = 0, tiles = 0;
   for (int i = 0; i < per; ++i) {
     const int e = tid * per + i;
     if (e >= n_entries) break;
-    const Entry x = entry_of(a, e);
-    blocks += x.tasks() * x.blocks;
+    const Entry x = entry_of(a, local, e);
+    if (per == 1) s_entries[e] = x;
+    units += x.tasks() * x.span();
     tiles += x.tiles();
   }
-  const int own_blocks = blocks, own_tiles = tiles;
+  const int own_units = units, own_tiles = tiles;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int ub = __shfl_up(blocks, d), ut = __shfl_up(tiles, d);
+    const int uu = __shfl_up(units, d), ut = __shfl_up(tiles, d);
     if (lane >= d) {
-      blocks += ub;
+      units += uu;
       tiles += ut;
     }
   }
   if (lane == 63) {
-    s_wave_blocks[wave] = blocks;
+    s_wave_units[wave] = units;
     s_wave_tiles[wave] = tiles;
   }
   __syncthreads();
-  blocks -= own_blocks;
+  units -= own_units;
   tiles -= own_tiles;
   for (int i = 0; i < wave; ++i) {
-    blocks += s_wave_blocks[i];
+    units += s_wave_units[i];
     tiles += s_wave_tiles[i];
   }
-  const int all = __builtin_amdgcn_readfirstlane(s_wave_blocks[0] + s_wave_blocks[1] + s_wave_blocks[2] + s_wave_blocks[3]);
+  const int all = __builtin_amdgcn_readfirstlane(s_wave_units[0] + s_wave_units[1] + s_wave_units[2] + s_wave_units[3]);
   const int all_tiles = __builtin_amdgcn_readfirstlane(s_wave_tiles[0] + s_wave_tiles[1] + s_wave_tiles[2] + s_wave_tiles[3]);
   const int run = max(kCacheMinRun, (all + a.head_workers - 1) / a.head_workers);
-  if (blockIdx.x == 0) {  // for cache_merge
-    int before = blocks, tiles_before = tiles;
+  const int begin = w * run;
+  // for cache_merge, and the entry where the run begins
+  if (blockIdx.x == 0 || (units <= begin && begin < units + own_units)) {
+    int before = units, tiles_before = tiles;
     for (int i = 0; i < per; ++i) {
       const int e = tid * per + i;
       if (e >= n_entries) break;
-      const Entry x = entry_of(a, e);
-      entries_in(a.ws)[e] = {before, tiles_before, x.blocks, x.rows, x.token0, x.own ? group_of(a, x.b0) : -1, {0, 0}};
-      before += x.tasks() * x.blocks;
-      tiles_before += x.tiles();
-      if (x.own && length_of(c, x.b0) != c.lens[x.b0]) tell(c, kCacheBadLength);
-    }
-    if (tid == 0) *plan_in(a.ws) = {run, all_tiles, {0, 0, 0, 0, 0, 0}};
-  }
-  const int begin = w * run;
-  if (begin >= all) return;
-  int left = min(run, all - begin);
-  // the entry where the run begins
-  if (blocks <= begin && begin < blocks + own_blocks) {
-    for (int i = 0; i < per; ++i) {
-      const int e = tid * per + i;
-      const Entry x = entry_of(a, e);
-      const int n = x.tasks() * x.blocks;
-      if (begin < blocks + n) {
+      const Entry x = per == 1 ? s_entries[e] : entry_of(a, local, e);
+      const int n = x.tasks() * x.span();
+      if (before <= begin && begin < before + n) {
         s_entry = e;
-        s_first = begin - blocks;
-        s_tiles = tiles;
-        break;
+        s_first = begin - before;
+        s_tiles = tiles_before;
       }
-      blocks += n;
-      tiles += x.tiles();
+      if (blockIdx.x == 0) {
+        entries_in(a.ws)[e] = {before, tiles_before, x.blocks, x.rows, x.token0, x.group, {0, 0}};
+        if (x.own && x.end != c.lens[x.b0]) tell(c, kCacheBadLength);
+      }
+      before += n;
+      tiles_before += x.tiles();
     }
+    if (blockIdx.x == 0 && tid == 0) *plan_in(a.ws) = {run, all_tiles, {0, 0, 0, 0, 0, 0}};
   }
+  if (begin >= all) return;
   __syncthreads();
+  int left = min(run, all - begin);
   int e = __builtin_amdgcn_readfirstlane(s_entry), in_entry = __builtin_amdgcn_readfirstlane(s_first);
   int tiles_before = __builtin_amdgcn_readfirstlane(s_tiles);
   const int64_t places = static_cast<int64_t>(kvh) * (all_tiles + 4 * a.head_workers) + 4 * w;
+  const Entry* sequences = per == 1 ? s_entries + a.n_groups : nullptr;
   while (left > 0) {
-    const Entry x = entry_of(a, e);
-    const int n = x.tasks() * x.blocks;
+    Entry x;
+    if (per == 1) {
+      // (the same in every lane)
+      x.token0 = __builtin_amdgcn_readfirstlane(s_entries[e].token0);
+      x.rows = __builtin_amdgcn_readfirstlane(s_entries[e].rows);
+      x.b0 = __builtin_amdgcn_readfirstlane(s_entries[e].b0);
+      x.b1 = __builtin_amdgcn_readfirstlane(s_entries[e].b1);
+      x.lo = __builtin_amdgcn_readfirstlane(s_entries[e].lo);
+      x.end = __builtin_amdgcn_readfirstlane(s_entries[e].end);
+      x.own = __builtin_amdgcn_readfirstlane(s_entries[e].own);
+      x.block0 = __builtin_amdgcn_readfirstlane(s_entries[e].block0);
+      x.blocks = __builtin_amdgcn_readfirstlane(s_entries[e].blocks);
+    } else {
+      x = entry_of(a, GlobalGroups{a}, e);
+    }
+    const int n = x.tasks() * x.span();
     if (in_entry < n) {
       Part p;
       p.kvh = kvh;
       const bool wide = x.wide();
-      const int task = wide ? __builtin_amdgcn_readfirstlane(in_entry / x.blocks) : 0;
-      const int first = in_entry - task * x.blocks;
-      const int count = min(x.blocks - first, left);
+      const int task = wide ? __builtin_amdgcn_readfirstlane(in_entry / x.span()) : 0;
+      const int from = in_entry - task * x.span(), take = min(x.span() - from, left);
+      const int first = max(0, from - kCacheTaskCost), count = from + take - kCacheTaskCost - first;
+      left -= take;
+      in_entry += take;
+      if (count <= 0) continue;
       p.table = c.table + static_cast<int64_t>(x.b0) * c.max_pages;
       p.lo = x.lo;
       p.key0 = (x.block0 + first) * kCacheBlock;
@@ -580,11 +628,9 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
       const int64_t place = places + tiles_before + p.tile;
       float* out = place < a.max_parts ? reinterpret_cast<float*>(a.ws + cache_plan_bytes() + place * cache_part_bytes(D)) : nullptr;
       if (wide)
-        wide_part<T, D, kPlain>(a, x, p, stage, out, lane, wave);
+        wide_part<T, D, kPlain>(a, x, sequences, p, stage, out, lane, wave);
       else
-        narrow_part<T, D, kPlain>(a, x, p, stage, s_ref, s_sum, out, lane, wave);
-      left -= count;
-      in_entry += count;
+        narrow_part<T, D, kPlain>(a, x, sequences, p, stage, s_ref, s_sum, out, lane, wave);
     } else {
       in_entry = 0;
       tiles_before += x.tiles();
@@ -616,7 +662,8 @@ __global__ __launch_bounds__(kThreads) void cache_merge(CacheAttnArgs a) {
     const int r = (token - x.token0) * G + (h - kvh * G);
     if (x.blocks == 0 || r < 0 || r >= x.rows) continue;
     const int tile = r / kCacheTileRows, in_tile = r % kCacheTileRows;
-    const int start = x.before + (x.rows > kCacheTileRows ? r / kCacheWideRows : 0) * x.blocks;
+    // the first block's unit of its task
+    const int start = x.before + (x.rows > kCacheTileRows ? r / kCacheWideRows : 0) * (x.blocks + kCacheTaskCost) + kCacheTaskCost;
     const int w0 = start / plan.run, w1 = (start + x.blocks - 1) / plan.run;
     const int64_t first = static_cast<int64_t>(kvh) * (plan.tiles + 4 * a.head_workers) + x.tiles + tile + 4 * w0;
     const int parts = static_cast<int>(min<int64_t>(w1 - w0 + 1, (a.max_parts - first + 3) / 4));
