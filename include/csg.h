@@ -527,7 +527,8 @@ typedef struct {
  * they are. Values of one document never reach another's results; within a document the
  * values of a masked key are multiplied with weights of 0, as in a product of matrices, so
  * they must be finite (masked keys may be anything).
- * Bounds that do not ascend or leave 0 .. rows select fewer rows, never memory outside. */
+ * Bounds that do not ascend or leave 0 .. rows touch no memory outside, but what the
+ * documents then hold is not said. */
 csg_status csg_doc_attn(const csg_doc_attn_cfg* cfg, const void* q, const void* k, const void* v,
                         const int32_t* q_ptr, const int32_t* k_ptr, const int32_t* prefix,
                         const float* slopes, void* o, void* lse, int device, void* stream);

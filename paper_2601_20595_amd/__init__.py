@@ -638,13 +638,16 @@ class AttnPlan(Plan):
                       copy_stream)
 
 
-def _arg(t, need: int, what: str, device: int) -> int:
-    """_buf's checks, and that the tensor lives on the calls' device; its address. (A few
-    queries of the tensor: a decode step's kernels take less time than careful ones.)"""
+def _arg(t, need: int, size: int, what: str, device: int) -> int:
+    """_buf's checks, that the tensor's elements have `size` bytes (0: any) and that it lives on
+    the calls' device; its address. (A few queries of the tensor: a decode step's kernels take
+    less time than careful ones.)"""
     if t is None:
         return 0
     if type(t) is int:
         return t
+    if size and t.itemsize != size:
+        raise ValueError("%s must have %d-byte elements" % (what, size))
     if t.is_contiguous() and t.nbytes >= need and t.get_device() == device:
         return t.data_ptr()
     _buf(t, need, what)
@@ -660,12 +663,15 @@ def _heads(t, rows: Optional[int], heads: int, head_dim: int, what: str, device:
                          % (what, "rows" if rows is None else rows, heads, head_dim, tuple(shape)))
     if t.itemsize != 2:
         raise ValueError("%s must have 2-byte elements" % what)
+    n = shape[0]
     row, head, one = t.stride()
-    if one != 1 or (heads > 1 and head != head_dim):
-        raise ValueError("%s: the heads of a row must lie behind each other" % what)
+    if n < 2:
+        row = heads * head_dim
+    if one != 1 or (heads > 1 and head != head_dim) or row < heads * head_dim:
+        raise ValueError("%s: the heads of a row must lie behind each other, and rows apart" % what)
     if t.get_device() != device:
         raise ValueError("%s must be on GPU %d" % (what, device))
-    return t.data_ptr(), shape[0], (row if shape[0] > 1 else heads * head_dim)
+    return t.data_ptr(), n, row
 
 
 class DocAttn:
@@ -700,9 +706,9 @@ class DocAttn:
         va, _, c.v_stride = _heads(v, m, hkv, d, "v", dev)
         c.q_rows, c.k_rows = n, m
         c.n_docs = docs = q_ptr.numel() - 1
-        return n, m, (qa, ka, va, _arg(q_ptr, 4 * (docs + 1), "q_ptr", dev), _arg(k_ptr, 4 * (docs + 1), "k_ptr", dev),
-                      _arg(prefix, 4 * docs, "prefix", dev), _arg(slopes, 4 * h, "slopes", dev),
-                      _arg(o, 2 * n * h * d, "o", dev), _arg(lse, 4 * n * h, "lse", dev))
+        return n, m, (qa, ka, va, _arg(q_ptr, 4 * (docs + 1), 4, "q_ptr", dev), _arg(k_ptr, 4 * (docs + 1), 4, "k_ptr", dev),
+                      _arg(prefix, 4 * docs, 4, "prefix", dev), _arg(slopes, 4 * h, 4, "slopes", dev),
+                      _arg(o, 2 * n * h * d, 2, "o", dev), _arg(lse, 4 * n * h, 4, "lse", dev))
 
     def forward(self, q, k, v, q_ptr, k_ptr, o, lse, prefix=None, slopes=None, stream=None):
         _, _, args = self._inputs(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
@@ -715,8 +721,8 @@ class DocAttn:
         dqa, _, c.dq_stride = _heads(dq, n, h, d, "dq", dev)
         dka, _, c.dk_stride = _heads(dk, m, hkv, d, "dk", dev)
         dva, _, c.dv_stride = _heads(dv, m, hkv, d, "dv", dev)
-        _check(_lib().csg_doc_attn_grad(c, *args, _arg(d_o, 2 * n * h * d, "d_o", dev), dqa, dka, dva,
-                                        _arg(workspace, 1, "workspace", dev), workspace.nbytes, dev, _stream(stream)),
+        _check(_lib().csg_doc_attn_grad(c, *args, _arg(d_o, 2 * n * h * d, 2, "d_o", dev), dqa, dka, dva,
+                                        _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes, dev, _stream(stream)),
                "csg_doc_attn_grad")
 
 
@@ -737,6 +743,7 @@ class PagedCache:
         self._shape = n_heads, n_kv_heads, head_dim
         self._batch = batch
         self._page_bytes = 2 * n_pages * n_kv_heads * page_size * head_dim
+        self._max_pages = max_pages
         self._table_bytes = 4 * batch * max_pages
 
     def workspace_bytes(self, tokens: int, n_groups: int = 0) -> int:
@@ -744,6 +751,11 @@ class PagedCache:
         c = csg_cache_cfg.from_buffer_copy(self._cfg)
         c.tokens, c.n_groups, c.q_stride = tokens, n_groups, 0
         return csg_cache_attn_workspace(c, self.device)
+
+    def _table(self, page_table) -> int:
+        if type(page_table) is not int and page_table.shape[-1] != self._max_pages:
+            raise ValueError("page_table must have %d pages a row" % self._max_pages)
+        return _arg(page_table, self._table_bytes, 4, "page_table", self.device)
 
     def append(self, k_pages, v_pages, k, v, q_ptr, lens, page_table, inv_freq=None, interleaved=False, q=None, q_out=None,
                status=None, stream=None):
@@ -757,14 +769,14 @@ class PagedCache:
         qa = qo = c.q_stride = 0
         if q is not None:
             qa, _, c.q_stride = _heads(q, n, h, d, "q", dev)
-            qo = _arg(q_out, 2 * n * h * d, "q_out", dev)
+            qo = _arg(q_out, 2 * n * h * d, 2, "q_out", dev)
         c.rot_dim = rot = 0 if inv_freq is None else 2 * inv_freq.numel()
         c.interleaved = interleaved
         _check(_lib().csg_cache_append(
-            c, _arg(k_pages, self._page_bytes, "k_pages", dev), _arg(v_pages, self._page_bytes, "v_pages", dev), ka, va, qa, qo,
-            _arg(q_ptr, 4 * batch + 4, "q_ptr", dev), _arg(lens, 4 * batch, "lens", dev),
-            _arg(page_table, self._table_bytes, "page_table", dev), _arg(inv_freq, 4 * rot, "inv_freq", dev),
-            _arg(status, 4, "status", dev), dev, _stream(stream)), "csg_cache_append")
+            c, _arg(k_pages, self._page_bytes, 2, "k_pages", dev), _arg(v_pages, self._page_bytes, 2, "v_pages", dev), ka, va, qa, qo,
+            _arg(q_ptr, 4 * batch + 4, 4, "q_ptr", dev), _arg(lens, 4 * batch, 4, "lens", dev),
+            self._table(page_table), _arg(inv_freq, 4 * rot, 8, "inv_freq", dev),
+            _arg(status, 4, 4, "status", dev), dev, _stream(stream)), "csg_cache_append")
 
     def attn(self, q, k_pages, v_pages, q_ptr, lens, page_table, o, lse, workspace, group_ptr=None, prefix=None, scale=0.0,
              softcap=0.0, slopes=None, status=None, stream=None):
@@ -777,9 +789,9 @@ class PagedCache:
         c.n_groups = groups = 0 if group_ptr is None else group_ptr.numel() - 1
         c.scale, c.softcap = scale, softcap
         _check(_lib().csg_cache_attn(
-            c, qa, _arg(k_pages, self._page_bytes, "k_pages", dev), _arg(v_pages, self._page_bytes, "v_pages", dev),
-            _arg(q_ptr, 4 * batch + 4, "q_ptr", dev), _arg(lens, 4 * batch, "lens", dev),
-            _arg(page_table, self._table_bytes, "page_table", dev), _arg(group_ptr, 4 * groups + 4, "group_ptr", dev),
-            _arg(prefix, 4 * groups, "prefix", dev), _arg(slopes, 4 * h, "slopes", dev), _arg(o, 2 * n * h * d, "o", dev),
-            _arg(lse, 4 * n * h, "lse", dev), _arg(workspace, 1, "workspace", dev), workspace.nbytes,
-            _arg(status, 4, "status", dev), dev, _stream(stream)), "csg_cache_attn")
+            c, qa, _arg(k_pages, self._page_bytes, 2, "k_pages", dev), _arg(v_pages, self._page_bytes, 2, "v_pages", dev),
+            _arg(q_ptr, 4 * batch + 4, 4, "q_ptr", dev), _arg(lens, 4 * batch, 4, "lens", dev),
+            self._table(page_table), _arg(group_ptr, 4 * groups + 4, 4, "group_ptr", dev),
+            _arg(prefix, 4 * groups, 4, "prefix", dev), _arg(slopes, 4 * h, 4, "slopes", dev), _arg(o, 2 * n * h * d, 2, "o", dev),
+            _arg(lse, 4 * n * h, 4, "lse", dev), _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes,
+            _arg(status, 4, 4, "status", dev), dev, _stream(stream)), "csg_cache_attn")

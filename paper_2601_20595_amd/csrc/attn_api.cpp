@@ -22,7 +22,7 @@ using csg::hip_fail;
 constexpr int kMaxDevices = 64;
 constexpr int64_t kMaxRows = int64_t{1} << 30;
 constexpr int64_t kMaxStride = int64_t{1} << 23;  // 63 rows of it stay within 32-bit byte offsets
-constexpr int64_t kMaxGrid = 0x7fffffff;
+constexpr int64_t kMaxGrid = 0xffffffff / 512;  // workgroups: a launch's threads are counted in 32 bits
 constexpr int32_t kDefaultCus = 256;
 
 // Compute units of `device`, checked once to be the one this library is built for.
@@ -284,6 +284,7 @@ csg_status csg_cache_append(const csg_cache_cfg* cfg, void* k_pages, void* v_pag
   const int64_t k_row = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
   CSG_CHECK(check_stride(&c.k_stride, k_row, "k_stride"));
   CSG_CHECK(check_stride(&c.v_stride, k_row, "v_stride"));
+  if (c.tokens > kMaxGrid) return fail(CSG_ERR_UNSUPPORTED, "too many tokens for one launch");
   if (c.rot_dim < 0 || c.rot_dim > c.head_dim || c.rot_dim % 16 != 0)
     return fail(CSG_ERR_INVALID, "rot_dim must be a multiple of 16 up to head_dim");
   if (c.interleaved != 0 && c.interleaved != 1) return fail(CSG_ERR_INVALID, "interleaved must be 0 or 1");

@@ -89,7 +89,7 @@ def test_documents_refuse_buffers():
 
 CACHE = HEADS[:8] + [({"n_pages": 0}, INVALID), ({"page_size": 0}, INVALID), ({"page_size": 8}, UNSUPPORTED),
                      ({"page_size": 48}, UNSUPPORTED), ({"batch": -1}, INVALID), ({"max_pages": 0}, INVALID),
-                     ({"tokens": -1}, INVALID), ({"tokens": 1 << 31}, INVALID), ({"n_groups": -1}, INVALID),
+                     ({"tokens": -1}, INVALID), ({"tokens": 1 << 31}, INVALID), ({"tokens": 1 << 24}, UNSUPPORTED), ({"n_groups": -1}, INVALID),
                      ({"max_pages": 1 << 27}, UNSUPPORTED), ({"q_stride": 100}, INVALID)]
 
 
@@ -158,6 +158,25 @@ def test_python_checks():
         a.forward(x.float(), x[:, :2], x[:, :2], None, None, x, x)
     with pytest.raises(ValueError):
         a.forward(x.transpose(0, 2), x[:, :2], x[:, :2], None, None, x, x)
+
+
+def test_python_checks_elements_and_rows():
+    torch = pytest.importorskip("torch")
+    x = torch.zeros((4, 8, 128), dtype=torch.bfloat16)
+    a = csg.DocAttn(8, 8, 128, "bf16")
+    with pytest.raises(ValueError, match="rows apart"):  # one row for all
+        a.forward(x[:1].expand(4, 8, 128), x, x, None, None, x, x)
+    with pytest.raises(ValueError, match="4-byte"):
+        csg._arg(torch.zeros(3, dtype=torch.int64), 12, 4, "q_ptr", 0)
+    with pytest.raises(ValueError, match="contiguous"):
+        csg._arg(torch.zeros((4, 4), dtype=torch.int32)[:, :2], 16, 4, "page_table", 0)
+    with pytest.raises(ValueError, match="holds"):
+        csg._arg(torch.zeros(3, dtype=torch.int32), 16, 4, "lens", 0)
+    with pytest.raises(ValueError, match="GPU"):
+        csg._arg(torch.zeros(3, dtype=torch.int32), 12, 4, "lens", 0)
+    c = csg.PagedCache(8, 8, 128, "bf16", 4, 16, 2, 5)
+    with pytest.raises(ValueError, match="5 pages a row"):
+        c._table(torch.zeros((2, 4), dtype=torch.int32))
 
 
 # ---- the oracle -----------------------------------------------------------------------------

@@ -123,6 +123,9 @@ ATTN = {
     "cap": ([1, 4], [333, 70], 8, 2, 128, 256, [], 6.0, False),
     "bias": ([1, 3, 1], [200, 97, 130], 8, 4, 64, 16, [(0, 3, 80)], 0.0, True),
     "cap and bias": ([2] * 5, [400, 30, 260, 64, 129], 5, 5, 128, 32, [], 10.0, True),
+    "groups of many sequences": ([1] * 300, [60 + (37 * i) % 90 for i in range(300)], 4, 2, 64, 16, [(0, 150, 48), (150, 300, 32)],
+                                 0.0, False),
+    "an empty group": ([1] * 5, [100, 90, 120, 80, 33], 4, 1, 64, 16, [(1, 3, 64), (3, 3, 32), (3, 5, 16)], 0.0, False),
     "many sequences": ([1] * 300, [1 + (37 * i) % 90 for i in range(300)], 4, 2, 64, 16, [], 0.0, False),
 }
 
@@ -180,6 +183,38 @@ def _attn_case(name, dtype, sharp=1.0, stream=None):
 @pytest.mark.parametrize("name", ATTN)
 def test_attention(name, dtype):
     _attn_case(name, dtype)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_long_runs(new):
+    """So many keys a workgroup that it asks for pages again (narrow tasks: after 32 blocks of a wave;
+    wide ones: after 64 steps), against fp64 on the GPU."""
+    H, D, page, n = 128, 64, 64, 20000
+    rng = np.random.default_rng(11)
+    table, pages = _table(rng, [n], page)
+    tab = torch.tensor(table, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    kp, vp = (torch.randn((pages, H, page, D), generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    x = torch.randn((new, H + 3, D), generator=g, device=DEV).to(torch.bfloat16)
+    q = x[:, 1:H + 1]  # a part of a wider tensor
+    c = csg.PagedCache(H, H, D, "bf16", pages, page, 1, table.shape[1])
+    o, ws = torch.empty((new, H, D), dtype=torch.bfloat16, device=DEV), torch.empty(c.workspace_bytes(new), dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    c.attn(q, kp, vp, ints([0, new]), ints([n]), tab, o, None, ws)  # (no log-sum-exp wanted)
+    torch.cuda.synchronize()
+    at = torch.arange(n, device=DEV)
+    place = tab[0].long()[at // page]
+    u = HALF_STEP["bf16"]
+    for h in range(0, H, 9):
+        k, v, qh = kp[place, h, at % page].double(), vp[place, h, at % page].double(), q[:, h].double()
+        s = (qh @ k.t()) * D ** -0.5
+        s[at[None] > n - new + torch.arange(new, device=DEV)[:, None]] = float("-inf")
+        p = torch.softmax(s, dim=1)
+        want = p @ v
+        # the oracle's bounds: a rounding of the output and of every weight, and 2^-17 of the scores' size
+        size = (qh.abs() @ k.abs().t()) * D ** -0.5 + s.abs().nan_to_num(posinf=0.0) + 1.0
+        bound = u * want.abs() + (p * (2 * 2.0 ** -17 * size + u)) @ v.abs()
+        assert bool(((o[:, h].double() - want).abs() <= bound).all()), h
 
 
 def test_sharp_scores_other_stream_same_bits():

@@ -28,6 +28,13 @@ CASES = {
     "cap, bias, not causal": ([100, 31], [60, 90], 7, 7, 128, False, None, 20.0, True),
     "long": ([700], [1500], 2, 1, 128, True, [300], 0.0, False),
     "many documents": ([3, 1, 7, 2] * 40, [3, 5, 7, 1] * 40, 4, 2, 64, True, None, 0.0, False),
+    # more tiles than two a CU: no teams, no parts
+    "many tiles": ([97, 130, 64] * 15, [97, 130, 70] * 15, 16, 16, 64, True, None, 0.0, False),
+    "many tiles of four heads": ([97, 130, 64] * 15, [97, 130, 70] * 15, 16, 4, 128, True, [10] * 45, 0.0, False),
+    "many tiles, cap and bias": ([97, 130, 64] * 15, [97, 130, 70] * 15, 16, 4, 128, True, None, 9.0, True),
+    # two or more parts of the rows, some of them without a step
+    "parts": ([300, 20], [300, 700], 8, 2, 128, True, [0, 500], 0.0, False),
+    "parts, small heads": ([520], [520], 6, 2, 64, True, None, 12.0, True),
 }
 
 
