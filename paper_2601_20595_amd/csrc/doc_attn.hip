@@ -18,6 +18,8 @@
 // tile + t, which leaves room for its last, part-filled one; a workgroup without rows ends.
 #include <hip/hip_runtime.h>
 
+#include <numeric>
+
 #include "attn_tile.hpp"
 #include "doc_attn.hpp"
 
@@ -58,14 +60,24 @@ __device__ __forceinline__ int visible(const DocAttnArgs& a, const Place& p, int
   return a.causal ? clamped(max(p.prefix, i + p.k_len - p.q_len + 1), 0, p.k_len) : p.k_len;
 }
 
-// This wave's share of the loads of 64 rows (fewer at the end: rows past `rows` read zero) of
-// one head into a tile at LDS byte `lds`. src: the head's part of the first row.
-template <int D>
+// How the waves of a workgroup share a tile of rows: kWaves of 32 (row, head) pairs each, and
+// kTeams of them, which take turns at the blocks of kKeys keys and add up their sums at the end.
+template <int W, int N, int K>
+struct Shape {
+  static constexpr int kWaves = W, kTeams = N, kKeys = K, kThreads = 64 * W * N;
+};
+using Whole = Shape<4, 1, 64>;
+using Halves = Shape<4, 2, 64>;
+using Quarters = Shape<2, 4, 32>;
+
+// This wave's share, one of kWaves, of the loads of kRows rows (fewer at the end: rows past `rows`
+// read zero) of one head into a tile at LDS byte `lds`. src: the head's part of the first row.
+template <int D, int kRows = kDocBlock, int kWaves = 4>
 __device__ __forceinline__ void load_tile(const uint16_t* src, int64_t stride, int rows, uint32_t lds, int wave,
                                           const LoadLane<D>& ll) {
-  const int n = rows < kDocBlock ? rows : kDocBlock;
+  const int n = rows < kRows ? rows : kRows;
   const __amdgpu_buffer_rsrc_t rs = make_rsrc(src, n > 0 ? static_cast<int>(((n - 1) * stride + D) * 2) : 0);
-  constexpr int kPer = kDocBlock / kLoadRows<D> / 4;
+  constexpr int kPer = kRows / kLoadRows<D> / kWaves;
   const int stride2 = static_cast<int>(2 * stride);
 #pragma unroll
   for (int q = 0; q < kPer; ++q) {
@@ -105,28 +117,32 @@ __device__ __forceinline__ void store_rows(uint16_t* head, int64_t stride, int r
     }
 }
 
-// Products of 64 keys with the wave's rows: lane (l32, hlf) has those of row l32.
-template <class T, int D>
-__device__ __forceinline__ void products(const unsigned char* t, const Frags<D>& f, const typename T::x8 (&qf)[D / 16],
-                                         f32x16_t (&sc)[2]) {
-  sc[0] = f32x16_t{};
-  sc[1] = f32x16_t{};
+// Sums of teams 1 .. to team 0: 16 bytes a lane side by side, a wave's after the other's.
+template <int D>
+__device__ __forceinline__ void put_sums(f32x4_t* to, const f32x16_t (&acc)[D / 32]) {
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s)
+  for (int k = 0; k < D / 8; ++k)
+    to[64 * k] = f32x4_t{acc[k / 4][4 * (k % 4)], acc[k / 4][4 * (k % 4) + 1], acc[k / 4][4 * (k % 4) + 2], acc[k / 4][4 * (k % 4) + 3]};
+}
+template <int D>
+__device__ __forceinline__ void add_sums(const f32x4_t* from, f32x16_t (&acc)[D / 32], float f, float g) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) sc[kb] = T::mfma(row_frag<T, D>(t, f, s, 32 * kb), qf[s], sc[kb]);
+  for (int k = 0; k < D / 8; ++k) {
+    const f32x4_t v = from[64 * k];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[k / 4][4 * (k % 4) + e] = fmaf(acc[k / 4][4 * (k % 4) + e], f, v[e] * g);
+  }
 }
 
 // ---- forward -----------------------------------------------------------------------------
-template <class T, int D, bool kPlain, int kSplit>
-__global__ __launch_bounds__(kSplit * kThreads, 2) void doc_forward(DocAttnArgs a) {
-  constexpr int kTile = kDocBlock * D * 2;
-  __shared__ __attribute__((aligned(1024))) unsigned char sK[kSplit * 2 * kTile];
-  __shared__ __attribute__((aligned(1024))) unsigned char sV[kSplit * 2 * kTile];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
-  const int team = kSplit == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+template <class T, int D, bool kPlain, class S>
+__global__ __launch_bounds__(S::kThreads, 2) void doc_forward(DocAttnArgs a) {
+  constexpr int kTeams = S::kTeams, kKeys = S::kKeys, kTile = kKeys * D * 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char stage[2 * kTeams * 2 * kTile];
+  const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = any_wave % S::kWaves, team = any_wave / S::kWaves;
   const int l32 = lane & 31, hlf = lane >> 5;
-  const int span = kDocTileRows / a.tile_heads, groups = a.H / a.tile_heads;
+  const int span = 32 * S::kWaves / a.tile_heads, groups = a.H / a.tile_heads;
   // a die runs every 8th workgroup: with the head fastest, it keeps to few key/value heads;
   // the last rows of a causal document, which see the most keys, come first
   const int hg = blockIdx.x % groups;
@@ -140,23 +156,25 @@ __global__ __launch_bounds__(kSplit * kThreads, 2) void doc_forward(DocAttnArgs 
   const bool ok = row < p.q_len;
   const int hi = visible(a, p, min(row, p.q_len - 1));
   const int wave_lo = visible(a, p, min(first, p.q_len - 1));  // seen by every row of the wave
-  const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kDocBlock - 1) / kDocBlock;
-  const int wave_nb = first < p.q_len ? (visible(a, p, min(first + 32, p.q_len) - 1) + kDocBlock - 1) / kDocBlock : 0;
+  const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kKeys - 1) / kKeys;
+  const int wave_nb = first < p.q_len ? (visible(a, p, min(first + 32, p.q_len) - 1) + kKeys - 1) / kKeys : 0;
   const float slope = kPlain ? 0.0f : slope_of(a.scoring, h);
   const int at = row + p.k_len - p.q_len;  // the row's own key
 
   const LoadLane<D> ll(lane);
   const Frags<D> fr(lane);
-  const int mine = team * 2 * kTile;  // the team's buffers
-  const uint32_t sK_addr = lds_address(sK) + mine, sV_addr = lds_address(sV) + mine;
+  // the team's two buffers of keys, and of values
+  const unsigned char* sK = stage + team * 4 * kTile;
+  const unsigned char* sV = sK + 2 * kTile;
+  const uint32_t sK_addr = lds_address(sK), sV_addr = lds_address(sV);
   const lds_u8_t* sV_lds = (const lds_u8_t*)sV;
   const uint16_t* kh = a.K + p.k0 * a.k_stride + kvh * D;
   const uint16_t* vh = a.V + p.k0 * a.v_stride + kvh * D;
   auto load = [&](int i, int j) {  // block j into buffer i % 2
-    load_tile<D>(kh + static_cast<int64_t>(j) * kDocBlock * a.k_stride, a.k_stride, p.k_len - j * kDocBlock,
-                 sK_addr + (i & 1) * kTile, wave, ll);
-    load_tile<D>(vh + static_cast<int64_t>(j) * kDocBlock * a.v_stride, a.v_stride, p.k_len - j * kDocBlock,
-                 sV_addr + (i & 1) * kTile, wave, ll);
+    load_tile<D, kKeys, S::kWaves>(kh + static_cast<int64_t>(j) * kKeys * a.k_stride, a.k_stride, p.k_len - j * kKeys,
+                                   sK_addr + (i & 1) * kTile, wave, ll);
+    load_tile<D, kKeys, S::kWaves>(vh + static_cast<int64_t>(j) * kKeys * a.v_stride, a.v_stride, p.k_len - j * kKeys,
+                                   sV_addr + (i & 1) * kTile, wave, ll);
   };
   if (team < nb) load(0, team);
 
@@ -168,19 +186,26 @@ __global__ __launch_bounds__(kSplit * kThreads, 2) void doc_forward(DocAttnArgs 
   RowSoftmax sm;
   const float c = a.scoring.unit * kLog2e;
 
-  for (int i = 0, j = team; i * kSplit < nb; ++i, j += kSplit) {
+  for (int i = 0, j = team; i * kTeams < nb; ++i, j += kTeams) {
     wait_vm<0>();
     __syncthreads();  // the team's block j is there, and everyone is done with the one before
-    if (j + kSplit < nb) load(i + 1, j + kSplit);
+    if (j + kTeams < nb) load(i + 1, j + kTeams);
     if (j >= wave_nb) continue;
-    const int buf = mine + (i & 1) * kTile;
-    const int key0 = j * kDocBlock;
-    f32x16_t sc[2];
+    const int buf = (i & 1) * kTile;
+    const int key0 = j * kKeys;
+    constexpr int kN = kKeys / 32;
+    f32x16_t sc[kN];
     __builtin_amdgcn_sched_barrier(0);
-    products<T, D>(sK + buf, fr, qf, sc);
+    // products of the keys with the wave's rows (lane (l32, hlf) has those of row l32), six reads ahead
+#pragma unroll
+    for (int kb = 0; kb < kN; ++kb) sc[kb] = f32x16_t{};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+      for (int kb = 0; kb < kN; ++kb) sc[kb] = T::mfma(row_frag<T, D>(sK + buf, fr, s, 32 * kb), qf[s], sc[kb]);
     __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
+    for (int i = 0; i < kN * D / 16; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
@@ -193,54 +218,50 @@ __global__ __launch_bounds__(kSplit * kThreads, 2) void doc_forward(DocAttnArgs 
     };
     read_values(0);
     if constexpr (!kPlain) {
-      cap_scores<2>(a.scoring, sc);
-      bias_scores<2, -1>(a.scoring, slope, at - key0, hlf, sc);
+      cap_scores<kN>(a.scoring, sc);
+      bias_scores<kN, -1>(a.scoring, slope, at - key0, hlf, sc);
     }
-    if (key0 + kDocBlock > wave_lo) {
+    if (key0 + kKeys > wave_lo) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < kN; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (key0 + 32 * kb + result_row(r, hlf) >= hi) sc[kb][r] = -__builtin_inff();
     }
-    typename T::x8 pb[4];
+    typename T::x8 pb[2 * kN];
     bool moved;
-    const float alpha = sm.block<T, 2>(sc, c, pb, moved);
+    const float alpha = sm.block<T, kN>(sc, c, pb, moved);
     if (moved) {
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
     }
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      if (t < 3) read_values(t + 1);
+    for (int t = 0; t < 2 * kN; ++t) {
+      if (t + 1 < 2 * kN) read_values(t + 1);
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) acc[db] = T::mfma(vf[t & 1][db], pb[t], acc[db]);
     }
   }
-  if constexpr (kSplit == 2) {
-    // the second team's sums, 16 bytes a lane side by side, to the first
-    static_assert(sizeof(sK) >= 4 * 64 * (D / 2) * 4, "a team's sums fit the keys' buffers");
-    f32x4_t* sums = reinterpret_cast<f32x4_t*>(sK) + wave * (D / 8) * 64 + lane;
-    float* state = reinterpret_cast<float*>(sV) + wave * 64 + lane;
+  if constexpr (kTeams > 1) {
+    __shared__ float s_state[kTeams - 1][S::kWaves][2][64];
+    static_assert(sizeof(stage) >= (kTeams - 1) * S::kWaves * 64 * (D / 2) * 4, "the teams' sums fit the buffers");
+    f32x4_t* sums = reinterpret_cast<f32x4_t*>(stage) + wave * (D / 8) * 64 + lane;
+    constexpr int kTeamSums = S::kWaves * (D / 8) * 64;
     __syncthreads();
-    if (team == 1) {
-#pragma unroll
-      for (int k = 0; k < D / 8; ++k)
-        sums[64 * k] = f32x4_t{acc[k / 4][4 * (k % 4)], acc[k / 4][4 * (k % 4) + 1], acc[k / 4][4 * (k % 4) + 2], acc[k / 4][4 * (k % 4) + 3]};
-      state[0] = sm.m;
-      state[256] = sm.l;
+    if (team > 0) {
+      put_sums<D>(sums + (team - 1) * kTeamSums, acc);
+      s_state[team - 1][wave][0][lane] = sm.m;
+      s_state[team - 1][wave][1][lane] = sm.l;
     }
     __syncthreads();
-    if (team == 1) return;
-    const float m = state[0], top = fmaxf(m, sm.m);
-    const float f = factor(sm.m, top, c), g = factor(m, top, c);
-    sm.m = top;
-    sm.l = fmaf(sm.l, f, state[256] * g);
+    if (team > 0) return;
 #pragma unroll
-    for (int k = 0; k < D / 8; ++k) {
-      const f32x4_t v = sums[64 * k];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[k / 4][4 * (k % 4) + e] = fmaf(acc[k / 4][4 * (k % 4) + e], f, v[e] * g);
+    for (int n = 0; n < kTeams - 1; ++n) {
+      const float m = s_state[n][wave][0][lane], top = fmaxf(m, sm.m);
+      const float f = factor(sm.m, top, c), g = factor(m, top, c);
+      sm.m = top;
+      sm.l = fmaf(sm.l, f, s_state[n][wave][1][lane] * g);
+      add_sums<D>(sums + n * kTeamSums, acc, f, g);
     }
   }
   if (!ok) return;
@@ -257,16 +278,15 @@ __global__ __launch_bounds__(kSplit * kThreads, 2) void doc_forward(DocAttnArgs 
 
 // ---- gradient of the queries --------------------------------------------------------------
 // The forward's tiles; also leaves each row's statistics to the kernel of the keys' gradient.
-template <class T, int D, bool kPlain, int kSplit>
-__global__ __launch_bounds__(kSplit * kThreads, 2) void doc_grad_q(DocAttnArgs a) {
-  constexpr int kTile = kDocBlock * D * 2;
-  __shared__ __attribute__((aligned(1024))) unsigned char sK[kSplit * 2 * kTile];
-  __shared__ __attribute__((aligned(1024))) unsigned char sV[kSplit * 2 * kTile];
-  __shared__ float s_more[kSplit][4][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6 & 3);
-  const int team = kSplit == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+template <class T, int D, bool kPlain, class S>
+__global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
+  constexpr int kTeams = S::kTeams, kKeys = S::kKeys, kTile = kKeys * D * 2;
+  __shared__ __attribute__((aligned(1024))) unsigned char stage[2 * kTeams * 2 * kTile];
+  __shared__ float s_more[kTeams][S::kWaves][64];
+  const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = any_wave % S::kWaves, team = any_wave / S::kWaves;
   const int l32 = lane & 31, hlf = lane >> 5;
-  const int span = kDocTileRows / a.tile_heads, groups = a.H / a.tile_heads;
+  const int span = 32 * S::kWaves / a.tile_heads, groups = a.H / a.tile_heads;
   const int hg = blockIdx.x % groups;
   const Place p = find_place(a, gridDim.x / groups - 1 - blockIdx.x / groups, span, false);
   if (!p.any) return;
@@ -278,23 +298,25 @@ __global__ __launch_bounds__(kSplit * kThreads, 2) void doc_grad_q(DocAttnArgs a
   const bool ok = row < p.q_len;
   const int hi = visible(a, p, min(row, p.q_len - 1));
   const int wave_lo = visible(a, p, min(first, p.q_len - 1));
-  const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kDocBlock - 1) / kDocBlock;
-  const int wave_nb = first < p.q_len ? (visible(a, p, min(first + 32, p.q_len) - 1) + kDocBlock - 1) / kDocBlock : 0;
+  const int nb = (visible(a, p, min(p.first + span, p.q_len) - 1) + kKeys - 1) / kKeys;
+  const int wave_nb = first < p.q_len ? (visible(a, p, min(first + 32, p.q_len) - 1) + kKeys - 1) / kKeys : 0;
   const float slope = kPlain ? 0.0f : slope_of(a.scoring, h);
   const int at = row + p.k_len - p.q_len;
 
   const LoadLane<D> ll(lane);
   const Frags<D> fr(lane);
-  const int mine = team * 2 * kTile;  // the team's buffers
-  const uint32_t sK_addr = lds_address(sK) + mine, sV_addr = lds_address(sV) + mine;
+  // the team's two buffers of keys, and of values
+  const unsigned char* sK = stage + team * 4 * kTile;
+  const unsigned char* sV = sK + 2 * kTile;
+  const uint32_t sK_addr = lds_address(sK), sV_addr = lds_address(sV);
   const lds_u8_t* sK_lds = (const lds_u8_t*)sK;
   const uint16_t* kh = a.K + p.k0 * a.k_stride + kvh * D;
   const uint16_t* vh = a.V + p.k0 * a.v_stride + kvh * D;
   auto load = [&](int i, int j) {  // block j into buffer i % 2
-    load_tile<D>(kh + static_cast<int64_t>(j) * kDocBlock * a.k_stride, a.k_stride, p.k_len - j * kDocBlock,
-                 sK_addr + (i & 1) * kTile, wave, ll);
-    load_tile<D>(vh + static_cast<int64_t>(j) * kDocBlock * a.v_stride, a.v_stride, p.k_len - j * kDocBlock,
-                 sV_addr + (i & 1) * kTile, wave, ll);
+    load_tile<D, kKeys, S::kWaves>(kh + static_cast<int64_t>(j) * kKeys * a.k_stride, a.k_stride, p.k_len - j * kKeys,
+                                   sK_addr + (i & 1) * kTile, wave, ll);
+    load_tile<D, kKeys, S::kWaves>(vh + static_cast<int64_t>(j) * kKeys * a.v_stride, a.v_stride, p.k_len - j * kKeys,
+                                   sV_addr + (i & 1) * kTile, wave, ll);
   };
   if (team < nb) load(0, team);
 
@@ -323,11 +345,11 @@ __global__ __launch_bounds__(kSplit * kThreads, 2) void doc_grad_q(DocAttnArgs a
   auto turn = [&](int i, int j, bool again) {
     wait_vm<0>();
     __syncthreads();
-    if (j + kSplit < nb)
-      load(i + 1, j + kSplit);
+    if (j + kTeams < nb)
+      load(i + 1, j + kTeams);
     else if (again && team < nb)
       load(i + 1, team);
-    return mine + (i & 1) * kTile;
+    return (i & 1) * kTile;
   };
   // P (do . v - delta) of keys key0 .. key0 + 31, times the cap's slip in the second pass; 0 where
   // masked.
@@ -363,22 +385,24 @@ __global__ __launch_bounds__(kSplit * kThreads, 2) void doc_grad_q(DocAttnArgs a
   // to sum small terms.
   float more = 0.0f;
   int i = 0;
-  for (int j = team; j - team < nb; j += kSplit, ++i) {
+  for (int j = team; j - team < nb; j += kTeams, ++i) {
     const int buf = turn(i, j, true);
     if (j >= wave_nb) continue;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < kKeys / 32; ++kb) {
       f32x16_t ds;
-      gradients(buf, kb, j * kDocBlock + 32 * kb, false, ds);
+      gradients(buf, kb, j * kKeys + 32 * kb, false, ds);
 #pragma unroll
       for (int r = 0; r < 16; ++r) more += ds[r];
     }
   }
   more = sum_halves(more);
-  if constexpr (kSplit == 2) {
+  if constexpr (kTeams > 1) {
     s_more[team][wave][lane] = more;
     __syncthreads();
-    more = s_more[0][wave][lane] + s_more[1][wave][lane];
+    more = 0.0f;
+#pragma unroll
+    for (int n = 0; n < kTeams; ++n) more += s_more[n][wave][lane];
   }
   delta += more;
   if (ok && hlf == 0 && team == 0) {
@@ -391,13 +415,13 @@ __global__ __launch_bounds__(kSplit * kThreads, 2) void doc_grad_q(DocAttnArgs a
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
 
-  for (int j = team; j - team < nb; j += kSplit, ++i) {
+  for (int j = team; j - team < nb; j += kTeams, ++i) {
     const int buf = turn(i, j, false);
     if (j >= wave_nb) continue;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < kKeys / 32; ++kb) {
       f32x16_t ds;
-      gradients(buf, kb, j * kDocBlock + 32 * kb, true, ds);
+      gradients(buf, kb, j * kKeys + 32 * kb, true, ds);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const typename T::x8 w = pack<T>(ds, t);
@@ -407,22 +431,16 @@ __global__ __launch_bounds__(kSplit * kThreads, 2) void doc_grad_q(DocAttnArgs a
       }
     }
   }
-  if constexpr (kSplit == 2) {
-    static_assert(sizeof(sK) >= 4 * 64 * (D / 2) * 4, "a team's sums fit the keys' buffers");
-    f32x4_t* sums = reinterpret_cast<f32x4_t*>(sK) + wave * (D / 8) * 64 + lane;
+  if constexpr (kTeams > 1) {
+    static_assert(sizeof(stage) >= (kTeams - 1) * S::kWaves * 64 * (D / 2) * 4, "the teams' sums fit the buffers");
+    f32x4_t* sums = reinterpret_cast<f32x4_t*>(stage) + wave * (D / 8) * 64 + lane;
+    constexpr int kTeamSums = S::kWaves * (D / 8) * 64;
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < D / 8; ++k)
-      if (team == 1)
-        sums[64 * k] = f32x4_t{acc[k / 4][4 * (k % 4)], acc[k / 4][4 * (k % 4) + 1], acc[k / 4][4 * (k % 4) + 2], acc[k / 4][4 * (k % 4) + 3]};
+    if (team > 0) put_sums<D>(sums + (team - 1) * kTeamSums, acc);
     __syncthreads();
-    if (team == 1) return;
+    if (team > 0) return;
 #pragma unroll
-    for (int k = 0; k < D / 8; ++k) {
-      const f32x4_t v = sums[64 * k];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[k / 4][4 * (k % 4) + e] += v[e];
-    }
+    for (int n = 0; n < kTeams - 1; ++n) add_sums<D>(sums + n * kTeamSums, acc, 1.0f, 1.0f);
   }
   if (ok) store_rows<T, D>(a.dQ + p.q0 * a.dq_stride + h * D, a.dq_stride, row, hlf, acc, a.scale);
 }
@@ -673,34 +691,45 @@ __global__ __launch_bounds__(kThreads) void sum_parts(DocAttnArgs a) {
   *reinterpret_cast<u32x2_t*>(to) = __builtin_bit_cast(u32x2_t, __builtin_convertvector(sum, typename T::x4));
 }
 
-// Workgroups of the forward kernel and the gradient of the queries, and whether two teams of waves
-// share a tile's keys.
+// Tiles of rows, at most.
+template <class S>
 int64_t row_tiles(const DocAttnArgs& a) {
-  return (a.q_rows / (kDocTileRows / a.tile_heads) + a.n_docs) * static_cast<int64_t>(a.H / a.tile_heads);
+  return (a.q_rows / (32 * S::kWaves / a.tile_heads) + a.n_docs) * static_cast<int64_t>(a.H / a.tile_heads);
 }
-// Two teams where the tiles are no more than two a CU: then the longest tile's way through its keys is
-// what a call takes, and halving it helps (32 heads on 8 of 128, one causal document of 1024 rows,
-// 264 tiles: forward 27.2 -> 22.4 us, 2048 rows, 520 tiles: 54.4 -> 47.3; 12 heads of 64, 4096 rows,
-// 396 tiles: 77.8 -> 49.4); with more, the teams only wait for each other (4096 rows, 1032 tiles:
-// 151.6 -> 156.5 us; 16 documents of 250 rows, 1128 tiles: 30.1 -> 43.6).
-bool split_tiles(const DocAttnArgs& a) { return row_tiles(a) <= 2 * a.cus + a.n_docs * static_cast<int64_t>(a.H / a.tile_heads); }
+
+template <class T, int D, bool kPlain, bool kGradient, class S>
+hipError_t launch_rows(DocAttnArgs a, hipStream_t stream) {
+  a.tile_heads = std::gcd(a.H / a.Hkv, S::kWaves);
+  const dim3 grid(row_tiles<S>(a)), block(S::kThreads);
+  if constexpr (kGradient)
+    hipLaunchKernelGGL((doc_grad_q<T, D, kPlain, S>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((doc_forward<T, D, kPlain, S>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
+
+// The shape of the tiles. While there are no more than CUs, the longest tile's way through its keys is
+// what a call takes: four teams on half as many rows; up to two a CU two teams; with more they would
+// only wait for each other. Forward, one causal document, whole / halves / quarters, us: 32 heads on 8 of
+// 128, 512 rows (136 tiles) 16.3 / 15.4 / 12.7; 1024 rows (264) 26.8 / 22.5 / 25.1; 2048 rows (520) 53.9 /
+// 47.8 / 69.0; 4096 rows (1032) 149 / 157 / 225; 12 heads of 64, 2048 rows (204) 36.0 / 25.6 / 19.2, 4096 rows
+// (396) 77.6 / 50.0 / 46.4 (and its gradient 210 / 183 / 191); 16 documents of 250 rows (564) 13.8 / 16.6 / 17.5.
+template <class T, int D, bool kPlain, bool kGradient>
+hipError_t launch_rows(const DocAttnArgs& a, hipStream_t stream) {
+  const int64_t tiles = row_tiles<Whole>(a);
+  if (tiles <= a.cus) return launch_rows<T, D, kPlain, kGradient, Quarters>(a, stream);
+  if (tiles <= 2 * a.cus) return launch_rows<T, D, kPlain, kGradient, Halves>(a, stream);
+  return launch_rows<T, D, kPlain, kGradient, Whole>(a, stream);
+}
 
 template <class T, int D, bool kPlain>
 hipError_t forward(const DocAttnArgs& a, hipStream_t stream) {
-  if (split_tiles(a))
-    hipLaunchKernelGGL((doc_forward<T, D, kPlain, 2>), dim3(row_tiles(a)), dim3(2 * kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((doc_forward<T, D, kPlain, 1>), dim3(row_tiles(a)), dim3(kThreads), 0, stream, a);
-  return hipGetLastError();
+  return launch_rows<T, D, kPlain, false>(a, stream);
 }
 
 template <class T, int D, bool kPlain>
 hipError_t grad(const DocAttnArgs& a, hipStream_t stream) {
-  if (split_tiles(a))
-    hipLaunchKernelGGL((doc_grad_q<T, D, kPlain, 2>), dim3(row_tiles(a)), dim3(2 * kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL((doc_grad_q<T, D, kPlain, 1>), dim3(row_tiles(a)), dim3(kThreads), 0, stream, a);
-  hipError_t e = hipGetLastError();
+  hipError_t e = launch_rows<T, D, kPlain, true>(a, stream);
   if (e != hipSuccess) return e;
   const int64_t k_tiles = doc_key_tiles(a.k_rows, a.n_docs) * a.Hkv;
   hipLaunchKernelGGL((doc_grad_kv<T, D, kPlain>), dim3(k_tiles * a.row_parts), dim3(kThreads), 0, stream, a);
