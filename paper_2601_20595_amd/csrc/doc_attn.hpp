@@ -51,6 +51,7 @@ inline int32_t doc_row_parts(int64_t q_rows, int64_t k_rows, int64_t n_docs, int
   const int64_t tiles = ((k_rows + kDocTileRows - 1) / kDocTileRows + n_docs / 2) * Hkv;
   const int64_t steps = (q_rows / (n_docs < 1 ? 1 : n_docs) + kDocBlock - 1) / kDocBlock * (H / Hkv);
   int32_t parts = 1;
+  if (k_rows == 0) return parts;
   while (parts < 16 && ((tiles * (parts + 1) <= cus && steps >= 4 * (parts + 1)) ||
                         (tiles * (parts + 1) <= 2 * static_cast<int64_t>(cus) && steps >= 16 * (parts + 1))))
     ++parts;

@@ -132,6 +132,24 @@ def test_gradient_against_differences():
         assert abs((f[0] - f[1]) / 2e-4 - (g * w).sum()) <= allowed, name
 
 
+@pytest.mark.parametrize("rows", [3, 700])
+def test_no_keys_at_all(rows):
+    """Rows without a key in the call: output and gradient 0, log-sum-exp -inf; and keys without rows."""
+    H, Hkv, D = 32, 8, 128
+    a = csg.DocAttn(H, Hkv, D, "bf16")
+    for n, m in ((rows, 0), (0, rows)):
+        q, k, v, do = (normal(i, s, "bf16")[0].to(DEV)
+                       for i, s in enumerate(((n, H, D), (m, Hkv, D), (m, Hkv, D), (n, H, D))))
+        o, lse = torch.full_like(q, 17.0), torch.full((H, n), 17.0, device=DEV)
+        d = [torch.full_like(t, 17.0) for t in (q, k, v)]
+        ws = torch.full((max(16, a.workspace_bytes(n, m)),), 255, dtype=torch.uint8, device=DEV)
+        qp, kp = ints([0, n]), ints([0, m])
+        a.forward(q, k, v, qp, kp, o, lse)
+        a.backward(q, k, v, qp, kp, o, lse, do, *d, ws)
+        torch.cuda.synchronize()
+        assert all(bool((t == 0).all()) for t in (o, *d)) and bool((lse == float("-inf")).all())
+
+
 def test_masked_keys_may_be_anything():
     """Keys (not values) that the mask hides hold NaN and infinities, also inside a document."""
     H, D, n = 4, 128, 100
