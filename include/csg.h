@@ -590,8 +590,9 @@ csg_status csg_cache_attn_workspace(const csg_cache_cfg* cfg, int device, size_t
  * prompt's part) over the cache; each sees the keys up to its own position. Sequences
  * group_ptr[g] .. group_ptr[g+1] - 1 (int32[n_groups + 1], ascending; sequences outside every
  * group share nothing) have the same first prefix[g] tokens: their keys and values are read
- * once for the group, from the pages of its first sequence. A sequence shorter than that
- * shares what it has. o: [tokens][n_heads][head_dim]; lse: float[n_heads][tokens], or NULL.
+ * once for the group, from the pages of its first sequence; of the others' rows of the page
+ * table, only tokens behind the prefix are read. A sequence shorter than that shares what it
+ * has. o: [tokens][n_heads][head_dim]; lse: float[n_heads][tokens], or NULL.
  * Rows of no sequence are left as they are. workspace: csg_cache_attn_workspace bytes, any
  * content. At most 2048 sequences and groups. */
 csg_status csg_cache_attn(const csg_cache_cfg* cfg, const void* q, const void* k_pages,

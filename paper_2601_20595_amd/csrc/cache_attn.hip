@@ -270,9 +270,9 @@ __device__ __forceinline__ void load_queries(const CacheAttnArgs& a, const Part&
   }
 }
 
-// The page of a key, -1 if it has none to read.
+// The page of keys key .. key + 15, -1 if it has none to read.
 __device__ __forceinline__ int page_of(const CacheArgs& c, const Part& p, int key) {
-  if (key >= p.end) return -1;
+  if (key >= p.end || key + 16 <= p.lo) return -1;
   const int page = p.table[key >> c.page_shift];
   if (page >= 0 && page < c.n_pages) return page;
   tell(c, kCacheBadPage);
@@ -280,13 +280,23 @@ __device__ __forceinline__ int page_of(const CacheArgs& c, const Part& p, int ke
 }
 
 // Keys (or values) key .. key + 15, which lie in one page, into LDS; what is behind the part's
-// end reads zero.
+// end or before its entry's keys (a sequence need not have its group's tokens in pages of its
+// own) reads zero.
 template <int D>
 __device__ __forceinline__ void load_16(const CacheArgs& c, const uint16_t* pages, const Part& p, int page, int key, uint32_t lds,
                                         const LoadLane<D>& ll) {
   const int rows = page < 0 ? 0 : clamped(p.end - key, 0, 16);
   const int64_t row = ((static_cast<int64_t>(max(page, 0)) * c.Hkv + p.kvh) << c.page_shift) + (key & ((1 << c.page_shift) - 1));
   const __amdgpu_buffer_rsrc_t rs = make_rsrc(pages + row * D, rows * 2 * D);
+  if (key < p.lo) {
+    const int skip = (p.lo - key) * 2 * D;
+#pragma unroll
+    for (int i = 0; i < 16 / kLoadRows<D>; ++i) {
+      const int at = ll.offset(i, 2 * D);
+      load_to_lds(rs, lds + 1024u * i, at < skip ? 1 << 30 : at);
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < 16 / kLoadRows<D>; ++i) load_to_lds(rs, lds + 1024u * i, ll.offset(i, 2 * D));
 }

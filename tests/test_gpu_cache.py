@@ -186,6 +186,39 @@ def test_attention(name, dtype):
 
 
 @pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("D,shared", [(64, 23), (128, 48), (128, 87)])
+def test_a_groups_tokens_are_read_from_its_first_sequence(D, shared, new):
+    """The others have no pages for them, and NaN where such a token would share a page with later ones."""
+    H, Hkv, page, lens = 8, 2, 16, [200, 130, 150]
+    rng = np.random.default_rng(5)
+    table, pages = _table(rng, lens, page)
+    kp, vp = (normal(s, (pages, Hkv, page, D), "bf16")[0] for s in (1, 2))
+    for b in (1, 2):
+        x = np.arange(shared)
+        for t in (kp, vp):
+            t[table[b][x // page], :, x % page] = t[table[0][x // page], :, x % page]
+    q = normal(3, (3 * new, H, D), "bf16")[0].to(DEV)
+    c = csg.PagedCache(H, Hkv, D, "bf16", pages, page, 3, table.shape[1])
+    ws = torch.zeros(c.workspace_bytes(3 * new, 1), dtype=torch.uint8, device=DEV)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out = []
+    for gone in (False, True):
+        if gone:
+            for b in (1, 2):
+                x = np.arange(shared)
+                for t in (kp, vp):
+                    t[table[b][x // page], :, x % page] = float("nan")
+                table[b, :shared // page] = -1
+        o, lse = torch.zeros_like(q), torch.zeros((H, 3 * new), device=DEV)
+        c.attn(q, kp.to(DEV), vp.to(DEV), ints(pointers([new] * 3)), ints(lens), torch.tensor(table, device=DEV), o, lse, ws,
+               group_ptr=ints([0, 3]), prefix=ints([shared]), status=st)
+        torch.cuda.synchronize()
+        out.append((o, lse))
+    assert int(st) == 0
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+
+
+@pytest.mark.parametrize("new", [1, 40])
 def test_long_runs(new):
     """So many keys a workgroup that it asks for pages again (narrow tasks: after 32 blocks of a wave;
     wide ones: after 64 steps), against fp64 on the GPU."""
