@@ -589,7 +589,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
       }
       if (blockIdx.x == 0) {
         entries_in(a.ws)[e] = {before, tiles_before, x.blocks, x.rows, x.token0, x.group, {0, 0}};
-        if (x.own && x.end != c.lens[x.b0]) tell(c, kCacheBadLength);
+        if (x.own && (x.end != c.lens[x.b0] || x.rows / (c.H / c.Hkv) > x.end)) tell(c, kCacheBadLength);
       }
       before += n;
       tiles_before += x.tiles();

@@ -277,6 +277,20 @@ def test_bad_pages_and_lengths_touch_nothing_else():
     assert bool((o[3] == 0).all()) and bool((lse[:, 3] == float("-inf")).all())
 
 
+def test_more_new_tokens_than_the_sequence_has():
+    H, D, page = 2, 64, 16
+    kp, _ = normal(2, (2, 1, page, D), "bf16")
+    q, _ = normal(1, (5, H, D), "bf16")
+    c = csg.PagedCache(H, 1, D, "bf16", 2, page, 1, 2)
+    ws = torch.zeros(c.workspace_bytes(5), dtype=torch.uint8, device=DEV)
+    for n, bits in ((5, 0), (4, 2)):
+        o = torch.zeros((5, H, D), dtype=torch.bfloat16, device=DEV)
+        st = torch.zeros(1, dtype=torch.int32, device=DEV)
+        c.attn(q.to(DEV), kp.to(DEV), kp.to(DEV), ints([0, 5]), ints([n]), ints([[0, 1]]), o, None, ws, status=st)
+        torch.cuda.synchronize()
+        assert int(st) == bits
+
+
 def test_captured_and_replayed():
     """A decode step (append, attention) as one graph, replayed as the sequences grow."""
     H, Hkv, D, page, batch = 8, 2, 128, 16, 5
