@@ -52,20 +52,25 @@ csg_status check_heads(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, in
   return CSG_OK;
 }
 
-csg_status check_scores(float* scale, float softcap, int32_t head_dim) {
-  if (*scale == 0.0f) *scale = 1.0f / std::sqrt(static_cast<float>(head_dim));
-  if (!(*scale > 0.0f) || !std::isfinite(*scale)) return fail(CSG_ERR_INVALID, "scale must be positive and finite");
-  if (!(softcap >= 0.0f) || !std::isfinite(softcap)) return fail(CSG_ERR_INVALID, "softcap must be finite and not negative");
-  return CSG_OK;
-}
+constexpr float kLog2e = 1.4426950408889634f;
 
 csg::Scoring scoring(float scale, float softcap, const float* slopes) {
-  constexpr float kLog2e = 1.4426950408889634f;
   csg::Scoring s{};
   s.unit = softcap > 0.0f ? softcap : scale;
   if (softcap > 0.0f) s.cap_in = 2.0f * scale * kLog2e / softcap;
   s.slopes = slopes;
   return s;
+}
+
+csg_status check_scores(float* scale, float softcap, int32_t head_dim) {
+  if (*scale == 0.0f) *scale = 1.0f / std::sqrt(static_cast<float>(head_dim));
+  if (!(*scale > 0.0f) || !std::isfinite(*scale)) return fail(CSG_ERR_INVALID, "scale must be positive and finite");
+  if (!(softcap >= 0.0f) || !std::isfinite(softcap)) return fail(CSG_ERR_INVALID, "softcap must be finite and not negative");
+  // the kernels' factors: 0 times an infinite one would be NaN
+  const csg::Scoring s = scoring(*scale, softcap, nullptr);
+  if (!std::isnormal(s.unit) || !std::isfinite(s.unit * kLog2e) || (softcap > 0.0f && !std::isnormal(s.cap_in)))
+    return fail(CSG_ERR_INVALID, "scale and softcap, and scale / softcap, must be normal numbers");
+  return CSG_OK;
 }
 
 // Default and check of a row stride.

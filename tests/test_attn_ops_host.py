@@ -42,7 +42,9 @@ HEADS = [({"n_heads": 0}, INVALID), ({"n_heads": 7}, INVALID), ({"n_kv_heads": 0
          ({"n_heads": 1 << 20}, INVALID), ({"dtype": 9}, INVALID), ({"dtype": csg.CSG_F32}, UNSUPPORTED),
          ({"head_dim": 96}, UNSUPPORTED), ({"head_dim": 0}, UNSUPPORTED), ({"scale": -1.0}, INVALID),
          ({"scale": float("nan")}, INVALID), ({"scale": float("inf")}, INVALID), ({"softcap": -1.0}, INVALID),
-         ({"softcap": float("nan")}, INVALID), ({"softcap": float("inf")}, INVALID)]
+         ({"softcap": float("nan")}, INVALID), ({"softcap": float("inf")}, INVALID),
+         ({"scale": 1e-40}, INVALID), ({"scale": 3e38}, INVALID), ({"softcap": 1e-40}, INVALID), ({"softcap": 3e38}, INVALID),
+         ({"scale": 1e30, "softcap": 1e-10}, INVALID), ({"scale": 1e-30, "softcap": 1e10}, INVALID)]
 DOCS = HEADS + [({"causal": 2}, INVALID), ({"n_docs": -1}, INVALID), ({"q_rows": -1}, INVALID), ({"k_rows": 1 << 31}, INVALID),
                 ({"q_stride": 8 * 128 - 8}, INVALID), ({"k_stride": 2 * 128 + 4}, INVALID), ({"v_stride": (1 << 23) + 8}, UNSUPPORTED),
                 ({"n_docs": 1 << 29, "n_heads": 64}, UNSUPPORTED)]
