@@ -257,6 +257,26 @@ def test_sharp_scores_other_stream_same_bits():
     assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
 
 
+def test_far_pages():
+    """Pages beyond 2^32 elements of a cache, bit for bit as near ones."""
+    H, Hkv, D, page, n = 16, 8, 128, 256, 700
+    x = normal(1, (n, H + 2 * Hkv, D), "bf16")[0].to(DEV)
+    out = []
+    for pages in (3, 18000):
+        kp, vp = (torch.empty((pages, Hkv, page, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        c = csg.PagedCache(H, Hkv, D, "bf16", pages, page, 1, 3)
+        tab, ptr, lens = ints([[pages - 1, 0, pages - 2]]), ints([0, n]), ints([n])
+        o, lse = torch.zeros((n, H, D), dtype=torch.bfloat16, device=DEV), torch.zeros((H, n), device=DEV)
+        ws = torch.zeros(c.workspace_bytes(n), dtype=torch.uint8, device=DEV)
+        c.append(kp, vp, x[:, H:H + Hkv], x[:, H + Hkv:], ptr, lens, tab)
+        c.attn(x[:, :H], kp, vp, ptr, lens, tab, o, lse, ws)
+        torch.cuda.synchronize()
+        last = n - 2 * page
+        out.append((o, lse, kp[-1].clone(), vp[-1].clone(), kp[-2, :, :last].clone()))
+    for one, two in zip(*out):
+        assert torch.equal(one, two)
+
+
 def test_bad_pages_and_lengths_touch_nothing_else():
     H, Hkv, D, page = 4, 2, 64, 16
     lens = [40, 40, 1000, -3]

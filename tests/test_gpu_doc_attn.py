@@ -32,6 +32,9 @@ CASES = {
     "many tiles": ([97, 130, 64] * 15, [97, 130, 70] * 15, 16, 16, 64, True, None, 0.0, False),
     "many tiles of four heads": ([97, 130, 64] * 15, [97, 130, 70] * 15, 16, 4, 128, True, [10] * 45, 0.0, False),
     "many tiles, cap and bias": ([97, 130, 64] * 15, [97, 130, 70] * 15, 16, 4, 128, True, None, 9.0, True),
+    # two teams of waves, that have several blocks of keys each
+    "two teams": ([150, 400], [150, 600], 64, 16, 128, True, [0, 500], 0.0, False),
+    "two teams, cap and bias": ([300, 100], [300, 90], 64, 64, 64, True, None, 9.0, True),
     # two or more parts of the rows, some of them without a step
     "parts": ([300, 20], [300, 700], 8, 2, 128, True, [0, 500], 0.0, False),
     "parts, small heads": ([520], [520], 6, 2, 64, True, None, 12.0, True),
@@ -192,6 +195,34 @@ def test_other_documents_may_be_anything():
         torch.cuda.synchronize()
         out.append([torch.cat([t[:40], t[90:]]) for t in (o, *d)])
     for one, two in zip(*out):
+        assert torch.equal(one, two)
+
+
+def test_far_rows():
+    """Rows 16 MiB apart, elements beyond 2^32 of one tensor, bit for bit as dense ones."""
+    H, Hkv, D, n, stride = 4, 2, 64, 600, 1 << 23
+    x = [normal(i, (n, h, D), "bf16")[0].to(DEV) for i, h in enumerate((H, Hkv, Hkv, H))]
+    a = csg.DocAttn(H, Hkv, D, "bf16")
+    p = ints([0, 50, n])
+    o, lse = torch.zeros((n, H, D), dtype=torch.bfloat16, device=DEV), torch.zeros((H, n), device=DEV)
+    ws = torch.zeros(a.workspace_bytes(n, n), dtype=torch.uint8, device=DEV)
+    d = [torch.zeros_like(t) for t in x[:3]]
+    a.forward(*x[:3], p, p, o, lse)
+    a.backward(*x[:3], p, p, o, lse, x[3], *d, ws)
+    torch.cuda.synchronize()
+    wide = torch.empty((n, stride), dtype=torch.bfloat16, device=DEV)
+    far, at = [], 0
+    for t in x[:3] + d:
+        w = t.shape[1] * D
+        far.append(wide[:, at:at + w].unflatten(1, (t.shape[1], D)))
+        at += w
+    for t, f in zip(x[:3], far):
+        f.copy_(t)
+    o2, lse2 = torch.zeros_like(o), torch.zeros_like(lse)
+    a.forward(*far[:3], p, p, o2, lse2)
+    a.backward(*far[:3], p, p, o2, lse2, x[3], *far[3:], ws)
+    torch.cuda.synchronize()
+    for one, two in zip((o, lse, *d), (o2, lse2, *far[3:])):
         assert torch.equal(one, two)
 
 
