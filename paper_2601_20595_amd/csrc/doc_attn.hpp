@@ -9,7 +9,7 @@
 
 namespace csg {
 
-constexpr int kDocTileRows = 128;  // (row, head) pairs of a tile: 4 waves of 32
+constexpr int kDocTileRows = 128;  // keys of a tile of the keys' gradient: 4 waves of 32
 constexpr int kDocBlock = 64;      // keys (gradient of keys and values: rows) per inner step
 
 struct DocAttnArgs {
@@ -30,7 +30,7 @@ struct DocAttnArgs {
   int64_t q_stride, k_stride, v_stride, dq_stride, dk_stride, dv_stride;
   int32_t q_rows, k_rows, n_docs;
   int32_t H, Hkv;
-  int32_t tile_heads;  // heads of a group that share a tile: 1, 2 or 4, a divisor of H / Hkv
+  int32_t tile_heads;  // heads of a group that share a tile of rows: 1, 2 or 4, a divisor of H / Hkv
   int32_t causal;
   int32_t cus;         // of the device
   int32_t row_parts;   // parts into which the keys' gradient cuts its rows
