@@ -81,11 +81,10 @@ __device__ __forceinline__ void load_tile(const uint16_t* src, int64_t stride, i
   const int stride2 = static_cast<int>(2 * stride);
 #pragma unroll
   for (int q = 0; q < kPer; ++q) {
-    // loads 4 q' of a wave: the turn of the pieces depends on q alone
     const int i = wave * kPer + q;
     constexpr int kTurns = 16 / kLoadRows<D>;
-    const int turn = swz<D>(kLoadRows<D> * (q % kTurns));
-    static_assert(kPer % kTurns == 0, "every wave starts at a multiple of 16 rows");
+    // (where every wave starts at a multiple of 16 rows, the turn of the pieces depends on q alone)
+    const int turn = swz<D>(kLoadRows<D> * ((kPer % kTurns == 0 ? q : i) % kTurns));
     const int voff = (kLoadRows<D> * i + ll.row) * stride2 + 16 * (ll.piece ^ turn);
     load_to_lds(rs, __builtin_amdgcn_readfirstlane(lds + 1024u * i), voff);
   }
@@ -287,13 +286,21 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_forward(DocAttnArgs a) {
 }
 
 // ---- gradient of the queries --------------------------------------------------------------
-// The forward's tiles; also leaves each row's statistics to the kernel of the keys' gradient. It
-// walks the keys twice, five products of the pairs in all. 8192 causal rows, 32 heads on 8 of 128:
-// 1.23 ms, 1.12 PFLOP/s, matrix instructions 56 % of the SIMDs' cycles, vector ones 43 %.
+// The forward's tiles; also leaves each row's statistics to the kernel of the keys' gradient.
+// D_i = sum_j P_ij (do_i . v_j) equals do_i . o_i, but for the rounding of o (and of the weights
+// that made it), which a row with few large weights cannot afford: there do . v_j - D cancels. With
+// it alone, gradients of 20 short documents were off by 3.7e-4 of their norm in fp16, not by 2.9e-4,
+// and of sharp scores in bf16 by 4.6e-3. One pass over the keys sums against D' = do_i . o_i:
+//   e_i = sum_j P_ij (do_i . v_j - D'_i) = D_i - D'_i,
+//   dQ_i / scale = sum_j P_ij (do_i . v_j - D'_i) (1 - tanh^2) k_j - e_i sum_j P_ij (1 - tanh^2) k_j.
+// For D = 128 the second sum takes the registers of the rows of do, which are read from LDS.
 template <class T, int D, bool kPlain, class S>
 __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
   constexpr int kTeams = S::kTeams, kKeys = S::kKeys, kTile = kKeys * D * 2;
+  constexpr bool kRowsInLds = D == 128;
   __shared__ __attribute__((aligned(1024))) unsigned char stage[2 * kTeams * 2 * kTile];
+  // by wave, fragment and lane; the teams hold the same
+  __shared__ u32x4_t s_rows[kRowsInLds ? S::kWaves * (D / 16) * 64 : 1];
   __shared__ float s_more[kTeams][S::kWaves][64];
   const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wave = any_wave % S::kWaves, team = any_wave / S::kWaves;
@@ -336,6 +343,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
   load_rows<T, D>(a.Q + p.q0 * a.q_stride + h * D, a.q_stride, row, ok, hlf, qf);
   const int64_t o_stride = static_cast<int64_t>(a.H) * D, o_head = p.q0 * o_stride + h * D;
   load_rows<T, D>(a.dO + o_head, o_stride, row, ok, hlf, gf);
+  u32x4_t* const my_rows = s_rows + (kRowsInLds ? wave * (D / 16) * 64 + lane : 0);
+  if constexpr (kRowsInLds) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) my_rows[64 * s] = __builtin_bit_cast(u32x4_t, gf[s]);
+  }
   const float c = a.scoring.unit * kLog2e;
   float delta = 0.0f, lse2 = 0.0f;
   {
@@ -352,60 +364,63 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
       lse2 = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
     }
   }
-  // The team's block j, whose loads have been issued, is there, and everyone is done with the one
-  // before; the next one's loads are issued, behind the last (`again`) the first one's.
-  auto turn = [&](int i, int j, bool again) {
-    wait_vm<0>();
-    __syncthreads();
-    if (j + kTeams < nb)
-      load(i + 1, j + kTeams);
-    else if (again && team < nb)
-      load(i + 1, team);
-    return (i & 1) * kTile;
-  };
-  // P (do . v - delta) of keys key0 .. key0 + 31, times the cap's slip in the second pass; 0 where
-  // masked.
-  auto gradients = [&](int buf, int kb, int key0, bool second, f32x16_t& ds) {
-    f32x16_t sc[1] = {f32x16_t{}}, dp{};
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      sc[0] = T::mfma(row_frag<T, D>(sK + buf, fr, s, 32 * kb), qf[s], sc[0]);
-      dp = T::mfma(row_frag<T, D>(sV + buf, fr, s, 32 * kb), gf[s], dp);
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] -= delta;
-    if constexpr (!kPlain) {
-      cap_scores<1>(a.scoring, sc);
-      if (second && a.scoring.cap_in != 0.0f) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] *= fmaf(-sc[0][r], sc[0][r], 1.0f);
-      }
-      bias_scores<1, -1>(a.scoring, slope, at - key0, hlf, sc);
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(sc[0][r], c, -lse2)) * dp[r];
-    if (key0 + 32 > wave_lo) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (key0 + result_row(r, hlf) >= hi) ds[r] = 0.0f;
-    }
-  };
-  // First pass: sum_j P_ij (do_i . v_j) itself. do_i . o_i equals it, but for the rounding of o
-  // (and of the weights that made it), which a row with few large weights cannot afford: there
-  // do . v_j - D cancels. With it alone, gradients of 20 short documents were off by 3.7e-4 of
-  // their norm in fp16, not by 2.9e-4, and of sharp scores in bf16 by 4.6e-3. It still serves
-  // to sum small terms.
   float more = 0.0f;
-  int i = 0;
-  for (int j = team; j - team < nb; j += kTeams, ++i) {
-    const int buf = turn(i, j, true);
+  f32x16_t acc[D / 32], keys[D / 32];  // the sums over the keys of the gradient against D', of the weights
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    acc[db] = f32x16_t{};
+    keys[db] = f32x16_t{};
+  }
+  for (int i = 0, j = team; i * kTeams < nb; ++i, j += kTeams) {
+    wait_vm<0>();
+    __syncthreads();  // the team's block j is there, and everyone is done with the one before
+    if (j + kTeams < nb) load(i + 1, j + kTeams);
     if (j >= wave_nb) continue;
+    const int buf = (i & 1) * kTile;
 #pragma unroll
     for (int kb = 0; kb < kKeys / 32; ++kb) {
-      f32x16_t ds;
-      gradients(buf, kb, j * kKeys + 32 * kb, false, ds);
+      const int key0 = j * kKeys + 32 * kb;
+      f32x16_t sc[1] = {f32x16_t{}}, dp{};
 #pragma unroll
-      for (int r = 0; r < 16; ++r) more += ds[r];
+      for (int s = 0; s < D / 16; ++s) {
+        sc[0] = T::mfma(row_frag<T, D>(sK + buf, fr, s, 32 * kb), qf[s], sc[0]);
+        const typename T::x8 g = kRowsInLds ? __builtin_bit_cast(typename T::x8, my_rows[64 * s]) : gf[s];
+        dp = T::mfma(row_frag<T, D>(sV + buf, fr, s, 32 * kb), g, dp);
+      }
+      f32x16_t slip{};
+      if constexpr (!kPlain) {
+        cap_scores<1>(a.scoring, sc);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) slip[r] = a.scoring.cap_in != 0.0f ? fmaf(-sc[0][r], sc[0][r], 1.0f) : 1.0f;
+        bias_scores<1, -1>(a.scoring, slope, at - key0, hlf, sc);
+      }
+      f32x16_t w;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) w[r] = __builtin_amdgcn_exp2f(fmaf(sc[0][r], c, -lse2));
+      if (key0 + 32 > wave_lo) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (key0 + result_row(r, hlf) >= hi) w[r] = dp[r] = 0.0f;  // (dp: it may be anything)
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        dp[r] = w[r] * (dp[r] - delta);
+        more += dp[r];
+        if constexpr (!kPlain) {
+          dp[r] *= slip[r];
+          w[r] *= slip[r];
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const typename T::x8 ds = pack<T>(dp, t), wt = pack<T>(w, t);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+          const typename T::x8 kf = col_frag<T, D>(sK_lds + buf, fr, db, 32 * kb + 16 * t);
+          acc[db] = T::mfma(kf, ds, acc[db]);
+          keys[db] = T::mfma(kf, wt, keys[db]);
+        }
+      }
     }
   }
   more = sum_halves(more);
@@ -416,33 +431,16 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
 #pragma unroll
     for (int n = 0; n < kTeams; ++n) more += s_more[n][wave][lane];
   }
-  delta += more;
   if (ok && hlf == 0 && team == 0) {
     const int64_t pitch = a.q_rows;
     float* st = a.stats + h * pitch + p.q0 + row;
     st[0] = lse2;
-    st[a.H * pitch] = -delta;
+    st[a.H * pitch] = -(delta + more);
   }
-  f32x16_t acc[D / 32];
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
-
-  for (int j = team; j - team < nb; j += kTeams, ++i) {
-    const int buf = turn(i, j, false);
-    if (j >= wave_nb) continue;
+  for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int kb = 0; kb < kKeys / 32; ++kb) {
-      f32x16_t ds;
-      gradients(buf, kb, j * kKeys + 32 * kb, true, ds);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const typename T::x8 w = pack<T>(ds, t);
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-          acc[db] = T::mfma(col_frag<T, D>(sK_lds + buf, fr, db, 32 * kb + 16 * t), w, acc[db]);
-      }
-    }
-  }
+    for (int r = 0; r < 16; ++r) acc[db][r] = fmaf(-more, keys[db][r], acc[db][r]);
   if constexpr (kTeams > 1) {
     static_assert(sizeof(stage) >= (kTeams - 1) * S::kWaves * 64 * (D / 2) * 4, "the teams' sums fit the buffers");
     f32x4_t* sums = reinterpret_cast<f32x4_t*>(stage) + wave * (D / 8) * 64 + lane;
@@ -719,7 +717,7 @@ hipError_t launch_rows(DocAttnArgs a, hipStream_t stream) {
   a.tile_heads = std::gcd(a.H / a.Hkv, S::kWaves);
   const dim3 grid(row_tiles<S>(a)), block(S::kThreads);
   if constexpr (kGradient)
-    hipLaunchKernelGGL((doc_grad_q<T, D, kPlain, S>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((doc_grad_q<T, D, kPlain, Shape<S::kWaves, S::kTeams, D == 128 ? 32 : S::kKeys>>), grid, block, 0, stream, a);
   else
     hipLaunchKernelGGL((doc_forward<T, D, kPlain, S>), grid, block, 0, stream, a);
   return hipGetLastError();
