@@ -458,22 +458,21 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
 // ---- gradients of the keys and values ------------------------------------------------------
 // A tile is 128 keys of one key/value head, 32 a wave, whose gradients stay in registers while
 // the rows that see them pass, head by head of the group: a sum over shared heads is no more
-// than a longer loop, in a fixed order. The accumulators leave room for one wave per SIMD (D =
-// 128), which has to keep its own loads ahead of their use. 8192 causal rows, 32 heads on 8 of 128:
-// 1.2 ms, four products of the pairs at 0.9 PFLOP/s, matrix instructions 40 % of the SIMDs' cycles
-// and vector ones 33 %: bound by one wave's waits between its phases. Reads without a phase's lead
-// 1.73 ms; two teams, one for each gradient, which both need the weights, 1.44; 64 keys a tile with
-// two workgroups a CU 1.41; products of the next rows during the weights spill (3.4).
+// than a longer loop, in a fixed order. For D = 128 the gradients take half of a wave's registers:
+// the rows of V are read from LDS, and a second team of waves takes the second half of each step's
+// rows, so that a SIMD has two waves although the longest causal tiles are as long as all of a CU's.
+template <int D>
+constexpr int kKvTeams = D == 128 ? 2 : 1;
+
 template <class T, int D, bool kPlain>
-__global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttnArgs a) {
-  constexpr int kTile = kDocBlock * D * 2;
-  constexpr bool kAhead = D == 128;
-  constexpr int kRing = kAhead ? 3 : 2;  // steps in LDS: the one at work, the next (kAhead: whose first rows it
-                                         // reads), and one loading
-  __shared__ __attribute__((aligned(1024))) unsigned char sQ[kRing * kTile];
-  __shared__ __attribute__((aligned(1024))) unsigned char sG[kRing * kTile];
-  __shared__ __attribute__((aligned(256))) float s_stats[kRing][2][kDocBlock];  // log-sum-exp, delta
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__global__ __launch_bounds__(256 * kKvTeams<D>, 2) void doc_grad_kv(DocAttnArgs a) {
+  constexpr int kTile = kDocBlock * D * 2, kTeams = kKvTeams<D>;
+  constexpr bool kRowsInLds = D == 128;
+  __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * kTile];  // rows of Q, of dO: two steps each
+  __shared__ u32x4_t s_rows[kRowsInLds ? 4 * (D / 16) * 64 : 1];  // of V, by wave, fragment and lane; the teams hold the same
+  __shared__ __attribute__((aligned(256))) float s_stats[2][2][kDocBlock];  // log-sum-exp, delta
+  const int lane = threadIdx.x & 63, any_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = any_wave & 3, team = any_wave >> 2;
   const int l32 = lane & 31, hlf = lane >> 5;
   const int kvh = blockIdx.x % a.Hkv, part = blockIdx.x / a.Hkv % a.row_parts;
   const Place p = find_place(a, blockIdx.x / (a.Hkv * a.row_parts), kDocTileRows, true);  // (the first keys have the most rows)
@@ -497,34 +496,39 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
 
   const LoadLane<D> ll(lane);
   const Frags<D> fr(lane);
+  const unsigned char* const sQ = stage;
+  const unsigned char* const sG = stage + 2 * kTile;
   const uint32_t sQ_addr = lds_address(sQ), sG_addr = lds_address(sG), st_addr = lds_address(s_stats);
   const int64_t o_stride = static_cast<int64_t>(a.H) * D;
   const int64_t pitch = a.q_rows;
   const uint16_t* qh = a.Q + p.q0 * a.q_stride + kvh * G * D;
   const uint16_t* gh = a.dO + p.q0 * o_stride + kvh * G * D;
   const int first_g = nb > 0 ? begin / nb : 0, first_j = begin - first_g * nb;
-  int load_g = first_g, load_j = first_j, load_at = 0;  // the next step to load: block load_j of head load_g, place in the ring
-  auto load = [&]() {
+  int load_g = first_g, load_j = first_j;  // the next step to load: block load_j of head load_g
+  auto load = [&](int at) {
     const int64_t r = r0 + load_j * kDocBlock;
     const int rows = p.q_len - static_cast<int>(r);
-    load_tile<D>(qh + r * a.q_stride + load_g * D, a.q_stride, rows, sQ_addr + load_at * kTile, wave, ll);
-    load_tile<D>(gh + r * o_stride + load_g * D, o_stride, rows, sG_addr + load_at * kTile, wave, ll);
-    if (wave < 2) {  // (as loads of the tile, or waiting for them would wait for the tile)
-      const float* st = a.stats + (wave * a.H + kvh * G + load_g) * pitch + p.q0 + r;
-      load_dword_to_lds(make_rsrc(st, 4 * min(kDocBlock, rows)), st_addr + 4 * kDocBlock * (load_at * 2 + wave), 4 * lane);
+    load_tile<D, kDocBlock, 4 * kTeams>(qh + r * a.q_stride + load_g * D, a.q_stride, rows, sQ_addr + at * kTile, any_wave, ll);
+    load_tile<D, kDocBlock, 4 * kTeams>(gh + r * o_stride + load_g * D, o_stride, rows, sG_addr + at * kTile, any_wave, ll);
+    if (any_wave < 2) {  // (as loads of the tile, or waiting for them would wait for the tile)
+      const float* st = a.stats + (any_wave * a.H + kvh * G + load_g) * pitch + p.q0 + r;
+      load_dword_to_lds(make_rsrc(st, 4 * min(kDocBlock, rows)), st_addr + 4 * kDocBlock * (at * 2 + any_wave), 4 * lane);
     }
-    load_at = load_at + 1 < kRing ? load_at + 1 : 0;
     if (++load_j == nb) {
       load_j = 0;
       ++load_g;
     }
   };
-  if (steps > 0) load();
-  if (kAhead && steps > 1) load();
+  if (steps > 0) load(0);
 
   typename T::x8 kf[D / 16], vf[D / 16];
   load_rows<T, D>(a.K + p.k0 * a.k_stride + kvh * D, a.k_stride, key, ok, hlf, kf);
   load_rows<T, D>(a.V + p.k0 * a.v_stride + kvh * D, a.v_stride, key, ok, hlf, vf);
+  u32x4_t* const my_rows = s_rows + (kRowsInLds ? wave * (D / 16) * 64 + lane : 0);
+  if constexpr (kRowsInLds) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) my_rows[64 * s] = __builtin_bit_cast(u32x4_t, vf[s]);
+  }
   f32x16_t dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) {
@@ -533,149 +537,107 @@ __global__ __launch_bounds__(kThreads, D == 64 ? 2 : 1) void doc_grad_kv(DocAttn
   }
   const float c = a.scoring.unit * kLog2e;
 
-  // kAhead: fragments are read from LDS a phase before they are multiplied: the rows of the next
-  // 32 while the last 32 are summed up, their columns while the products are formed.
-  typename T::x8 rq[D / 16], rg[D / 16], cq[2][D / 32], cg[2][D / 32];
-  f32x4_t lse2[4], delta[4];
-  auto read_stats = [&](int at, int rb) {
+  for (int i = 0, g = first_g, j = first_j; i < steps; ++i) {
+    wait_vm<0>();
+    __syncthreads();  // step i is there, and everyone is done with step i - 1
+    const int at = i & 1;
+    if (i + 1 < steps) load(at ^ 1);
+    const float slope = kPlain ? 0.0f : slope_of(a.scoring, kvh * G + g);
+    const unsigned char *tq = sQ + at * kTile, *tg = sG + at * kTile;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      lse2[b] = *reinterpret_cast<const f32x4_t*>(&s_stats[at][0][32 * rb + 8 * b + 4 * hlf]);
-      delta[b] = *reinterpret_cast<const f32x4_t*>(&s_stats[at][1][32 * rb + 8 * b + 4 * hlf]);
-    }
-  };
-  auto row_q = [&](int at, int rb, int s) { return row_frag<T, D>(sQ + at * kTile, fr, s, 32 * rb); };
-  auto row_g = [&](int at, int rb, int s) { return row_frag<T, D>(sG + at * kTile, fr, s, 32 * rb); };
-  auto col_q = [&](int at, int rb, int t, int db) {
-    return col_frag<T, D>((const lds_u8_t*)(sQ + at * kTile), fr, db, 32 * rb + 16 * t);
-  };
-  auto col_g = [&](int at, int rb, int t, int db) {
-    return col_frag<T, D>((const lds_u8_t*)(sG + at * kTile), fr, db, 32 * rb + 16 * t);
-  };
-  auto read_rows = [&](int at, int rb) {
-    read_stats(at, rb);
+    for (int n = 0; n < kDocBlock / 32 / kTeams; ++n) {
+      const int rb = kTeams == 1 ? n : team;
+      const int row0 = r0 + j * kDocBlock + 32 * rb;
+      if (row0 + 32 <= wave_lo || row0 >= p.q_len) continue;
+      // q . k and do . v - delta of 32 rows and the wave's keys
+      f32x16_t x{}, ds;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      rq[s] = row_q(at, rb, s);
-      rg[s] = row_g(at, rb, s);
-    }
-  };
-  // q . k and do . v - delta of 32 rows (half rb of the step in place `at`) and the wave's keys
-  auto products = [&](int at, int rb, f32x16_t& sc, f32x16_t& dp) {
-    if constexpr (!kAhead) read_stats(at, rb);
-    sc = f32x16_t{};
+      for (int b = 0; b < 4; ++b) {
+        const f32x4_t delta = *reinterpret_cast<const f32x4_t*>(&s_stats[at][1][32 * rb + 8 * b + 4 * hlf]);  // (negative)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] = delta[r >> 2][r & 3];  // (negative)
+        for (int r = 0; r < 4; ++r) ds[4 * b + r] = delta[r];
+      }
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) {
-      sc = T::mfma(kAhead ? rq[s] : row_q(at, rb, s), kf[s], sc);
-      dp = T::mfma(kAhead ? rg[s] : row_g(at, rb, s), vf[s], dp);
-    }
-    if constexpr (kAhead) {
+      for (int s = 0; s < D / 16; ++s) {
+        x = T::mfma(row_frag<T, D>(tq, fr, s, 32 * rb), kf[s], x);
+        const typename T::x8 v = kRowsInLds ? __builtin_bit_cast(typename T::x8, my_rows[64 * s]) : vf[s];
+        ds = T::mfma(row_frag<T, D>(tg, fr, s, 32 * rb), v, ds);
+      }
+      // them to weights and gradients of scores
+      if constexpr (!kPlain) {
+        f32x16_t sc[1] = {x};
+        cap_scores<1>(a.scoring, sc);
+        if (a.scoring.cap_in != 0.0f) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+          for (int r = 0; r < 16; ++r) ds[r] *= fmaf(-sc[0][r], sc[0][r], 1.0f);
+        }
+        bias_scores<1, 1>(a.scoring, slope, row0 + shift - key, hlf, sc);
+        x = sc[0];
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const f32x4_t lse2 = *reinterpret_cast<const f32x4_t*>(&s_stats[at][0][32 * rb + 8 * b + 4 * hlf]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[4 * b + r] = __builtin_amdgcn_exp2f(fmaf(x[4 * b + r], c, -lse2[r]));
+          ds[4 * b + r] *= x[4 * b + r];
+        }
+      }
+      if (row0 < wave_hi || row0 + 32 > p.q_len) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = row0 + result_row(r, hlf);
+          const bool out = row < lo || row >= p.q_len;
+          x[r] = out ? 0.0f : x[r];
+          ds[r] = out ? 0.0f : ds[r];
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const typename T::x8 wt = pack<T>(x, t), dt = pack<T>(ds, t);
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) {
-          cg[t][db] = col_g(at, rb, t, db);
-          cq[t][db] = col_q(at, rb, t, db);
+          dv[db] = T::mfma(col_frag<T, D>((const lds_u8_t*)tg, fr, db, 32 * rb + 16 * t), wt, dv[db]);
+          dk[db] = T::mfma(col_frag<T, D>((const lds_u8_t*)tq, fr, db, 32 * rb + 16 * t), dt, dk[db]);
         }
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);    // a product
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);  // reads from LDS
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  // them to weights and gradients of scores
-  auto weigh = [&](int row0, float slope, bool masked, f32x16_t& x, f32x16_t& dp) {
-    f32x16_t sc[1] = {x};
-    if constexpr (!kPlain) {
-      cap_scores<1>(a.scoring, sc);
-      if (a.scoring.cap_in != 0.0f) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] *= fmaf(-sc[0][r], sc[0][r], 1.0f);
-      }
-      bias_scores<1, 1>(a.scoring, slope, row0 + shift - key, hlf, sc);
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      x[r] = __builtin_amdgcn_exp2f(fmaf(sc[0][r], c, -lse2[r >> 2][r & 3]));
-      dp[r] *= x[r];
-    }
-    if (masked) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int row = row0 + result_row(r, hlf);
-        const bool out = row < lo || row >= p.q_len;
-        x[r] = out ? 0.0f : x[r];
-        dp[r] = out ? 0.0f : dp[r];
       }
     }
-  };
-  auto accumulate = [&](int at, int rb, int next_at, int next_rb, const f32x16_t& w, const f32x16_t& ds) {
-    if constexpr (kAhead) {
-      __builtin_amdgcn_sched_barrier(0);
-      read_rows(next_at, next_rb);
-    }
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const typename T::x8 wt = pack<T>(w, t), dt = pack<T>(ds, t);
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        dv[db] = T::mfma(kAhead ? cg[t][db] : col_g(at, rb, t, db), wt, dv[db]);
-        dk[db] = T::mfma(kAhead ? cq[t][db] : col_q(at, rb, t, db), dt, dk[db]);
-      }
-    }
-    if constexpr (kAhead) {
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  for (int i = 0, g = first_g, j = first_j, at = 0; i < steps; ++i) {
-    wait_vm<0>();
-    __syncthreads();  // step i (kAhead: i + 1 too) is there, and everyone is done with step i - 1
-    if (i + kRing - 1 < steps) load();
-    if (kAhead && i == 0) read_rows(0, 0);
-    const int next = at + 1 < kRing ? at + 1 : 0;
-    const int row0 = r0 + j * kDocBlock;
-    const float slope = kPlain ? 0.0f : slope_of(a.scoring, kvh * G + g);
-    const bool masked = row0 < wave_hi || row0 + kDocBlock > p.q_len;
-    if (kAhead || row0 + kDocBlock > wave_lo) {
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
-        f32x16_t sc, dp;
-        products(at, rb, sc, dp);
-        weigh(row0 + 32 * rb, slope, masked, sc, dp);
-        accumulate(at, rb, rb == 0 ? at : next, rb ^ 1, sc, dp);  // (behind the last step: old rows, unused)
-      }
-    }
-    at = next;
     if (++j == nb) {
       j = 0;
       ++g;
     }
   }
+  // the teams' sums: team 0 finishes those of the keys, team 1 those of the values
+  if constexpr (kTeams == 2) {
+    static_assert(sizeof(stage) >= 4 * 64 * (D / 2) * 4, "the sums fit the buffers");
+    f32x4_t* sums = reinterpret_cast<f32x4_t*>(stage) + wave * (D / 8) * 64 + lane;
+    __syncthreads();
+    if (team == 1) put_sums<D>(sums, dk);
+    __syncthreads();
+    if (team == 0) {
+      add_sums<D>(sums, dk, 1.0f, 1.0f);
+      put_sums<D>(sums, dv);  // (each lane in the places that it has read)
+    }
+    __syncthreads();
+    if (team == 1) add_sums<D>(sums, dv, 1.0f, 1.0f);
+  }
   if (!ok) return;
+  const bool has_dk = team == 0, has_dv = kTeams == 1 || team == 1;
   if (a.row_parts > 1) {  // for sum_parts
     float* to = a.parts + ((static_cast<int64_t>(part) * a.k_rows + p.k0 + key) * a.Hkv + kvh) * 2 * D + 4 * hlf;
+    auto put = [&](float* to, const f32x16_t (&x)[D / 32]) {
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+      for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        *reinterpret_cast<f32x4_t*>(to + 32 * db + 8 * b) =
-            f32x4_t{dk[db][4 * b], dk[db][4 * b + 1], dk[db][4 * b + 2], dk[db][4 * b + 3]};
-        *reinterpret_cast<f32x4_t*>(to + D + 32 * db + 8 * b) =
-            f32x4_t{dv[db][4 * b], dv[db][4 * b + 1], dv[db][4 * b + 2], dv[db][4 * b + 3]};
-      }
+        for (int b = 0; b < 4; ++b)
+          *reinterpret_cast<f32x4_t*>(to + 32 * db + 8 * b) = f32x4_t{x[db][4 * b], x[db][4 * b + 1], x[db][4 * b + 2], x[db][4 * b + 3]};
+    };
+    if (has_dk) put(to, dk);
+    if (has_dv) put(to + D, dv);
     return;
   }
-  store_rows<T, D>(a.dK + p.k0 * a.dk_stride + kvh * D, a.dk_stride, key, hlf, dk, a.scale);
-  store_rows<T, D>(a.dV + p.k0 * a.dv_stride + kvh * D, a.dv_stride, key, hlf, dv, 1.0f);
+  if (has_dk) store_rows<T, D>(a.dK + p.k0 * a.dk_stride + kvh * D, a.dk_stride, key, hlf, dk, a.scale);
+  if (has_dv) store_rows<T, D>(a.dV + p.k0 * a.dv_stride + kvh * D, a.dv_stride, key, hlf, dv, 1.0f);
 }
 
 // Sums the parts of the keys' and values' gradients, in their order: four elements a thread. Keys
@@ -747,7 +709,7 @@ hipError_t grad(const DocAttnArgs& a, hipStream_t stream) {
   hipError_t e = launch_rows<T, D, kPlain, true>(a, stream);
   if (e != hipSuccess) return e;
   const int64_t k_tiles = doc_key_tiles(a.k_rows, a.n_docs) * a.Hkv;
-  hipLaunchKernelGGL((doc_grad_kv<T, D, kPlain>), dim3(k_tiles * a.row_parts), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((doc_grad_kv<T, D, kPlain>), dim3(k_tiles * a.row_parts), dim3(256 * kKvTeams<D>), 0, stream, a);
   e = hipGetLastError();
   if (e != hipSuccess || a.row_parts == 1) return e;
   const int64_t sums = static_cast<int64_t>(a.k_rows) * a.Hkv * (2 * D / 4);
