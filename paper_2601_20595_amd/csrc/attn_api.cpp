@@ -146,7 +146,7 @@ csg::DocAttnArgs doc_args(const csg_doc_attn_cfg& c, int32_t cus, const void* q,
 int64_t stats_bytes(const csg_doc_attn_cfg& c) { return (2 * c.q_rows * c.n_heads * 4 + 15) / 16 * 16; }
 int64_t part_bytes(const csg_doc_attn_cfg& c) { return c.k_rows * c.n_kv_heads * 2 * c.head_dim * 4; }
 int32_t row_parts(const csg_doc_attn_cfg& c, int64_t n_docs, int32_t cus) {
-  return csg::doc_row_parts(c.q_rows, c.k_rows, n_docs, c.n_heads, c.n_kv_heads, cus);
+  return csg::doc_row_parts(c.q_rows, c.k_rows, n_docs, c.n_heads, c.n_kv_heads, c.head_dim, cus);
 }
 int64_t grad_workspace(const csg_doc_attn_cfg& c, int64_t n_docs, int32_t cus) {
   const int32_t parts = row_parts(c, n_docs, cus);

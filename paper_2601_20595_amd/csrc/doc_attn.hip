@@ -293,7 +293,10 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_forward(DocAttnArgs a) {
 // and of sharp scores in bf16 by 4.6e-3. One pass over the keys sums against D' = do_i . o_i:
 //   e_i = sum_j P_ij (do_i . v_j - D'_i) = D_i - D'_i,
 //   dQ_i / scale = sum_j P_ij (do_i . v_j - D'_i) (1 - tanh^2) k_j - e_i sum_j P_ij (1 - tanh^2) k_j.
-// For D = 128 the second sum takes the registers of the rows of do, which are read from LDS.
+// For D = 128 the second sum takes the registers of the rows of do, which are read from LDS. 8192 causal
+// rows, 32 heads on 8 of 128: 0.88 ms, four products of the pairs at 1.25 PFLOP/s, which is what a
+// large matrix product of the library reaches on the card: bound by the matrix instructions and the
+// clock that their power leaves. A pass of its own for D took five products and 1.23 ms.
 template <class T, int D, bool kPlain, class S>
 __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
   constexpr int kTeams = S::kTeams, kKeys = S::kKeys, kTile = kKeys * D * 2;
@@ -461,6 +464,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
 // than a longer loop, in a fixed order. For D = 128 the gradients take half of a wave's registers:
 // the rows of V are read from LDS, and a second team of waves takes the second half of each step's
 // rows, so that a SIMD has two waves although the longest causal tiles are as long as all of a CU's.
+// 8192 causal rows, 32 heads on 8 of 128: 1.10 ms, four products of the pairs at 1.0 PFLOP/s; both teams
+// meet at each step's barrier, and what a wave does between its products is not all hidden. One team,
+// fragments read a phase ahead: 1.27; without that 1.73; a team for each gradient, which both need the
+// weights, 1.44; tiles of 64 keys with two workgroups a CU 1.41; the second team's sums a step late,
+// behind the first team's products, 1.14. Two teams for heads of 64: packed documents of up to 900
+// rows 94 instead of 89 us, 4096 rows 135 instead of 155.
 template <int D>
 constexpr int kKvTeams = D == 128 ? 2 : 1;
 
@@ -686,16 +695,21 @@ hipError_t launch_rows(DocAttnArgs a, hipStream_t stream) {
 }
 
 // The shape of the tiles. While there are no more than CUs, the longest tile's way through its keys is
-// what a call takes: four teams on half as many rows; up to two a CU two teams; with more they would
-// only wait for each other. Forward, one causal document, whole / halves / quarters, us: 32 heads on 8 of
-// 128, 512 rows (136 tiles) 16.3 / 15.4 / 12.7; 1024 rows (264) 26.8 / 22.5 / 25.1; 2048 rows (520) 53.9 /
-// 47.8 / 69.0; 4096 rows (1032) 149 / 157 / 225; 12 heads of 64, 2048 rows (204) 36.0 / 25.6 / 19.2, 4096 rows
-// (396) 77.6 / 50.0 / 46.4 (and its gradient 210 / 183 / 191); 16 documents of 250 rows (564) 13.8 / 16.6 / 17.5.
+// what a call takes: four teams on half as many rows; up to two a CU two teams (heads of 64 forward, of
+// which a CU holds two such workgroups: four); with more they would only wait for each other. Forward, one
+// causal document, whole / halves / quarters, us: 32 heads on 8 of 128, 512 rows (136 tiles) 16.3 / 15.4 /
+// 12.7; 1024 rows (264) 26.8 / 22.5 / 25.1; 1700 rows, capped (432) - / 46.4 / 64.4; 2048 rows (520) 53.9 / 47.8 /
+// 69.0; 4096 rows (1032) 149 / 157 / 225; 12 heads of 64, 2048 rows (204) 36.0 / 25.6 / 19.2; 4096 rows (396) 77.6 /
+// 50.0 / 46.1; 5 documents of 700 (384) - / 21.3 / 19.0; 3000 rows, capped (288) - / 53.4 / 38.4; 16 documents of
+// 250 (564) 13.8 / 16.6 / 17.5. The gradient of heads of 64: 4096 rows (396) - / 155 / 165, 8 documents of 500,
+// capped (468) - / 60 / 64, 8 of 700 (612) 61 / 68 / -; of 128, 5 documents of 700 (912) 160 / 175 / -.
 template <class T, int D, bool kPlain, bool kGradient>
 hipError_t launch_rows(const DocAttnArgs& a, hipStream_t stream) {
   const int64_t tiles = row_tiles<Whole>(a);
-  if (tiles <= a.cus) return launch_rows<T, D, kPlain, kGradient, Quarters>(a, stream);
-  if (tiles <= 2 * a.cus) return launch_rows<T, D, kPlain, kGradient, Halves>(a, stream);
+  if (tiles <= (!kGradient && D == 64 ? 2 : 1) * a.cus) return launch_rows<T, D, kPlain, kGradient, Quarters>(a, stream);
+  if constexpr (kGradient || D == 128) {
+    if (tiles <= 2 * a.cus) return launch_rows<T, D, kPlain, kGradient, Halves>(a, stream);
+  }
   return launch_rows<T, D, kPlain, kGradient, Whole>(a, stream);
 }
 

@@ -43,17 +43,18 @@ inline int64_t doc_key_tiles(int64_t k_rows, int64_t n_docs) { return k_rows / k
 // A tile of keys walks the rows of all heads of its group one after the other: where the tiles
 // leave CUs idle, the rows are cut into parts, whose sums are added up in a kernel of their own.
 // There is a part for every CU while each has four steps (documents being of the same length),
-// and for every half CU, which evens out the causal tiles, while each has 16; at most 16. 32
-// heads on 8 of 128, causal, the whole gradient: 512 rows 106 -> 56 us (7 parts), 1024 rows 194 ->
-// 95 (7), 2048 rows 375 -> 201 (3), 4096 rows 846 -> 647 (2); but 16 documents of 250 rows, 256
-// tiles of 16 steps, 110 -> 129 us with two parts.
-inline int32_t doc_row_parts(int64_t q_rows, int64_t k_rows, int64_t n_docs, int32_t H, int32_t Hkv, int32_t cus) {
+// and two for every workgroup that the CUs hold (one each, of heads of 64 two), which evens out the
+// causal tiles, while each has 16; at most 16. The whole gradient, causal: 32 heads on 8 of 128, 512
+// rows 106 -> 47 us (7 parts), 1024 rows 194 -> 82 (7), 3000 rows 457 -> 331 (2), 4096 rows 685 -> 540 (2), with
+// half as many again 2048 rows 180 -> 198; 32 on 8 of 64, 8192 rows 1237 -> 1070 (2); but 16 documents of 250
+// rows, 256 tiles of 16 steps of 128 elements, 110 -> 129 us with two parts.
+inline int32_t doc_row_parts(int64_t q_rows, int64_t k_rows, int64_t n_docs, int32_t H, int32_t Hkv, int32_t head_dim, int32_t cus) {
   const int64_t tiles = ((k_rows + kDocTileRows - 1) / kDocTileRows + n_docs / 2) * Hkv;
   const int64_t steps = (q_rows / (n_docs < 1 ? 1 : n_docs) + kDocBlock - 1) / kDocBlock * (H / Hkv);
   int32_t parts = 1;
   if (k_rows == 0) return parts;
   while (parts < 16 && ((tiles * (parts + 1) <= cus && steps >= 4 * (parts + 1)) ||
-                        (tiles * (parts + 1) <= 2 * static_cast<int64_t>(cus) && steps >= 16 * (parts + 1))))
+                        (tiles * (parts + 1) <= (head_dim == 64 ? 4 : 2) * static_cast<int64_t>(cus) && steps >= 16 * (parts + 1))))
     ++parts;
   return parts;
 }
