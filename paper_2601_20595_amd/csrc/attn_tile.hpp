@@ -123,6 +123,23 @@ __device__ __forceinline__ void wait_vm() {
 
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+// The values, loaded by ordinary loads, are there. To be called ahead of a loop that only
+// uses them: the compiler, which does not see the loads to LDS, would otherwise wait before
+// their use in each turn until nothing is in flight, the tiles that the turn has just asked for included.
+template <class X8, int N>
+__device__ __forceinline__ void arrived(X8 (&f)[N]) {
+#pragma unroll
+  for (int s = 0; s < N; ++s) {
+    u32x4_t raw = __builtin_bit_cast(u32x4_t, f[s]);
+    asm volatile("" : "+v"(raw));
+    f[s] = __builtin_bit_cast(X8, raw);
+  }
+}
+__device__ __forceinline__ float arrived(float x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Rows one load_to_lds fills (1 KiB), and the loads of a tile of `rows` rows.
 template <int D>
 constexpr int kLoadRows = 512 / D;

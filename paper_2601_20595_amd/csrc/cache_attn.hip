@@ -367,6 +367,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
   RowSoftmax sm;
+  arrived(qf);
   for (int n = 0; n < mine_n; ++n) {
     const bool more = n + 1 < mine_n;
     wait_vm<kLoads>();  // the keys are there; the values may be on their way
@@ -476,6 +477,7 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
   for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
   RowSoftmax sm;
   const bool idle = p.tile * kCacheTileRows >= x.rows;  // no row in this wave
+  arrived(qf);
   for (int n = 0; n < nb; ++n) {
     wait_vm<0>();
     __syncthreads();  // block n is there, and everyone is done with block n - 1

@@ -194,6 +194,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_forward(DocAttnArgs a) {
   for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
   RowSoftmax sm;
   const float c = a.scoring.unit * kLog2e;
+  arrived(qf);
 
   for (int i = 0, j = team; i * kTeams < nb; ++i, j += kTeams) {
     wait_vm<0>();
@@ -374,6 +375,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
     acc[db] = f32x16_t{};
     keys[db] = f32x16_t{};
   }
+  arrived(qf);
+  if constexpr (!kRowsInLds) arrived(gf);
   for (int i = 0, j = team; i * kTeams < nb; ++i, j += kTeams) {
     wait_vm<0>();
     __syncthreads();  // the team's block j is there, and everyone is done with the one before
@@ -545,13 +548,16 @@ __global__ __launch_bounds__(256 * kKvTeams<D>, 2) void doc_grad_kv(DocAttnArgs 
     dv[db] = f32x16_t{};
   }
   const float c = a.scoring.unit * kLog2e;
+  arrived(kf);
+  if constexpr (!kRowsInLds) arrived(vf);
 
+  auto slope_at = [&](int g) { return kPlain ? 0.0f : arrived(slope_of(a.scoring, kvh * G + g)); };
+  float slope = steps > 0 ? slope_at(first_g) : 0.0f;
   for (int i = 0, g = first_g, j = first_j; i < steps; ++i) {
     wait_vm<0>();
     __syncthreads();  // step i is there, and everyone is done with step i - 1
     const int at = i & 1;
     if (i + 1 < steps) load(at ^ 1);
-    const float slope = kPlain ? 0.0f : slope_of(a.scoring, kvh * G + g);
     const unsigned char *tq = sQ + at * kTile, *tg = sG + at * kTile;
 #pragma unroll
     for (int n = 0; n < kDocBlock / 32 / kTeams; ++n) {
@@ -613,7 +619,7 @@ __global__ __launch_bounds__(256 * kKvTeams<D>, 2) void doc_grad_kv(DocAttnArgs 
     }
     if (++j == nb) {
       j = 0;
-      ++g;
+      if (++g < G) slope = slope_at(g);
     }
   }
   // the teams' sums: team 0 finishes those of the keys, team 1 those of the values
