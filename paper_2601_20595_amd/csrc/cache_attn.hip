@@ -133,11 +133,11 @@ __global__ __launch_bounds__(kThreads) void cache_append(AppendArgs a) {
 // which cache_merge joins. With the tiles counted through, tile t of run w is in place t + 4 w:
 // of two parts one after the other, the second has a later tile, or the next run and at most
 // the three tiles before.
-// Bound by the memory where keys are many: 2 sequences of over 100000, 918 MB in 163 us and the merge
+// Bound by the memory where keys are many: 2 sequences of over 100000, 918 MB in 160 us and the merge
 // 7, 5.4 TB/s; 64 sequences of up to 8000, 483 MB, 94 and 6. With few keys by a chain of latencies
-// (bounds, page numbers, keys, products, partial results), 8 to 9 us for 900 keys; where 16
+// (bounds, page numbers, keys, products, partial results), 9 us for 900 keys; where 16
 // sequences' rows share 8192 keys by what a part costs besides its keys and by 16 MB of partial
-// results (38 us and 8; the keys alone would take 27).
+// results (36 us and 8; the keys alone would take 27).
 struct Entry {
   int token0, rows;    // first token, (token, head) rows
   int b0, b1;          // its sequences; the first one's pages are read

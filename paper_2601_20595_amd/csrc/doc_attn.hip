@@ -138,12 +138,12 @@ __device__ __forceinline__ void add_sums(const f32x4_t* from, f32x16_t (&acc)[D 
 // computes keys x rows, so that a row's scores, maximum and sum stay in two lanes and the rounded
 // weights already are the operand of values x weights: nothing but keys and values passes LDS.
 // Long documents are bound by the SIMDs' issue: per block of 64 keys, 32 products and some 200
-// vector instructions of the softmax. 8192 causal rows, 32 heads on 8 of 128: 549 us, 1.0 PFLOP/s of
-// visible pairs; matrix instructions take 47 % of the SIMDs' cycles, vector ones 41 %, LDS 24 %,
-// without a bank conflict, at 2.0 GHz. Priorities around the products (553 us) and blocks cut into
-// halves of 32 keys (569) did no better; products of the next block during the softmax spill.
-// Capped scores of few long documents are bound by tanh on the longest one's tiles (92 us, 5
-// documents of up to 3500 keys).
+// vector instructions of the softmax. 8192 causal rows, 32 heads on 8 of 128: 521 us, 1.06 PFLOP/s of
+// visible pairs; matrix instructions take 52 % of the SIMDs' cycles, vector ones 45 %, LDS 26 %,
+// without a bank conflict, at 1.95 GHz. Priorities around the products and blocks cut into halves of
+// 32 keys (3 % slower) did no better; products of the next block during the softmax spill.
+// Capped scores of few long documents are bound by tanh on the longest one's tiles (83 us, 5
+// documents of up to 2446 keys, 16 heads on 2).
 template <class T, int D, bool kPlain, class S>
 __global__ __launch_bounds__(S::kThreads, 2) void doc_forward(DocAttnArgs a) {
   constexpr int kTeams = S::kTeams, kKeys = S::kKeys, kTile = kKeys * D * 2;
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_forward(DocAttnArgs a) {
 //   e_i = sum_j P_ij (do_i . v_j - D'_i) = D_i - D'_i,
 //   dQ_i / scale = sum_j P_ij (do_i . v_j - D'_i) (1 - tanh^2) k_j - e_i sum_j P_ij (1 - tanh^2) k_j.
 // For D = 128 the second sum takes the registers of the rows of do, which are read from LDS. 8192 causal
-// rows, 32 heads on 8 of 128: 0.88 ms, four products of the pairs at 1.25 PFLOP/s, which is what a
+// rows, 32 heads on 8 of 128: 0.88 to 0.92 ms, four products of the pairs at 1.2 PFLOP/s, which is what a
 // large matrix product of the library reaches on the card: bound by the matrix instructions and the
 // clock that their power leaves. A pass of its own for D took five products and 1.23 ms.
 template <class T, int D, bool kPlain, class S>
@@ -467,11 +467,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
 // than a longer loop, in a fixed order. For D = 128 the gradients take half of a wave's registers:
 // the rows of V are read from LDS, and a second team of waves takes the second half of each step's
 // rows, so that a SIMD has two waves although the longest causal tiles are as long as all of a CU's.
-// 8192 causal rows, 32 heads on 8 of 128: 1.10 ms, four products of the pairs at 1.0 PFLOP/s; both teams
+// 8192 causal rows, 32 heads on 8 of 128: 1.05 to 1.10 ms, four products of the pairs at 1.0 PFLOP/s, 47 % matrix
+// and 24 % vector instructions; both teams
 // meet at each step's barrier, and what a wave does between its products is not all hidden. One team,
 // fragments read a phase ahead: 1.27; without that 1.73; a team for each gradient, which both need the
 // weights, 1.44; tiles of 64 keys with two workgroups a CU 1.41; the second team's sums a step late,
-// behind the first team's products, 1.14. Two teams for heads of 64: packed documents of up to 900
+// behind the first team's products, 1.14. Two teams for heads of 64: packed documents of up to 721
 // rows 94 instead of 89 us, 4096 rows 135 instead of 155.
 template <int D>
 constexpr int kKvTeams = D == 128 ? 2 : 1;

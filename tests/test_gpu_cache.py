@@ -1,5 +1,8 @@
 """The paged key/value cache on the GPU: append and attention, element by element against the
 fp64 oracle, and a run of both with attention over documents."""
+import os
+import re
+
 import numpy as np
 import pytest
 
@@ -399,3 +402,22 @@ def test_prompt_drafts_and_decoding_agree_with_documents():
         # the two see the same rounded keys: only the order of sums and of weights' references differs
         both = 2 * ref[1]
         close(o, f64(o2), both, "cache against documents")
+
+
+def test_readme_example():
+    """The attention example of README.md runs, and its cache gives what its documents give."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    blocks = re.findall(r"```py\n(.*?)```", text, re.S)
+    assert len(blocks) == 1
+    names = {}
+    exec(compile(blocks[0], "README.md", "exec"), names)
+    torch.cuda.synchronize()
+    got = names["o"].clone()
+    # the same rotated queries and keys as documents: the keys of a sequence from its pages
+    pages, table, lens = names["k_pages"], names["table"].long(), names["lens"].tolist()
+    k = torch.cat([pages[table[b]].permute(0, 2, 1, 3).reshape(-1, 8, 128)[:n] for b, n in enumerate(lens)])
+    names["attn"].forward(names["q"], k, names["v"], names["ptr"], names["ptr"], names["o"], names["lse"])
+    torch.cuda.synchronize()
+    # a rounding of each of the two outputs and of their weights: values are averaged, |v| < 6
+    assert float((got.float() - names["o"].float()).abs().max()) <= 4 * HALF_STEP["bf16"] * 6
+    assert all(bool(torch.isfinite(names[x].float()).all()) for x in ("dq", "dk", "dv", "lse"))
