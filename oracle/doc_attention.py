@@ -59,6 +59,12 @@ def _head(q, k, sc: Scores, h: int, prefix: int):
     return np.where(visible(rows, keys, sc.causal, prefix), s, -np.inf), t, size
 
 
+# The least normal fp32 number (and bf16 number). Below it a value may count as 0, which it is then off
+# by at most: a weight, so that its gradient of a score is off by that times do . v - D, that gradient
+# itself, a result.
+LEAST = 2.0 ** -126
+
+
 def _weights(s):
     if s.shape[1] == 0:
         return np.zeros_like(s), np.full(s.shape[0], -np.inf)
@@ -83,8 +89,8 @@ def attention(q, k, v, sc: Scores, prefix: int = 0, u: float = 0.0, tiny: float 
         vh = v[:, h // G]
         es = 2.0 ** -17 * size
         o[:, h] = p @ vh
-        wide = (np.where(p > 0, p * (2 * es + u), 0.0) + tiny * np.isfinite(s)) @ np.abs(vh)
-        eo[:, h] = u * np.abs(o[:, h]) + tiny + wide
+        wide = (np.where(p > 0, p * (2 * es + u), 0.0) + (tiny + LEAST) * np.isfinite(s)) @ np.abs(vh)
+        eo[:, h] = u * np.abs(o[:, h]) + tiny + LEAST + wide
         el[h] = (p * es).sum(axis=1) + 2.0 ** -20 * (1 + np.abs(np.where(np.isfinite(lse[h]), lse[h], 0.0)))
     return o, lse, eo, el
 
@@ -109,8 +115,8 @@ def attention_grad(q, k, v, do, sc: Scores, prefix: int = 0, u: float = 0.0, tin
         ds = p * (dp - delta) * slip
         e_delta = (np.abs(do[:, h]) * (eo[:, h] + 2.0 ** -17 * np.abs(o[:, h]))).sum(axis=1, keepdims=True)
         e_dp = 2.0 ** -17 * (np.abs(do[:, h]) @ np.abs(v[:, g]).T)
-        e_ds = np.abs(ds) * (2 * es + u) + p * (e_delta + e_dp) + 2.0 ** -20 * p * np.abs(dp - delta) + tiny * seen
-        e_p = p * (2 * es + u) + tiny * seen
+        e_ds = np.abs(ds) * (2 * es + u) + p * (e_delta + e_dp) + 2.0 ** -20 * p * np.abs(dp - delta) + (tiny + LEAST * (1 + np.abs(dp - delta))) * seen
+        e_p = p * (2 * es + u) + (tiny + LEAST) * seen
         d[0][:, h] = scale * ds @ k[:, g]
         e[0][:, h] = scale * e_ds @ np.abs(k[:, g])
         d[1][:, g] += scale * ds.T @ q[:, h]
@@ -118,7 +124,7 @@ def attention_grad(q, k, v, do, sc: Scores, prefix: int = 0, u: float = 0.0, tin
         d[2][:, g] += p.T @ do[:, h]
         e[2][:, g] += e_p.T @ np.abs(do[:, h])
     for x, b in zip(d, e):
-        b += u * np.abs(x) + tiny
+        b += u * np.abs(x) + tiny + LEAST
     return tuple(d), tuple(e)
 
 

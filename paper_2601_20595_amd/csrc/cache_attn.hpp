@@ -13,9 +13,9 @@ constexpr int kCacheTileRows = 32;     // (token, head) rows of a tile, one wave
 constexpr int kCacheWideRows = 128;    // rows of a wide task: a tile for each of four waves
 constexpr int kCacheBlock = 32;        // keys per inner step of a wave, and unit of work
 constexpr int kCacheWideBlock = 64;    // keys per inner step of a wide task
-// What beginning and ending a task costs, in blocks. 64 sequences on four shared prompts 54.6 us with 0,
-// 53.4 with 4, 56.2 with 8, 63.1 with 16; 12 sequences of 5 tokens on one 25.2, 21.6, 22.5, 21.7; 64
-// unrelated sequences 102, 99.6, 100.8, 103.5.
+// What beginning and ending a task costs, in blocks. 64 sequences on four shared prompts 47.9 us with 3,
+// 48.8 with 4, 49.0 with 6, 49.6 with 8; 12 sequences of 5 tokens on one 23.1, 22.5, 20.7, 22.0; 64 unrelated
+// sequences 99.4, 100, 99.7, 98.7: it matters where the cuts happen to fall, and no value is best for all.
 constexpr int kCacheTaskCost = 4;
 constexpr int kCacheMinRun = 4;  // units a workgroup takes at least: a block for each wave
 constexpr int kMaxCacheEntries = 2048; // sequences and groups of one call

@@ -702,21 +702,23 @@ hipError_t launch_rows(DocAttnArgs a, hipStream_t stream) {
 }
 
 // The shape of the tiles. While there are no more than CUs, the longest tile's way through its keys is
-// what a call takes: four teams on half as many rows; up to two a CU two teams (heads of 64 forward, of
-// which a CU holds two such workgroups: four); with more they would only wait for each other. Forward, one
-// causal document, whole / halves / quarters, us: 32 heads on 8 of 128, 512 rows (136 tiles) 16.3 / 15.4 /
-// 12.7; 1024 rows (264) 26.8 / 22.5 / 25.1; 1700 rows, capped (432) - / 46.4 / 64.4; 2048 rows (520) 53.9 / 47.8 /
-// 69.0; 4096 rows (1032) 149 / 157 / 225; 12 heads of 64, 2048 rows (204) 36.0 / 25.6 / 19.2; 4096 rows (396) 77.6 /
-// 50.0 / 46.1; 5 documents of 700 (384) - / 21.3 / 19.0; 3000 rows, capped (288) - / 53.4 / 38.4; 16 documents of
-// 250 (564) 13.8 / 16.6 / 17.5. The gradient of heads of 64: 4096 rows (396) - / 155 / 165, 8 documents of 500,
-// capped (468) - / 60 / 64, 8 of 700 (612) 61 / 68 / -; of 128, 5 documents of 700 (912) 160 / 175 / -.
+// what a call takes: four teams on half as many rows. Up to two a CU it still is if the documents are
+// long, of 1000 keys on the average: two teams (forward with heads of 64, of which a CU holds two such
+// workgroups, four teams a little beyond a tile a CU). With more tiles or shorter documents the teams
+// would only wait for each other. Whole / halves / quarters, us, forward, documents causal and of one
+// length: 32 heads on 8 of 128, 512 rows (136 tiles) 16.2 / 15.5 / 12.9; 1024 (264) 26.0 / 22.3 / 25.6; 2 of
+// 1000 (512) 37.0 / 32.9 / 50.5; 2048 (520) 50.2 / 47.4 / 68.1; 4096 (1032) 148 / 153 / 210; 12 heads of 64, 2048 rows
+// (204) 33.6 / 24.7 / 18.7, 3000 (288) 46.4 / 32.9 / 28.9, capped 64.0 / 52.1 / 39.0, 4096 (396) 62.7 / 44.3 / 46.3; 32 on
+// 8 of 64, 2 of 1000 (512) 25.2 / 22.5 / 26.9; 12 heads of 64, 4 documents of 250 (132) 8.7 / 9.0 / 7.8, 5 of 700
+// (384) 17.2 / 20.4 / 17.9, 16 of 250 (564) 13.2 / 16.9 / 17.7; 16 on 4 of 128, capped, 10 of 250 (352) 17.1 /
+// 24.6 / 29.9. With the gradient: 16 on 4 of 128, capped, 3000 rows (376) 338 / 289 / 344, 10 of 250 81 / 98 / 117.
 template <class T, int D, bool kPlain, bool kGradient>
 hipError_t launch_rows(const DocAttnArgs& a, hipStream_t stream) {
   const int64_t tiles = row_tiles<Whole>(a);
-  if (tiles <= (!kGradient && D == 64 ? 2 : 1) * a.cus) return launch_rows<T, D, kPlain, kGradient, Quarters>(a, stream);
-  if constexpr (kGradient || D == 128) {
-    if (tiles <= 2 * a.cus) return launch_rows<T, D, kPlain, kGradient, Halves>(a, stream);
-  }
+  const bool long_docs = a.k_rows >= int64_t{1000} * a.n_docs;
+  if (tiles <= a.cus || (!kGradient && D == 64 && long_docs && 4 * tiles <= 5 * static_cast<int64_t>(a.cus)))
+    return launch_rows<T, D, kPlain, kGradient, Quarters>(a, stream);
+  if (tiles <= 2 * a.cus && long_docs) return launch_rows<T, D, kPlain, kGradient, Halves>(a, stream);
   return launch_rows<T, D, kPlain, kGradient, Whole>(a, stream);
 }
 

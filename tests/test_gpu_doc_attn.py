@@ -33,8 +33,10 @@ CASES = {
     "many tiles of four heads": ([97, 130, 64] * 15, [97, 130, 70] * 15, 16, 4, 128, True, [10] * 45, 0.0, False),
     "many tiles, cap and bias": ([97, 130, 64] * 15, [97, 130, 70] * 15, 16, 4, 128, True, None, 9.0, True),
     # two teams of waves, that have several blocks of keys each
-    "two teams": ([150, 400], [150, 600], 64, 16, 128, True, [0, 500], 0.0, False),
-    "two teams, cap and bias": ([300, 100], [300, 90], 64, 64, 64, True, None, 9.0, True),
+    "two teams": ([400, 150], [1600, 600], 64, 16, 128, True, [0, 500], 0.0, False),
+    "two teams, cap and bias": ([400], [1000], 96, 96, 64, True, None, 9.0, True),
+    "four teams, small heads": ([300], [1100], 96, 96, 64, True, None, 0.0, False),
+    "short documents, more tiles than CUs": ([150, 400], [150, 600], 64, 16, 128, True, [0, 500], 0.0, False),
     # two or more parts of the rows, some of them without a step
     "parts": ([300, 20], [300, 700], 8, 2, 128, True, [0, 500], 0.0, False),
     "parts, small heads": ([520], [520], 6, 2, 64, True, None, 12.0, True),
