@@ -90,12 +90,15 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 
 // One 16-byte-per-lane load of 1 KiB into LDS at lds (lane l: byte 16 l), from byte voff of
 // the resource. In inline asm (M0 saved and restored), so that the compiler does not wait for
-// it before every LDS read: the caller waits (wait_vm) before the tile is read.
+// it before every LDS read: the caller waits (wait_vm) before the tile is read. A load to LDS
+// may read M0 no sooner than one instruction after it was written (s_nop), and the compiler
+// does not look for such pairs inside of asm.
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rs, uint32_t lds, int voff) {
   uint32_t saved;
   asm volatile(
       "s_mov_b32 %0, m0\n\t"
       "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
       "buffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved)
@@ -109,6 +112,7 @@ __device__ __forceinline__ void load_dword_to_lds(__amdgpu_buffer_rsrc_t rs, uin
   asm volatile(
       "s_mov_b32 %0, m0\n\t"
       "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
       "buffer_load_dword %2, %3, 0 offen lds\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved)

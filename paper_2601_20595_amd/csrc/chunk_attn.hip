@@ -163,7 +163,8 @@ __device__ __forceinline__ int v_swz(int q) { return 2 * q + (q >> 1); }
 // covers; the resource spans exactly the block's 64 rows of head g. Issued as inline asm
 // (M0 saved and restored) so that the compiler does not wait for it before every LDS
 // read: completion is waited for explicitly (wait_vm_all) before the barrier that
-// publishes the tile.
+// publishes the tile. The offset is added between M0's write and the load, which must not
+// follow each other directly.
 __device__ __forceinline__ void dma_tile(const uint16_t* src, int hkv, int g, int kv0, uint32_t lds_tile, int wave,
                                          int voff0, int step_bytes) {
   const int64_t row = static_cast<int64_t>(hkv) * D;  // elements between consecutive keys
@@ -175,9 +176,9 @@ __device__ __forceinline__ void dma_tile(const uint16_t* src, int hkv, int g, in
     uint32_t saved;
     int voff;
     asm volatile(
-        "v_add_u32 %1, %3, %4\n\t"
         "s_mov_b32 %0, m0\n\t"
         "s_mov_b32 m0, %2\n\t"
+        "v_add_u32 %1, %3, %4\n\t"
         "buffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved), "=&v"(voff)

@@ -230,14 +230,16 @@ struct TileGeom {
 // asm so the compiler neither inserts a wait for it in front of every LDS read (it
 // cannot tell that the reads target the other stage) nor hoists one offset register
 // per load out of the tile loop; the whole offset sits in the VGPR operand, which the
-// buffer range check covers. M0 is saved and restored around the load.
+// buffer range check covers. M0 is saved and restored around the load; the offset is added
+// between M0's write and the load, which must not follow each other directly (the compiler
+// does not look for such pairs inside of asm).
 __device__ __forceinline__ void dma16(const __amdgpu_buffer_rsrc_t& rs, uint32_t lds_off, int vbase, int sadd) {
   uint32_t saved;
   int voff;
   asm volatile(
-      "v_add_u32 %1, %3, %4\n\t"
       "s_mov_b32 %0, m0\n\t"
       "s_mov_b32 m0, %2\n\t"
+      "v_add_u32 %1, %3, %4\n\t"
       "buffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
       "s_mov_b32 m0, %0"
       : "=&s"(saved), "=&v"(voff)
@@ -293,6 +295,7 @@ __device__ __forceinline__ void warm_lines(const __amdgpu_buffer_rsrc_t& rs, int
     asm volatile(
         "s_mov_b32 %0, m0\n\t"
         "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
         "buffer_load_dword %2, %3, 0 offen lds\n\t"
         "s_mov_b32 m0, %0"
         : "=&s"(saved)
