@@ -568,6 +568,7 @@ typedef struct {
  * of sequence b lies in page page_table[b * max_pages + x / page_size], row x % page_size.
  * lens[b] is the sequence's length, its new tokens included: rows q_ptr[b] .. q_ptr[b+1] - 1
  * of q, k and v (int32[batch + 1], ascending; a sequence may have none), which are its last.
+ * q_ptr[0] need not be 0: a call may take a part of a larger batch's pointers and its whole q, k, v.
  * status: int32 on the device or NULL; a call sets bit 0 if it met a page number outside 0 ..
  * n_pages - 1 where a token lies, bit 1 for a length beyond max_pages pages or a new token
  * before position 0; it never clears them. Such tokens are not written, their keys count as

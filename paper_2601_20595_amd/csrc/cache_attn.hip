@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kThreads) void cache_append(AppendArgs a) {
   constexpr int kCols = D / 16, kHeads = kThreads / kCols;
   const CacheArgs& c = a.c;
   const int t = blockIdx.x;
-  if (t >= first_token(c, c.batch)) return;
+  if (t < first_token(c, 0) || t >= first_token(c, c.batch)) return;  // (a row of no sequence)
   const int b = last_below(c.batch, [&](int i) { return c.q_ptr[i] <= t; });
   const int pos = c.lens[b] - (c.q_ptr[b + 1] - t);
   const int slot = pos >> c.page_shift;
@@ -670,7 +670,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge(CacheAttnArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int token = static_cast<int>(row / c.H), h = static_cast<int>(row - static_cast<int64_t>(token) * c.H);
-  if (token >= first_token(c, c.batch)) return;
+  if (token < first_token(c, 0) || token >= first_token(c, c.batch)) return;  // (a row of no sequence)
   const int G = c.H / c.Hkv, kvh = h / G;
   const int b = last_below(c.batch, [&](int i) { return c.q_ptr[i] <= token; });
   const Plan plan = *plan_in(a.ws);
