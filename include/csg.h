@@ -572,7 +572,9 @@ typedef struct {
  * status: int32 on the device or NULL; a call sets bit 0 if it met a page number outside 0 ..
  * n_pages - 1 where a token lies, bit 1 for a length beyond max_pages pages or a new token
  * before position 0; it never clears them. Such tokens are not written, their keys count as
- * zeros, and the outputs of the sequence mean nothing; no memory outside is touched. */
+ * zeros, and the outputs of the sequence mean nothing; no memory outside is touched. Nor is it by
+ * bounds (q_ptr, group_ptr) that do not ascend or leave 0 .. tokens (batch): no output of such a call
+ * means anything, and bit 1 is set where they name more rows than there are. */
 
 /* Puts the new tokens' keys and values into the cache, the keys (and queries) rotated by
  * their position: pair (x, y) number i of a head becomes (x cos a - y sin a, y cos a + x sin a),

@@ -173,8 +173,10 @@ csg_status check_cache_attn(csg_cache_cfg* c) {
   if (static_cast<int64_t>(c->batch) + c->n_groups > csg::kMaxCacheEntries)
     return fail(CSG_ERR_UNSUPPORTED, "at most %d sequences and groups", csg::kMaxCacheEntries);
   if (c->tokens * c->n_heads > kMaxGrid) return fail(CSG_ERR_UNSUPPORTED, "too many tokens and heads for one launch");
-  // blocks of keys times tasks that read them, at most; they are counted in 32 bits
-  const int64_t tasks = 2 * (c->tokens * (c->n_heads / c->n_kv_heads) / csg::kCacheWideRows) + c->batch + c->n_groups;
+  // blocks of keys times tasks that read them, at most; they are counted in 32 bits. (A task has at
+  // least a tile, one of four tiles and more as many as four go into it, rounded up.)
+  const int64_t tiles = csg::cache_max_tiles(c->n_heads, c->n_kv_heads, c->tokens, c->batch, c->n_groups);
+  const int64_t tasks = tiles / 4 + c->batch + c->n_groups;
   const int64_t blocks = static_cast<int64_t>(c->max_pages) * c->page_size / csg::kCacheBlock + 1;
   if (tasks > 0 && blocks + csg::kCacheTaskCost > 0x7fffffff / tasks)
     return fail(CSG_ERR_UNSUPPORTED, "max_pages pages for every sequence are too many keys for one launch");
@@ -357,6 +359,7 @@ csg_status csg_cache_attn(const csg_cache_cfg* cfg, const void* q, const void* k
   a.head_workers = csg::cache_head_workers(cus, c.n_kv_heads);
   a.dies = 8 / std::gcd(8, c.n_kv_heads);
   a.max_parts = csg::cache_max_parts(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups, a.head_workers);
+  a.max_tiles = csg::cache_max_tiles(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups);
   a.ws = static_cast<unsigned char*>(workspace);
   a.scoring = scoring(c.scale, c.softcap, slopes);
   CSG_HIP(csg::launch_cache_attn(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));

@@ -523,7 +523,8 @@ template <class T, int D, bool kPlain>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * 2 * kCacheBlock * 2 * D];
   __shared__ float s_ref[4][32], s_sum[4][32];
-  __shared__ int s_wave_units[4], s_wave_tiles[4], s_entry, s_first, s_tiles;
+  __shared__ uint32_t s_wave_units[4], s_wave_tiles[4];
+  __shared__ int s_entry, s_first, s_tiles;
   __shared__ Entry s_entries[kThreads];
   static_assert(sizeof(stage) == 2 * 2 * kCacheWideBlock * 2 * D, "the same memory holds the wide parts' buffers");
   static_assert(sizeof(stage) >= 4 * 32 * D * 4, "and the waves' results");
@@ -551,7 +552,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
   // Each thread counts some entries; units and tiles before each of them by a scan. Where a thread
   // has one entry, everyone finds it in LDS.
   const int per = (n_entries + kThreads - 1) / kThreads;
-  int units = 0, tiles = 0;
+  uint32_t units = 0, tiles = 0;
   for (int i = 0; i < per; ++i) {
     const int e = tid * per + i;
     if (e >= n_entries) break;
@@ -560,10 +561,10 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
     units += x.tasks() * x.span();
     tiles += x.tiles();
   }
-  const int own_units = units, own_tiles = tiles;
+  const uint32_t own_units = units, own_tiles = tiles;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int uu = __shfl_up(units, d), ut = __shfl_up(tiles, d);
+    const uint32_t uu = __shfl_up(units, d), ut = __shfl_up(tiles, d);
     if (lane >= d) {
       units += uu;
       tiles += ut;
@@ -580,12 +581,15 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
     units += s_wave_units[i];
     tiles += s_wave_tiles[i];
   }
-  const int all = __builtin_amdgcn_readfirstlane(s_wave_units[0] + s_wave_units[1] + s_wave_units[2] + s_wave_units[3]);
   const int all_tiles = __builtin_amdgcn_readfirstlane(s_wave_tiles[0] + s_wave_tiles[1] + s_wave_tiles[2] + s_wave_tiles[3]);
+  // Bounds that do not ascend may name rows several times, and with them more units than 32 bits count: then
+  // there is nothing to do. (As many tiles as the host has reckoned with have no more units than it has.)
+  const bool fits = static_cast<uint32_t>(all_tiles) <= a.max_tiles;
+  const int all = fits ? __builtin_amdgcn_readfirstlane(s_wave_units[0] + s_wave_units[1] + s_wave_units[2] + s_wave_units[3]) : 0;
   const int run = max(kCacheMinRun, (all + a.head_workers - 1) / a.head_workers);
   const int begin = w * run;
   // for cache_merge, and the entry where the run begins
-  if (blockIdx.x == 0 || (units <= begin && begin < units + own_units)) {
+  if (blockIdx.x == 0 || (static_cast<int>(units) <= begin && begin < static_cast<int>(units + own_units))) {
     int before = units, tiles_before = tiles;
     for (int i = 0; i < per; ++i) {
       const int e = tid * per + i;
@@ -598,13 +602,16 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
         s_tiles = tiles_before;
       }
       if (blockIdx.x == 0) {
-        entries_in(a.ws)[e] = {before, tiles_before, x.blocks, x.rows, x.token0, x.group, {0, 0}};
+        entries_in(a.ws)[e] = {before, tiles_before, fits ? x.blocks : 0, x.rows, x.token0, x.group, {0, 0}};
         if (x.own && (x.end != c.lens[x.b0] || x.rows / (c.H / c.Hkv) > x.end)) tell(c, kCacheBadLength);
       }
       before += n;
       tiles_before += x.tiles();
     }
-    if (blockIdx.x == 0 && tid == 0) *plan_in(a.ws) = {run, all_tiles, {0, 0, 0, 0, 0, 0}};
+    if (blockIdx.x == 0 && tid == 0) {
+      *plan_in(a.ws) = {run, all_tiles, {0, 0, 0, 0, 0, 0}};
+      if (!fits) tell(c, kCacheBadLength);
+    }
   }
   if (begin >= all) return;
   __syncthreads();

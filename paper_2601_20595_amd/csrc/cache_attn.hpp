@@ -58,6 +58,7 @@ struct CacheAttnArgs {
   int32_t head_workers;  // workgroups that share the blocks of keys of a key/value head
   int32_t dies;          // dies that its workgroups are on
   int64_t max_parts;     // places of partial results in the workspace
+  int64_t max_tiles;     // tiles of a key/value head, if the bounds ascend
   unsigned char* ws;
   Scoring scoring;
 };
@@ -68,10 +69,13 @@ constexpr int64_t cache_part_bytes(int head_dim) { return kCacheTileRows * (head
 // Workgroups for each key/value head, all of them as many as are on the device at once (two a
 // CU, by their registers and, for 128 elements a head, 64 KiB of LDS).
 constexpr int32_t cache_head_workers(int32_t cus, int32_t Hkv) { return 2 * cus > Hkv ? 2 * cus / Hkv : 1; }
+// Tiles of a key/value head, at most: every token in its sequence and, maybe, its group.
+inline int64_t cache_max_tiles(int32_t H, int32_t Hkv, int64_t tokens, int32_t batch, int32_t n_groups) {
+  return tokens * (H / Hkv) / kCacheTileRows * (n_groups > 0 ? 2 : 1) + batch + n_groups;
+}
 // Places of parts: the tiles and four for each workgroup.
 inline int64_t cache_max_parts(int32_t H, int32_t Hkv, int64_t tokens, int32_t batch, int32_t n_groups, int32_t head_workers) {
-  const int64_t tiles = tokens * (H / Hkv) / kCacheTileRows * (n_groups > 0 ? 2 : 1) + batch + n_groups;
-  return (tiles + int64_t{4} * head_workers) * Hkv;
+  return (cache_max_tiles(H, Hkv, tokens, batch, n_groups) + int64_t{4} * head_workers) * Hkv;
 }
 
 hipError_t launch_cache_append(const AppendArgs& a, bool f16, int head_dim, hipStream_t stream);
