@@ -24,6 +24,11 @@ constexpr int64_t kMaxRows = int64_t{1} << 30;
 constexpr int64_t kMaxStride = int64_t{1} << 23;  // 63 rows of it stay within 32-bit byte offsets
 constexpr int64_t kMaxGrid = 0xffffffff / 512;  // workgroups: a launch's threads are counted in 32 bits
 constexpr int32_t kDefaultCus = 256;
+// Rows of a cache's attention: four are a workgroup of the merge, and the tiles of as many as 2048 entries
+// with all of the rows each are still counted in 32 bits.
+constexpr int64_t kMaxCacheRows = int64_t{1} << 25;
+static_assert(kMaxCacheRows / 4 <= kMaxGrid * 2, "workgroups of 256 threads");
+static_assert(kMaxCacheRows / csg::kCacheTileRows * csg::kMaxCacheEntries < (int64_t{1} << 32), "tiles");
 
 // Compute units of `device`, checked once to be the one this library is built for.
 csg_status device_cus(int device, int32_t* cus) {
@@ -172,7 +177,7 @@ csg_status check_cache_attn(csg_cache_cfg* c) {
   if (c->n_groups > c->batch) return fail(CSG_ERR_INVALID, "more groups than sequences");
   if (static_cast<int64_t>(c->batch) + c->n_groups > csg::kMaxCacheEntries)
     return fail(CSG_ERR_UNSUPPORTED, "at most %d sequences and groups", csg::kMaxCacheEntries);
-  if (c->tokens * c->n_heads > kMaxGrid) return fail(CSG_ERR_UNSUPPORTED, "too many tokens and heads for one launch");
+  if (c->tokens * c->n_heads > kMaxCacheRows) return fail(CSG_ERR_UNSUPPORTED, "too many tokens and heads for one launch");
   // blocks of keys times tasks that read them, at most; they are counted in 32 bits. (A task has at
   // least a tile, one of four tiles and more as many as four go into it, rounded up.)
   const int64_t tiles = csg::cache_max_tiles(c->n_heads, c->n_kv_heads, c->tokens, c->batch, c->n_groups);
