@@ -533,8 +533,8 @@ csg_status csg_doc_attn(const csg_doc_attn_cfg* cfg, const void* q, const void* 
                         const int32_t* q_ptr, const int32_t* k_ptr, const int32_t* prefix,
                         const float* slopes, void* o, void* lse, int device, void* stream);
 
-/* Bytes of workspace that csg_doc_attn_grad needs for cfg's rows on device, whatever the
- * documents are (device < 0: on a device of 256 CUs). */
+/* Bytes of workspace that csg_doc_attn_grad needs for up to cfg's rows and keys on device, whatever
+ * the documents are (device < 0: on a device of 256 CUs). */
 csg_status csg_doc_attn_grad_workspace(const csg_doc_attn_cfg* cfg, int device, size_t* bytes);
 
 /* The gradient: from d_o (layout of o) and the forward call's o and lse to dq, dk, dv (rows

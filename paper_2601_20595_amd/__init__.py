@@ -691,7 +691,7 @@ class DocAttn:
         self._shape = n_heads, n_kv_heads, head_dim
 
     def workspace_bytes(self, q_rows: int, k_rows: int) -> int:
-        """Bytes of the workspace that backward needs."""
+        """Bytes of the workspace that backward needs for up to that many rows and keys."""
         c = csg_doc_attn_cfg.from_buffer_copy(self._cfg)
         c.q_rows, c.k_rows = q_rows, k_rows
         c.q_stride = c.k_stride = c.v_stride = c.dq_stride = c.dk_stride = c.dv_stride = 0

@@ -145,17 +145,19 @@ csg::DocAttnArgs doc_args(const csg_doc_attn_cfg& c, int32_t cus, const void* q,
   return a;
 }
 
-// Bytes of the rows' statistics, and of everything: the sums of the parts behind them. The number of
-// documents is not known where a workspace is made for all calls up to some rows: fewer documents
-// make more parts.
+// Bytes of the rows' statistics, and of everything: the sums of the parts behind them.
 int64_t stats_bytes(const csg_doc_attn_cfg& c) { return (2 * c.q_rows * c.n_heads * 4 + 15) / 16 * 16; }
-int64_t part_bytes(const csg_doc_attn_cfg& c) { return c.k_rows * c.n_kv_heads * 2 * c.head_dim * 4; }
-int32_t row_parts(const csg_doc_attn_cfg& c, int64_t n_docs, int32_t cus) {
-  return csg::doc_row_parts(c.q_rows, c.k_rows, n_docs, c.n_heads, c.n_kv_heads, c.head_dim, cus);
+int64_t part_bytes(const csg_doc_attn_cfg& c, int64_t rows) { return rows * c.n_kv_heads * 2 * c.head_dim * 4; }
+int32_t row_parts(const csg_doc_attn_cfg& c, int32_t cus) {
+  return csg::doc_row_parts(c.q_rows, c.k_rows, c.n_docs, c.n_heads, c.n_kv_heads, c.head_dim, cus);
 }
-int64_t grad_workspace(const csg_doc_attn_cfg& c, int64_t n_docs, int32_t cus) {
-  const int32_t parts = row_parts(c, n_docs, cus);
-  return stats_bytes(c) + (parts > 1 ? parts * part_bytes(c) : 0);
+int64_t grad_workspace(const csg_doc_attn_cfg& c, int32_t cus) {
+  const int32_t parts = row_parts(c, cus);
+  return stats_bytes(c) + (parts > 1 ? part_bytes(c, parts * c.k_rows) : 0);
+}
+// What any call of up to cfg's rows and keys needs, whatever its documents are.
+int64_t max_grad_workspace(const csg_doc_attn_cfg& c, int32_t cus) {
+  return stats_bytes(c) + part_bytes(c, csg::doc_max_part_rows(c.q_rows, c.k_rows, c.n_heads, c.n_kv_heads, c.head_dim, cus));
 }
 
 csg_status check_cache(csg_cache_cfg* c) {
@@ -249,7 +251,7 @@ csg_status csg_doc_attn_grad_workspace(const csg_doc_attn_cfg* cfg, int device, 
   CSG_CHECK(check_docs(&c, true));
   int32_t cus = kDefaultCus;
   if (device >= 0) CSG_CHECK(device_cus(device, &cus));
-  *bytes = static_cast<size_t>(grad_workspace(c, 1, cus));
+  *bytes = static_cast<size_t>(max_grad_workspace(c, cus));
   return CSG_OK;
 }
 
@@ -268,9 +270,9 @@ csg_status csg_doc_attn_grad(const csg_doc_attn_cfg* cfg, const void* q, const v
     return fail(CSG_ERR_INVALID, "buffers must be 16-byte aligned");
   int32_t cus = 0;
   CSG_CHECK(device_cus(device, &cus));
-  if (static_cast<int64_t>(workspace_bytes) < grad_workspace(c, c.n_docs, cus))
+  if (static_cast<int64_t>(workspace_bytes) < grad_workspace(c, cus))
     return fail(CSG_ERR_INVALID, "the workspace holds %zu bytes; the call needs %lld", workspace_bytes,
-                static_cast<long long>(grad_workspace(c, c.n_docs, cus)));
+                static_cast<long long>(grad_workspace(c, cus)));
   DeviceGuard g(device);
   if (g.err != hipSuccess) return hip_fail(g.err, "hipSetDevice");
   csg::DocAttnArgs a = doc_args(c, cus, q, k, v, q_ptr, k_ptr, prefix, slopes);
@@ -281,7 +283,7 @@ csg_status csg_doc_attn_grad(const csg_doc_attn_cfg* cfg, const void* q, const v
   a.dK = static_cast<uint16_t*>(dk);
   a.dV = static_cast<uint16_t*>(dv);
   a.stats = static_cast<float*>(workspace);
-  a.row_parts = row_parts(c, c.n_docs, cus);
+  a.row_parts = row_parts(c, cus);
   a.parts = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + stats_bytes(c));
   CSG_HIP(csg::launch_doc_grad(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));
   return CSG_OK;

@@ -48,15 +48,34 @@ inline int64_t doc_key_tiles(int64_t k_rows, int64_t n_docs) { return k_rows / k
 // rows 106 -> 47 us (7 parts), 1024 rows 194 -> 82 (7), 3000 rows 457 -> 331 (2), 4096 rows 685 -> 540 (2), with
 // half as many again 2048 rows 180 -> 198; 32 on 8 of 64, 8192 rows 1237 -> 1070 (2); but 16 documents of 250
 // rows, 256 tiles of 16 steps of 128 elements, 110 -> 129 us with two parts.
+constexpr int32_t kDocMaxParts = 16;
+inline int64_t doc_steps(int64_t q_rows, int64_t n_docs, int32_t H, int32_t Hkv) {
+  return (q_rows / (n_docs < 1 ? 1 : n_docs) + kDocBlock - 1) / kDocBlock * (H / Hkv);
+}
+// The most tiles of keys that are cut into that many parts (0: not even one is).
+inline int64_t doc_part_tiles(int32_t parts, int64_t steps, int32_t head_dim, int32_t cus) {
+  if (steps >= 16 * parts) return (head_dim == 64 ? 4 : 2) * static_cast<int64_t>(cus) / parts;
+  return steps >= 4 * parts ? cus / parts : 0;
+}
 inline int32_t doc_row_parts(int64_t q_rows, int64_t k_rows, int64_t n_docs, int32_t H, int32_t Hkv, int32_t head_dim, int32_t cus) {
   const int64_t tiles = ((k_rows + kDocTileRows - 1) / kDocTileRows + n_docs / 2) * Hkv;
-  const int64_t steps = (q_rows / (n_docs < 1 ? 1 : n_docs) + kDocBlock - 1) / kDocBlock * (H / Hkv);
+  const int64_t steps = doc_steps(q_rows, n_docs, H, Hkv);
   int32_t parts = 1;
   if (k_rows == 0) return parts;
-  while (parts < 16 && ((tiles * (parts + 1) <= cus && steps >= 4 * (parts + 1)) ||
-                        (tiles * (parts + 1) <= (head_dim == 64 ? 4 : 2) * static_cast<int64_t>(cus) && steps >= 16 * (parts + 1))))
-    ++parts;
+  while (parts < kDocMaxParts && tiles <= doc_part_tiles(parts + 1, steps, head_dim, cus)) ++parts;
   return parts;
+}
+// Parts times their keys, 0 if there is one, at most, of any call of up to so many rows and keys. Fewer
+// keys may be cut into more parts: for each number of parts, the most keys that have it.
+inline int64_t doc_max_part_rows(int64_t q_rows, int64_t k_rows, int32_t H, int32_t Hkv, int32_t head_dim, int32_t cus) {
+  const int64_t steps = doc_steps(q_rows, 1, H, Hkv);  // (fewer rows, or more documents: fewer steps)
+  int64_t most = 0;
+  for (int32_t parts = 2; parts <= kDocMaxParts; ++parts) {
+    const int64_t keys = doc_part_tiles(parts, steps, head_dim, cus) / Hkv * kDocTileRows;
+    const int64_t rows = parts * (keys < k_rows ? keys : k_rows);
+    if (rows > most) most = rows;
+  }
+  return most;
 }
 
 // `f16`: elements are IEEE half precision, otherwise bfloat16. head_dim: 64 or 128.
