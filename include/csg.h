@@ -542,7 +542,7 @@ csg_status csg_doc_attn_grad_workspace(const csg_doc_attn_cfg* cfg, int device, 
  * others left as they are. dk and dv are summed over the heads that share a key/value
  * head. The slopes are constants. Every row and key of a document must be finite here, masked
  * ones too: they are multiplied with gradients of 0. workspace: csg_doc_attn_grad_workspace bytes, any
- * content. dq, dk and dv may not overlap the inputs. */
+ * content (NULL if that is 0, as it is without rows). dq, dk and dv may not overlap the inputs. */
 csg_status csg_doc_attn_grad(const csg_doc_attn_cfg* cfg, const void* q, const void* k, const void* v,
                              const int32_t* q_ptr, const int32_t* k_ptr, const int32_t* prefix,
                              const float* slopes, const void* o, const void* lse, const void* d_o,

@@ -722,7 +722,7 @@ class DocAttn:
         dka, _, c.dk_stride = _heads(dk, m, hkv, d, "dk", dev)
         dva, _, c.dv_stride = _heads(dv, m, hkv, d, "dv", dev)
         _check(_lib().csg_doc_attn_grad(c, *args, _arg(d_o, 2 * n * h * d, 2, "d_o", dev), dqa, dka, dva,
-                                        _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes, dev, _stream(stream)),
+                                        _arg(workspace, min(n, 1), 0, "workspace", dev), workspace.nbytes, dev, _stream(stream)),
                "csg_doc_attn_grad")
 
 

@@ -263,7 +263,8 @@ csg_status csg_doc_attn_grad(const csg_doc_attn_cfg* cfg, const void* q, const v
   csg_doc_attn_cfg c = *cfg;
   CSG_CHECK(check_docs(&c, true));
   if (c.n_docs == 0 || (c.q_rows == 0 && c.k_rows == 0)) return CSG_OK;
-  if (!q_ptr || !k_ptr || !workspace || (c.q_rows > 0 && (!q || !o || !lse || !d_o || !dq)) ||
+  // (without rows there are no statistics and no parts: the workspace is empty)
+  if (!q_ptr || !k_ptr || (c.q_rows > 0 && (!q || !o || !lse || !d_o || !dq || !workspace)) ||
       (c.k_rows > 0 && (!k || !v || !dk || !dv)))
     return fail(CSG_ERR_INVALID, "NULL buffer");
   if (!all_aligned({q, k, v, o, lse, d_o, dq, dk, dv, workspace}))

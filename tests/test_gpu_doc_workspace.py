@@ -26,3 +26,15 @@ def test_a_workspace_of_more_rows_serves_fewer():
         torch.cuda.synchronize()
         for one, two in zip(*d):
             assert torch.equal(one, two), n
+
+
+def test_no_rows_need_no_workspace():
+    H, Hkv, D, m = 8, 2, 128, 100
+    a = csg.DocAttn(H, Hkv, D, "bf16")
+    q, k, v = (normal(i, s, "bf16")[0].to(DEV) for i, s in enumerate(((0, H, D), (m, Hkv, D), (m, Hkv, D))))
+    o, lse = torch.empty_like(q), torch.empty((H, 0), device=DEV)
+    dq, dk, dv = (torch.full_like(t, 17.0) for t in (q, k, v))
+    ws = torch.empty(a.workspace_bytes(0, m), dtype=torch.uint8, device=DEV)
+    a.backward(q, k, v, ints([0, 0]), ints([0, m]), o, lse, torch.empty_like(q), dq, dk, dv, ws)
+    torch.cuda.synchronize()
+    assert bool((dk == 0).all()) and bool((dv == 0).all())
