@@ -487,8 +487,9 @@ csg_status csg_ring_attn(csg_plan* p, const void* q, void* k_landing, void* v_la
  * with p_i the key that row i stands at: rows are the last ones of their document or
  * sequence (p_i = i + keys - rows). The output is sum_j exp(s_ij - lse_i) v_j over the keys
  * that row i sees, lse_i = log sum_j exp(s_ij), natural logarithm; a row that sees none has
- * output 0 and lse -inf. Partial results over disjoint keys (ring attention's among them)
- * join by their lse.
+ * output 0 and lse -inf. Partial results over disjoint keys (ring attention's among them, whose
+ * lse carries its weights' rounding, 2^-8 at most) join by their lse: lse = log sum_s exp(lse_s),
+ * o = sum_s exp(lse_s - lse) o_s.
  *
  * These calls own nothing: no plan, no allocation, no host wait, and no copy. They queue
  * their kernels on `stream` (a hipStream_t of `device`; the device current before is
@@ -515,6 +516,8 @@ typedef struct {
     int64_t q_rows, k_rows;       /* rows of q (o, gradients of either) and of k and v */
     int64_t q_stride, k_stride, v_stride;
     int64_t dq_stride, dk_stride, dv_stride;
+    int32_t joined;               /* csg_doc_attn_grad: o and lse are of more keys than the call's */
+    int32_t reserved;
 } csg_doc_attn_cfg;
 
 /* Attention over packed documents: document t's rows are q_ptr[t] .. q_ptr[t+1] - 1, its
@@ -539,7 +542,11 @@ csg_status csg_doc_attn_grad_workspace(const csg_doc_attn_cfg* cfg, int device, 
 
 /* The gradient: from d_o (layout of o) and the forward call's o and lse to dq, dk, dv (rows
  * as q, k, v, strides dq_stride ...), overwritten for every row and key of a document,
- * others left as they are. dk and dv are summed over the heads that share a key/value
+ * others left as they are. With cfg->joined = 0, o and lse have to be those of the same call's
+ * csg_doc_attn: the sum D_i of a row's weights times d_o_i . v_j is then taken over the keys,
+ * exactly. With 1 they are of a larger set of keys that holds the call's, joined from partial results:
+ * D_i is d_o_i . o_i, with o's rounding; dk and dv are these keys' gradients, dq is their share
+ * of the queries' (the shares of all keys add up). dk and dv are summed over the heads that share a key/value
  * head. The slopes are constants. Every row and key of a document must be finite here, masked
  * ones too: they are multiplied with gradients of 0. workspace: csg_doc_attn_grad_workspace bytes, any
  * content (NULL if that is 0, as it is without rows). dq, dk and dv may not overlap the inputs. */

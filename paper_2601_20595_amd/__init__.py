@@ -99,7 +99,7 @@ class csg_doc_attn_cfg(ctypes.Structure):
                 ("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("q_rows", ctypes.c_int64),
                 ("k_rows", ctypes.c_int64), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
                 ("v_stride", ctypes.c_int64), ("dq_stride", ctypes.c_int64), ("dk_stride", ctypes.c_int64),
-                ("dv_stride", ctypes.c_int64)]
+                ("dv_stride", ctypes.c_int64), ("joined", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class csg_cache_cfg(ctypes.Structure):
@@ -714,13 +714,17 @@ class DocAttn:
         _, _, args = self._inputs(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
         _check(_lib().csg_doc_attn(self._cfg, *args, self.device, _stream(stream)), "csg_doc_attn")
 
-    def backward(self, q, k, v, q_ptr, k_ptr, o, lse, d_o, dq, dk, dv, workspace, prefix=None, slopes=None, stream=None):
+    def backward(self, q, k, v, q_ptr, k_ptr, o, lse, d_o, dq, dk, dv, workspace, prefix=None, slopes=None, stream=None,
+                 joined=False):
+        """joined: o and lse are of more keys than these, joined from partial results; dq is these
+        keys' share."""
         n, m, args = self._inputs(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
         c, dev = self._cfg, self.device
         h, hkv, d = self._shape
         dqa, _, c.dq_stride = _heads(dq, n, h, d, "dq", dev)
         dka, _, c.dk_stride = _heads(dk, m, hkv, d, "dk", dev)
         dva, _, c.dv_stride = _heads(dv, m, hkv, d, "dv", dev)
+        c.joined = joined
         _check(_lib().csg_doc_attn_grad(c, *args, _arg(d_o, 2 * n * h * d, 2, "d_o", dev), dqa, dka, dva,
                                         _arg(workspace, min(n, 1), 0, "workspace", dev), workspace.nbytes, dev, _stream(stream)),
                "csg_doc_attn_grad")

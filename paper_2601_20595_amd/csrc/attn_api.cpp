@@ -97,6 +97,7 @@ csg_status check_docs(csg_doc_attn_cfg* c, bool gradient) {
   CSG_CHECK(check_heads(c->n_heads, c->n_kv_heads, c->head_dim, c->dtype));
   CSG_CHECK(check_scores(&c->scale, c->softcap, c->head_dim));
   if (c->causal != 0 && c->causal != 1) return fail(CSG_ERR_INVALID, "causal must be 0 or 1");
+  if (c->joined != 0 && c->joined != 1) return fail(CSG_ERR_INVALID, "joined must be 0 or 1");
   if (c->n_docs < 0 || c->q_rows < 0 || c->k_rows < 0 || c->q_rows > kMaxRows || c->k_rows > kMaxRows ||
       c->n_docs > kMaxRows)
     return fail(CSG_ERR_INVALID, "rows or documents out of range");
@@ -138,6 +139,7 @@ csg::DocAttnArgs doc_args(const csg_doc_attn_cfg& c, int32_t cus, const void* q,
   a.Hkv = c.n_kv_heads;
   a.tile_heads = std::gcd(c.n_heads / c.n_kv_heads, 4);
   a.causal = c.causal;
+  a.joined = c.joined;
   a.cus = cus;
   a.row_parts = 1;
   a.scale = c.scale;

@@ -294,6 +294,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_forward(DocAttnArgs a) {
 // and of sharp scores in bf16 by 4.6e-3. One pass over the keys sums against D' = do_i . o_i:
 //   e_i = sum_j P_ij (do_i . v_j - D'_i) = D_i - D'_i,
 //   dQ_i / scale = sum_j P_ij (do_i . v_j - D'_i) (1 - tanh^2) k_j - e_i sum_j P_ij (1 - tanh^2) k_j.
+// (Against the output of more keys than the call's, whose weights do not sum to 1 here, e_i would be
+// those keys' part of the sum: then it is 0, and D is D'.)
 // For D = 128 the second sum takes the registers of the rows of do, which are read from LDS. 8192 causal
 // rows, 32 heads on 8 of 128: 0.88 to 0.92 ms, four products of the pairs at 1.2 PFLOP/s, which is what a
 // large matrix product of the library reaches on the card: bound by the matrix instructions and the
@@ -437,6 +439,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
 #pragma unroll
     for (int n = 0; n < kTeams; ++n) more += s_more[n][wave][lane];
   }
+  if (a.joined) more = 0.0f;
   if (ok && hlf == 0 && team == 0) {
     const int64_t pitch = a.q_rows;
     float* st = a.stats + h * pitch + p.q0 + row;

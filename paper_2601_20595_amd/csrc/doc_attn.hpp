@@ -32,6 +32,7 @@ struct DocAttnArgs {
   int32_t H, Hkv;
   int32_t tile_heads;  // heads of a group that share a tile of rows: 1, 2 or 4, a divisor of H / Hkv
   int32_t causal;
+  int32_t joined;      // gradient: o and lse are of more keys
   int32_t cus;         // of the device
   int32_t row_parts;   // parts into which the keys' gradient cuts its rows
   float scale;

@@ -33,3 +33,10 @@ def test_a_gradients_workspace_serves_fewer_rows_too(heads, kv, d):
         assert row == sorted(row)
     for column in zip(*table):
         assert list(column) == sorted(column)
+
+
+def test_joined_is_a_truth_value():
+    c = csg.csg_doc_attn_cfg(n_heads=8, n_kv_heads=2, head_dim=128, dtype=csg.CSG_BF16, n_docs=1, q_rows=1, k_rows=1, joined=2)
+    with pytest.raises(csg.CsgError) as e:
+        csg.csg_doc_attn_grad(c, *([1 << 20] * 5), 0, 0, *([1 << 20] * 7), 1 << 30)
+    assert e.value.status == csg.CSG_ERR_INVALID and "joined" in str(e.value)
