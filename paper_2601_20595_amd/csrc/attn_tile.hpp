@@ -53,6 +53,7 @@ struct Bf16 {
   // reference; a larger one moves the reference to the row's maximum. Weights stay exact
   // to their type's 8 bits at any size.
   static constexpr float kRowSumLimit = 65536.0f;
+  static constexpr bool kShortRange = false;
   static __device__ __forceinline__ f32x16_t mfma(x8 a, x8 b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   }
@@ -63,6 +64,7 @@ struct F16 {
   using x4 = f16x4_t;
   // (the type ends at 65504, and what is below 2^-14 loses bits: weights stay near 1)
   static constexpr float kRowSumLimit = 1024.0f;
+  static constexpr bool kShortRange = true;
   static __device__ __forceinline__ f32x16_t mfma(x8 a, x8 b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }

@@ -286,6 +286,50 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_forward(DocAttnArgs a) {
     a.LSE[static_cast<int64_t>(h) * a.q_rows + p.q0 + row] = fmaf(log2f(total), kLn2, sm.m * a.scoring.unit);
 }
 
+// ---- numbers of the gradients in f16 ----------------------------------------------------------
+// Over thousands of keys weights of a row are below f16's smallest normal number, 2^-14, and so are the
+// gradients of scores dS that a small gradient of the output gives; there the type loses bits (3000 keys,
+// do of 1e-3: dq off by 3.7e-3 of its norm; as below 6e-4, of which its own rounding is most). So weights
+// are made 2^14 times as large by the exponent's argument, and dS takes a power of two of each lane's own
+// row (key): the lane's largest so far lies below 2^15 with it, and was above 2^10 when it was set, so that
+// nothing overflows and what is lost is below 2^-35 of the largest. Sums in fp32 are brought back exactly.
+// The look at the largest costs the two kernels 3.7 and 1.6 us of 32 and 30 for packed documents of up to
+// 721 rows, heads of 64: its branch stands between a block's scores and its products. Without a branch 4.7
+// and 2.7; one for 64 keys spills; with a factor only where it is needed, or the products or fragments of
+// the next 32 keys ahead of it, within 1 us of the same.
+constexpr float kLog2Shift = 14.0f, kUnshift = 1.0f / 16384.0f;
+template <class T>
+constexpr float kWeightShift = T::kShortRange ? kLog2Shift : 0.0f;
+template <class T>
+constexpr float kWeightUnit = T::kShortRange ? kUnshift : 1.0f;
+
+template <class T>
+struct Reach {
+  uint32_t bits = 227u << 23;  // of the factor, 2^100 until there is anything
+  // What the lane's sums are to be multiplied with (1 if its factor stays) in order to take more of x, which
+  // is multiplied with the factor.
+  template <int N>
+  __device__ __forceinline__ void take(f32x16_t& x, f32x16_t (&sums)[N]) {
+    if constexpr (T::kShortRange) {
+      float m = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) m = fmaxf(m, fabsf(x[r]));
+      m = max_halves(m);
+      const bool move = m * __uint_as_float(bits) > 32768.0f;
+      if (__builtin_amdgcn_ballot_w64(move) != 0) {
+        const uint32_t to = min(264u - (__float_as_uint(m) >> 23), 227u) << 23;  // m becomes 2^10 .. 2^11
+        const float f = move ? __uint_as_float(to) * back() : 1.0f;
+        bits = move ? to : bits;
+#pragma unroll
+        for (int k = 0; k < N; ++k) sums[k] *= f;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] *= __uint_as_float(bits);
+    }
+  }
+  __device__ __forceinline__ float back() const { return T::kShortRange ? __uint_as_float((254u << 23) - bits) : 1.0f; }
+};
+
 // ---- gradient of the queries --------------------------------------------------------------
 // The forward's tiles; also leaves each row's statistics to the kernel of the keys' gradient.
 // D_i = sum_j P_ij (do_i . v_j) equals do_i . o_i, but for the rounding of o (and of the weights
@@ -367,7 +411,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
     if (ok) {
       const float lse = a.LSE[static_cast<int64_t>(h) * a.q_rows + p.q0 + row];
       // a row that sees nothing: against +inf every weight is 0
-      lse2 = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+      lse2 = lse == -__builtin_inff() ? __builtin_inff() : fmaf(lse, kLog2e, -kWeightShift<T>);
     }
   }
   float more = 0.0f;
@@ -377,6 +421,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
     acc[db] = f32x16_t{};
     keys[db] = f32x16_t{};
   }
+  Reach<T> reach;
   arrived(qf);
   if constexpr (!kRowsInLds) arrived(gf);
   for (int i = 0, j = team; i * kTeams < nb; ++i, j += kTeams) {
@@ -419,6 +464,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
           w[r] *= slip[r];
         }
       }
+      reach.take(dp, acc);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const typename T::x8 ds = pack<T>(dp, t), wt = pack<T>(w, t);
@@ -439,7 +485,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
 #pragma unroll
     for (int n = 0; n < kTeams; ++n) more += s_more[n][wave][lane];
   }
-  if (a.joined) more = 0.0f;
+  more = a.joined ? 0.0f : more * kWeightUnit<T>;
   if (ok && hlf == 0 && team == 0) {
     const int64_t pitch = a.q_rows;
     float* st = a.stats + h * pitch + p.q0 + row;
@@ -449,7 +495,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_grad_q(DocAttnArgs a) {
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[db][r] = fmaf(-more, keys[db][r], acc[db][r]);
+    for (int r = 0; r < 16; ++r)
+      acc[db][r] = fmaf(-more * kWeightUnit<T>, keys[db][r], acc[db][r] * (reach.back() * kWeightUnit<T>));
   if constexpr (kTeams > 1) {
     static_assert(sizeof(stage) >= (kTeams - 1) * S::kWaves * 64 * (D / 2) * 4, "the teams' sums fit the buffers");
     f32x4_t* sums = reinterpret_cast<f32x4_t*>(stage) + wave * (D / 8) * 64 + lane;
@@ -551,6 +598,7 @@ __global__ __launch_bounds__(256 * kKvTeams<D>, 2) void doc_grad_kv(DocAttnArgs 
     dk[db] = f32x16_t{};
     dv[db] = f32x16_t{};
   }
+  Reach<T> reach;
   const float c = a.scoring.unit * kLog2e;
   arrived(kf);
   if constexpr (!kRowsInLds) arrived(vf);
@@ -611,6 +659,7 @@ __global__ __launch_bounds__(256 * kKvTeams<D>, 2) void doc_grad_kv(DocAttnArgs 
           ds[r] = out ? 0.0f : ds[r];
         }
       }
+      reach.take(ds, dk);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const typename T::x8 wt = pack<T>(x, t), dt = pack<T>(ds, t);
@@ -624,6 +673,13 @@ __global__ __launch_bounds__(256 * kKvTeams<D>, 2) void doc_grad_kv(DocAttnArgs 
     if (++j == nb) {
       j = 0;
       if (++g < G) slope = slope_at(g);
+    }
+  }
+  if constexpr (T::kShortRange) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      dk[db] *= reach.back() * kUnshift;
+      dv[db] *= kUnshift;
     }
   }
   // the teams' sums: team 0 finishes those of the keys, team 1 those of the values

@@ -22,7 +22,7 @@ struct DocAttnArgs {
   uint16_t* dQ;
   uint16_t* dK;
   uint16_t* dV;
-  float* stats;        // [2][H][q_rows]: log-sum-exp in base 2, then less sum_j P_ij (dO_i . V_j)
+  float* stats;        // [2][H][q_rows]: log-sum-exp in base 2 (f16: less 14), then less sum_j P_ij (dO_i . V_j)
   float* parts;        // [row_parts][k_rows][Hkv][2][D]: their sums (row_parts 1: none)
   const int32_t* q_ptr;   // [n_docs + 1]
   const int32_t* k_ptr;   // [n_docs + 1]

@@ -1,0 +1,102 @@
+"""The gradient of attention over packed documents on the GPU: its norm against the fp64
+definition, small, uneven and large gradients among them."""
+import numpy as np
+import pytest
+
+import paper_2601_20595_amd as csg
+from grad_norms import check_norm, gradient_errors
+from oracle import doc_attention as oda
+
+torch = pytest.importorskip("torch")
+if torch.cuda.is_available():
+    from attn_util import DEV, HALF_STEP, TINY, TORCH, close, f64, ints, normal, pointers
+
+pytestmark = pytest.mark.gpu
+
+
+def _values(case, dtype, sharp, size, ramps=False):
+    rows, keys, H, Hkv, D = case[:5]
+    n, m = sum(rows), sum(keys)
+    x = [normal(i + 1, s, dtype, f)[0] for i, (s, f) in enumerate((((n, H, D), sharp), ((m, Hkv, D), 1.0), ((m, Hkv, D), 1.0), ((n, H, D), size)))]
+    if ramps:  # values and gradients of the output grow, by powers of two, along the rows
+        for i, lo, hi in ((2, -7, 5), (3, -8, 4)):
+            f = 2.0 ** torch.linspace(lo, hi, x[i].shape[0]).round()
+            x[i] = (x[i].float() * f[:, None, None]).to(TORCH[dtype])
+    return x
+
+
+def _slopes(case):
+    return (2.0 ** -np.arange(1, case[2] + 1)).astype(np.float32) if case[8] else None
+
+
+def _reference(case, x, dtype, **kw):
+    rows, keys, H, Hkv, D, causal, prefix, cap, _ = case
+    qp, kp = pointers(rows), pointers(keys)
+    y = [t.double().numpy() for t in x]
+    d, e = [], []
+    for t in range(len(rows)):
+        r, c = slice(qp[t], qp[t + 1]), slice(kp[t], kp[t + 1])
+        one = gradient_errors(y[0][r], y[1][c], y[2][c], y[3][r], oda.Scores(None, cap, _slopes(case), causal),
+                              prefix[t] if prefix else 0, HALF_STEP[dtype], TINY[dtype], **kw)
+        d.append(one[0])
+        e.append(one[1])
+    return [[np.concatenate([z[i] for z in w]) for i in range(3)] for w in (d, e)]
+
+
+def _gradients(case, x, dtype):
+    rows, keys, H, Hkv, D, causal, prefix, cap, _ = case
+    a = csg.DocAttn(H, Hkv, D, dtype, causal=causal, softcap=cap)
+    q, k, v, do = (t.to(DEV) for t in x)
+    n, m = q.shape[0], k.shape[0]
+    o, lse = torch.empty_like(q), torch.empty((H, n), device=DEV)
+    d = [torch.empty_like(t) for t in (q, k, v)]
+    ws = torch.empty(a.workspace_bytes(n, m), dtype=torch.uint8, device=DEV)
+    slopes = _slopes(case)
+    p = {"prefix": None if prefix is None else ints(prefix), "slopes": None if slopes is None else torch.tensor(slopes, device=DEV)}
+    qp, kp = ints(pointers(rows)), ints(pointers(keys))
+    a.forward(q, k, v, qp, kp, o, lse, **p)
+    a.backward(q, k, v, qp, kp, o, lse, do, *d, ws, **p)
+    torch.cuda.synchronize()
+    return [f64(t) for t in d]
+
+
+# rows and keys of the documents, heads, key/value heads, head_dim, causal, prefixes, cap, bias
+LONG = ([300], [3000], 4, 2, 64, True, None, 0.0, False)
+CASES = {
+    "cap and bias": (([140, 300], [140, 350], 6, 3, 64, True, None, 12.0, True), 8.0, 1.0),
+    "small": (LONG, 1.0, 1e-3),
+    "smaller": (LONG, 1.0, 1e-4),
+    "small, capped": (([200, 150], [2500, 150], 4, 1, 128, True, None, 8.0, False), 1.0, 1e-4),
+    "small, no mask": (([500], [2000], 8, 8, 128, False, None, 0.0, False), 1.0, 1e-4),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("name", CASES)
+def test_norms(name, dtype):
+    case, sharp, size = CASES[name]
+    x = _values(case, dtype, sharp, size)
+    want, error = _reference(case, x, dtype)
+    for what, g, w, e in zip(("dq", "dk", "dv"), _gradients(case, x, dtype), want, error):
+        check_norm(g, w, e, what)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_norms_of_uneven_gradients_in_f16(D):
+    """Gradients of scores that grow along the keys and along the rows, over more than f16's range."""
+    case = ([700], [700], 2, 1, D, False, None, 0.0, False)
+    x = _values(case, "f16", 1.0, 1.0, ramps=True)
+    want, error = _reference(case, x, "f16")
+    for what, g, w, e in zip(("dq", "dk", "dv"), _gradients(case, x, "f16"), want, error):
+        check_norm(g, w, e, what)
+
+
+def test_large_gradients_of_scores_in_f16():
+    """Gradients of scores beyond f16's largest number, whose sums are not: the keys are small."""
+    case = ([64], [64], 1, 1, 64, False, None, 0.0, False)
+    x = _values(case, "f16", 1.0, 300.0)
+    x[0], x[1], x[2] = x[0] * 2.0 ** -7, x[1] * 2.0 ** -7, x[2] * 2.0 ** 10
+    assert np.abs(f64(x[3])[:, 0] @ f64(x[2])[:, 0].T).max() / 64 > 65504
+    want, error = _reference(case, x, "f16")
+    for what, g, w, e in zip(("dq", "dk", "dv"), _gradients(case, x, "f16"), want, error):
+        check_norm(g, w, e, what)
