@@ -1,10 +1,10 @@
-"""The gradient of attention over packed documents on the GPU: its norm against the fp64
-definition, small, uneven and large gradients among them."""
+"""The gradient of attention over packed documents on the GPU: its norm and its direction against
+the fp64 definition, small, uneven and large gradients among them."""
 import numpy as np
 import pytest
 
 import paper_2601_20595_amd as csg
-from grad_norms import check_norm, gradient_errors
+from grad_norms import check_along, check_norm, gradient_errors
 from oracle import doc_attention as oda
 
 torch = pytest.importorskip("torch")
@@ -63,6 +63,13 @@ def _gradients(case, x, dtype):
 # rows and keys of the documents, heads, key/value heads, head_dim, causal, prefixes, cap, bias
 LONG = ([300], [3000], 4, 2, 64, True, None, 0.0, False)
 CASES = {
+    # (sharp scores and short documents are where D from a rounded output shows)
+    "sharp": (([200, 60], [200, 90], 4, 2, 128, True, None, 0.0, False), 20.0, 1.0),
+    "sharp, small heads": (([150, 200], [150, 200], 6, 2, 64, True, [0, 30], 0.0, False), 12.0, 1.0),
+    "sharp, many tiles": (([97, 130, 64] * 15, [97, 130, 70] * 15, 16, 4, 128, True, None, 0.0, False), 12.0, 1.0),
+    "sharp, many tiles of small heads": (([97, 130, 64] * 15, [97, 130, 70] * 15, 12, 12, 64, True, None, 0.0, False), 12.0, 1.0),
+    "sharp, two teams": (([400, 150], [1600, 600], 64, 16, 128, True, [0, 500], 0.0, False), 8.0, 1.0),
+    "short documents": (([40, 31, 33, 17] * 5, [40, 31, 33, 17] * 5, 4, 4, 64, True, None, 0.0, False), 4.0, 1.0),
     "cap and bias": (([140, 300], [140, 350], 6, 3, 64, True, None, 12.0, True), 8.0, 1.0),
     "small": (LONG, 1.0, 1e-3),
     "smaller": (LONG, 1.0, 1e-4),
@@ -100,3 +107,24 @@ def test_large_gradients_of_scores_in_f16():
     want, error = _reference(case, x, "f16")
     for what, g, w, e in zip(("dq", "dk", "dv"), _gradients(case, x, "f16"), want, error):
         check_norm(g, w, e, what)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_along_the_gradient(dtype):
+    """The derivative along each gradient's own direction, by differences of the fp64 definition."""
+    case = ([150, 90, 20, 64], [150, 200, 20, 10], 5, 1, 128, True, [64, 100, 33, 10], 0.0, False)
+    x = _values(case, dtype, 1.0, 1.0)
+    want, error = _reference(case, x, dtype)
+    got = _gradients(case, x, dtype)
+    y = [t.double().numpy() for t in x]
+    rows, keys, prefix = case[0], case[1], case[6]
+    qp, kp = pointers(rows), pointers(keys)
+    for i, what in enumerate(("dq", "dk", "dv")):
+        w = want[i] / np.linalg.norm(want[i])
+        f = []
+        for h in (1e-3, -1e-3):
+            z = list(y)
+            z[i] = y[i] + h * w
+            f.append(sum((oda.attention(z[0][qp[t]:qp[t + 1]], z[1][kp[t]:kp[t + 1]], z[2][kp[t]:kp[t + 1]], oda.Scores(), prefix[t])[0]
+                          * y[3][qp[t]:qp[t + 1]]).sum() for t in range(len(rows))))
+        check_along(got[i], want[i], error[i], (f[0] - f[1]) / 2e-3, what)
