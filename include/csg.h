@@ -501,8 +501,9 @@ csg_status csg_ring_attn(csg_plan* p, const void* q, void* k_landing, void* v_la
  * Buffers are 16-byte aligned. Tensors of heads are rows of n_heads (n_kv_heads) heads of
  * head_dim elements; a stride is the number of elements between rows (0 = dense), a
  * multiple of 8 and at most 2^23, so that q, k and v may be parts of one projection's
- * output. Statistics and sums are fp32; weights (in the gradient those of scores too, in f16
- * times powers of two that keep small ones) are rounded to dtype before their products. Every sum has a fixed order: equal calls give equal bits.
+ * output. Statistics and sums are fp32; weights and gradients of scores are rounded to dtype
+ * before their products (in the gradient in f16 times powers of two, which keep small ones). Every
+ * sum has a fixed order: equal calls give equal bits.
  * CSG_ERR_INVALID for a malformed request, CSG_ERR_UNSUPPORTED for another type, head
  * dimension or device, or sizes that a launch cannot hold; nothing is queued then. */
 

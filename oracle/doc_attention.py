@@ -12,7 +12,8 @@ off whose weights (and gradients of scores) are rounded to a type with relative 
 smallest step `tiny` before they are multiplied, whose products are summed in fp32 and whose
 outputs are rounded to the type once. They are first-order worst cases:
     a score:    es = 2^-17 (scale |q| . |k| + |s| + 1): 128 fp32 products summed in any order
-                (2^-24 each), and a few roundings of exp2's argument
+                (2^-24 each), and a few roundings of exp2's argument; with a cap c up to 64
+                2^-22 c for tanh (beyond, tanh is exact to its own size)
     a weight:   p (2 es + u) + tiny, times |v|, summed
     an output:  u |o| + tiny on top (an fp16 output below 2^-14 is a multiple of 2^-24 too)
     D = do . o: |do| . (u |o| + the bound of o); dP: 2^-17 |do| . |v|
@@ -55,7 +56,7 @@ def _head(q, k, sc: Scores, h: int, prefix: int):
         d = sc.slopes[h] * np.abs(p - np.arange(keys)[None, :])
         s = s - d
         size = size + d
-    size = size + np.abs(s) + 1.0 + sc.cap
+    size = size + np.abs(s) + 1.0 + min(sc.cap, 64.0) / 32
     return np.where(visible(rows, keys, sc.causal, prefix), s, -np.inf), t, size
 
 

@@ -230,11 +230,21 @@ __device__ __forceinline__ float sum_halves(float x) {
 // Row of a tile that a result's register r holds in this lane.
 __device__ __forceinline__ constexpr int result_row(int r, int hlf) { return 8 * (r >> 2) + 4 * hlf + (r & 3); }
 
-// tanh(x) = 1 - 2 / (1 + e^(2x)) from y = 2 x log2 e; off by some 1e-7 at most, and +-1 where e^(2x)
+// tanh(x) = 1 - 2 / (1 + e^(2x)) from y = 2 x log2 e; off by 2^-22 at most, and +-1 where e^(2x)
 // overflows or vanishes.
 __device__ __forceinline__ float tanh_from_log2(float y) {
   return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y));
 }
+// The same, off by 2^-20 of itself at most: below 0.3 by the series
+// x - x^3/3 + 2 x^5/15 - 17 x^7/315 + 62 x^9/2835, whose next term is 5e-8 of it there.
+__device__ __forceinline__ float tanh_from_log2_near_0(float y) {
+  const float x = y * (0.5f * kLn2), z = x * x;
+  const float p = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f) * x;
+  return fabsf(x) < 0.3f ? p : tanh_from_log2(y);
+}
+// Caps up to this take the short form: a score is off by 2^-22 times the cap, 1.5e-5 at 64, which is nothing
+// beside the rounding of weights. Larger ones would lose their small scores' digits (0.1 at a cap of 1e6).
+constexpr float kNearCap = 64.0f;
 
 // A head's slope in units of x.
 __device__ __forceinline__ float slope_of(const Scoring& p, int h) { return p.slopes ? p.slopes[h] / p.unit : 0.0f; }
@@ -245,10 +255,17 @@ __device__ __forceinline__ float slope_of(const Scoring& p, int h) { return p.sl
 template <int N>
 __device__ __forceinline__ void cap_scores(const Scoring& p, f32x16_t (&x)[N]) {
   if (p.cap_in == 0.0f) return;
+  if (p.unit <= kNearCap) {
 #pragma unroll
-  for (int n = 0; n < N; ++n)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[n][r] = tanh_from_log2(x[n][r] * p.cap_in);
+      for (int r = 0; r < 16; ++r) x[n][r] = tanh_from_log2(x[n][r] * p.cap_in);
+  } else {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[n][r] = tanh_from_log2_near_0(x[n][r] * p.cap_in);
+  }
 }
 template <int N, int sign>
 __device__ __forceinline__ void bias_scores(const Scoring& p, float slope, int at, int hlf, f32x16_t (&x)[N]) {
