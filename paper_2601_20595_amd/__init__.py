@@ -638,31 +638,54 @@ class AttnPlan(Plan):
                       copy_stream)
 
 
-def _arg(t, need: int, size: int, what: str, device: int) -> int:
-    """_buf's checks, that the tensor's elements have `size` bytes (0: any) and that it lives on
-    the calls' device; its address. (A few queries of the tensor: a decode step's kernels take
-    less time than careful ones.)"""
+class _Type:
+    """Element types that an argument may have, by name; `known`: those of them that tensors had."""
+
+    def __init__(self, size: int, *names: str):
+        self.size, self.names, self.known = size, names, set()
+
+    def learn(self, t, what: str) -> None:
+        name = str(t.dtype).rpartition(".")[2]
+        if t.itemsize != self.size:
+            raise ValueError("%s must have %d-byte elements" % (what, self.size))
+        if name not in self.names:
+            raise ValueError("%s must be %s; it is %s" % (what, self.names[0], name))
+        self.known.add(t.dtype)
+
+
+# (tensors of heads may also hold bit patterns, as a plan's may)
+_HEAD_TYPES = {CSG_BF16: _Type(2, "bfloat16", "int16", "uint16"), CSG_F16: _Type(2, "float16", "int16", "uint16")}
+_INT32, _FLOAT32, _FLOAT64 = _Type(4, "int32"), _Type(4, "float32"), _Type(8, "float64")
+
+
+def _arg(t, need: int, elements, what: str, device: int) -> int:
+    """_buf's checks, that the tensor's elements are of a _Type or have so many bytes (0: any)
+    and that it lives on the calls' device; its address. (A few queries of the tensor: a decode
+    step's kernels take less time than careful ones.)"""
     if t is None:
         return 0
     if type(t) is int:
         return t
-    if size and t.itemsize != size:
-        raise ValueError("%s must have %d-byte elements" % (what, size))
+    if type(elements) is _Type:
+        if t.dtype not in elements.known:
+            elements.learn(t, what)
+    elif elements and t.itemsize != elements:
+        raise ValueError("%s must have %d-byte elements" % (what, elements))
     if t.is_contiguous() and t.nbytes >= need and t.get_device() == device:
         return t.data_ptr()
     _buf(t, need, what)
     raise ValueError("%s must be on GPU %d" % (what, device))
 
 
-def _heads(t, rows: Optional[int], heads: int, head_dim: int, what: str, device: int):
+def _heads(t, rows: Optional[int], heads: int, head_dim: int, elements: _Type, what: str, device: int):
     """Checks a tensor of rows of heads, which may be part of a wider one: (address, rows, row
     stride in elements)."""
     shape = t.shape
     if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim or (rows is not None and shape[0] != rows):
         raise ValueError("%s must be (%s, %d, %d); it is %s"
                          % (what, "rows" if rows is None else rows, heads, head_dim, tuple(shape)))
-    if t.itemsize != 2:
-        raise ValueError("%s must have 2-byte elements" % what)
+    if t.dtype not in elements.known:
+        elements.learn(t, what)
     n = shape[0]
     row, head, one = t.stride()
     if n < 2:
@@ -688,7 +711,7 @@ class DocAttn:
                                      dtype=DTYPES[dtype] if isinstance(dtype, str) else int(dtype), causal=int(causal),
                                      scale=scale, softcap=softcap)
         csg_doc_attn_grad_workspace(self._cfg, -1)  # checks the configuration
-        self._shape = n_heads, n_kv_heads, head_dim
+        self._shape = n_heads, n_kv_heads, head_dim, _HEAD_TYPES[self._cfg.dtype]
 
     def workspace_bytes(self, q_rows: int, k_rows: int) -> int:
         """Bytes of the workspace that backward needs for up to that many rows and keys."""
@@ -700,15 +723,15 @@ class DocAttn:
     def _inputs(self, q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes):
         """Checks what both calls take and sets the configuration: rows, keys, addresses."""
         c, dev = self._cfg, self.device
-        h, hkv, d = self._shape
-        qa, n, c.q_stride = _heads(q, None, h, d, "q", dev)
-        ka, m, c.k_stride = _heads(k, None, hkv, d, "k", dev)
-        va, _, c.v_stride = _heads(v, m, hkv, d, "v", dev)
+        h, hkv, d, ty = self._shape
+        qa, n, c.q_stride = _heads(q, None, h, d, ty, "q", dev)
+        ka, m, c.k_stride = _heads(k, None, hkv, d, ty, "k", dev)
+        va, _, c.v_stride = _heads(v, m, hkv, d, ty, "v", dev)
         c.q_rows, c.k_rows = n, m
         c.n_docs = docs = q_ptr.numel() - 1
-        return n, m, (qa, ka, va, _arg(q_ptr, 4 * (docs + 1), 4, "q_ptr", dev), _arg(k_ptr, 4 * (docs + 1), 4, "k_ptr", dev),
-                      _arg(prefix, 4 * docs, 4, "prefix", dev), _arg(slopes, 4 * h, 4, "slopes", dev),
-                      _arg(o, 2 * n * h * d, 2, "o", dev), _arg(lse, 4 * n * h, 4, "lse", dev))
+        return n, m, (qa, ka, va, _arg(q_ptr, 4 * (docs + 1), _INT32, "q_ptr", dev), _arg(k_ptr, 4 * (docs + 1), _INT32, "k_ptr", dev),
+                      _arg(prefix, 4 * docs, _INT32, "prefix", dev), _arg(slopes, 4 * h, _FLOAT32, "slopes", dev),
+                      _arg(o, 2 * n * h * d, ty, "o", dev), _arg(lse, 4 * n * h, _FLOAT32, "lse", dev))
 
     def forward(self, q, k, v, q_ptr, k_ptr, o, lse, prefix=None, slopes=None, stream=None):
         _, _, args = self._inputs(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
@@ -720,12 +743,12 @@ class DocAttn:
         keys' share."""
         n, m, args = self._inputs(q, k, v, q_ptr, k_ptr, o, lse, prefix, slopes)
         c, dev = self._cfg, self.device
-        h, hkv, d = self._shape
-        dqa, _, c.dq_stride = _heads(dq, n, h, d, "dq", dev)
-        dka, _, c.dk_stride = _heads(dk, m, hkv, d, "dk", dev)
-        dva, _, c.dv_stride = _heads(dv, m, hkv, d, "dv", dev)
+        h, hkv, d, ty = self._shape
+        dqa, _, c.dq_stride = _heads(dq, n, h, d, ty, "dq", dev)
+        dka, _, c.dk_stride = _heads(dk, m, hkv, d, ty, "dk", dev)
+        dva, _, c.dv_stride = _heads(dv, m, hkv, d, ty, "dv", dev)
         c.joined = joined
-        _check(_lib().csg_doc_attn_grad(c, *args, _arg(d_o, 2 * n * h * d, 2, "d_o", dev), dqa, dka, dva,
+        _check(_lib().csg_doc_attn_grad(c, *args, _arg(d_o, 2 * n * h * d, ty, "d_o", dev), dqa, dka, dva,
                                         _arg(workspace, min(n, 1), 0, "workspace", dev), workspace.nbytes, dev, _stream(stream)),
                "csg_doc_attn_grad")
 
@@ -744,7 +767,7 @@ class PagedCache:
                                   dtype=DTYPES[dtype] if isinstance(dtype, str) else int(dtype), n_pages=n_pages,
                                   page_size=page_size, batch=batch, max_pages=max_pages)
         csg_cache_attn_workspace(self._cfg, -1)  # checks the configuration
-        self._shape = n_heads, n_kv_heads, head_dim
+        self._shape = n_heads, n_kv_heads, head_dim, _HEAD_TYPES[self._cfg.dtype]
         self._batch = batch
         self._page_bytes = 2 * n_pages * n_kv_heads * page_size * head_dim
         self._max_pages = max_pages
@@ -759,43 +782,43 @@ class PagedCache:
     def _table(self, page_table) -> int:
         if type(page_table) is not int and page_table.shape[-1] != self._max_pages:
             raise ValueError("page_table must have %d pages a row" % self._max_pages)
-        return _arg(page_table, self._table_bytes, 4, "page_table", self.device)
+        return _arg(page_table, self._table_bytes, _INT32, "page_table", self.device)
 
     def append(self, k_pages, v_pages, k, v, q_ptr, lens, page_table, inv_freq=None, interleaved=False, q=None, q_out=None,
                status=None, stream=None):
         """Keys are rotated in their first 2 * inv_freq.numel() elements (float64), and so are
         the queries q, into q_out."""
         c, dev, batch = self._cfg, self.device, self._batch
-        h, hkv, d = self._shape
-        ka, n, c.k_stride = _heads(k, None, hkv, d, "k", dev)
-        va, _, c.v_stride = _heads(v, n, hkv, d, "v", dev)
+        h, hkv, d, ty = self._shape
+        ka, n, c.k_stride = _heads(k, None, hkv, d, ty, "k", dev)
+        va, _, c.v_stride = _heads(v, n, hkv, d, ty, "v", dev)
         c.tokens = n
         qa = qo = c.q_stride = 0
         if q is not None:
-            qa, _, c.q_stride = _heads(q, n, h, d, "q", dev)
-            qo = _arg(q_out, 2 * n * h * d, 2, "q_out", dev)
+            qa, _, c.q_stride = _heads(q, n, h, d, ty, "q", dev)
+            qo = _arg(q_out, 2 * n * h * d, ty, "q_out", dev)
         c.rot_dim = rot = 0 if inv_freq is None else 2 * inv_freq.numel()
         c.interleaved = interleaved
         _check(_lib().csg_cache_append(
-            c, _arg(k_pages, self._page_bytes, 2, "k_pages", dev), _arg(v_pages, self._page_bytes, 2, "v_pages", dev), ka, va, qa, qo,
-            _arg(q_ptr, 4 * batch + 4, 4, "q_ptr", dev), _arg(lens, 4 * batch, 4, "lens", dev),
-            self._table(page_table), _arg(inv_freq, 4 * rot, 8, "inv_freq", dev),
-            _arg(status, 4, 4, "status", dev), dev, _stream(stream)), "csg_cache_append")
+            c, _arg(k_pages, self._page_bytes, ty, "k_pages", dev), _arg(v_pages, self._page_bytes, ty, "v_pages", dev), ka, va, qa, qo,
+            _arg(q_ptr, 4 * batch + 4, _INT32, "q_ptr", dev), _arg(lens, 4 * batch, _INT32, "lens", dev),
+            self._table(page_table), _arg(inv_freq, 4 * rot, _FLOAT64, "inv_freq", dev),
+            _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_cache_append")
 
     def attn(self, q, k_pages, v_pages, q_ptr, lens, page_table, o, lse, workspace, group_ptr=None, prefix=None, scale=0.0,
              softcap=0.0, slopes=None, status=None, stream=None):
         """group_ptr int32 (groups + 1) and prefix int32 (groups): sequences that share their
         first tokens; lse may be None."""
         c, dev, batch = self._cfg, self.device, self._batch
-        h, hkv, d = self._shape
-        qa, n, c.q_stride = _heads(q, None, h, d, "q", dev)
+        h, hkv, d, ty = self._shape
+        qa, n, c.q_stride = _heads(q, None, h, d, ty, "q", dev)
         c.tokens = n
         c.n_groups = groups = 0 if group_ptr is None else group_ptr.numel() - 1
         c.scale, c.softcap = scale, softcap
         _check(_lib().csg_cache_attn(
-            c, qa, _arg(k_pages, self._page_bytes, 2, "k_pages", dev), _arg(v_pages, self._page_bytes, 2, "v_pages", dev),
-            _arg(q_ptr, 4 * batch + 4, 4, "q_ptr", dev), _arg(lens, 4 * batch, 4, "lens", dev),
-            self._table(page_table), _arg(group_ptr, 4 * groups + 4, 4, "group_ptr", dev),
-            _arg(prefix, 4 * groups, 4, "prefix", dev), _arg(slopes, 4 * h, 4, "slopes", dev), _arg(o, 2 * n * h * d, 2, "o", dev),
-            _arg(lse, 4 * n * h, 4, "lse", dev), _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes,
-            _arg(status, 4, 4, "status", dev), dev, _stream(stream)), "csg_cache_attn")
+            c, qa, _arg(k_pages, self._page_bytes, ty, "k_pages", dev), _arg(v_pages, self._page_bytes, ty, "v_pages", dev),
+            _arg(q_ptr, 4 * batch + 4, _INT32, "q_ptr", dev), _arg(lens, 4 * batch, _INT32, "lens", dev),
+            self._table(page_table), _arg(group_ptr, 4 * groups + 4, _INT32, "group_ptr", dev),
+            _arg(prefix, 4 * groups, _INT32, "prefix", dev), _arg(slopes, 4 * h, _FLOAT32, "slopes", dev), _arg(o, 2 * n * h * d, ty, "o", dev),
+            _arg(lse, 4 * n * h, _FLOAT32, "lse", dev), _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes,
+            _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_cache_attn")
