@@ -793,10 +793,10 @@ class PagedCache:
         ka, n, c.k_stride = _heads(k, None, hkv, d, ty, "k", dev)
         va, _, c.v_stride = _heads(v, n, hkv, d, ty, "v", dev)
         c.tokens = n
-        qa = qo = c.q_stride = 0
+        qa = c.q_stride = 0
         if q is not None:
             qa, _, c.q_stride = _heads(q, n, h, d, ty, "q", dev)
-            qo = _arg(q_out, 2 * n * h * d, ty, "q_out", dev)
+        qo = _arg(q_out, 2 * n * h * d, ty, "q_out", dev)
         c.rot_dim = rot = 0 if inv_freq is None else 2 * inv_freq.numel()
         c.interleaved = interleaved
         _check(_lib().csg_cache_append(

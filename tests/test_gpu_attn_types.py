@@ -48,3 +48,11 @@ def test_cache():
                 o=_heads(H), lse=torch.zeros((H, N), device=DEV), workspace=torch.zeros(c.workspace_bytes(N, 1), dtype=torch.uint8, device=DEV),
                 group_ptr=ints([0, 1]), prefix=ints([2]), slopes=torch.zeros(H, device=DEV), status=ints([0]))
     _refuses_each(c.attn, args)
+
+
+def test_queries_and_their_output_go_together():
+    c = csg.PagedCache(H, HKV, D, "bf16", 2, 16, 1, 2)
+    pages = [torch.zeros((2, HKV, 16, D), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    for p in ({"q": _heads(H)}, {"q_out": _heads(H)}):
+        with pytest.raises(csg.CsgError, match="go together"):
+            c.append(*pages, _heads(HKV), _heads(HKV), ints([0, N]), ints([5]), ints([[0, 1]]), **p)
