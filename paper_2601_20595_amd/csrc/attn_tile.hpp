@@ -285,7 +285,7 @@ struct RowSoftmax {
   float m = -__builtin_inff();
   float mc = -__builtin_inff();  // c m
   float l = 0.0f;                // this lane's weights, summed before they are rounded
-  bool wide = false;             // some row's c m may overflow: c x - c m would lose its weights
+  bool wide = false;             // the row's c m may overflow: c x - c m would lose its weights
 
   // Weights of one block, rounded, as second operand of the value product, and the factor
   // by which what was summed before has to be multiplied if `moved`.
@@ -307,10 +307,9 @@ struct RowSoftmax {
       alpha = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
       m = to;
       mc = m * c;
-      const bool far = !none && fabsf(mc) > 1e37f;
-      wide = __builtin_amdgcn_ballot_w64(far) != 0;
+      wide = !none && fabsf(mc) > 1e37f;
       l *= alpha;
-      sum = weights<T, N, true>(x, c, none ? 0.0f : mc, pb, none ? 0.0f : m, far);
+      sum = weights<T, N, true>(x, c, none ? 0.0f : mc, pb, none ? 0.0f : m, wide);
     }
     l += sum;
     return alpha;
