@@ -604,7 +604,8 @@ csg_status csg_cache_attn_workspace(const csg_cache_cfg* cfg, int device, size_t
  * group share nothing) have the same first prefix[g] tokens: their keys and values are read
  * once for the group, from the pages of its first sequence; of the others' rows of the page
  * table, only tokens behind the prefix are read. A sequence shorter than that shares what it
- * has. o: [tokens][n_heads][head_dim]; lse: float[n_heads][tokens], or NULL.
+ * has, and a first one that is shorter makes the prefix as short. Values of keys that a row does not
+ * see, of its sequence or its group's prefix, are multiplied with weights of 0: they must be finite. o: [tokens][n_heads][head_dim]; lse: float[n_heads][tokens], or NULL.
  * Rows of no sequence are left as they are. workspace: csg_cache_attn_workspace bytes, any
  * content. At most 2048 sequences and groups. */
 csg_status csg_cache_attn(const csg_cache_cfg* cfg, const void* q, const void* k_pages,

@@ -338,7 +338,8 @@ struct Reach {
 // and of sharp scores in bf16 by 4.6e-3. One pass over the keys sums against D' = do_i . o_i:
 //   e_i = sum_j P_ij (do_i . v_j - D'_i) = D_i - D'_i,
 //   dQ_i / scale = sum_j P_ij (do_i . v_j - D'_i) (1 - tanh^2) k_j - e_i sum_j P_ij (1 - tanh^2) k_j.
-// (Against the output of more keys than the call's, whose weights do not sum to 1 here, e_i would be
+// (What multiplies e_i is a sum of rounded weights; e_i itself is of the size of a rounding, so that this
+// is of second order. Against the output of more keys than the call's, whose weights do not sum to 1 here, e_i would be
 // those keys' part of the sum: then it is 0, and D is D'.)
 // For D = 128 the second sum takes the registers of the rows of do, which are read from LDS. 8192 causal
 // rows, 32 heads on 8 of 128: 0.88 to 0.92 ms, four products of the pairs at 1.2 PFLOP/s, which is what a
