@@ -293,10 +293,12 @@ __global__ __launch_bounds__(S::kThreads, 2) void doc_forward(DocAttnArgs a) {
 // are made 2^14 times as large by the exponent's argument, and dS takes a power of two of each lane's own
 // row (key): the lane's largest so far lies below 2^15 with it, and was above 2^10 when it was set, so that
 // nothing overflows and what is lost is below 2^-35 of the largest. Sums in fp32 are brought back exactly.
-// The look at the largest costs the two kernels 3.7 and 1.6 us of 32 and 30 for packed documents of up to
-// 721 rows, heads of 64: its branch stands between a block's scores and its products. Without a branch 4.7
-// and 2.7; one for 64 keys spills; with a factor only where it is needed, or the products or fragments of
-// the next 32 keys ahead of it, within 1 us of the same.
+// The look at the largest costs: packed documents of up to 721 rows, heads of 64, queries' gradient 32.1 ->
+// 35.5 us, keys' 30.0 -> 31.6; 8191 rows, 32 heads on 8 of 128, 948 -> 1040 and 1085 -> 1131. The factor
+// alone costs nothing; the branch stands between a block's scores and its products. Without a branch 36.7
+// and 32.7; in one branch with the mask 38.5 and 32.9; the bits of the rounded numbers instead of the
+// largest 37.1 and 32.4; one for 64 keys spills; a factor only where it is needed, or the weights' products
+// or the next 32 keys' ahead of it, within 1 us of the same.
 constexpr float kLog2Shift = 14.0f, kUnshift = 1.0f / 16384.0f;
 template <class T>
 constexpr float kWeightShift = T::kShortRange ? kLog2Shift : 0.0f;
