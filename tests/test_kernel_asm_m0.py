@@ -31,7 +31,7 @@ def loads_behind_m0(asm: str):
     return bad
 
 
-def test_checker_flags_a_load_right_behind_the_write():
+def test_the_search_finds_a_load_right_behind_the_write():
     load = "buffer_load_dwordx4 v2, s[4:7], 0 offen lds"
     assert loads_behind_m0("\ts_mov_b32 m0, s2\n\t%s\n" % load) == [load]
     assert loads_behind_m0("\ts_add_i32 m0, s2, s3 ; note\n.LBB0_1:  ; loop\n\t;;#ASMSTART\n\tglobal_load_lds_dword v[0:1], off\n") != []
