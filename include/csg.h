@@ -614,6 +614,39 @@ csg_status csg_cache_attn(const csg_cache_cfg* cfg, const void* q, const void* k
                           const float* slopes, void* o, void* lse, void* workspace,
                           size_t workspace_bytes, int32_t* status, int device, void* stream);
 
+/* The same cache in 4 bits: k_pages and v_pages are [n_pages][n_kv_heads] blocks of page_size *
+ * (head_dim / 2 + head_dim / 32) bytes: the rows' elements, 2 i in the low half of byte i of a row and
+ * 2 i + 1 in the high half, then the rows' scales, one byte for each 32 elements (the OCP microscaling
+ * format MXFP4). An element is a sign (8) and a code 0 .. 7 for 0, 0.5, 1, 1.5, 2, 3, 4, 6; a scale
+ * x stands for 2^(x - 127). A block's scale is the least that leaves no element beyond 7 times it, within 2 .. 252
+ * (f16: 104 .. 140), so that every value is exact in dtype; elements are rounded to the nearest, ties to
+ * the even code, 6 beyond. A block with an infinity or a NaN has scale 255, and all of it stands for NaN.
+ * Arguments, layouts, errors, and what may be captured are those of the cache in 16 bits; q, k, v
+ * and o are of dtype. */
+
+/* As csg_cache_append. Keys are rotated in 64 bits, rounded to dtype, then to 4 bits. */
+csg_status csg_cache4_append(const csg_cache_cfg* cfg, void* k_pages, void* v_pages, const void* k,
+                             const void* v, const void* q, void* q_out, const int32_t* q_ptr,
+                             const int32_t* lens, const int32_t* page_table, const double* inv_freq,
+                             int32_t* status, int device, void* stream);
+
+/* The last tokens of the sequences, as the values that the cache holds, into k and v ([tokens][n_kv_heads]
+ * [head_dim] of dtype, strides k_stride and v_stride): sequence b's last k_ptr[b+1] - k_ptr[b] tokens (int32
+ * [batch + 1], ascending; with lens summed up, all of it) into rows k_ptr[b] .. k_ptr[b+1] - 1, as csg_doc_attn takes
+ * them. Tokens without a page read zeros and set status; rows of no sequence are left as they are. k and v
+ * may be parts of one tensor, and may not overlap each other or the pages. */
+csg_status csg_cache4_read(const csg_cache_cfg* cfg, const void* k_pages, const void* v_pages,
+                           const int32_t* k_ptr, const int32_t* lens, const int32_t* page_table, void* k,
+                           void* v, int32_t* status, int device, void* stream);
+
+/* As csg_cache_attn_workspace and csg_cache_attn. */
+csg_status csg_cache4_attn_workspace(const csg_cache_cfg* cfg, int device, size_t* bytes);
+csg_status csg_cache4_attn(const csg_cache_cfg* cfg, const void* q, const void* k_pages,
+                           const void* v_pages, const int32_t* q_ptr, const int32_t* lens,
+                           const int32_t* page_table, const int32_t* group_ptr, const int32_t* prefix,
+                           const float* slopes, void* o, void* lse, void* workspace,
+                           size_t workspace_bytes, int32_t* status, int device, void* stream);
+
 /* Waits for the plan's last call to complete (its kernel and every copy it issued)
  * and reports its diagnostics.
  * CSG_ERR_TIMEOUT if a wait expired (details in *out); CSG_ERR_STATE if the kernel

@@ -51,7 +51,7 @@ ABI_FUNCTIONS = (
     "csg_plan_trace", "csg_plan_destroy", "csg_attn_plan_create", "csg_ring_attn", "csg_plan_join",
     "csg_measure_mfma_peak", "csg_ag_gemm_noalloc",
     "csg_doc_attn", "csg_doc_attn_grad", "csg_doc_attn_grad_workspace", "csg_cache_append", "csg_cache_attn",
-    "csg_cache_attn_workspace",
+    "csg_cache_attn_workspace", "csg_cache4_append", "csg_cache4_read", "csg_cache4_attn", "csg_cache4_attn_workspace",
 )
 
 
@@ -162,6 +162,10 @@ def _lib():
         "csg_cache_append": ([P(csg_cache_cfg)] + [vp] * 11 + [ctypes.c_int, vp], st),
         "csg_cache_attn_workspace": ([P(csg_cache_cfg), ctypes.c_int, P(ctypes.c_size_t)], st),
         "csg_cache_attn": ([P(csg_cache_cfg)] + [vp] * 12 + [ctypes.c_size_t, vp, ctypes.c_int, vp], st),
+        "csg_cache4_append": ([P(csg_cache_cfg)] + [vp] * 11 + [ctypes.c_int, vp], st),
+        "csg_cache4_read": ([P(csg_cache_cfg)] + [vp] * 8 + [ctypes.c_int, vp], st),
+        "csg_cache4_attn_workspace": ([P(csg_cache_cfg), ctypes.c_int, P(ctypes.c_size_t)], st),
+        "csg_cache4_attn": ([P(csg_cache_cfg)] + [vp] * 12 + [ctypes.c_size_t, vp, ctypes.c_int, vp], st),
         "csg_measure_mfma_peak": ([ctypes.c_int, i32, P(ctypes.c_double), P(ctypes.c_double), P(ctypes.c_double)],
                                   st),
     }
@@ -460,6 +464,32 @@ def csg_cache_attn(cfg: csg_cache_cfg, q, k_pages, v_pages, q_ptr, lens, page_ta
                                  workspace_bytes, _ptr(status), device, _stream(stream)), "csg_cache_attn")
 
 
+def csg_cache4_append(cfg: csg_cache_cfg, k_pages, v_pages, k, v, q, q_out, q_ptr, lens, page_table, inv_freq, status=None,
+                      device=0, stream=None) -> None:
+    _check(_lib().csg_cache4_append(cfg, _ptr(k_pages), _ptr(v_pages), _ptr(k), _ptr(v), _ptr(q), _ptr(q_out), _ptr(q_ptr),
+                                    _ptr(lens), _ptr(page_table), _ptr(inv_freq), _ptr(status), device, _stream(stream)),
+           "csg_cache4_append")
+
+
+def csg_cache4_read(cfg: csg_cache_cfg, k_pages, v_pages, k_ptr, lens, page_table, k, v, status=None, device=0,
+                    stream=None) -> None:
+    _check(_lib().csg_cache4_read(cfg, _ptr(k_pages), _ptr(v_pages), _ptr(k_ptr), _ptr(lens), _ptr(page_table), _ptr(k), _ptr(v),
+                                  _ptr(status), device, _stream(stream)), "csg_cache4_read")
+
+
+def csg_cache4_attn_workspace(cfg: csg_cache_cfg, device=0) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib().csg_cache4_attn_workspace(cfg, device, ctypes.byref(n)), "csg_cache4_attn_workspace")
+    return n.value
+
+
+def csg_cache4_attn(cfg: csg_cache_cfg, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse,
+                    workspace, workspace_bytes: int, status=None, device=0, stream=None) -> None:
+    _check(_lib().csg_cache4_attn(cfg, _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(q_ptr), _ptr(lens), _ptr(page_table),
+                                  _ptr(group_ptr), _ptr(prefix), _ptr(slopes), _ptr(o), _ptr(lse), _ptr(workspace),
+                                  workspace_bytes, _ptr(status), device, _stream(stream)), "csg_cache4_attn")
+
+
 def csg_plan_join(plan: int, stream) -> None:
     """Queues on `stream` a wait, on the device, for every copy of the plan's last call."""
     _check(_lib().csg_plan_join(plan, _stream(stream)), "csg_plan_join")
@@ -655,7 +685,7 @@ class _Type:
 
 # (tensors of heads may also hold bit patterns, as a plan's may)
 _HEAD_TYPES = {CSG_BF16: _Type(2, "bfloat16", "int16", "uint16"), CSG_F16: _Type(2, "float16", "int16", "uint16")}
-_INT32, _FLOAT32, _FLOAT64 = _Type(4, "int32"), _Type(4, "float32"), _Type(8, "float64")
+_INT32, _FLOAT32, _FLOAT64, _UINT8 = _Type(4, "int32"), _Type(4, "float32"), _Type(8, "float64"), _Type(1, "uint8")
 
 
 def _arg(t, need: int, elements, what: str, device: int) -> int:
@@ -769,9 +799,18 @@ class PagedCache:
         csg_cache_attn_workspace(self._cfg, -1)  # checks the configuration
         self._shape = n_heads, n_kv_heads, head_dim, _HEAD_TYPES[self._cfg.dtype]
         self._batch = batch
-        self._page_bytes = 2 * n_pages * n_kv_heads * page_size * head_dim
+        self._pages = n_pages * n_kv_heads * page_size * self._row_bytes(head_dim), self._page_type()
         self._max_pages = max_pages
         self._table_bytes = 4 * batch * max_pages
+
+    _append, _attn = "csg_cache_append", "csg_cache_attn"
+
+    @staticmethod
+    def _row_bytes(head_dim: int) -> int:
+        return 2 * head_dim
+
+    def _page_type(self) -> _Type:
+        return self._shape[3]
 
     def workspace_bytes(self, tokens: int, n_groups: int = 0) -> int:
         """Bytes of the workspace that attn needs for up to that many new tokens and groups."""
@@ -799,11 +838,12 @@ class PagedCache:
         qo = _arg(q_out, 2 * n * h * d, ty, "q_out", dev)
         c.rot_dim = rot = 0 if inv_freq is None else 2 * inv_freq.numel()
         c.interleaved = interleaved
-        _check(_lib().csg_cache_append(
-            c, _arg(k_pages, self._page_bytes, ty, "k_pages", dev), _arg(v_pages, self._page_bytes, ty, "v_pages", dev), ka, va, qa, qo,
+        size, page = self._pages
+        _check(getattr(_lib(), self._append)(
+            c, _arg(k_pages, size, page, "k_pages", dev), _arg(v_pages, size, page, "v_pages", dev), ka, va, qa, qo,
             _arg(q_ptr, 4 * batch + 4, _INT32, "q_ptr", dev), _arg(lens, 4 * batch, _INT32, "lens", dev),
             self._table(page_table), _arg(inv_freq, 4 * rot, _FLOAT64, "inv_freq", dev),
-            _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_cache_append")
+            _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), self._append)
 
     def attn(self, q, k_pages, v_pages, q_ptr, lens, page_table, o, lse, workspace, group_ptr=None, prefix=None, scale=0.0,
              softcap=0.0, slopes=None, status=None, stream=None):
@@ -815,10 +855,40 @@ class PagedCache:
         c.tokens = n
         c.n_groups = groups = 0 if group_ptr is None else group_ptr.numel() - 1
         c.scale, c.softcap = scale, softcap
-        _check(_lib().csg_cache_attn(
-            c, qa, _arg(k_pages, self._page_bytes, ty, "k_pages", dev), _arg(v_pages, self._page_bytes, ty, "v_pages", dev),
+        size, page = self._pages
+        _check(getattr(_lib(), self._attn)(
+            c, qa, _arg(k_pages, size, page, "k_pages", dev), _arg(v_pages, size, page, "v_pages", dev),
             _arg(q_ptr, 4 * batch + 4, _INT32, "q_ptr", dev), _arg(lens, 4 * batch, _INT32, "lens", dev),
             self._table(page_table), _arg(group_ptr, 4 * groups + 4, _INT32, "group_ptr", dev),
             _arg(prefix, 4 * groups, _INT32, "prefix", dev), _arg(slopes, 4 * h, _FLOAT32, "slopes", dev), _arg(o, 2 * n * h * d, ty, "o", dev),
             _arg(lse, 4 * n * h, _FLOAT32, "lse", dev), _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes,
-            _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_cache_attn")
+            _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), self._attn)
+
+
+class PagedCache4(PagedCache):
+    """The same cache in 4 bits: append, attn and read (csg_cache4_append, csg_cache4_attn,
+    csg_cache4_read). The pages are uint8, (n_pages, n_kv_heads, page_size * (head_dim / 2 + head_dim /
+    32)); everything else is as in PagedCache, dtype that of q, k, v and o."""
+
+    _append, _attn = "csg_cache4_append", "csg_cache4_attn"
+
+    @staticmethod
+    def _row_bytes(head_dim: int) -> int:
+        return head_dim // 2 + head_dim // 32
+
+    def _page_type(self) -> _Type:
+        return _UINT8
+
+    def read(self, k_pages, v_pages, k_ptr, lens, page_table, k, v, status=None, stream=None):
+        """The sequences' last tokens, k_ptr (int32, batch + 1) being their rows in k and v, (tokens,
+        n_kv_heads, head_dim), which may be slices of a wider tensor."""
+        c, dev, batch = self._cfg, self.device, self._batch
+        _, hkv, d, ty = self._shape
+        ka, n, c.k_stride = _heads(k, None, hkv, d, ty, "k", dev)
+        va, _, c.v_stride = _heads(v, n, hkv, d, ty, "v", dev)
+        c.tokens = n
+        size, page = self._pages
+        _check(_lib().csg_cache4_read(
+            c, _arg(k_pages, size, page, "k_pages", dev), _arg(v_pages, size, page, "v_pages", dev),
+            _arg(k_ptr, 4 * batch + 4, _INT32, "k_ptr", dev), _arg(lens, 4 * batch, _INT32, "lens", dev), self._table(page_table),
+            ka, va, _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_cache4_read")

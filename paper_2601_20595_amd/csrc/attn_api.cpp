@@ -1,4 +1,4 @@
-// Entry points of attention over packed documents and of the paged key/value cache: checks of
+// Entry points of attention over packed documents and of the paged key/value caches: checks of
 // the arguments, then the launches. Nothing here allocates, waits or keeps state, apart from
 // what is known of each device.
 #include <algorithm>
@@ -7,6 +7,7 @@
 #include <initializer_list>
 #include <numeric>
 
+#include "cache4.hpp"
 #include "cache_attn.hpp"
 #include "csg.h"
 #include "doc_attn.hpp"
@@ -225,6 +226,82 @@ bool all_aligned(std::initializer_list<const void*> list) {
   return true;
 }
 
+// The checks and the launch of both caches' append.
+csg_status cache_append(hipError_t (*launch)(const csg::AppendArgs&, bool, int, hipStream_t), const csg_cache_cfg* cfg, void* k_pages, void* v_pages, const void* k, const void* v, const void* q,
+                            void* q_out, const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table,
+                            const double* inv_freq, int32_t* status, int device, void* stream) {
+  if (!cfg) return fail(CSG_ERR_INVALID, "cfg is NULL");
+  csg_cache_cfg c = *cfg;
+  CSG_CHECK(check_cache(&c));
+  const int64_t k_row = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
+  CSG_CHECK(check_stride(&c.k_stride, k_row, "k_stride"));
+  CSG_CHECK(check_stride(&c.v_stride, k_row, "v_stride"));
+  if (c.tokens > kMaxGrid) return fail(CSG_ERR_UNSUPPORTED, "too many tokens for one launch");
+  if (c.rot_dim < 0 || c.rot_dim > c.head_dim || c.rot_dim % 16 != 0)
+    return fail(CSG_ERR_INVALID, "rot_dim must be a multiple of 16 up to head_dim");
+  if (c.interleaved != 0 && c.interleaved != 1) return fail(CSG_ERR_INVALID, "interleaved must be 0 or 1");
+  if ((q != nullptr) != (q_out != nullptr)) return fail(CSG_ERR_INVALID, "q and q_out go together");
+  if (q && q == q_out && c.q_stride != static_cast<int64_t>(c.n_heads) * c.head_dim)
+    return fail(CSG_ERR_INVALID, "q_out is dense: it can be q only if q is");
+  if (c.tokens == 0 || c.batch == 0) return CSG_OK;
+  if (!k_pages || !v_pages || !k || !v || !q_ptr || !lens || !page_table || (c.rot_dim > 0 && !inv_freq))
+    return fail(CSG_ERR_INVALID, "NULL buffer");
+  if (!all_aligned({k_pages, v_pages, k, v, q, q_out})) return fail(CSG_ERR_INVALID, "buffers must be 16-byte aligned");
+  int32_t cus = 0;
+  CSG_CHECK(device_cus(device, &cus));
+  DeviceGuard g(device);
+  if (g.err != hipSuccess) return hip_fail(g.err, "hipSetDevice");
+  csg::AppendArgs a{};
+  a.c = cache_args(c, k_pages, v_pages, q, q_ptr, lens, page_table, status);
+  a.K = static_cast<const uint16_t*>(k);
+  a.V = static_cast<const uint16_t*>(v);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.inv_freq = inv_freq;
+  a.k_stride = c.k_stride;
+  a.v_stride = c.v_stride;
+  a.half = c.rot_dim / 2;
+  a.interleaved = c.interleaved;
+  CSG_HIP(launch(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));
+  return CSG_OK;
+}
+
+// The same of both caches' attention.
+csg_status cache_attn(hipError_t (*launch)(const csg::CacheAttnArgs&, bool, int, hipStream_t), const csg_cache_cfg* cfg, const void* q, const void* k_pages, const void* v_pages,
+                          const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table, const int32_t* group_ptr,
+                          const int32_t* prefix, const float* slopes, void* o, void* lse, void* workspace,
+                          size_t workspace_bytes, int32_t* status, int device, void* stream) {
+  if (!cfg) return fail(CSG_ERR_INVALID, "cfg is NULL");
+  csg_cache_cfg c = *cfg;
+  CSG_CHECK(check_cache_attn(&c));
+  if (c.tokens == 0 || c.batch == 0) return CSG_OK;
+  if (!q || !k_pages || !v_pages || !q_ptr || !lens || !page_table || !o || !workspace ||
+      (c.n_groups > 0 && (!group_ptr || !prefix)))
+    return fail(CSG_ERR_INVALID, "NULL buffer");
+  if (!all_aligned({q, k_pages, v_pages, o, workspace})) return fail(CSG_ERR_INVALID, "buffers must be 16-byte aligned");
+  int32_t cus = 0;
+  CSG_CHECK(device_cus(device, &cus));
+  if (static_cast<int64_t>(workspace_bytes) < cache_workspace(c, cus))
+    return fail(CSG_ERR_INVALID, "the workspace holds %zu bytes; the call needs %lld", workspace_bytes,
+                static_cast<long long>(cache_workspace(c, cus)));
+  DeviceGuard g(device);
+  if (g.err != hipSuccess) return hip_fail(g.err, "hipSetDevice");
+  csg::CacheAttnArgs a{};
+  a.c = cache_args(c, k_pages, v_pages, q, q_ptr, lens, page_table, status);
+  a.O = static_cast<uint16_t*>(o);
+  a.LSE = static_cast<float*>(lse);
+  a.group_ptr = group_ptr;
+  a.prefix = prefix;
+  a.n_groups = c.n_groups;
+  a.head_workers = csg::cache_head_workers(cus, c.n_kv_heads);
+  a.dies = 8 / std::gcd(8, c.n_kv_heads);
+  a.max_parts = csg::cache_max_parts(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups, a.head_workers);
+  a.max_tiles = csg::cache_max_tiles(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups);
+  a.ws = static_cast<unsigned char*>(workspace);
+  a.scoring = scoring(c.scale, c.softcap, slopes);
+  CSG_HIP(launch(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));
+  return CSG_OK;
+}
+
 }  // namespace
 
 csg_status csg_doc_attn(const csg_doc_attn_cfg* cfg, const void* q, const void* k, const void* v, const int32_t* q_ptr,
@@ -295,39 +372,8 @@ csg_status csg_doc_attn_grad(const csg_doc_attn_cfg* cfg, const void* q, const v
 csg_status csg_cache_append(const csg_cache_cfg* cfg, void* k_pages, void* v_pages, const void* k, const void* v, const void* q,
                             void* q_out, const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table,
                             const double* inv_freq, int32_t* status, int device, void* stream) {
-  if (!cfg) return fail(CSG_ERR_INVALID, "cfg is NULL");
-  csg_cache_cfg c = *cfg;
-  CSG_CHECK(check_cache(&c));
-  const int64_t k_row = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
-  CSG_CHECK(check_stride(&c.k_stride, k_row, "k_stride"));
-  CSG_CHECK(check_stride(&c.v_stride, k_row, "v_stride"));
-  if (c.tokens > kMaxGrid) return fail(CSG_ERR_UNSUPPORTED, "too many tokens for one launch");
-  if (c.rot_dim < 0 || c.rot_dim > c.head_dim || c.rot_dim % 16 != 0)
-    return fail(CSG_ERR_INVALID, "rot_dim must be a multiple of 16 up to head_dim");
-  if (c.interleaved != 0 && c.interleaved != 1) return fail(CSG_ERR_INVALID, "interleaved must be 0 or 1");
-  if ((q != nullptr) != (q_out != nullptr)) return fail(CSG_ERR_INVALID, "q and q_out go together");
-  if (q && q == q_out && c.q_stride != static_cast<int64_t>(c.n_heads) * c.head_dim)
-    return fail(CSG_ERR_INVALID, "q_out is dense: it can be q only if q is");
-  if (c.tokens == 0 || c.batch == 0) return CSG_OK;
-  if (!k_pages || !v_pages || !k || !v || !q_ptr || !lens || !page_table || (c.rot_dim > 0 && !inv_freq))
-    return fail(CSG_ERR_INVALID, "NULL buffer");
-  if (!all_aligned({k_pages, v_pages, k, v, q, q_out})) return fail(CSG_ERR_INVALID, "buffers must be 16-byte aligned");
-  int32_t cus = 0;
-  CSG_CHECK(device_cus(device, &cus));
-  DeviceGuard g(device);
-  if (g.err != hipSuccess) return hip_fail(g.err, "hipSetDevice");
-  csg::AppendArgs a{};
-  a.c = cache_args(c, k_pages, v_pages, q, q_ptr, lens, page_table, status);
-  a.K = static_cast<const uint16_t*>(k);
-  a.V = static_cast<const uint16_t*>(v);
-  a.q_out = static_cast<uint16_t*>(q_out);
-  a.inv_freq = inv_freq;
-  a.k_stride = c.k_stride;
-  a.v_stride = c.v_stride;
-  a.half = c.rot_dim / 2;
-  a.interleaved = c.interleaved;
-  CSG_HIP(csg::launch_cache_append(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));
-  return CSG_OK;
+  return cache_append(csg::launch_cache_append, cfg, k_pages, v_pages, k, v, q, q_out, q_ptr, lens, page_table, inv_freq, status,
+                      device, stream);
 }
 
 csg_status csg_cache_attn_workspace(const csg_cache_cfg* cfg, int device, size_t* bytes) {
@@ -344,34 +390,54 @@ csg_status csg_cache_attn(const csg_cache_cfg* cfg, const void* q, const void* k
                           const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table, const int32_t* group_ptr,
                           const int32_t* prefix, const float* slopes, void* o, void* lse, void* workspace,
                           size_t workspace_bytes, int32_t* status, int device, void* stream) {
+  return cache_attn(csg::launch_cache_attn, cfg, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse,
+                    workspace, workspace_bytes, status, device, stream);
+}
+
+csg_status csg_cache4_append(const csg_cache_cfg* cfg, void* k_pages, void* v_pages, const void* k, const void* v, const void* q,
+                             void* q_out, const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table,
+                             const double* inv_freq, int32_t* status, int device, void* stream) {
+  return cache_append(csg::launch_cache4_append, cfg, k_pages, v_pages, k, v, q, q_out, q_ptr, lens, page_table, inv_freq, status,
+                      device, stream);
+}
+
+csg_status csg_cache4_read(const csg_cache_cfg* cfg, const void* k_pages, const void* v_pages, const int32_t* k_ptr,
+                           const int32_t* lens, const int32_t* page_table, void* k, void* v, int32_t* status, int device,
+                           void* stream) {
   if (!cfg) return fail(CSG_ERR_INVALID, "cfg is NULL");
   csg_cache_cfg c = *cfg;
-  CSG_CHECK(check_cache_attn(&c));
+  c.q_stride = 0;  // (there are no queries)
+  CSG_CHECK(check_cache(&c));
+  const int64_t k_row = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
+  CSG_CHECK(check_stride(&c.k_stride, k_row, "k_stride"));
+  CSG_CHECK(check_stride(&c.v_stride, k_row, "v_stride"));
+  if ((c.tokens / csg::kReadRows + 1) * c.n_kv_heads > kMaxGrid)
+    return fail(CSG_ERR_UNSUPPORTED, "too many tokens and heads for one launch");
   if (c.tokens == 0 || c.batch == 0) return CSG_OK;
-  if (!q || !k_pages || !v_pages || !q_ptr || !lens || !page_table || !o || !workspace ||
-      (c.n_groups > 0 && (!group_ptr || !prefix)))
-    return fail(CSG_ERR_INVALID, "NULL buffer");
-  if (!all_aligned({q, k_pages, v_pages, o, workspace})) return fail(CSG_ERR_INVALID, "buffers must be 16-byte aligned");
+  if (!k_pages || !v_pages || !k_ptr || !lens || !page_table || !k || !v) return fail(CSG_ERR_INVALID, "NULL buffer");
+  if (!all_aligned({k_pages, v_pages, k, v})) return fail(CSG_ERR_INVALID, "buffers must be 16-byte aligned");
   int32_t cus = 0;
   CSG_CHECK(device_cus(device, &cus));
-  if (static_cast<int64_t>(workspace_bytes) < cache_workspace(c, cus))
-    return fail(CSG_ERR_INVALID, "the workspace holds %zu bytes; the call needs %lld", workspace_bytes,
-                static_cast<long long>(cache_workspace(c, cus)));
   DeviceGuard g(device);
   if (g.err != hipSuccess) return hip_fail(g.err, "hipSetDevice");
-  csg::CacheAttnArgs a{};
-  a.c = cache_args(c, k_pages, v_pages, q, q_ptr, lens, page_table, status);
-  a.O = static_cast<uint16_t*>(o);
-  a.LSE = static_cast<float*>(lse);
-  a.group_ptr = group_ptr;
-  a.prefix = prefix;
-  a.n_groups = c.n_groups;
-  a.head_workers = csg::cache_head_workers(cus, c.n_kv_heads);
-  a.dies = 8 / std::gcd(8, c.n_kv_heads);
-  a.max_parts = csg::cache_max_parts(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups, a.head_workers);
-  a.max_tiles = csg::cache_max_tiles(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups);
-  a.ws = static_cast<unsigned char*>(workspace);
-  a.scoring = scoring(c.scale, c.softcap, slopes);
-  CSG_HIP(csg::launch_cache_attn(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));
+  csg::ReadArgs a{};
+  a.c = cache_args(c, k_pages, v_pages, nullptr, k_ptr, lens, page_table, status);
+  a.K = static_cast<uint16_t*>(k);
+  a.V = static_cast<uint16_t*>(v);
+  a.k_stride = c.k_stride;
+  a.v_stride = c.v_stride;
+  CSG_HIP(csg::launch_cache4_read(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));
   return CSG_OK;
+}
+
+csg_status csg_cache4_attn_workspace(const csg_cache_cfg* cfg, int device, size_t* bytes) {
+  return csg_cache_attn_workspace(cfg, device, bytes);
+}
+
+csg_status csg_cache4_attn(const csg_cache_cfg* cfg, const void* q, const void* k_pages, const void* v_pages,
+                          const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table, const int32_t* group_ptr,
+                          const int32_t* prefix, const float* slopes, void* o, void* lse, void* workspace,
+                          size_t workspace_bytes, int32_t* status, int device, void* stream) {
+  return cache_attn(csg::launch_cache4_attn, cfg, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse,
+                    workspace, workspace_bytes, status, device, stream);
 }

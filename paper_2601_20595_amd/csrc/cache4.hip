@@ -1,0 +1,459 @@
+// A paged key/value cache in 4 bits for gfx950 (CDNA4): new tokens go in, rows come out, attention
+// reads it. Pages, tables and lengths are those of the cache in 16 bits.
+//
+// An element is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (e2m1, in the order of its code); each 32
+// elements of a head share a scale 2^e, held as the byte e + 127 (e8m0): the OCP microscaling format
+// MXFP4, whose conversions the hardware has. e is the least with |x| <= 7 2^e in the block: what
+// lies between 6 and 7 is off by no more than half the step above 4, as a rounding is; with the largest
+// element below 8 2^e instead, an element of 7.9 would be off by 1.9.
+// e is held within what leaves every value a normal number of bf16 (-125 .. 125), or exact in f16
+// (-23 .. 13). A head's rows of a page lie behind each other, elements 2 i and 2 i + 1 in the low and the
+// high half of byte i, and the page's scales behind them.
+#include <hip/hip_runtime.h>
+
+#include "cache4.hpp"
+#include "cache_plan.hpp"
+
+namespace csg {
+namespace {
+
+using namespace cache;
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+
+template <class T>
+struct Four;  // conversions between T and 4 bits, and the limits of the scales' bytes
+template <>
+struct Four<Bf16> {
+  static constexpr int kLeast = 127 - 125, kMost = 127 + 125;
+  template <int byte>
+  static __device__ __forceinline__ uint32_t from(uint32_t codes, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, byte));
+  }
+  template <int byte>
+  static __device__ __forceinline__ uint32_t to(uint32_t old, uint32_t pair, float scale) {
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, __builtin_bit_cast(bf16x2_t, pair), scale, byte);
+  }
+  static __device__ __forceinline__ float widen(uint32_t bits) { return __uint_as_float(bits << 16); }
+};
+template <>
+struct Four<F16> {
+  static constexpr int kLeast = 127 - 23, kMost = 127 + 13;
+  template <int byte>
+  static __device__ __forceinline__ uint32_t from(uint32_t codes, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, byte));
+  }
+  template <int byte>
+  static __device__ __forceinline__ uint32_t to(uint32_t old, uint32_t pair, float scale) {
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(old, __builtin_bit_cast(f16x2_t, pair), scale, byte);
+  }
+  static __device__ __forceinline__ float widen(uint32_t bits) {
+    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(bits)));
+  }
+};
+
+constexpr uint32_t kNanScale = 255;  // (the format's)
+
+// The factor that a scale's byte stands for.
+__device__ __forceinline__ float scale_of(uint32_t byte) {
+  return __uint_as_float(byte == kNanScale ? 0x7fc00000u : byte << 23);
+}
+
+// Eight elements from their codes, of one block.
+template <class T>
+__device__ __forceinline__ u32x4_t values(uint32_t codes, float scale) {
+  return u32x4_t{Four<T>::template from<0>(codes, scale), Four<T>::template from<1>(codes, scale),
+                 Four<T>::template from<2>(codes, scale), Four<T>::template from<3>(codes, scale)};
+}
+
+// Bytes of a head's rows of a page, and where they begin.
+template <int D>
+__device__ __forceinline__ int64_t head_bytes(const CacheArgs& c) {
+  return static_cast<int64_t>(cache4_row_bytes(D)) << c.page_shift;
+}
+template <int D>
+__device__ __forceinline__ int64_t head_of(const CacheArgs& c, int page, int kvh) {
+  return (static_cast<int64_t>(page) * c.Hkv + kvh) * head_bytes<D>(c);
+}
+
+// ---- new tokens into the cache --------------------------------------------------------------
+// A workgroup per token, as in the cache of 16 bits; but keys are rotated in 64 bits (sines and cosines
+// once a token, 6 operations a pair and head), so that their rounding to T and from there to a
+// code, next to a border too, follows from the definition and not from the order of a kernel's operations. Eight
+// lanes (D = 64: four) have a head; its rotated elements go through LDS, since a block's elements come from
+// pairs of two places, and two lanes quantise a block.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void cache4_append(AppendArgs a) {
+  constexpr int kCols = D / 16, kHeads = kThreads / kCols;
+  __shared__ double s_cos[D / 2], s_sin[D / 2];
+  __shared__ __attribute__((aligned(16))) uint16_t s_row[kHeads][D];
+  const CacheArgs& c = a.c;
+  const int t = blockIdx.x;
+  if (t < first_token(c, 0) || t >= first_token(c, c.batch)) return;  // (a row of no sequence)
+  const int b = last_below(c.batch, [&](int i) { return c.q_ptr[i] <= t; });
+  const int pos = c.lens[b] - (c.q_ptr[b + 1] - t);
+  const int slot = pos >> c.page_shift;
+  int page = -1;
+  if (pos < 0 || slot >= c.max_pages) {
+    if (threadIdx.x == 0) tell(c, kCacheBadLength);
+  } else {
+    page = c.table[static_cast<int64_t>(b) * c.max_pages + slot];
+    if (page < 0 || page >= c.n_pages) {
+      page = -1;
+      if (threadIdx.x == 0) tell(c, kCacheBadPage);
+    }
+  }
+  if (static_cast<int>(threadIdx.x) < a.half) {
+    double sn, cs;
+    sincos(static_cast<double>(pos) * a.inv_freq[threadIdx.x], &sn, &cs);
+    s_cos[threadIdx.x] = cs;
+    s_sin[threadIdx.x] = sn;
+  }
+  __syncthreads();
+  const int lane_head = threadIdx.x / kCols, col = threadIdx.x % kCols;
+  const bool turns = 8 * col < a.half;
+  const bool split = turns && !a.interleaved;
+  const int x0 = split ? 8 * col : 16 * col, x1 = split ? a.half + 8 * col : 16 * col + 8;
+  if (c.Q) {
+    float cs[8], sn[8];
+    if (turns) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        cs[e] = static_cast<float>(s_cos[8 * col + e]);
+        sn[e] = static_cast<float>(s_sin[8 * col + e]);
+      }
+    }
+    for (int i = lane_head; i < c.H; i += kHeads) {
+      const uint16_t* src = c.Q + t * c.q_stride + i * D;
+      uint16_t* dst = a.q_out + (static_cast<int64_t>(t) * c.H + i) * D;
+      const typename T::x8 y[2] = {*reinterpret_cast<const typename T::x8*>(src + x0), *reinterpret_cast<const typename T::x8*>(src + x1)};
+      f32x8_t z[2] = {__builtin_convertvector(y[0], f32x8_t), __builtin_convertvector(y[1], f32x8_t)};
+      if (turns) {
+        if (split) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float u = z[0][e], v = z[1][e];
+            z[0][e] = fmaf(u, cs[e], -v * sn[e]);
+            z[1][e] = fmaf(v, cs[e], u * sn[e]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float u = z[e / 4][2 * (e & 3)], v = z[e / 4][2 * (e & 3) + 1];
+            z[e / 4][2 * (e & 3)] = fmaf(u, cs[e], -v * sn[e]);
+            z[e / 4][2 * (e & 3) + 1] = fmaf(v, cs[e], u * sn[e]);
+          }
+        }
+      }
+      // (a head that is not turned keeps its bits: the type's own values are exact in 32 bits)
+      *reinterpret_cast<typename T::x8*>(dst + x0) = turns ? __builtin_convertvector(z[0], typename T::x8) : y[0];
+      *reinterpret_cast<typename T::x8*>(dst + x1) = turns ? __builtin_convertvector(z[1], typename T::x8) : y[1];
+    }
+  }
+  if (page < 0) return;
+  const int row = pos & ((1 << c.page_shift) - 1);
+  for (int i = lane_head; i < 2 * c.Hkv; i += kHeads) {
+    const bool is_v = i >= c.Hkv;
+    const int h = i - (is_v ? c.Hkv : 0);
+    const uint16_t* src = (is_v ? a.V + t * a.v_stride : a.K + t * a.k_stride) + h * D;
+    u32x4_t w[2];  // elements 16 col .. + 15
+    if (is_v || a.half == 0) {
+      w[0] = *reinterpret_cast<const u32x4_t*>(src + 16 * col);
+      w[1] = *reinterpret_cast<const u32x4_t*>(src + 16 * col + 8);
+    } else {
+      uint16_t* mine = s_row[lane_head];
+      typename T::x8 y[2] = {*reinterpret_cast<const typename T::x8*>(src + x0), *reinterpret_cast<const typename T::x8*>(src + x1)};
+      if (turns) {
+        f32x8_t z[2];
+        auto turn = [&](int e, float x, float y, float& u, float& v) {
+          const double cs = s_cos[8 * col + e], sn = s_sin[8 * col + e];
+          u = static_cast<float>(x * cs - y * sn);
+          v = static_cast<float>(y * cs + x * sn);
+        };
+        float u, v;
+        if (split) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            turn(e, static_cast<float>(y[0][e]), static_cast<float>(y[1][e]), u, v);
+            z[0][e] = u;
+            z[1][e] = v;
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            turn(e, static_cast<float>(y[e / 4][2 * (e & 3)]), static_cast<float>(y[e / 4][2 * (e & 3) + 1]), u, v);
+            z[e / 4][2 * (e & 3)] = u;
+            z[e / 4][2 * (e & 3) + 1] = v;
+          }
+        }
+        y[0] = __builtin_convertvector(z[0], typename T::x8);
+        y[1] = __builtin_convertvector(z[1], typename T::x8);
+      }
+      *reinterpret_cast<u32x4_t*>(mine + x0) = __builtin_bit_cast(u32x4_t, y[0]);
+      *reinterpret_cast<u32x4_t*>(mine + x1) = __builtin_bit_cast(u32x4_t, y[1]);
+      // the lanes of a head are of one wave, whose LDS accesses are done in order
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      w[0] = *reinterpret_cast<const u32x4_t*>(mine + 16 * col);
+      w[1] = *reinterpret_cast<const u32x4_t*>(mine + 16 * col + 8);
+      __builtin_amdgcn_wave_barrier();
+    }
+    // the largest absolute value, compared as bits (a NaN is larger than all)
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t pair = w[j / 4][j % 4];
+      top = max(top, max(pair & 0x7fffu, pair >> 16 & 0x7fffu));
+    }
+    top = max(top, __shfl_xor(top, 1));
+    const uint32_t wide = __float_as_uint(Four<T>::widen(top));
+    // m 2^k with 1 <= m < 2: e = k - 2 up to m = 1.75, k - 1 beyond
+    const int e = static_cast<int>((wide + 0x1fffffu) >> 23) - 2;
+    const bool none = wide >= 0x7f800000u;
+    const uint32_t byte = none ? kNanScale : static_cast<uint32_t>(clamped(e, Four<T>::kLeast, Four<T>::kMost));
+    const float scale = __uint_as_float(byte << 23);
+    u32x2_t codes{0u, 0u};
+    if (!none) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        codes[j] = Four<T>::template to<0>(codes[j], w[j][0], scale);
+        codes[j] = Four<T>::template to<1>(codes[j], w[j][1], scale);
+        codes[j] = Four<T>::template to<2>(codes[j], w[j][2], scale);
+        codes[j] = Four<T>::template to<3>(codes[j], w[j][3], scale);
+      }
+    }
+    unsigned char* head = reinterpret_cast<unsigned char*>(is_v ? c.v_pages : c.k_pages) + head_of<D>(c, page, h);
+    *reinterpret_cast<u32x2_t*>(head + row * (D / 2) + 8 * col) = codes;
+    if (col % 2 == 0) head[((D / 2) << c.page_shift) + row * (D / 32) + col / 2] = static_cast<unsigned char>(byte);
+  }
+}
+
+// ---- rows out of the cache ------------------------------------------------------------------
+// A workgroup has kReadRows rows of one head, keys and values. D / 8 lanes have a row: 4 bytes in, 16
+// bytes out, rows of a page behind each other.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void cache4_read(ReadArgs a) {
+  constexpr int kLanes = D / 8, kAtOnce = kThreads / kLanes;
+  __shared__ int s_page[kReadRows], s_row[kReadRows];
+  const CacheArgs& c = a.c;
+  const int row0 = blockIdx.x / c.Hkv * kReadRows, kvh = blockIdx.x % c.Hkv;
+  if (threadIdx.x < kReadRows) {
+    const int t = row0 + threadIdx.x;
+    int page = -1, row = -1;  // row -1: a row of no sequence
+    if (t >= first_token(c, 0) && t < first_token(c, c.batch)) {
+      int b = 0;
+      for (int n = c.batch; n > 1;) {  // the last sequence that starts by then
+        const int half = n / 2;
+        const bool up = c.q_ptr[b + half] <= t;
+        b = up ? b + half : b;
+        n = up ? n - half : half;
+      }
+      const int pos = c.lens[b] - (c.q_ptr[b + 1] - t);
+      const int slot = pos >> c.page_shift;
+      row = pos & ((1 << c.page_shift) - 1);
+      if (pos < 0 || slot >= c.max_pages) {
+        tell(c, kCacheBadLength);
+      } else {
+        page = c.table[static_cast<int64_t>(b) * c.max_pages + slot];
+        if (page < 0 || page >= c.n_pages) {
+          page = -1;
+          tell(c, kCacheBadPage);
+        }
+      }
+    }
+    s_page[threadIdx.x] = page;
+    s_row[threadIdx.x] = row;
+  }
+  __syncthreads();
+  const int col = threadIdx.x % kLanes;
+#pragma unroll
+  for (int i = threadIdx.x / kLanes; i < kReadRows; i += kAtOnce) {
+    const int page = s_page[i], row = s_row[i];
+    if (row < 0) continue;
+#pragma unroll
+    for (int is_v = 0; is_v < 2; ++is_v) {
+      u32x4_t x{0u, 0u, 0u, 0u};
+      if (page >= 0) {
+        const unsigned char* head = reinterpret_cast<const unsigned char*>(is_v ? c.v_pages : c.k_pages) + head_of<D>(c, page, kvh);
+        const uint32_t codes = *reinterpret_cast<const uint32_t*>(head + row * (D / 2) + 4 * col);
+        x = values<T>(codes, scale_of(head[((D / 2) << c.page_shift) + row * (D / 32) + col / 4]));
+      }
+      uint16_t* to = is_v ? a.V + (row0 + i) * a.v_stride : a.K + (row0 + i) * a.k_stride;
+      *reinterpret_cast<u32x4_t*>(to + kvh * D + 8 * col) = x;
+    }
+  }
+}
+
+// ---- attention over the cache ---------------------------------------------------------------
+// Entries, tasks and runs are those of the cache in 16 bits (cache_plan.hpp), and so are the parts, which
+// its cache_merge joins.
+
+// Codes and scale of a lane's elements of 16 rows of a head: lane l has a quarter of row l / 4.
+template <int D>
+struct Quarter {
+  uint32_t codes[D / 32];
+  uint32_t byte;
+  // Rows key .. key + 15 of page (-1: none); those outside of the part's keys read zeros.
+  __device__ __forceinline__ void load(const CacheArgs& c, const uint16_t* pages, const Part& p, int page, int key, int lane) {
+    const int row = lane >> 2, quarter = lane & 3;
+    const unsigned char* head = reinterpret_cast<const unsigned char*>(pages) + head_of<D>(c, max(page, 0), p.kvh);
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(head, page < 0 ? 0 : static_cast<int>(head_bytes<D>(c)));
+    const int r = (key & ((1 << c.page_shift) - 1)) + row;
+    const bool in = key + row >= p.lo && key + row < p.end;
+    const int at = in ? r * (D / 2) + quarter * (D / 8) : 1 << 30;
+    const int scale_at = in ? ((D / 2) << c.page_shift) + r * (D / 32) + quarter * (D / 32) / 4 : 1 << 30;
+    if constexpr (D == 128) {
+      const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) codes[i] = x[i];
+    } else {
+      const u32x2_t x = __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0);
+      codes[0] = x[0];
+      codes[1] = x[1];
+    }
+    byte = __builtin_amdgcn_raw_buffer_load_b8(rs, scale_at, 0, 0);
+  }
+  // Into a tile of 16-bit rows, the 16 rows beginning at `to`.
+  template <class T>
+  __device__ __forceinline__ void store(unsigned char* to, int lane) const {
+    const int row = lane >> 2, quarter = lane & 3;
+    const float scale = scale_of(byte);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+      *reinterpret_cast<u32x4_t*>(to + row * 2 * D + 16 * ((quarter * (D / 32) + i) ^ swz<D>(row))) = values<T>(codes[i], scale);
+  }
+};
+
+// A part, whose waves share blocks of 64 keys: each brings 16 keys and values, in 16 bits into one of two
+// buffers.
+template <class T, int D, bool kPlain>
+__device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, Part& p, unsigned char* stage, float* out, int lane,
+                                          int wave) {
+  constexpr int kTile = kCacheWideBlock * 2 * D;
+  const CacheArgs& c = a.c;
+  const int l32 = lane & 31, hlf = lane >> 5;
+  const int nb = (p.end - p.key0 + kCacheWideBlock - 1) / kCacheWideBlock;
+  // lane n holds the page of the wave's keys of block n (64 blocks at a time)
+  int pages = -1;
+  auto fetch = [&](int n) { pages = page_of(c, p, p.key0 + (n + lane) * kCacheWideBlock + 16 * wave); };
+  Quarter<D> k, v;
+  auto load = [&](int n) {
+    if (n > 0 && (n & 63) == 0) fetch(n);
+    const int page = __builtin_amdgcn_readlane(pages, n & 63), key = p.key0 + n * kCacheWideBlock + 16 * wave;
+    k.load(c, c.k_pages, p, page, key, lane);
+    v.load(c, c.v_pages, p, page, key, lane);
+  };
+  fetch(0);
+  load(0);
+  locate_row(a, x, local, l32, p);
+  typename T::x8 qf[D / 16];
+  load_queries<T, D>(a, p, hlf, qf);
+  const float slope = kPlain ? 0.0f : slope_of(a.scoring, p.h);
+  const float cexp = a.scoring.unit * kLog2e;
+  const Frags<D> fr(lane);
+  f32x16_t acc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
+  RowSoftmax sm;
+  const bool idle = p.tile * kCacheTileRows >= x.rows;  // no row in this wave
+  for (int n = 0; n < nb; ++n) {
+    unsigned char* kt = stage + (n & 1) * 2 * kTile;
+    k.template store<T>(kt + wave * 16 * 2 * D, lane);
+    v.template store<T>(kt + kTile + wave * 16 * 2 * D, lane);
+    if (n + 1 < nb) load(n + 1);
+    __syncthreads();  // block n is there, and everyone is done with block n - 1
+    if (idle) continue;
+    f32x16_t sc[2] = {f32x16_t{}, f32x16_t{}};
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) sc[kb] = T::mfma(row_frag<T, D>(kt, fr, s, 32 * kb), qf[s], sc[kb]);
+    finish_scores<2, kPlain>(a, p, slope, p.key0 + n * kCacheWideBlock, hlf, sc);
+    typename T::x8 pb[4];
+    bool moved;
+    const float alpha = sm.block<T, 2>(sc, cexp, pb, moved);
+    if (moved) {
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        acc[db] = T::mfma(col_frag<T, D>((const lds_u8_t*)(kt + kTile), fr, db, 16 * t), pb[t], acc[db]);
+  }
+  const float l = sum_halves(sm.l);
+  if (out && p.ok) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4_t*>(out + l32 * D + 32 * db + 8 * q + 4 * hlf) =
+            f32x4_t{acc[db][4 * q], acc[db][4 * q + 1], acc[db][4 * q + 2], acc[db][4 * q + 3]};
+    if (hlf == 0) {
+      out[32 * D + l32] = sm.m;
+      out[32 * D + 32 + l32] = l;
+    }
+  }
+  __syncthreads();  // the buffers are free again
+}
+
+template <class T, int D, bool kPlain>
+__global__ __launch_bounds__(kThreads, 2) void cache4_attn(CacheAttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char stage[2 * 2 * kCacheWideBlock * 2 * D];
+  static_assert(sizeof(stage) >= kCacheGroupBytes, "the groups, before the buffers");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  auto wide = [&](const Entry& x, const Entry* local, Part& p, float* out) {
+    wide_part<T, D, kPlain>(a, x, local, p, stage, out, lane, wave);
+  };
+  cache_run<D>(
+      a, stage,
+      [&](const Entry& x, const Entry* local, Part& p, float* out) {
+        p.tile = wave;  // (the rows are the first wave's)
+        wide(x, local, p, out);
+      },
+      wide);
+}
+
+template <class T, int D>
+hipError_t append(const AppendArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((cache4_append<T, D>), dim3(a.c.tokens), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+template <class T, int D>
+hipError_t read(const ReadArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((cache4_read<T, D>), dim3((a.c.tokens + kReadRows - 1) / kReadRows * a.c.Hkv), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+template <class T, int D>
+hipError_t attend(const CacheAttnArgs& a, hipStream_t s) {
+  const dim3 grid(a.head_workers * a.c.Hkv);
+  if (a.scoring.plain())
+    hipLaunchKernelGGL((cache4_attn<T, D, true>), grid, dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((cache4_attn<T, D, false>), grid, dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache4_append(const AppendArgs& a, bool f16, int head_dim, hipStream_t s) {
+  if (head_dim == 128) return f16 ? append<F16, 128>(a, s) : append<Bf16, 128>(a, s);
+  return f16 ? append<F16, 64>(a, s) : append<Bf16, 64>(a, s);
+}
+
+hipError_t launch_cache4_read(const ReadArgs& a, bool f16, int head_dim, hipStream_t s) {
+  if (head_dim == 128) return f16 ? read<F16, 128>(a, s) : read<Bf16, 128>(a, s);
+  return f16 ? read<F16, 64>(a, s) : read<Bf16, 64>(a, s);
+}
+
+hipError_t launch_cache4_attn(const CacheAttnArgs& a, bool f16, int head_dim, hipStream_t s) {
+  hipError_t e = head_dim == 128 ? (f16 ? attend<F16, 128>(a, s) : attend<Bf16, 128>(a, s))
+                                 : (f16 ? attend<F16, 64>(a, s) : attend<Bf16, 64>(a, s));
+  return e != hipSuccess ? e : launch_cache_merge(a, f16, head_dim, s);
+}
+
+}  // namespace csg

@@ -5,27 +5,13 @@
 // other. A call's new tokens q_ptr[b] .. q_ptr[b+1] - 1 are the last of sequence b.
 #include <hip/hip_runtime.h>
 
-#include "attn_tile.hpp"
 #include "cache_attn.hpp"
+#include "cache_plan.hpp"
 
 namespace csg {
 namespace {
 
-using namespace tile;
-
-constexpr int kThreads = 256;
-
-__device__ __forceinline__ void tell(const CacheArgs& c, int bit) {
-  if (c.status) atomicOr(c.status, bit);
-}
-
-// Tokens of sequence b in the cache, as far as its row of the page table goes.
-__device__ __forceinline__ int length_of(const CacheArgs& c, int b) {
-  const int64_t room = static_cast<int64_t>(c.max_pages) << c.page_shift;
-  const int n = c.lens[b];
-  return n < 0 ? 0 : n > room ? static_cast<int>(room) : n;
-}
-__device__ __forceinline__ int first_token(const CacheArgs& c, int b) { return clamped(c.q_ptr[b], 0, c.tokens); }
+using namespace cache;
 
 // ---- new tokens into the cache --------------------------------------------------------------
 // A workgroup per token. Pair i of a head (elements i and half + i, or 2 i and 2 i + 1) turns by
@@ -138,155 +124,6 @@ __global__ __launch_bounds__(kThreads) void cache_append(AppendArgs a) {
 // (bounds, page numbers, keys, products, partial results), 9 us for 900 keys; where 16
 // sequences' rows share 8192 keys by what a part costs besides its keys and by 16 MB of partial
 // results (36 us and 8; the keys alone would take 27).
-struct Entry {
-  int token0, rows;    // first token, (token, head) rows
-  int b0, b1;          // its sequences; the first one's pages are read
-  int lo, end;         // keys
-  int own;             // the keys of one sequence, up to its end
-  int group;           // its group, -1: none
-  int block0, blocks;  // blocks of keys that hold them
-  __device__ __forceinline__ int tiles() const { return (rows + kCacheTileRows - 1) / kCacheTileRows; }
-  __device__ __forceinline__ bool wide() const { return rows > kCacheTileRows; }
-  __device__ __forceinline__ int tasks() const { return wide() ? (rows + kCacheWideRows - 1) / kCacheWideRows : 1; }
-  // a task's units of work: its blocks, behind what beginning and ending it costs
-  __device__ __forceinline__ int span() const { return blocks > 0 ? kCacheTaskCost + blocks : 0; }
-};
-
-// The groups of a call where they are given.
-struct GlobalGroups {
-  const CacheAttnArgs& a;
-  __device__ __forceinline__ int first(int g) const { return clamped(a.group_ptr[g], 0, a.c.batch); }
-  __device__ __forceinline__ int prefix(int g) const {  // no longer than the first sequence
-    const int b = first(g);
-    return b < a.c.batch ? clamped(a.prefix[g], 0, length_of(a.c, b)) : 0;
-  }
-};
-// The same, copied into LDS.
-struct LocalGroups {
-  const int32_t* firsts;
-  const int32_t* prefixes;
-  __device__ __forceinline__ int first(int g) const { return firsts[g]; }
-  __device__ __forceinline__ int prefix(int g) const { return prefixes[g]; }
-};
-
-// The group of sequence b, -1 if it has none.
-template <class Groups>
-__device__ __forceinline__ int group_of(const CacheAttnArgs& a, const Groups& groups, int b) {
-  if (a.n_groups == 0 || b < groups.first(0) || b >= groups.first(a.n_groups)) return -1;
-  int lo = 0, n = a.n_groups;
-  while (n > 1) {
-    const int half = n / 2;
-    if (groups.first(lo + half) <= b) {
-      lo += half;
-      n -= half;
-    } else {
-      n = half;
-    }
-  }
-  return lo;
-}
-
-template <class Groups>
-__device__ __forceinline__ Entry entry_of(const CacheAttnArgs& a, const Groups& groups, int e) {
-  const CacheArgs& c = a.c;
-  Entry x;
-  x.group = -1;
-  if (e < a.n_groups) {
-    x.own = 0;
-    x.b0 = groups.first(e);
-    x.b1 = max(x.b0, groups.first(e + 1));
-    x.lo = 0;
-    x.end = x.b1 > x.b0 ? groups.prefix(e) : 0;
-  } else {
-    x.own = 1;
-    x.b0 = e - a.n_groups;
-    x.b1 = x.b0 + 1;
-    x.end = length_of(c, x.b0);
-    x.group = group_of(a, groups, x.b0);
-    x.lo = x.group < 0 ? 0 : min(groups.prefix(x.group), x.end);
-  }
-  x.token0 = first_token(c, x.b0);
-  x.rows = x.b1 > x.b0 ? max(0, first_token(c, x.b1) - x.token0) * (c.H / c.Hkv) : 0;
-  x.block0 = x.lo / kCacheBlock;
-  x.blocks = x.end > x.lo && x.rows > 0 ? (x.end + kCacheBlock - 1) / kCacheBlock - x.block0 : 0;
-  return x;
-}
-
-// The plan of a call in the workspace, for cache_merge: an entry's units and tiles before it,
-// its own blocks, rows and first token; of a sequence, its group's entry too (-1: none).
-struct PlanEntry {
-  int32_t before, tiles, blocks, rows, token0, group, unused[2];
-};
-struct Plan {
-  int32_t run;    // units of a run
-  int32_t tiles;  // tiles of one key/value head
-  int32_t unused[6];
-};
-__device__ __forceinline__ Plan* plan_in(unsigned char* ws) { return reinterpret_cast<Plan*>(ws); }
-__device__ __forceinline__ PlanEntry* entries_in(unsigned char* ws) { return reinterpret_cast<PlanEntry*>(ws + sizeof(Plan)); }
-static_assert(sizeof(Plan) + kMaxCacheEntries * sizeof(PlanEntry) <= cache_plan_bytes(), "the plan fits");
-
-// A workgroup's part of a task, and this lane's row of it.
-struct Part {
-  int kvh, tile;       // key/value head; the wave's tile of 32 rows in the entry
-  int key0, end;       // keys of the part (those below the entry's lo are masked)
-  int lo;
-  const int32_t* table;
-  bool ok;             // the lane has a row
-  int token, h, pos;   // its token, head, position
-  int hi;              // it sees keys below this (lanes without a row, whose queries are 0: all)
-  int all_hi;          // every row of the wave sees keys below this
-};
-
-// `local`: the sequences' entries, where they are in LDS.
-__device__ __forceinline__ void locate_row(const CacheAttnArgs& a, const Entry& x, const Entry* local, int l32, Part& p) {
-  const CacheArgs& c = a.c;
-  const int G = c.H / c.Hkv;
-  const int r = p.tile * kCacheTileRows + l32;
-  p.ok = r < x.rows;
-  p.token = x.token0 + (p.ok ? r / G : 0);
-  p.h = p.kvh * G + (p.ok ? r % G : 0);
-  if (x.own) {
-    p.pos = x.end - (x.token0 + x.rows / G - p.token);
-  } else {
-    int b = x.b0;
-    for (int n = x.b1 - x.b0; n > 1;) {  // the last of the group's sequences that starts by then
-      const int half = n / 2;
-      const bool up = (local ? local[b + half].token0 : first_token(c, b + half)) <= p.token;
-      b = up ? b + half : b;
-      n = up ? n - half : half;
-    }
-    if (local)
-      p.pos = local[b].end - (local[b].token0 + local[b].rows / G - p.token);
-    else
-      p.pos = length_of(c, b) - (first_token(c, b + 1) - p.token);
-  }
-  p.hi = p.ok ? min(p.pos + 1, p.end) : p.end;
-  int all_hi = p.hi;
-#pragma unroll
-  for (int d = 1; d < 32; d *= 2) all_hi = min(all_hi, __shfl_xor(all_hi, d));
-  p.all_hi = __builtin_amdgcn_readfirstlane(all_hi);
-}
-
-template <class T, int D>
-__device__ __forceinline__ void load_queries(const CacheAttnArgs& a, const Part& p, int hlf, typename T::x8 (&qf)[D / 16]) {
-  const uint16_t* q = a.c.Q + p.token * a.c.q_stride + p.h * D + 8 * hlf;
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    const u32x4_t raw = p.ok ? *reinterpret_cast<const u32x4_t*>(q + 16 * s) : u32x4_t{0u, 0u, 0u, 0u};
-    qf[s] = __builtin_bit_cast(typename T::x8, raw);
-  }
-}
-
-// The page of keys key .. key + 15, -1 if it has none to read.
-__device__ __forceinline__ int page_of(const CacheArgs& c, const Part& p, int key) {
-  if (key >= p.end || key + 16 <= p.lo) return -1;
-  const int page = p.table[key >> c.page_shift];
-  if (page >= 0 && page < c.n_pages) return page;
-  tell(c, kCacheBadPage);
-  return -1;
-}
-
 // Keys (or values) key .. key + 15, which lie in one page, into LDS; what is behind the part's
 // end or before its entry's keys (a sequence need not have its group's tokens in pages of its
 // own) reads zero.
@@ -307,24 +144,6 @@ __device__ __forceinline__ void load_16(const CacheArgs& c, const uint16_t* page
   }
 #pragma unroll
   for (int i = 0; i < 16 / kLoadRows<D>; ++i) load_to_lds(rs, lds + 1024u * i, ll.offset(i, 2 * D));
-}
-
-// Scores of a block of 32 N keys from its products: cap, bias, mask.
-template <int N, bool kPlain>
-__device__ __forceinline__ void finish_scores(const CacheAttnArgs& a, const Part& p, float slope, int key0, int hlf, f32x16_t (&sc)[N]) {
-  if constexpr (!kPlain) {
-    cap_scores<N>(a.scoring, sc);
-    bias_scores<N, -1>(a.scoring, slope, p.pos - key0, hlf, sc);
-  }
-  if (key0 + 32 * N > p.all_hi || key0 < p.lo) {
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = key0 + 32 * n + result_row(i, hlf);
-        if (key >= p.hi || key < p.lo) sc[n][i] = -__builtin_inff();
-      }
-  }
 }
 
 // A narrow part: each wave takes every fourth block, through 16 KiB (D = 128) of LDS of its own:
@@ -523,147 +342,18 @@ template <class T, int D, bool kPlain>
 __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char stage[4 * 2 * kCacheBlock * 2 * D];
   __shared__ float s_ref[4][32], s_sum[4][32];
-  __shared__ uint32_t s_wave_units[4], s_wave_tiles[4];
-  __shared__ int s_entry, s_first, s_tiles;
-  __shared__ Entry s_entries[kThreads];
   static_assert(sizeof(stage) == 2 * 2 * kCacheWideBlock * 2 * D, "the same memory holds the wide parts' buffers");
   static_assert(sizeof(stage) >= 4 * 32 * D * 4, "and the waves' results");
-  static_assert(sizeof(stage) >= (2 * kMaxCacheEntries + 1) * 4, "and, before, the groups");
-
-  const CacheArgs& c = a.c;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n_entries = a.n_groups + c.batch;
-  // a die runs every 8th workgroup: with the head fastest, it has few heads, and runs that follow
-  // each other, whose tasks may read the same keys
-  const int kvh = blockIdx.x % c.Hkv;
-  int w = blockIdx.x / c.Hkv;
-  if (a.head_workers % a.dies == 0) w = w % a.dies * (a.head_workers / a.dies) + w / a.dies;
-
-  int32_t* firsts = reinterpret_cast<int32_t*>(stage);
-  const LocalGroups local{firsts, firsts + a.n_groups + 1};
-  if (a.n_groups > 0) {
-    const GlobalGroups global{a};
-    for (int g = tid; g <= a.n_groups; g += kThreads) {
-      firsts[g] = global.first(g);
-      if (g < a.n_groups) firsts[a.n_groups + 1 + g] = global.prefix(g);
-    }
-    __syncthreads();
-  }
-  // Each thread counts some entries; units and tiles before each of them by a scan. Where a thread
-  // has one entry, everyone finds it in LDS.
-  const int per = (n_entries + kThreads - 1) / kThreads;
-  uint32_t units = 0, tiles = 0;
-  for (int i = 0; i < per; ++i) {
-    const int e = tid * per + i;
-    if (e >= n_entries) break;
-    const Entry x = entry_of(a, local, e);
-    if (per == 1) s_entries[e] = x;
-    units += x.tasks() * x.span();
-    tiles += x.tiles();
-  }
-  const uint32_t own_units = units, own_tiles = tiles;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const uint32_t uu = __shfl_up(units, d), ut = __shfl_up(tiles, d);
-    if (lane >= d) {
-      units += uu;
-      tiles += ut;
-    }
-  }
-  if (lane == 63) {
-    s_wave_units[wave] = units;
-    s_wave_tiles[wave] = tiles;
-  }
-  __syncthreads();
-  units -= own_units;
-  tiles -= own_tiles;
-  for (int i = 0; i < wave; ++i) {
-    units += s_wave_units[i];
-    tiles += s_wave_tiles[i];
-  }
-  const int all_tiles = __builtin_amdgcn_readfirstlane(s_wave_tiles[0] + s_wave_tiles[1] + s_wave_tiles[2] + s_wave_tiles[3]);
-  // Bounds that do not ascend may name rows several times, and with them more units than 32 bits count: then
-  // there is nothing to do. (As many tiles as the host has reckoned with have no more units than it has.)
-  const bool fits = static_cast<uint32_t>(all_tiles) <= a.max_tiles;
-  const int all = fits ? __builtin_amdgcn_readfirstlane(s_wave_units[0] + s_wave_units[1] + s_wave_units[2] + s_wave_units[3]) : 0;
-  const int run = max(kCacheMinRun, (all + a.head_workers - 1) / a.head_workers);
-  const int begin = w * run;
-  // for cache_merge, and the entry where the run begins
-  if (blockIdx.x == 0 || (static_cast<int>(units) <= begin && begin < static_cast<int>(units + own_units))) {
-    int before = units, tiles_before = tiles;
-    for (int i = 0; i < per; ++i) {
-      const int e = tid * per + i;
-      if (e >= n_entries) break;
-      const Entry x = per == 1 ? s_entries[e] : entry_of(a, local, e);
-      const int n = x.tasks() * x.span();
-      if (before <= begin && begin < before + n) {
-        s_entry = e;
-        s_first = begin - before;
-        s_tiles = tiles_before;
-      }
-      if (blockIdx.x == 0) {
-        entries_in(a.ws)[e] = {before, tiles_before, fits ? x.blocks : 0, x.rows, x.token0, x.group, {0, 0}};
-        if (x.own && (x.end != c.lens[x.b0] || x.rows / (c.H / c.Hkv) > x.end)) tell(c, kCacheBadLength);
-      }
-      before += n;
-      tiles_before += x.tiles();
-    }
-    if (blockIdx.x == 0 && tid == 0) {
-      *plan_in(a.ws) = {run, all_tiles, {0, 0, 0, 0, 0, 0}};
-      if (!fits) tell(c, kCacheBadLength);
-    }
-  }
-  if (begin >= all) return;
-  __syncthreads();
-  int left = min(run, all - begin);
-  int e = __builtin_amdgcn_readfirstlane(s_entry), in_entry = __builtin_amdgcn_readfirstlane(s_first);
-  int tiles_before = __builtin_amdgcn_readfirstlane(s_tiles);
-  const int64_t places = static_cast<int64_t>(kvh) * (all_tiles + 4 * a.head_workers) + 4 * w;
-  const Entry* sequences = per == 1 ? s_entries + a.n_groups : nullptr;
-  while (left > 0) {
-    Entry x;
-    if (per == 1) {
-      // (the same in every lane)
-      x.token0 = __builtin_amdgcn_readfirstlane(s_entries[e].token0);
-      x.rows = __builtin_amdgcn_readfirstlane(s_entries[e].rows);
-      x.b0 = __builtin_amdgcn_readfirstlane(s_entries[e].b0);
-      x.b1 = __builtin_amdgcn_readfirstlane(s_entries[e].b1);
-      x.lo = __builtin_amdgcn_readfirstlane(s_entries[e].lo);
-      x.end = __builtin_amdgcn_readfirstlane(s_entries[e].end);
-      x.own = __builtin_amdgcn_readfirstlane(s_entries[e].own);
-      x.block0 = __builtin_amdgcn_readfirstlane(s_entries[e].block0);
-      x.blocks = __builtin_amdgcn_readfirstlane(s_entries[e].blocks);
-    } else {
-      x = entry_of(a, GlobalGroups{a}, e);
-    }
-    const int n = x.tasks() * x.span();
-    if (in_entry < n) {
-      Part p;
-      p.kvh = kvh;
-      const bool wide = x.wide();
-      const int task = wide ? __builtin_amdgcn_readfirstlane(in_entry / x.span()) : 0;
-      const int from = in_entry - task * x.span(), take = min(x.span() - from, left);
-      const int first = max(0, from - kCacheTaskCost), count = from + take - kCacheTaskCost - first;
-      left -= take;
-      in_entry += take;
-      if (count <= 0) continue;
-      p.table = c.table + static_cast<int64_t>(x.b0) * c.max_pages;
-      p.lo = x.lo;
-      p.key0 = (x.block0 + first) * kCacheBlock;
-      p.end = min(x.end, p.key0 + count * kCacheBlock);
-      p.tile = wide ? 4 * task + wave : 0;
-      const int64_t place = places + tiles_before + p.tile;
-      float* out = place < a.max_parts ? reinterpret_cast<float*>(a.ws + cache_plan_bytes() + place * cache_part_bytes(D)) : nullptr;
-      if (wide)
-        wide_part<T, D, kPlain>(a, x, sequences, p, stage, out, lane, wave);
-      else
-        narrow_part<T, D, kPlain>(a, x, sequences, p, stage, s_ref, s_sum, out, lane, wave);
-    } else {
-      in_entry = 0;
-      tiles_before += x.tiles();
-      ++e;
-    }
-  }
+  static_assert(sizeof(stage) >= kCacheGroupBytes, "and, before, the groups");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  cache_run<D>(
+      a, stage,
+      [&](const Entry& x, const Entry* local, Part& p, float* out) {
+        narrow_part<T, D, kPlain>(a, x, local, p, stage, s_ref, s_sum, out, lane, wave);
+      },
+      [&](const Entry& x, const Entry* local, Part& p, float* out) {
+        wide_part<T, D, kPlain>(a, x, local, p, stage, out, lane, wave);
+      });
 }
 
 // One wave joins the parts of one row, as sum_w f_w acc_w / sum_w f_w l_w with f_w = e^(m_w - max m). A
@@ -757,14 +447,18 @@ hipError_t append(const AppendArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <class T, int D>
+hipError_t merge(const CacheAttnArgs& a, hipStream_t s) {
+  const int64_t rows = static_cast<int64_t>(a.c.tokens) * a.c.H;
+  hipLaunchKernelGGL((cache_merge<T, D>), dim3((rows + 3) / 4), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
 template <class T, int D, bool kPlain>
 hipError_t attend(const CacheAttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((cache_attn<T, D, kPlain>), dim3(a.head_workers * a.c.Hkv), dim3(kThreads), 0, s, a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int64_t rows = static_cast<int64_t>(a.c.tokens) * a.c.H;
-  hipLaunchKernelGGL((cache_merge<T, D>), dim3((rows + 3) / 4), dim3(kThreads), 0, s, a);
-  return hipGetLastError();
+  return e != hipSuccess ? e : merge<T, D>(a, s);
 }
 
 template <class T, int D>
@@ -782,6 +476,11 @@ hipError_t launch_cache_append(const AppendArgs& a, bool f16, int head_dim, hipS
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool f16, int head_dim, hipStream_t s) {
   if (head_dim == 128) return f16 ? attend<F16, 128>(a, s) : attend<Bf16, 128>(a, s);
   return f16 ? attend<F16, 64>(a, s) : attend<Bf16, 64>(a, s);
+}
+
+hipError_t launch_cache_merge(const CacheAttnArgs& a, bool f16, int head_dim, hipStream_t s) {
+  if (head_dim == 128) return f16 ? merge<F16, 128>(a, s) : merge<Bf16, 128>(a, s);
+  return f16 ? merge<F16, 64>(a, s) : merge<Bf16, 64>(a, s);
 }
 
 }  // namespace csg

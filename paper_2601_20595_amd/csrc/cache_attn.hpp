@@ -19,6 +19,7 @@ constexpr int kCacheWideBlock = 64;    // keys per inner step of a wide task
 constexpr int kCacheTaskCost = 4;
 constexpr int kCacheMinRun = 4;  // units a workgroup takes at least: a block for each wave
 constexpr int kMaxCacheEntries = 2048; // sequences and groups of one call
+constexpr int kCacheGroupBytes = (2 * kMaxCacheEntries + 1) * 4;  // LDS that holds a call's groups
 
 // status bits
 constexpr int kCacheBadPage = 1, kCacheBadLength = 2;
@@ -80,5 +81,7 @@ inline int64_t cache_max_parts(int32_t H, int32_t Hkv, int64_t tokens, int32_t b
 
 hipError_t launch_cache_append(const AppendArgs& a, bool f16, int head_dim, hipStream_t stream);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool f16, int head_dim, hipStream_t stream);
+// The join of the parts alone.
+hipError_t launch_cache_merge(const CacheAttnArgs& a, bool f16, int head_dim, hipStream_t stream);
 
 }  // namespace csg

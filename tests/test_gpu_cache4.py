@@ -1,0 +1,436 @@
+"""The cache in 4 bits on the GPU: append and read bit for bit, attention element by element against
+the fp64 oracle, and a run of them with attention over documents."""
+import numpy as np
+import pytest
+
+import paper_2601_20595_amd as csg
+from oracle import cache4
+from oracle import doc_attention as oda
+
+torch = pytest.importorskip("torch")
+if torch.cuda.is_available():
+    from attn_util import DEV, HALF_STEP, TINY, TORCH, close, f64, ints, normal, pointers
+    from cache4_util import pages4, values4
+    from test_gpu_cache import APPEND, ATTN, _table
+
+pytestmark = pytest.mark.gpu
+BITS = {"bf16": 0x7F80, "f16": 0x7C00}  # infinity
+
+
+def _same(got, want, what):
+    """Bit for bit, apart from the sign of a zero; NaN where NaN is wanted."""
+    got = f64(got) if torch.is_tensor(got) else got
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    at = ~np.isnan(want)
+    assert np.array_equal(got[at], want[at]), what
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_every_code_and_scale_is_read(dtype, D):
+    lo, hi = cache4.LIMITS[dtype]
+    scales = np.array(list(range(lo, hi + 1)) + [255])
+    n, Hkv, page = len(scales), 2, 16
+    pages = -(-n // page)
+    codes = np.zeros((pages, Hkv, page, D), dtype=np.uint8)
+    codes[:] = np.arange(D) % 16
+    codes[:, 1] = (np.arange(D) * 7 + 3) % 16
+    by = np.full((pages, Hkv, page, D // 32), 127, dtype=np.uint8)
+    for i, x in enumerate(scales):
+        by[i // page, :, i % page] = x
+        by[i // page, 1, i % page, 0] = scales[(i * 5) % n]
+    kp = torch.tensor(cache4.pack(codes, by), device=DEV)
+    vp = torch.tensor(cache4.pack(codes[::-1], by[::-1]), device=DEV)
+    c = csg.PagedCache4(2, Hkv, D, dtype, pages, page, 1, pages)
+    k, v = (torch.full((n, Hkv, D), 5.0, dtype=TORCH[dtype], device=DEV) for _ in range(2))
+    c.read(kp, vp, ints([0, n]), ints([n]), ints([range(pages)]), k, v)
+    torch.cuda.synchronize()
+    want = cache4.values(codes, by)
+    _same(k, oda.cached_rows(want, range(pages), n), "keys")
+    _same(v, oda.cached_rows(want[::-1], range(pages), n), "values")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_every_value_is_quantised(dtype, D):
+    """All patterns of the type, with neighbours of all sizes, and next to ones that are not finite."""
+    rng = np.random.default_rng(D)
+    x = np.arange(65536, dtype=np.uint16)
+    finite = x[(x & 0x7FFF) < BITS[dtype]]
+    near = np.concatenate([np.sort(finite).reshape(-1, 32)[rng.permutation(len(finite) // 32)].reshape(-1) for _ in range(1)])
+    mixed = rng.permutation(finite)
+    # ties: multiples of a quarter of a scale beside 7 or 4 of it, which set the scale
+    top = torch.tensor([7.0, -4.0]).to(TORCH[dtype]).view(torch.int16).numpy().view(np.uint16)
+    ties = torch.arange(-28, 28).div(4.0).to(TORCH[dtype]).view(torch.int16).numpy().view(np.uint16)
+    blocks = [np.concatenate([[t], rng.choice(ties, 31)]) for t in top for _ in range(64)]
+    bad = rng.permutation(x)[:4096 - 128 * 0]
+    row = np.concatenate([near, mixed, np.concatenate(blocks), bad])
+    row = row[:len(row) // (2 * D) * (2 * D)].reshape(-1, 2, D)
+    n, page = len(row), 64
+    width = -(-n // page)
+    v = torch.tensor(row.view(np.int16)).view(TORCH[dtype])
+    k = v.flip(0).contiguous()
+    c = csg.PagedCache4(2, 2, D, dtype, width, page, 1, width)
+    kp, vp = (torch.zeros((width, 2, page * (D // 2 + D // 32)), dtype=torch.uint8, device=DEV) for _ in range(2))
+    c.append(kp, vp, k.to(DEV), v.to(DEV), ints([0, n]), ints([n]), ints([range(width)]))
+    torch.cuda.synchronize()
+    for got, x in ((kp, k), (vp, v)):
+        codes, scales = cache4.quantise(x.double().numpy(), dtype)
+        _same(oda.cached_rows(values4(got, page, D), range(width), n), cache4.values(codes, scales), "values")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("name", APPEND)
+def test_append_and_read(name, dtype):
+    new, lens, H, Hkv, D, page, rot, pairs = APPEND[name]
+    rng = np.random.default_rng(3)
+    n, tail = sum(new), 3
+    if name == "far positions":  # only the last pages exist
+        width = max(-(-x // page) for x in lens)
+        table, pages = np.full((len(lens), width), -1, dtype=np.int32), 4
+        for b, x in enumerate(lens):
+            table[b, (x - 1) // page], table[b, (x - 2) // page] = 2 * b, 2 * b + (((x - 1) // page) != ((x - 2) // page))
+    else:
+        table, pages = _table(rng, lens, page)
+    k, k64 = normal(1, (n + tail, Hkv, D), dtype)
+    v, v64 = normal(2, (n + tail, Hkv, D), dtype)
+    q, q64 = normal(3, (n + tail, H, D), dtype)
+    kp, kp64 = pages4(4, pages, Hkv, page, D, dtype)
+    vp, vp64 = pages4(5, pages, Hkv, page, D, dtype)
+    freq = 10000.0 ** (-np.arange(0, rot, 2) / max(rot, 1))
+    pos = np.concatenate([np.arange(x - a, x) for a, x in zip(new, lens)]) if n else np.zeros(0, dtype=int)
+    seq = np.repeat(np.arange(len(new)), new)
+    # keys: rotated in fp64, rounded to fp32 and the type, then to 4 bits
+    kr = torch.tensor(oda.rotate(k64[:n], pos, freq, pairs)).float().to(TORCH[dtype]).double().numpy()
+    at = (table[seq, pos // page], slice(None), pos % page)
+    kp64[at], vp64[at] = (cache4.values(*cache4.quantise(x, dtype)) for x in (kr, v64[:n]))
+    qr = oda.rotate(q64[:n], pos, freq, pairs)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    dk, dv = kp.to(DEV), vp.to(DEV)
+    out = torch.full((n + tail, H, D), 17.0, dtype=TORCH[dtype], device=DEV)
+    c = csg.PagedCache4(H, Hkv, D, dtype, pages, page, len(new), table.shape[1])
+    inv = torch.tensor(freq, device=DEV) if rot else None
+    x = torch.cat([q, k, v], dim=1).to(DEV)  # the projection's output
+    ptr, ln, tab = ints(pointers(new)), ints(lens), torch.tensor(table, device=DEV)
+    torch.cuda.synchronize()
+    c.append(dk, dv, x[:, H:H + Hkv], x[:, H + Hkv:], ptr, ln, tab, inv_freq=inv, interleaved=pairs, q=x[:, :H], q_out=out, status=st)
+    # read back into parts of a wider tensor
+    back = torch.full((n + tail, 2 * Hkv + 1, D), 9.0, dtype=TORCH[dtype], device=DEV)
+    c.read(dk, dv, ptr, ln, tab, back[:, :Hkv], back[:, Hkv:2 * Hkv], status=st)
+    torch.cuda.synchronize()
+    assert int(st) == 0
+    _same(values4(dk, page, D), kp64, "keys")
+    _same(values4(dv, page, D), vp64, "values")
+    _same(back[:n, :Hkv], kp64[at], "keys read")
+    _same(back[:n, Hkv:2 * Hkv], vp64[at], "values read")
+    assert bool((back[n:] == 9.0).all()) and bool((back[:, 2 * Hkv:] == 9.0).all())
+    # a rounding of the result, and four of fp32 on the way: sine, cosine, product, sum
+    size = np.abs(q64[:n]).max(axis=-1, keepdims=True)
+    close(out[:n], qr, (HALF_STEP[dtype] * np.abs(qr) + 2.0 ** -21 * size + TINY[dtype]) if rot else np.zeros_like(qr), "queries")
+    assert bool((out[n:] == 17.0).all())
+
+
+def test_bad_pages_and_other_rows_are_left():
+    H, Hkv, D, page = 4, 2, 64, 16
+    new, lens = [1, 1, 1, 2], [3, 20, 100, 1]
+    table = np.array([[0, -1], [1, 99], [2, 3], [4, 5]], dtype=np.int32)
+    k, k64 = normal(1, (7, Hkv, D), "bf16")
+    v, v64 = normal(2, (7, Hkv, D), "bf16")
+    kp, vp = (torch.full((6, Hkv, page * 34), 0x5A, dtype=torch.uint8, device=DEV) for _ in range(2))
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    c = csg.PagedCache4(H, Hkv, D, "bf16", 6, page, 4, 2)
+    ptr = ints(np.array(pointers(new)) + 1)  # rows before the first sequence and behind the last
+    kd, vd, ln, tab = k.to(DEV), v.to(DEV), ints(lens), torch.tensor(table, device=DEV)
+    c.append(kp, vp, kd, vd, ptr, ln, tab, status=st)
+    torch.cuda.synchronize()
+    # written: sequence 0's token at 2, sequence 3's at 0; page 99, position 99 of 32 and position -1 are not
+    assert int(st) == 3
+    for got, x in ((kp, k64), (vp, v64)):
+        codes, scales = (y.copy() for y in cache4.unpack(np.full((6, Hkv, page * 34), 0x5A, dtype=np.uint8), page, D))
+        qc, qs = cache4.quantise(x, "bf16")
+        for p, r, t in ((0, 2, 1), (4, 0, 5)):
+            codes[p, :, r], scales[p, :, r] = qc[t], qs[t]
+        _same(values4(got, page, D), cache4.values(codes, scales), "pages")
+    st.zero_()
+    ko, vo = (torch.full((7, Hkv, D), 3.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    c.read(kp, vp, ptr, ln, tab, ko, vo, status=st)
+    torch.cuda.synchronize()
+    assert int(st) == 3
+    for got, x in ((ko, k64), (vo, v64)):
+        want = np.zeros((7, Hkv, D))
+        held = cache4.values(*cache4.quantise(x, "bf16"))
+        want[[1, 5]] = held[[1, 5]]
+        want[[0, 6]] = 3.0
+        _same(got, want, "rows")
+
+
+def _attn_case(name, dtype, sharp=1.0, stream=None):
+    new, lens, H, Hkv, D, page, groups, cap, bias = ATTN[name]
+    rng = np.random.default_rng(7)
+    n, tail = sum(new), 2
+    table, pages = _table(rng, lens, page, shared=groups)
+    q, q64 = normal(1, (n + tail, H, D), dtype, sharp)
+    used = np.zeros((pages, page), dtype=bool)
+    for b, x in enumerate(lens):
+        i = np.arange(x)
+        used[table[b][i // page], i % page] = True
+    kp, kp64 = pages4(2, pages, Hkv, page, D, dtype, ~used)
+    vp, vp64 = pages4(3, pages, Hkv, page, D, dtype, ~used)
+    slopes = (2.0 ** -np.arange(1, H + 1)).astype(np.float32) if bias else None
+    sc = oda.Scores(None, cap, slopes, True)
+    ptr = pointers(new)
+    want = [np.zeros((n, H, D)), np.zeros((H, n)), np.zeros((n, H, D)), np.zeros((H, n))]
+    for b, x in enumerate(lens):
+        r = slice(ptr[b], ptr[b + 1])
+        got = oda.attention(q64[r], oda.cached_rows(kp64, table[b], x), oda.cached_rows(vp64, table[b], x), sc, 0,
+                            HALF_STEP[dtype], TINY[dtype])
+        want[0][r], want[1][:, r], want[2][r], want[3][:, r] = got
+    c = csg.PagedCache4(H, Hkv, D, dtype, pages, page, len(new), table.shape[1])
+    o = torch.full((n + tail, H, D), 17.0, dtype=TORCH[dtype], device=DEV)
+    lse = torch.full((H, n + tail), 17.0, device=DEV)
+    ws = torch.full((c.workspace_bytes(n + tail, len(groups)),), 255, dtype=torch.uint8, device=DEV)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    args = {"status": st, "softcap": cap, "stream": stream}
+    if groups:
+        args["group_ptr"] = ints([g[0] for g in groups] + [groups[-1][1]])
+        args["prefix"] = ints([g[2] for g in groups])
+    if bias:
+        args["slopes"] = torch.tensor(slopes, device=DEV)
+    dev = [q.to(DEV), kp.to(DEV), vp.to(DEV), ints(ptr), ints(lens), torch.tensor(table, device=DEV)]
+    torch.cuda.synchronize()
+    c.attn(*dev, o, lse, ws, **args)
+    torch.cuda.synchronize()
+    assert int(st) == 0
+    close(o[:n], want[0], want[2], "o")
+    close(lse[:, :n], want[1], want[3], "lse")
+    assert bool((o[n:] == 17.0).all()) and bool((lse[:, n:] == 17.0).all())
+    return o, lse
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("name", ATTN)
+def test_attention(name, dtype):
+    _attn_case(name, dtype)
+
+
+def test_sharp_scores_other_stream_same_bits():
+    st = torch.cuda.Stream(device=DEV)
+    one = _attn_case("groups between others", "f16", 5.0, st)
+    two = _attn_case("groups between others", "f16", 5.0)
+    assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("D,shared", [(64, 23), (128, 48), (128, 87)])
+def test_a_groups_tokens_are_read_from_its_first_sequence(D, shared, new):
+    """The others have no pages for them, and NaN where such a token would share a page with later ones."""
+    H, Hkv, page, lens = 8, 2, 16, [200, 130, 150]
+    rng = np.random.default_rng(5)
+    table, pages = _table(rng, lens, page)
+    sets = []
+    for seed in (1, 2):
+        codes, scales = cache4.quantise(normal(seed, (pages, Hkv, page, D), "bf16")[1], "bf16")
+        for b in (1, 2):
+            x = np.arange(shared)
+            for t in (codes, scales):
+                t[table[b][x // page], :, x % page] = t[table[0][x // page], :, x % page]
+        sets.append((codes, scales))
+    q = normal(3, (3 * new, H, D), "bf16")[0].to(DEV)
+    c = csg.PagedCache4(H, Hkv, D, "bf16", pages, page, 3, table.shape[1])
+    ws = torch.zeros(c.workspace_bytes(3 * new, 1), dtype=torch.uint8, device=DEV)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out = []
+    for gone in (False, True):
+        if gone:
+            for b in (1, 2):
+                x = np.arange(shared)
+                for _, scales in sets:
+                    scales[table[b][x // page], :, x % page] = cache4.NAN
+                table[b, :shared // page] = -1
+        kp, vp = (torch.tensor(cache4.pack(*s), device=DEV) for s in sets)
+        o, lse = torch.zeros_like(q), torch.zeros((H, 3 * new), device=DEV)
+        c.attn(q, kp, vp, ints(pointers([new] * 3)), ints(lens), torch.tensor(table, device=DEV), o, lse, ws,
+               group_ptr=ints([0, 3]), prefix=ints([shared]), status=st)
+        torch.cuda.synchronize()
+        out.append((o, lse))
+    assert int(st) == 0 and bool(torch.isfinite(out[0][0].float()).all())
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+
+
+@pytest.mark.parametrize("new", [1, 20, 40])
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("f16", 128)])
+def test_long_runs(dtype, D, new):
+    """So many keys a workgroup that it asks for pages again, against fp64 on the GPU."""
+    H, page, n = 128, 64, 20000
+    rng = np.random.default_rng(11)
+    table, pages = _table(rng, [n], page)
+    tab = torch.tensor(table, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    codes = [torch.randint(0, 256, (pages, H, page * (D // 2 + D // 32)), generator=g, device=DEV).to(torch.uint8) for _ in range(2)]
+    for p in codes:
+        p[..., page * D // 2:] = 125 + p[..., page * D // 2:] % 3
+    x = torch.randn((new, H + 3, D), generator=g, device=DEV).to(TORCH[dtype])
+    q = x[:, 1:H + 1]  # a part of a wider tensor
+    c = csg.PagedCache4(H, H, D, dtype, pages, page, 1, table.shape[1])
+    o, ws = torch.empty((new, H, D), dtype=TORCH[dtype], device=DEV), torch.empty(c.workspace_bytes(new), dtype=torch.uint8, device=DEV)
+    k, v = (torch.empty((n, H, D), dtype=TORCH[dtype], device=DEV) for _ in range(2))
+    torch.cuda.synchronize()
+    c.attn(q, codes[0], codes[1], ints([0, new]), ints([n]), tab, o, None, ws)  # (no log-sum-exp wanted)
+    c.read(codes[0], codes[1], ints([0, n]), ints([n]), tab, k, v)
+    torch.cuda.synchronize()
+    at = torch.arange(n, device=DEV)
+    u = HALF_STEP[dtype]
+    for h in range(0, H, 9):
+        kh, vh, qh = k[:, h].double(), v[:, h].double(), q[:, h].double()
+        s = (qh @ kh.t()) * D ** -0.5
+        s[at[None] > n - new + torch.arange(new, device=DEV)[:, None]] = float("-inf")
+        p = torch.softmax(s, dim=1)
+        want = p @ vh
+        # the oracle's bounds: a rounding of the output and of every weight, and 2^-17 of the scores' size
+        size = (qh.abs() @ kh.abs().t()) * D ** -0.5 + s.abs().nan_to_num(posinf=0.0) + 1.0
+        bound = u * want.abs() + (p * (2 * 2.0 ** -17 * size + u) + TINY[dtype]) @ vh.abs() + TINY[dtype]
+        assert bool(((o[:, h].double() - want).abs() <= bound).all()), h
+
+
+def test_far_pages():
+    """Pages beyond 2^32 bytes of a cache, bit for bit as near ones."""
+    H, Hkv, D, page, n = 16, 8, 128, 256, 700
+    x = normal(1, (n, H + 2 * Hkv, D), "bf16")[0].to(DEV)
+    out = []
+    for pages in (3, 33000):
+        kp, vp = (torch.empty((pages, Hkv, page * 68), dtype=torch.uint8, device=DEV) for _ in range(2))
+        c = csg.PagedCache4(H, Hkv, D, "bf16", pages, page, 1, 3)
+        tab, ptr, lens = ints([[pages - 1, 0, pages - 2]]), ints([0, n]), ints([n])
+        o, lse = torch.zeros((n, H, D), dtype=torch.bfloat16, device=DEV), torch.zeros((H, n), device=DEV)
+        k, v = (torch.zeros((n, Hkv, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        ws = torch.zeros(c.workspace_bytes(n), dtype=torch.uint8, device=DEV)
+        c.append(kp, vp, x[:, H:H + Hkv], x[:, H + Hkv:], ptr, lens, tab)
+        c.attn(x[:, :H], kp, vp, ptr, lens, tab, o, lse, ws)
+        c.read(kp, vp, ptr, lens, tab, k, v)
+        torch.cuda.synchronize()
+        out.append((o, lse, kp[-1].clone(), vp[-1].clone(), k, v))
+    for one, two in zip(*out):
+        assert torch.equal(one, two)
+
+
+def test_bad_pages_and_lengths_touch_nothing_else():
+    H, Hkv, D, page = 4, 2, 64, 16
+    lens = [40, 40, 1000, -3]
+    table = np.array([[0, 1, 2], [3, -7, 1 << 30], [6, 7, 0], [1, 1, 1]], dtype=np.int32)
+    kp, kp64 = pages4(2, 8, Hkv, page, D, "bf16")
+    vp, vp64 = pages4(3, 8, Hkv, page, D, "bf16")
+    q, q64 = normal(1, (4, H, D), "bf16")
+    c = csg.PagedCache4(H, Hkv, D, "bf16", 8, page, 4, 3)
+    o, lse = torch.zeros((4, H, D), dtype=torch.bfloat16, device=DEV), torch.zeros((H, 4), device=DEV)
+    ws = torch.zeros(c.workspace_bytes(4), dtype=torch.uint8, device=DEV)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    c.attn(q.to(DEV), kp.to(DEV), vp.to(DEV), ints([0, 1, 2, 3, 4]), ints(lens), torch.tensor(table, device=DEV), o, lse, ws, status=st)
+    torch.cuda.synchronize()
+    assert int(st) == 3
+    k0, v0 = (oda.cached_rows(x, table[0], 40) for x in (kp64, vp64))
+    want = oda.attention(q64[:1], k0, v0, oda.Scores(), 0, HALF_STEP["bf16"])
+    close(o[:1], want[0], want[2], "the good sequence")
+    assert bool((o[3] == 0).all()) and bool((lse[:, 3] == float("-inf")).all())
+    with pytest.raises(csg.CsgError):  # a short workspace
+        c.attn(q.to(DEV), kp.to(DEV), vp.to(DEV), ints([0, 1, 2, 3, 4]), ints(lens), torch.tensor(table, device=DEV), o, lse, ws[:100])
+
+
+@pytest.mark.parametrize("new", [1, 12])
+def test_a_nan_stays_with_its_rows(new):
+    """A block of NaN reaches the rows that see its key, and no others."""
+    H, Hkv, D, page, n = 6, 2, 128, 16, 100
+    rng = np.random.default_rng(3)
+    table, pages = _table(rng, [n, n], page)
+    kp, _ = pages4(2, pages, Hkv, page, D, "bf16")
+    vp, _ = pages4(3, pages, Hkv, page, D, "bf16")
+    q = normal(1, (2 * new, H, D), "bf16")[0].to(DEV)
+    c = csg.PagedCache4(H, Hkv, D, "bf16", pages, page, 2, table.shape[1])
+    ws = torch.zeros(c.workspace_bytes(2 * new), dtype=torch.uint8, device=DEV)
+    out = []
+    for bad in (False, True):
+        if bad:  # the key at 7 of sequence 0, head 0
+            kp[table[0, 0], 0, page * D // 2 + 7 * (D // 32)] = 255
+        o = torch.zeros((2 * new, H, D), dtype=torch.bfloat16, device=DEV)
+        c.attn(q, kp.to(DEV), vp.to(DEV), ints([0, new, 2 * new]), ints([n, n]), torch.tensor(table, device=DEV), o, None, ws)
+        torch.cuda.synchronize()
+        out.append(o)
+    assert bool(torch.isnan(out[1][:new, :3]).all())
+    assert torch.equal(out[0][new:], out[1][new:]) and torch.equal(out[0][:, 3:], out[1][:, 3:])
+
+
+def test_captured_and_replayed():
+    """A decode step (append, attention, read) as one graph, replayed as the sequences grow."""
+    H, Hkv, D, page, batch = 8, 2, 128, 16, 5
+    rng = np.random.default_rng(1)
+    table, pages = _table(rng, [200] * batch, page)
+    c = csg.PagedCache4(H, Hkv, D, "bf16", pages, page, batch, table.shape[1])
+    kp, vp = (pages4(s, pages, Hkv, page, D, "bf16")[0].to(DEV) for s in (1, 2))
+    x = torch.zeros((batch, H + 2 * Hkv, D), dtype=torch.bfloat16, device=DEV)
+    qo, o = (torch.zeros((batch, H, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ko, vo = (torch.zeros((batch, Hkv, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    lse = torch.zeros((H, batch), device=DEV)
+    ws = torch.zeros(c.workspace_bytes(batch), dtype=torch.uint8, device=DEV)
+    ptr, lens, tab = ints(range(batch + 1)), ints([1] * batch), torch.tensor(table, device=DEV)
+    inv = torch.tensor(10000.0 ** (-np.arange(0, D, 2) / D), device=DEV)
+
+    def step(stream):
+        c.append(kp, vp, x[:, H:H + Hkv], x[:, H + Hkv:], ptr, lens, tab, inv_freq=inv, q=x[:, :H], q_out=qo, stream=stream)
+        c.attn(qo, kp, vp, ptr, lens, tab, o, lse, ws, stream=stream)
+        c.read(kp, vp, ptr, lens, tab, ko, vo, stream=stream)
+
+    st = torch.cuda.Stream(device=DEV)
+    step(st)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=st):
+        step(st)
+    for t, lengths in enumerate(([1, 15, 16, 17, 100], [2, 16, 17, 18, 101], [180, 3, 64, 65, 1])):
+        x.copy_(normal(20 + t, tuple(x.shape), "bf16")[0])
+        lens.copy_(ints(lengths))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        got = [y.clone() for y in (kp, vp, o, lse, ko, vo)]
+        step(None)
+        torch.cuda.synchronize()
+        for one, two in zip(got, (kp, vp, o, lse, ko, vo)):
+            assert torch.equal(one, two)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_prompt_drafts_and_decoding_agree_with_documents(dtype):
+    """A run as a model makes it: prompts into the cache, then tokens and drafts; what the cache
+    holds, read, through attention over documents gives the same."""
+    H, Hkv, D, page = 8, 2, 128, 16
+    total = [90, 45]
+    rng = np.random.default_rng(2)
+    table, pages = _table(rng, total, page)
+    freq = torch.tensor(10000.0 ** (-np.arange(0, D, 2) / D), device=DEV)
+    x = [normal(3 + b, (total[b], H + 2 * Hkv, D), dtype)[0] for b in range(2)]
+    c = csg.PagedCache4(H, Hkv, D, dtype, pages, page, 2, table.shape[1])
+    a = csg.DocAttn(H, Hkv, D, dtype)
+    kp, vp = (torch.full((pages, Hkv, page * 68), 255, dtype=torch.uint8, device=DEV) for _ in range(2))
+    tab = torch.tensor(table, device=DEV)
+    at = [0, 0]
+    for new in ([70, 33], [1, 1], [4, 0], [1, 3], [14, 8]):
+        n = sum(new)
+        rows = [slice(s, s + d) for s, d in zip(at, new)]
+        at = [s + d for s, d in zip(at, new)]
+        y = torch.cat([x[b][rows[b]] for b in range(2)]).to(DEV)
+        q, o, o2 = (torch.empty((n, H, D), dtype=TORCH[dtype], device=DEV) for _ in range(3))
+        lse, lse2 = torch.empty((H, n), device=DEV), torch.empty((H, n), device=DEV)
+        ws = torch.empty(c.workspace_bytes(n), dtype=torch.uint8, device=DEV)
+        ptr, lens, k_ptr = ints(pointers(new)), ints(at), ints(pointers(at))
+        c.append(kp, vp, y[:, H:H + Hkv], y[:, H + Hkv:], ptr, lens, tab, inv_freq=freq, q=y[:, :H], q_out=q)
+        c.attn(q, kp, vp, ptr, lens, tab, o, lse, ws)
+        k, v = (torch.empty((sum(at), Hkv, D), dtype=TORCH[dtype], device=DEV) for _ in range(2))
+        c.read(kp, vp, k_ptr, lens, tab, k, v)
+        a.forward(q, k, v, ptr, k_ptr, o2, lse2)
+        torch.cuda.synchronize()
+        kp_, qp_ = pointers(at), pointers(new)
+        for b in range(2):
+            r, s = slice(qp_[b], qp_[b + 1]), slice(kp_[b], kp_[b + 1])
+            want = oda.attention(f64(q)[r], f64(k)[s], f64(v)[s], oda.Scores(), 0, HALF_STEP[dtype], TINY[dtype])
+            close(o[r], want[0], want[2], "cache")
+            close(o2[r], want[0], want[2], "documents")
+            close(lse[:, r], want[1], want[3], "lse")
