@@ -647,6 +647,67 @@ csg_status csg_cache4_attn(const csg_cache_cfg* cfg, const void* q, const void* 
                            const float* slopes, void* o, void* lse, void* workspace,
                            size_t workspace_bytes, int32_t* status, int device, void* stream);
 
+/* ---- the pages of a paged cache ----------------------------------------------------
+ *
+ * The page table, the lengths and a count per page, all on the device, from one step to the next: sequences fork and
+ * end, get pages for new tokens, give some back, and the pages in use move together. A sequence of n
+ * tokens holds the first ceil(n / page_size) entries of its row; entries behind them are not read, and are -1 in
+ * every table written. refs[p] (int32[n_pages]) counts the rows that hold page p, and what else the caller
+ * counts (+ 1 for a prefix to be kept); a page of count 0 is free. The calls read one table and write another (their outputs
+ * may not overlap what they read, nor each other), so that a step can be prepared while the one before still reads its
+ * own. They own nothing, wait for nothing and may be captured, as the calls above; 4-byte alignment is enough,
+ * but for the workspace (csg_pages_workspace bytes, any content, 16) and the pages (16).
+ * status: int32 on the device or NULL, as above: bit 0 for a page number outside 0 .. n_pages - 1, or (compact) of
+ * a free page, in an entry that is held; bit 1 for a length outside its row's, or a parent that there is not (no sequence);
+ * bit 2 where no page was free. Tables that break the rules (counts that do not hold, two
+ * moves to a page) touch no memory outside, but what comes out is not said. Every result has one
+ * value, whatever the order of the device's work: page numbers are given lowest first, by sequence and place.
+ * At most 2^24 pages and 2^20 sequences (CSG_ERR_UNSUPPORTED). */
+
+typedef struct {
+    int32_t n_pages;
+    int32_t page_size;            /* tokens per page: 16, 32, 64, 128 or 256 */
+    int32_t batch, max_pages;     /* sequences; entries of a row of the page table */
+    int32_t reserved;             /* 0 */
+} csg_pages_cfg;
+
+/* Bytes of workspace that csg_pages_extend and csg_pages_compact need. */
+csg_status csg_pages_workspace(const csg_pages_cfg* cfg, size_t* bytes);
+
+/* Sequence b becomes what sequence parent[b] was (int32[batch]): b itself to stay, negative for none (it has ended), and
+ * any number of sequences one parent (beams, samples of a prompt), which share its pages from then on.
+ * No page is copied; csg_pages_extend copies a shared page before one of them writes to it. */
+csg_status csg_pages_fork(const csg_pages_cfg* cfg, const int32_t* page_table, const int32_t* lens, const int32_t* refs,
+                          const int32_t* parent, int32_t* table_out, int32_t* lens_out, int32_t* refs_out,
+                          int32_t* status, int device, void* stream);
+
+/* Sequence b grows by grow[b] tokens (int32[batch]), or gives its last -grow[b] back. Where tokens are added behind a
+ * last page that is partly filled and counted more than once, that page is replaced by a
+ * free one and the pair (page, its copy) appended to moves (int32[batch][2], by sequence; *n_moves of them, int32; entries
+ * behind are left as they were). Each page asked for, a sequence's copy before its new pages, sequences in
+ * order, is the next lowest free one; pages given back in the same call are not free yet. The first sequence for which
+ * there are not enough, and every later one that asks for pages, is left as it was (bit 2), as is one that would
+ * outgrow its row (bit 1; what it asked for stays free). One that gives back more than it has is empty then (bit 1). */
+csg_status csg_pages_extend(const csg_pages_cfg* cfg, const int32_t* page_table, const int32_t* lens, const int32_t* refs,
+                            const int32_t* grow, int32_t* table_out, int32_t* lens_out, int32_t* refs_out, int32_t* moves,
+                            int32_t* n_moves, void* workspace, size_t workspace_bytes, int32_t* status, int device,
+                            void* stream);
+
+/* Of U pages in use, those numbered U and more go to the free numbers below U, both in ascending order: moves
+ * (int32[n_pages / 2][2], *n_moves of them, as in csg_pages_extend). renamed (int32[n_pages]): each page's new
+ * number, -1 for a free one. Lengths stay. */
+csg_status csg_pages_compact(const csg_pages_cfg* cfg, const int32_t* page_table, const int32_t* lens, const int32_t* refs,
+                             int32_t* table_out, int32_t* refs_out, int32_t* renamed, int32_t* moves, int32_t* n_moves,
+                             void* workspace, size_t workspace_bytes, int32_t* status, int device, void* stream);
+
+/* Copies page moves[i][0] onto page moves[i][1], i < min(*n_moves, max_moves), in each of n_buffers buffers of n_pages pages of
+ * page_bytes bytes (every layer's keys and values; `buffers` is an array of the host's, read before the call
+ * returns). No page may be both a source and a destination, nor a destination twice; pairs that name no page
+ * set bit 0 and are left out. */
+csg_status csg_pages_copy(int32_t n_pages, int64_t page_bytes, int32_t n_buffers, void* const* buffers,
+                          const int32_t* moves, int32_t max_moves, const int32_t* n_moves, int32_t* status, int device,
+                          void* stream);
+
 /* Waits for the plan's last call to complete (its kernel and every copy it issued)
  * and reports its diagnostics.
  * CSG_ERR_TIMEOUT if a wait expired (details in *out); CSG_ERR_STATE if the kernel

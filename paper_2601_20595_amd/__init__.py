@@ -52,6 +52,7 @@ ABI_FUNCTIONS = (
     "csg_measure_mfma_peak", "csg_ag_gemm_noalloc",
     "csg_doc_attn", "csg_doc_attn_grad", "csg_doc_attn_grad_workspace", "csg_cache_append", "csg_cache_attn",
     "csg_cache_attn_workspace", "csg_cache4_append", "csg_cache4_read", "csg_cache4_attn", "csg_cache4_attn_workspace",
+    "csg_pages_workspace", "csg_pages_fork", "csg_pages_extend", "csg_pages_compact", "csg_pages_copy",
 )
 
 
@@ -111,6 +112,11 @@ class csg_cache_cfg(ctypes.Structure):
                 ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
+class csg_pages_cfg(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 class csg_diag(ctypes.Structure):
     _fields_ = [("timed_out", ctypes.c_int32), ("chunk", ctypes.c_int32), ("tile", ctypes.c_int32),
                 ("observed", ctypes.c_uint32), ("epoch", ctypes.c_uint32), ("reserved", ctypes.c_int32)]
@@ -166,6 +172,11 @@ def _lib():
         "csg_cache4_read": ([P(csg_cache_cfg)] + [vp] * 8 + [ctypes.c_int, vp], st),
         "csg_cache4_attn_workspace": ([P(csg_cache_cfg), ctypes.c_int, P(ctypes.c_size_t)], st),
         "csg_cache4_attn": ([P(csg_cache_cfg)] + [vp] * 12 + [ctypes.c_size_t, vp, ctypes.c_int, vp], st),
+        "csg_pages_workspace": ([P(csg_pages_cfg), P(ctypes.c_size_t)], st),
+        "csg_pages_fork": ([P(csg_pages_cfg)] + [vp] * 8 + [ctypes.c_int, vp], st),
+        "csg_pages_extend": ([P(csg_pages_cfg)] + [vp] * 10 + [ctypes.c_size_t, vp, ctypes.c_int, vp], st),
+        "csg_pages_compact": ([P(csg_pages_cfg)] + [vp] * 9 + [ctypes.c_size_t, vp, ctypes.c_int, vp], st),
+        "csg_pages_copy": ([i32, i64, i32, P(vp), vp, i32, vp, vp, ctypes.c_int, vp], st),
         "csg_measure_mfma_peak": ([ctypes.c_int, i32, P(ctypes.c_double), P(ctypes.c_double), P(ctypes.c_double)],
                                   st),
     }
@@ -488,6 +499,41 @@ def csg_cache4_attn(cfg: csg_cache_cfg, q, k_pages, v_pages, q_ptr, lens, page_t
     _check(_lib().csg_cache4_attn(cfg, _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(q_ptr), _ptr(lens), _ptr(page_table),
                                   _ptr(group_ptr), _ptr(prefix), _ptr(slopes), _ptr(o), _ptr(lse), _ptr(workspace),
                                   workspace_bytes, _ptr(status), device, _stream(stream)), "csg_cache4_attn")
+
+
+def csg_pages_workspace(cfg: csg_pages_cfg) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib().csg_pages_workspace(cfg, ctypes.byref(n)), "csg_pages_workspace")
+    return n.value
+
+
+def csg_pages_fork(cfg: csg_pages_cfg, page_table, lens, refs, parent, table_out, lens_out, refs_out, status=None, device=0,
+                   stream=None) -> None:
+    _check(_lib().csg_pages_fork(cfg, _ptr(page_table), _ptr(lens), _ptr(refs), _ptr(parent), _ptr(table_out), _ptr(lens_out),
+                                 _ptr(refs_out), _ptr(status), device, _stream(stream)), "csg_pages_fork")
+
+
+def csg_pages_extend(cfg: csg_pages_cfg, page_table, lens, refs, grow, table_out, lens_out, refs_out, moves, n_moves, workspace,
+                     workspace_bytes: int, status=None, device=0, stream=None) -> None:
+    _check(_lib().csg_pages_extend(cfg, _ptr(page_table), _ptr(lens), _ptr(refs), _ptr(grow), _ptr(table_out), _ptr(lens_out),
+                                   _ptr(refs_out), _ptr(moves), _ptr(n_moves), _ptr(workspace), workspace_bytes, _ptr(status),
+                                   device, _stream(stream)), "csg_pages_extend")
+
+
+def csg_pages_compact(cfg: csg_pages_cfg, page_table, lens, refs, table_out, refs_out, renamed, moves, n_moves, workspace,
+                      workspace_bytes: int, status=None, device=0, stream=None) -> None:
+    _check(_lib().csg_pages_compact(cfg, _ptr(page_table), _ptr(lens), _ptr(refs), _ptr(table_out), _ptr(refs_out), _ptr(renamed),
+                                    _ptr(moves), _ptr(n_moves), _ptr(workspace), workspace_bytes, _ptr(status), device,
+                                    _stream(stream)), "csg_pages_compact")
+
+
+def csg_pages_copy(n_pages: int, page_bytes: int, buffers: Sequence, moves, max_moves: int, n_moves, status=None, device=0,
+                   stream=None) -> None:
+    """buffers: tensors or addresses."""
+    n = len(buffers)
+    at = (ctypes.c_void_p * n)(*[_ptr(b) for b in buffers])
+    _check(_lib().csg_pages_copy(n_pages, page_bytes, n, at, _ptr(moves), max_moves, _ptr(n_moves), _ptr(status), device,
+                                 _stream(stream)), "csg_pages_copy")
 
 
 def csg_plan_join(plan: int, stream) -> None:
@@ -892,3 +938,78 @@ class PagedCache4(PagedCache):
             c, _arg(k_pages, size, page, "k_pages", dev), _arg(v_pages, size, page, "v_pages", dev),
             _arg(k_ptr, 4 * batch + 4, _INT32, "k_ptr", dev), _arg(lens, 4 * batch, _INT32, "lens", dev), self._table(page_table),
             ka, va, _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_cache4_read")
+
+
+class PagePool:
+    """The pages of a paged cache (csg_pages_fork, csg_pages_extend, csg_pages_compact, csg_pages_copy).
+
+    Keeps the cache's geometry; page_table, int32 (batch, max_pages), lens, int32 (batch), and refs, int32
+    (n_pages), are the caller's, and so are those that the calls write, which share no memory with them.
+    moves is int32 (pairs, 2), n_moves and status one int32 each."""
+
+    def __init__(self, n_pages, page_size, batch, max_pages, device: int = 0):
+        self.device = device
+        self._cfg = csg_pages_cfg(n_pages=n_pages, page_size=page_size, batch=batch, max_pages=max_pages)
+        self._workspace = csg_pages_workspace(self._cfg)  # (checks the configuration)
+        self._table_bytes, self._batch_bytes, self._refs_bytes = 4 * batch * max_pages, 4 * batch, 4 * n_pages
+        self._batch, self._pages, self._max_pages = batch, n_pages, max_pages
+
+    def workspace_bytes(self) -> int:
+        """Bytes of the workspace that extend and compact need."""
+        return self._workspace
+
+    def _table(self, t, what: str) -> int:
+        if type(t) is not int and t.shape[-1] != self._max_pages:
+            raise ValueError("%s must have %d pages a row" % (what, self._max_pages))
+        return _arg(t, self._table_bytes, _INT32, what, self.device)
+
+    def _lens(self, t, what: str) -> int:
+        return _arg(t, self._batch_bytes, _INT32, what, self.device)
+
+    def _refs(self, t, what: str) -> int:
+        return _arg(t, self._refs_bytes, _INT32, what, self.device)
+
+    def fork(self, page_table, lens, refs, parent, table_out, lens_out, refs_out, status=None, stream=None):
+        """Sequence b becomes what sequence parent[b], int32 (batch), was; negative: none."""
+        dev = self.device
+        _check(_lib().csg_pages_fork(
+            self._cfg, self._table(page_table, "page_table"), self._lens(lens, "lens"), self._refs(refs, "refs"),
+            self._lens(parent, "parent"), self._table(table_out, "table_out"), self._lens(lens_out, "lens_out"),
+            self._refs(refs_out, "refs_out"), _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_pages_fork")
+
+    def extend(self, page_table, lens, refs, grow, table_out, lens_out, refs_out, moves, n_moves, workspace, status=None,
+               stream=None):
+        """Sequences grow by grow, int32 (batch), tokens, or shrink; moves (at least batch pairs) are
+        to be copied before anything is appended."""
+        dev = self.device
+        _check(_lib().csg_pages_extend(
+            self._cfg, self._table(page_table, "page_table"), self._lens(lens, "lens"), self._refs(refs, "refs"),
+            self._lens(grow, "grow"), self._table(table_out, "table_out"), self._lens(lens_out, "lens_out"),
+            self._refs(refs_out, "refs_out"), _arg(moves, 2 * self._batch_bytes, _INT32, "moves", dev), _arg(n_moves, 4, _INT32, "n_moves", dev),
+            _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes, _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)),
+               "csg_pages_extend")
+
+    def compact(self, page_table, lens, refs, table_out, refs_out, renamed, moves, n_moves, workspace, status=None, stream=None):
+        """The pages in use get the lowest numbers: renamed, int32 (n_pages); moves has room for n_pages // 2
+        pairs."""
+        dev = self.device
+        _check(_lib().csg_pages_compact(
+            self._cfg, self._table(page_table, "page_table"), self._lens(lens, "lens"), self._refs(refs, "refs"),
+            self._table(table_out, "table_out"), self._refs(refs_out, "refs_out"), self._refs(renamed, "renamed"),
+            _arg(moves, 8 * (self._pages // 2), _INT32, "moves", dev), _arg(n_moves, 4, _INT32, "n_moves", dev),
+            _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes, _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)),
+               "csg_pages_compact")
+
+    def copy(self, buffers, moves, n_moves, status=None, stream=None):
+        """Copies the pages of moves in every buffer (tensors whose first dimension is the pages, each
+        page of as many bytes), up to as many pairs as moves has."""
+        dev, pages = self.device, self._pages
+        size = buffers[0].nbytes // pages if buffers else 0
+        for b in buffers:
+            if b.shape[0] != pages or b.nbytes != size * pages:
+                raise ValueError("buffers must be (%d, ...), with pages of the same size" % pages)
+        at = (ctypes.c_void_p * len(buffers))(*[_arg(b, size * pages, 0, "buffers", dev) for b in buffers])
+        room = moves.numel() // 2
+        _check(_lib().csg_pages_copy(pages, size, len(buffers), at, _arg(moves, 8 * room, _INT32, "moves", dev), room,
+                                     _arg(n_moves, 4, _INT32, "n_moves", dev), _arg(status, 4, _INT32, "status", dev), dev,
+                                     _stream(stream)), "csg_pages_copy")

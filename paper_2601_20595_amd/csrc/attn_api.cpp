@@ -13,26 +13,11 @@
 #include "doc_attn.hpp"
 #include "errors.hpp"
 
-namespace {
+namespace csg {
 
-using csg::aligned16;
-using csg::DeviceGuard;
-using csg::fail;
-using csg::hip_fail;
-
-constexpr int kMaxDevices = 64;
-constexpr int64_t kMaxRows = int64_t{1} << 30;
-constexpr int64_t kMaxStride = int64_t{1} << 23;  // 63 rows of it stay within 32-bit byte offsets
-constexpr int64_t kMaxGrid = 0xffffffff / 512;  // workgroups: a launch's threads are counted in 32 bits
-constexpr int32_t kDefaultCus = 256;
-// Rows of a cache's attention: four are a workgroup of the merge, and the tiles of as many as 2048 entries
-// with all of the rows each are still counted in 32 bits.
-constexpr int64_t kMaxCacheRows = int64_t{1} << 25;
-static_assert(kMaxCacheRows / 4 <= kMaxGrid * 2, "workgroups of 256 threads");
-static_assert(kMaxCacheRows / csg::kCacheTileRows * csg::kMaxCacheEntries < (int64_t{1} << 32), "tiles");
-
-// Compute units of `device`, checked once to be the one this library is built for.
 csg_status device_cus(int device, int32_t* cus) {
+  constexpr int kMaxDevices = 64;
+  constexpr int32_t kDefaultCus = 256;
   static std::mutex mu;
   static int32_t known[kMaxDevices] = {};
   if (device < 0 || device >= kMaxDevices) return fail(CSG_ERR_INVALID, "device %d out of range", device);
@@ -48,6 +33,26 @@ csg_status device_cus(int device, int32_t* cus) {
   *cus = known[device];
   return CSG_OK;
 }
+
+}  // namespace csg
+
+namespace {
+
+using csg::aligned16;
+using csg::device_cus;
+using csg::DeviceGuard;
+using csg::fail;
+using csg::hip_fail;
+
+constexpr int64_t kMaxRows = int64_t{1} << 30;
+constexpr int64_t kMaxStride = int64_t{1} << 23;  // 63 rows of it stay within 32-bit byte offsets
+constexpr int64_t kMaxGrid = 0xffffffff / 512;  // workgroups: a launch's threads are counted in 32 bits
+constexpr int32_t kDefaultCus = 256;
+// Rows of a cache's attention: four are a workgroup of the merge, and the tiles of as many as 2048 entries
+// with all of the rows each are still counted in 32 bits.
+constexpr int64_t kMaxCacheRows = int64_t{1} << 25;
+static_assert(kMaxCacheRows / 4 <= kMaxGrid * 2, "workgroups of 256 threads");
+static_assert(kMaxCacheRows / csg::kCacheTileRows * csg::kMaxCacheEntries < (int64_t{1} << 32), "tiles");
 
 csg_status check_heads(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype) {
   if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads != 0 || n_heads > 65536)

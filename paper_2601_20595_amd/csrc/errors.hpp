@@ -38,6 +38,9 @@ struct DeviceGuard {
   }
 };
 
+// Compute units of `device`, checked once to be the one this library is built for.
+csg_status device_cus(int device, int32_t* cus);
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace csg

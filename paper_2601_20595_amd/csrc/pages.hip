@@ -1,0 +1,461 @@
+// The pages of a paged cache, managed on the device for gfx950 (CDNA4): sequences fork, end, grow and give
+// tokens back, pages move together. Tables and counts are small and every kernel here is a chain of
+// latencies; only the copies of pages are bound by the memory.
+//
+// refs[p] counts the rows of the page table that hold page p (and whatever else the caller counts);
+// a page of count 0 is free. A sequence of n tokens holds the first ceil(n / page size) entries of its row.
+#include <hip/hip_runtime.h>
+
+#include "cache_attn.hpp"
+#include "pages.hpp"
+
+namespace csg {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kSlots = 1024;  // entries of a row that a workgroup has
+
+__device__ __forceinline__ void tell(int32_t* status, int bit) {
+  if (status) atomicOr(status, bit);
+}
+
+// A sequence's tokens, as far as its row goes, and the entries that it holds.
+struct Held {
+  int tokens, pages;
+  bool bad;
+};
+__device__ __forceinline__ Held held(const PagesArgs& a, int tokens) {
+  const int room = static_cast<int>(min(static_cast<int64_t>(a.max_pages) << a.page_shift, int64_t{1} << 30));
+  Held h;
+  h.tokens = min(max(tokens, 0), room);
+  h.bad = h.tokens != tokens;
+  h.pages = (h.tokens + (1 << a.page_shift) - 1) >> a.page_shift;
+  return h;
+}
+
+__device__ __forceinline__ bool names_page(const PagesArgs& a, int p) { return p >= 0 && p < a.n_pages; }
+__device__ __forceinline__ void count(const PagesArgs& a, int p, int by) {
+  if (names_page(a, p))
+    atomicAdd(a.refs_out + p, by);
+  else
+    tell(a.status, kCacheBadPage);
+}
+
+// ---- fork ------------------------------------------------------------------------------------
+__device__ __forceinline__ Held parent_of(const PagesArgs& a, int b, int* parent) {
+  int p = a.change[b];
+  if (p >= a.batch) {
+    if (threadIdx.x == 0) tell(a.status, kCacheBadLength);
+    p = -1;
+  }
+  *parent = p;
+  return held(a, p < 0 ? 0 : a.lens[p]);
+}
+
+// Rows of the new table, and the counts as they were.
+__global__ __launch_bounds__(kThreads) void fork_rows(PagesArgs a, int row_blocks, int across) {
+  const int tid = threadIdx.x;
+  if (static_cast<int>(blockIdx.x) >= row_blocks) {
+    const int64_t p0 = static_cast<int64_t>(blockIdx.x - row_blocks) * kPageChunk;
+    for (int64_t p = p0 + tid; p < min(p0 + kPageChunk, static_cast<int64_t>(a.n_pages)); p += kThreads) a.refs_out[p] = a.refs[p];
+    return;
+  }
+  const int b = blockIdx.x / across, s0 = blockIdx.x % across * kSlots;
+  int parent;
+  const Held h = parent_of(a, b, &parent);
+  const int32_t* from = a.table + static_cast<int64_t>(max(parent, 0)) * a.max_pages;
+  int32_t* to = a.table_out + static_cast<int64_t>(b) * a.max_pages;
+  for (int s = s0 + tid; s < min(s0 + kSlots, a.max_pages); s += kThreads) to[s] = s < h.pages ? from[s] : -1;
+  if (s0 == 0 && tid == 0) {
+    a.lens_out[b] = h.tokens;
+    if (h.bad) tell(a.status, kCacheBadLength);
+  }
+}
+
+// The counts: less the old rows, more the new ones.
+__global__ __launch_bounds__(kThreads) void fork_counts(PagesArgs a, int across) {
+  const int b = blockIdx.x / across, s0 = blockIdx.x % across * kSlots;
+  int parent;
+  const Held now = parent_of(a, b, &parent);
+  if (parent == b) return;
+  const Held old = held(a, a.lens[b]);
+  const int64_t row = static_cast<int64_t>(b) * a.max_pages;
+  for (int s = s0 + static_cast<int>(threadIdx.x); s < min(s0 + kSlots, max(old.pages, now.pages)); s += kThreads) {
+    if (s < old.pages) count(a, a.table[row + s], -1);
+    if (s < now.pages) count(a, a.table_out[row + s], 1);
+  }
+}
+
+// ---- sums ------------------------------------------------------------------------------------
+template <class V>
+__device__ __forceinline__ V sum_before(V x, V* total, V (&s_wave)[kThreads / 64]) {
+  // exclusive, over the workgroup's threads
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  V sum = x;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const V up = __shfl_up(sum, d);
+    if (lane >= d) sum += up;
+  }
+  __syncthreads();  // (s_wave is free)
+  if (lane == 63) s_wave[wave] = sum;
+  __syncthreads();
+  V before = sum - x, all = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    if (w < wave) before += s_wave[w];
+    all += s_wave[w];
+  }
+  *total = all;
+  return before;
+}
+
+// The workspace of extend and compact.
+struct Sums {
+  int64_t need;    // pages that are asked for
+  int64_t unused;
+};
+__device__ __forceinline__ Sums* sums_in(const PagesArgs& a) { return reinterpret_cast<Sums*>(a.ws); }
+__device__ __forceinline__ int32_t* counts_in(const PagesArgs& a) { return reinterpret_cast<int32_t*>(a.ws + 64); }
+__device__ __forceinline__ int32_t* list_in(const PagesArgs& a) { return counts_in(a) + 2 * (page_chunks(a.n_pages) / 2 + 1); }
+__device__ __forceinline__ int32_t* ranks_in(const PagesArgs& a) { return list_in(a) + a.n_pages; }
+__device__ __forceinline__ int64_t* first_in(const PagesArgs& a) { return reinterpret_cast<int64_t*>(ranks_in(a) + a.n_pages); }
+__device__ __forceinline__ int32_t* splits_in(const PagesArgs& a) { return reinterpret_cast<int32_t*>(first_in(a) + a.batch); }
+
+constexpr int kEach = kPageChunk / kThreads;  // pages of a thread, one after the other
+
+// Whether this thread's pages of chunk c are in use, one bit each (pages that there are not: 0), and `there`.
+__device__ __forceinline__ uint32_t used_bits(const PagesArgs& a, int c, uint32_t* there) {
+  const int p0 = c * kPageChunk + static_cast<int>(threadIdx.x) * kEach;
+  uint32_t used = 0, is = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int p = p0 + i;
+    if (p < a.n_pages) {
+      is |= 1u << i;
+      if (a.refs[p] != 0) used |= 1u << i;
+    }
+  }
+  *there = is;
+  return used;
+}
+
+// Pages in use in the chunks before `c`, and in all.
+__device__ __forceinline__ int used_before(const PagesArgs& a, int c, int* all, int (&s_wave)[kThreads / 64]) {
+  int before = 0, total = 0;
+  for (int i = threadIdx.x; i < page_chunks(a.n_pages); i += kThreads) {
+    const int n = counts_in(a)[i];
+    total += n;
+    if (i < c) before += n;
+  }
+  int sum_b, sum_t;
+  sum_before(before, &sum_b, s_wave);
+  sum_before(total, &sum_t, s_wave);
+  *all = sum_t;
+  return sum_b;
+}
+
+// ---- extend ----------------------------------------------------------------------------------
+// What sequence b asks for. Its requests are places first .. first + need - 1 of the row of all requests, and request
+// i takes the i-th lowest free page.
+struct Growth {
+  Held before, after;
+  int need;
+  bool split;  // the last page is to be written and not the sequence's alone: it gets a copy
+  bool fits;   // (in its row)
+};
+__device__ __forceinline__ Growth growth_of(const PagesArgs& a, int b) {
+  Growth g;
+  g.before = held(a, a.lens[b]);
+  const int by = a.change[b];
+  const int64_t tokens = static_cast<int64_t>(g.before.tokens) + by;
+  const int64_t room = min(static_cast<int64_t>(a.max_pages) << a.page_shift, int64_t{1} << 30);
+  g.fits = tokens <= room;
+  const int want = static_cast<int>(max(int64_t{0}, min(tokens, int64_t{1} << 30)));
+  g.after.tokens = want;
+  g.after.pages = (want + (1 << a.page_shift) - 1) >> a.page_shift;
+  g.after.bad = tokens < 0 || !g.fits;
+  g.split = false;
+  if (by > 0 && (g.before.tokens & ((1 << a.page_shift) - 1)) != 0) {
+    const int last = a.table[static_cast<int64_t>(b) * a.max_pages + g.before.pages - 1];
+    g.split = names_page(a, last) && a.refs[last] > 1;
+  }
+  g.need = max(0, g.after.pages - g.before.pages) + g.split;
+  return g;
+}
+
+// The chunks' pages in use, and the counts as they were; the last workgroup puts the sequences' requests in a row.
+__global__ __launch_bounds__(kThreads) void extend_count(PagesArgs a) {
+  __shared__ int s_wave[kThreads / 64];
+  __shared__ int64_t s_wave64[kThreads / 64];
+  const int chunks = page_chunks(a.n_pages), c = blockIdx.x, tid = threadIdx.x;
+  if (c < chunks) {
+    uint32_t there;
+    const uint32_t used = used_bits(a, c, &there);
+    const int64_t p0 = static_cast<int64_t>(c) * kPageChunk;
+    for (int64_t p = p0 + tid; p < min(p0 + kPageChunk, static_cast<int64_t>(a.n_pages)); p += kThreads) a.refs_out[p] = a.refs[p];
+    int all;
+    sum_before(static_cast<int>(__popc(used)), &all, s_wave);
+    if (tid == 0) counts_in(a)[c] = all;
+    return;
+  }
+  int64_t need = 0;
+  int splits = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kThreads) {
+    const int b = b0 + tid;
+    Growth g{};
+    if (b < a.batch) g = growth_of(a, b);
+    int64_t all;
+    const int64_t first = need + sum_before(static_cast<int64_t>(g.need), &all, s_wave64);
+    need += all;
+    int all_splits;
+    const int split = splits + sum_before(g.split && g.fits ? 1 : 0, &all_splits, s_wave);
+    splits += all_splits;
+    if (b < a.batch) {
+      first_in(a)[b] = first;
+      splits_in(a)[b] = split;
+    }
+  }
+  if (tid == 0) {
+    sums_in(a)->need = need;
+    *a.n_moves = 0;
+  }
+}
+
+// The lowest free pages, as many as are asked for.
+__global__ __launch_bounds__(kThreads) void extend_list(PagesArgs a) {
+  __shared__ int s_wave[kThreads / 64];
+  const int c = blockIdx.x;
+  int used_all;
+  const int used = used_before(a, c, &used_all, s_wave);
+  const int free = c * kPageChunk - used;
+  const int64_t need = sums_in(a)->need;
+  if (free >= need) return;  // (the same in every thread)
+  uint32_t there;
+  const uint32_t bits = ~used_bits(a, c, &there) & there;
+  int all;
+  int at = free + sum_before(static_cast<int>(__popc(bits)), &all, s_wave);
+  for (int i = 0; i < kEach; ++i)
+    if (bits >> i & 1) {
+      if (at < need) list_in(a)[at] = c * kPageChunk + static_cast<int>(threadIdx.x) * kEach + i;
+      ++at;
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void extend_rows(PagesArgs a, int across) {
+  __shared__ int s_wave[kThreads / 64];
+  const int b = blockIdx.x / across, s0 = blockIdx.x % across * kSlots, tid = threadIdx.x;
+  int used;
+  used_before(a, 0, &used, s_wave);
+  Growth g = growth_of(a, b);
+  const int64_t first = first_in(a)[b];
+  const bool none = first + g.need > a.n_pages - used;
+  const bool granted = g.need == 0 ? g.fits : g.fits && !none;
+  if (s0 == 0 && tid == 0) {
+    if (g.before.bad || g.after.bad) tell(a.status, kCacheBadLength);
+    if (g.need > 0 && g.fits && none) tell(a.status, kPagesNone);
+  }
+  if (!granted) {
+    g.after = g.before;
+    g.split = false;
+  }
+  const int64_t row = static_cast<int64_t>(b) * a.max_pages;
+  const int last = g.before.pages - 1;
+  for (int s = s0 + tid; s < min(s0 + kSlots, a.max_pages); s += kThreads) {
+    const int old = s < g.before.pages ? a.table[row + s] : -1;
+    int now = s < g.after.pages ? old : -1;
+    if (s == last && g.split) {
+      now = list_in(a)[first];
+      count(a, old, -1);
+      count(a, now, 1);
+      const int at = splits_in(a)[b];
+      a.moves[2 * at] = old;
+      a.moves[2 * at + 1] = now;
+      atomicMax(a.n_moves, at + 1);
+    } else if (s > last && s < g.after.pages) {
+      now = list_in(a)[first + g.split + (s - g.before.pages)];
+      count(a, now, 1);
+    } else if (s < g.before.pages && s >= g.after.pages) {
+      count(a, old, -1);
+    }
+    a.table_out[row + s] = now;
+  }
+  if (s0 == 0 && tid == 0) a.lens_out[b] = g.after.tokens;
+}
+
+// ---- compact ---------------------------------------------------------------------------------
+// With U pages in use, those at U and beyond go, in ascending order, to the free ones before U, in ascending order.
+__global__ __launch_bounds__(kThreads) void compact_count(PagesArgs a) {
+  __shared__ int s_wave[kThreads / 64];
+  uint32_t there;
+  const uint32_t used = used_bits(a, blockIdx.x, &there);
+  int all;
+  sum_before(static_cast<int>(__popc(used)), &all, s_wave);
+  if (threadIdx.x == 0) counts_in(a)[blockIdx.x] = all;
+}
+
+// The free pages before U by their rank, and the ranks of the pages in use among all in use.
+__global__ __launch_bounds__(kThreads) void compact_list(PagesArgs a) {
+  __shared__ int s_wave[kThreads / 64];
+  const int c = blockIdx.x;
+  int u;
+  const int before = used_before(a, c, &u, s_wave);
+  uint32_t there;
+  const uint32_t bits = used_bits(a, c, &there);
+  int all;
+  int used = before + sum_before(static_cast<int>(__popc(bits)), &all, s_wave);
+  for (int i = 0; i < kEach; ++i) {
+    const int p = c * kPageChunk + static_cast<int>(threadIdx.x) * kEach + i;
+    if (p >= a.n_pages) break;
+    if (bits >> i & 1) {
+      ranks_in(a)[p] = used++;
+    } else if (p < u) {
+      list_in(a)[p - used] = p;
+    }
+  }
+}
+
+// Where a page in use lies afterwards. As many pages in use lie at U and beyond as are free before it, `moving`; the
+// one of rank r among all in use is number r - (U - moving) of them.
+__device__ __forceinline__ int place_of(const PagesArgs& a, int p, int u, int moving) {
+  return p < u ? p : list_in(a)[moving - (u - ranks_in(a)[p])];
+}
+
+__global__ __launch_bounds__(kThreads) void compact_rows(PagesArgs a, int across) {
+  __shared__ int s_wave[kThreads / 64];
+  __shared__ int s_moving;
+  const int chunks = page_chunks(a.n_pages), tid = threadIdx.x;
+  int u;
+  used_before(a, 0, &u, s_wave);
+  // free pages before U: U less the pages in use there, which its chunk's are counted for
+  const int cu = u / kPageChunk;
+  int ignored;
+  const int low = used_before(a, cu, &ignored, s_wave);
+  int here = 0;
+  for (int p = cu * kPageChunk + tid; p < u; p += kThreads) here += a.refs[p] != 0;
+  int in_chunk;
+  sum_before(here, &in_chunk, s_wave);
+  if (tid == 0) s_moving = u - low - in_chunk;
+  __syncthreads();
+  const int moving = s_moving;
+  if (static_cast<int>(blockIdx.x) < chunks) {
+    if (blockIdx.x == 0 && tid == 0) *a.n_moves = moving;
+    for (int i = tid; i < kPageChunk; i += kThreads) {
+      const int p = blockIdx.x * kPageChunk + i;
+      if (p >= a.n_pages) break;
+      const int refs = a.refs[p];
+      if (refs == 0) {
+        a.renamed[p] = -1;
+        if (p >= u) a.refs_out[p] = 0;
+      } else {
+        const int to = place_of(a, p, u, moving);
+        a.renamed[p] = to;
+        a.refs_out[to] = refs;
+        if (p >= u) {
+          const int at = moving - (u - ranks_in(a)[p]);
+          a.refs_out[p] = 0;
+          a.moves[2 * at] = p;
+          a.moves[2 * at + 1] = to;
+        }
+      }
+    }
+    return;
+  }
+  const int item = blockIdx.x - chunks;
+  const int b = item / across, s0 = item % across * kSlots;
+  const Held h = held(a, a.lens[b]);
+  if (h.bad && s0 == 0 && tid == 0) tell(a.status, kCacheBadLength);
+  const int64_t row = static_cast<int64_t>(b) * a.max_pages;
+  for (int s = s0 + tid; s < min(s0 + kSlots, a.max_pages); s += kThreads) {
+    int now = -1;
+    if (s < h.pages) {
+      const int p = a.table[row + s];
+      if (names_page(a, p) && a.refs[p] != 0)
+        now = place_of(a, p, u, moving);
+      else
+        tell(a.status, kCacheBadPage);
+    }
+    a.table_out[row + s] = now;
+  }
+}
+
+// ---- copy ------------------------------------------------------------------------------------
+// Pieces of 16 KiB of the pages that move, buffer by buffer, dealt to the workgroups in turn.
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+constexpr int kPiece = 16384;
+
+__global__ __launch_bounds__(kThreads) void copy_pages(CopyArgs a) {
+  const int n = min(max(*a.n_moves, 0), a.max_moves);
+  const int64_t pieces = (a.page_bytes + kPiece - 1) / kPiece;
+  const int64_t items = pieces * n * a.n_buffers;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t page = item / pieces;
+    const int move = static_cast<int>(page % n), buffer = static_cast<int>(page / n);
+    const int from = a.moves[2 * move], to = a.moves[2 * move + 1];
+    if (from < 0 || from >= a.n_pages || to < 0 || to >= a.n_pages) {
+      if (threadIdx.x == 0) tell(a.status, kCacheBadPage);
+      continue;
+    }
+    const int64_t at = (item - page * pieces) * kPiece;
+    const int bytes = static_cast<int>(min(static_cast<int64_t>(kPiece), a.page_bytes - at));
+    const u32x4_t* src = reinterpret_cast<const u32x4_t*>(a.buffers[buffer] + from * a.page_bytes + at);
+    u32x4_t* dst = reinterpret_cast<u32x4_t*>(a.buffers[buffer] + to * a.page_bytes + at);
+    u32x4_t x[kPiece / 16 / kThreads];
+#pragma unroll
+    for (int i = 0; i < kPiece / 16 / kThreads; ++i) {
+      const int k = i * kThreads + static_cast<int>(threadIdx.x);
+      if (16 * k < bytes) x[i] = src[k];
+    }
+#pragma unroll
+    for (int i = 0; i < kPiece / 16 / kThreads; ++i) {
+      const int k = i * kThreads + static_cast<int>(threadIdx.x);
+      if (16 * k < bytes) dst[k] = x[i];
+    }
+  }
+}
+
+int rows_across(const PagesArgs& a) { return (a.max_pages + kSlots - 1) / kSlots; }
+
+}  // namespace
+
+hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t s) {
+  const int across = rows_across(a), rows = a.batch * across;
+  hipLaunchKernelGGL(fork_rows, dim3(rows + page_chunks(a.n_pages)), dim3(kThreads), 0, s, a, rows, across);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || rows == 0) return e;
+  hipLaunchKernelGGL(fork_counts, dim3(rows), dim3(kThreads), 0, s, a, across);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s) {
+  const int across = rows_across(a), rows = a.batch * across, chunks = page_chunks(a.n_pages);
+  hipLaunchKernelGGL(extend_count, dim3(chunks + 1), dim3(kThreads), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || rows == 0) return e;
+  hipLaunchKernelGGL(extend_list, dim3(chunks), dim3(kThreads), 0, s, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(extend_rows, dim3(rows), dim3(kThreads), 0, s, a, across);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s) {
+  const int across = rows_across(a), rows = a.batch * across, chunks = page_chunks(a.n_pages);
+  hipLaunchKernelGGL(compact_count, dim3(chunks), dim3(kThreads), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(compact_list, dim3(chunks), dim3(kThreads), 0, s, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(compact_rows, dim3(chunks + rows), dim3(kThreads), 0, s, a, across);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const CopyArgs& a, int cus, hipStream_t s) {
+  const int64_t items = (a.page_bytes + kPiece - 1) / kPiece * a.max_moves * a.n_buffers;
+  const int64_t most = int64_t{8} * cus;
+  hipLaunchKernelGGL(copy_pages, dim3(static_cast<uint32_t>(items < most ? items : most)), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace csg
