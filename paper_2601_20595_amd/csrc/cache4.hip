@@ -325,6 +325,299 @@ struct Quarter {
   }
 };
 
+// Combination of the four lanes of a row: lane ^ 16, then lane ^ 32, swapped as in max_halves.
+__device__ __forceinline__ float max_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// RowSoftmax for rows of four lanes, N / 4 tiles of 16 keys at a time. The reference moves where one of the row's lanes finds
+// its weights' sum beyond the limit: until then the lanes need not know each other's.
+struct QuarterSoftmax {
+  float m = -__builtin_inff();
+  float mc = -__builtin_inff();
+  float l = 0.0f;
+  bool wide = false;
+
+  template <class T, int N>
+  __device__ __forceinline__ float block(const float (&x)[N], float c, int l16, typename T::x8 (&pb)[N / 8], bool& moved) {
+    float sum = weights<T, N, false>(x, c, mc, pb);
+    const uint64_t beyond = __builtin_amdgcn_ballot_w64(wide || !(sum <= T::kRowSumLimit));
+    moved = beyond != 0;
+    float alpha = 1.0f;
+    if (moved) {
+      const bool move = (beyond >> l16 & 0x0001000100010001ull) != 0;
+      float mx = x[0];
+#pragma unroll
+      for (int r = 1; r < N; ++r) mx = fmaxf(mx, x[r]);
+      mx = max_quarters(mx);
+      const float to = move ? fmaxf(m, mx) : m;
+      const bool none = to == -__builtin_inff();  // against -inf the weights would be NaN: they are 0
+      alpha = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - to) * c);
+      m = to;
+      mc = m * c;
+      wide = !none && fabsf(mc) > 1e37f;
+      l *= alpha;
+      sum = weights<T, N, true>(x, c, none ? 0.0f : mc, pb, none ? 0.0f : m, wide);
+    }
+    l += sum;
+    return alpha;
+  }
+
+ private:
+  template <class T, int N, bool kAgain>
+  static __device__ __forceinline__ float weights(const float (&x)[N], float c, float refc, typename T::x8 (&pb)[N / 8], float ref = 0.0f,
+                                                  bool far = false) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < N / 8; ++t) {
+      f32x8_t w;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float v = x[8 * t + r];
+        w[r] = __builtin_amdgcn_exp2f(kAgain && far ? (v - ref) * c : fmaf(v, c, -refc));
+        sum += w[r];
+      }
+      pb[t] = __builtin_convertvector(w, typename T::x8);
+    }
+    return sum;
+  }
+};
+
+template <class T>
+struct Mfma16;
+template <>
+struct Mfma16<Bf16> {
+  static __device__ __forceinline__ f32x4_t run(bf16x8_t a, bf16x8_t b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mfma16<F16> {
+  static __device__ __forceinline__ f32x4_t run(f16x8_t a, f16x8_t b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+
+// Where the 16-byte pieces of a row of a wave's values lie: piece p at p ^ swz16(row). A store puts one piece of 16 rows
+// (all at different places), a transposing read takes two neighbouring pieces of 8 rows at a time (the
+// same).
+template <int D>
+__device__ __forceinline__ constexpr int swz16(int r) {
+  return D == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r >> 1 & 3) << 1 | (r >> 3 & 1);
+}
+
+// Codes and scales of 16 rows of a head, as v_mfma_f32_16x16x32 takes the rows: lane l has quarter l / 16 of row
+// l % 16, D / 4 elements. Every row of a page may be read, so nothing is checked here: scores of keys that are not the part's
+// are masked, and their values get scale 0 (own). Where there is no page, all lanes read one place of page 0.
+template <int D>
+struct Rows16 {
+  uint32_t codes[D / 32];
+  uint32_t byte;
+  __device__ __forceinline__ void load(const CacheArgs& c, const uint16_t* pages, int kvh, int page, int key, int lane) {
+    const int row0 = key & ((1 << c.page_shift) - 1);
+    const unsigned char* head = reinterpret_cast<const unsigned char*>(pages) + head_of<D>(c, max(page, 0), kvh);
+    const int row = lane & 15, quarter = lane >> 4;
+    const uint32_t at = page < 0 ? 0 : row * (D / 2) + quarter * (D / 8);
+    const uint32_t scale_at = page < 0 ? 0 : row * (D / 32) + quarter * (D / 32) / 4;
+    const unsigned char* from = head + row0 * (D / 2);
+    if constexpr (D == 128) {
+      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(from + at);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) codes[i] = x[i];
+    } else {
+      const u32x2_t x = *reinterpret_cast<const u32x2_t*>(from + at);
+      codes[0] = x[0];
+      codes[1] = x[1];
+    }
+    byte = head[((D / 2) << c.page_shift) + row0 * (D / 32) + scale_at];
+  }
+};
+
+// A narrow part: up to 16 R rows, whose four waves take every fourth step of 16 kTiles keys, each at its own pace. Keys go from
+// the loads' registers into the products (the elements of a head in the order in which the lanes have them, which
+// the queries follow); values through LDS, in 16 bits, where the transposing reads find them. The next
+// step's codes are asked for as soon as the last ones are converted.
+template <class T, int D, bool kPlain, int R, int kTiles>
+__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, const Part& p, unsigned char* stage,
+                                            float (&s_ref)[4][32], float (&s_sum)[4][32], float* out, int lane, int wave) {
+  using x8 = typename T::x8;
+  constexpr int kStep = 16 * kTiles, kAtOnce = 64 / kTiles;
+  constexpr int kParts = D / 32;  // products that a score sums
+  const CacheArgs& c = a.c;
+  const int l16 = lane & 15, g = lane >> 4;
+  unsigned char* mine = stage + wave * kStep * 2 * D;
+  const int steps = (p.end - p.key0 + kStep - 1) / kStep;
+  const int mine_n = steps > wave ? (steps - wave + 3) / 4 : 0;
+  auto key_of = [&](int n) { return p.key0 + (wave + 4 * n) * kStep; };
+  // lane n holds the page of the 16 keys n % kTiles of the wave's step n / kTiles (kAtOnce steps at a time); behind
+  // the part's end -1
+  auto page_at = [&](int n) { return page_of(c, p, key_of(n + lane / kTiles) + 16 * (lane % kTiles)); };
+  int pages = -1, next_pages = -1;
+  Rows16<D> k[kTiles], v[kTiles];
+  auto load = [&](int n, const uint16_t* from, Rows16<D> (&to)[kTiles]) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+      to[t].load(c, from, p.kvh, __builtin_amdgcn_readlane(pages, kTiles * (n % kAtOnce) + t), key_of(n) + 16 * t, lane);
+  };
+  if (mine_n > 0) {
+    pages = page_at(0);
+    load(0, c.k_pages, k);
+    load(0, c.v_pages, v);
+  }
+  Part pr[R];
+  x8 qf[R][kParts];
+  float slope[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    pr[i] = p;
+    locate_row(a, x, local, 16 * i + l16, pr[i]);
+    const uint16_t* q = c.Q + pr[i].token * c.q_stride + pr[i].h * D + (D / 4) * g;
+#pragma unroll
+    for (int s = 0; s < kParts; ++s) {
+      const u32x4_t raw = pr[i].ok ? *reinterpret_cast<const u32x4_t*>(q + 8 * s) : u32x4_t{0u, 0u, 0u, 0u};
+      qf[i][s] = __builtin_bit_cast(x8, raw);
+    }
+    slope[i] = kPlain ? 0.0f : slope_of(a.scoring, pr[i].h);
+  }
+  const float cexp = a.scoring.unit * kLog2e;
+  // places in LDS: a lane's stores (piece (D / 32) g + s of row l16), its transposing reads (4 rows of the lane's
+  // group, elements 16 db ..)
+  const int to = 2 * D * l16 + 16 * (((D / 32) * g) ^ swz16<D>(l16));
+  const int row = 4 * g + (l16 >> 2);
+  const int from = 2 * D * row + 16 * (((l16 & 3) >> 1) ^ swz16<D>(row)) + 8 * (l16 & 1);
+  f32x4_t acc[R][D / 16];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db) acc[i][db] = f32x4_t{};
+  QuarterSoftmax sm[R];
+  for (int n = 0; n < mine_n; ++n) {
+    if (n % kAtOnce == kAtOnce / 2) next_pages = page_at(n + kAtOnce / 2);
+    if (n % kAtOnce == kAtOnce - 1) pages = next_pages;
+    f32x4_t tile[R][kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const float scale = scale_of(k[t].byte);
+#pragma unroll
+      for (int i = 0; i < R; ++i) tile[i][t] = f32x4_t{};
+#pragma unroll
+      for (int s = 0; s < kParts; ++s) {
+        const x8 kf = __builtin_bit_cast(x8, values<T>(k[t].codes[s], scale));
+#pragma unroll
+        for (int i = 0; i < R; ++i) tile[i][t] = Mfma16<T>::run(kf, qf[i][s], tile[i][t]);
+      }
+    }
+    load(n + 1, c.k_pages, k);
+    x8 pb[R][kTiles / 2];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      float sc[4 * kTiles];  // of keys 16 (r / 4) + 4 g + r % 4
+#pragma unroll
+      for (int r = 0; r < 4 * kTiles; ++r) sc[r] = tile[i][r / 4][r % 4];
+      const int key0 = key_of(n);
+      if constexpr (!kPlain) {
+        if (a.scoring.cap_in != 0.0f) {
+          if (a.scoring.unit <= kNearCap) {
+#pragma unroll
+            for (float& y : sc) y = tanh_from_log2(y * a.scoring.cap_in);
+          } else {
+#pragma unroll
+            for (float& y : sc) y = tanh_from_log2_near_0(y * a.scoring.cap_in);
+          }
+        }
+        if (a.scoring.slopes) {
+          const float at = static_cast<float>(pr[i].pos - key0 - 4 * g);
+#pragma unroll
+          for (int r = 0; r < 4 * kTiles; ++r) sc[r] = fmaf(-slope[i], fabsf(at - static_cast<float>(16 * (r / 4) + r % 4)), sc[r]);
+        }
+      }
+      if (key0 + kStep > pr[i].all_hi || key0 < p.lo) {
+#pragma unroll
+        for (int r = 0; r < 4 * kTiles; ++r) {
+          const int key = key0 + 16 * (r / 4) + 4 * g + r % 4;
+          if (key >= pr[i].hi || key < p.lo) sc[r] = -__builtin_inff();
+        }
+      }
+      bool moved;
+      const float alpha = sm[i].template block<T>(sc, cexp, l16, pb[i], moved);
+      if (moved) {
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) acc[i][db] *= alpha;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const int key = key_of(n) + 16 * t + l16;
+      const float scale = key >= p.lo && key < p.end ? scale_of(v[t].byte) : 0.0f;
+#pragma unroll
+      for (int s = 0; s < kParts; ++s)
+        *reinterpret_cast<u32x4_t*>(mine + 32 * D * t + (to ^ 16 * s)) = values<T>(v[t].codes[s], scale);
+    }
+    load(n + 1, c.v_pages, v);
+    asm volatile("" ::: "memory");  // (a wave's LDS accesses are done in order)
+#pragma unroll
+    for (int u = 0; u < kTiles / 2; ++u)
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) {
+        const lds_u8_t* at = (const lds_u8_t*)mine + 64 * D * u + (from ^ 32 * db);
+        const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)at);
+        const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(at + 32 * D));
+        const x8 vf = __builtin_bit_cast(x8, (i16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}));
+#pragma unroll
+        for (int i = 0; i < R; ++i) acc[i][db] = Mfma16<T>::run(vf, pb[i][u], acc[i][db]);
+      }
+    asm volatile("" ::: "memory");
+  }
+
+  // the waves' results against their common reference, summed in the order of the waves; the
+  // 16-byte pieces of a row are turned by its number, against bank conflicts
+  float l[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    l[i] = sum_quarters(sm[i].l);
+    if (g == 0) {
+      s_ref[wave][16 * i + l16] = sm[i].m;
+      s_sum[wave][16 * i + l16] = l[i];
+    }
+  }
+  __syncthreads();  // (also: every wave has read its stage)
+  const int live = min(16 * R, x.rows);
+  constexpr int kPieces = D / 4;
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int r = 16 * i + l16;
+    if (r < live) {
+      const float top = fmaxf(fmaxf(s_ref[0][r], s_ref[1][r]), fmaxf(s_ref[2][r], s_ref[3][r]));
+      const float f = factor(sm[i].m, top, cexp);
+      f32x4_t* at = reinterpret_cast<f32x4_t*>(stage) + (wave * 16 * R + r) * kPieces;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) at[(4 * db + g) ^ (r & 7)] = acc[i][db] * f;
+    }
+  }
+  __syncthreads();
+  if (out) {
+    const f32x4_t* in = reinterpret_cast<const f32x4_t*>(stage);
+    const int tid = wave * 64 + lane;
+    for (int i = tid; i < live * kPieces; i += kThreads) {
+      const int r = i / kPieces, at = r * kPieces + ((i % kPieces) ^ (r & 7));
+      f32x4_t sum = in[at];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) sum += in[w * 16 * R * kPieces + at];
+      *reinterpret_cast<f32x4_t*>(out + 4 * i) = sum;
+    }
+    if (tid < live) {
+      const float top = fmaxf(fmaxf(s_ref[0][tid], s_ref[1][tid]), fmaxf(s_ref[2][tid], s_ref[3][tid]));
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) sum = fmaf(s_sum[w][tid], factor(s_ref[w][tid], top, cexp), sum);
+      out[32 * D + tid] = top;
+      out[32 * D + 32 + tid] = sum;
+    }
+  }
+  __syncthreads();  // the stages are free again
+}
+
 // A part, whose waves share blocks of 64 keys: each brings 16 keys and values, in 16 bits into one of two
 // buffers.
 template <class T, int D, bool kPlain>
@@ -402,18 +695,24 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
 template <class T, int D, bool kPlain>
 __global__ __launch_bounds__(kThreads, 2) void cache4_attn(CacheAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char stage[2 * 2 * kCacheWideBlock * 2 * D];
+  __shared__ float s_ref[4][32], s_sum[4][32];
   static_assert(sizeof(stage) >= kCacheGroupBytes, "the groups, before the buffers");
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  auto wide = [&](const Entry& x, const Entry* local, Part& p, float* out) {
-    wide_part<T, D, kPlain>(a, x, local, p, stage, out, lane, wave);
-  };
+  static_assert(sizeof(stage) >= 4 * 64 * 2 * D && sizeof(stage) >= 4 * 32 * D * 4, "the waves' values, and their results");
+  int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   cache_run<D>(
       a, stage,
       [&](const Entry& x, const Entry* local, Part& p, float* out) {
-        p.tile = wave;  // (the rows are the first wave's)
-        wide(x, local, p, out);
+        asm("" : "+v"(lane));  // (what the parts make of it is made again in each, and not kept through the others)
+        if (x.rows <= 16)
+          narrow_part<T, D, kPlain, 1, 4>(a, x, local, p, stage, s_ref, s_sum, out, lane, wave);
+        else
+          narrow_part<T, D, kPlain, 2, 2>(a, x, local, p, stage, s_ref, s_sum, out, lane, wave);
       },
-      wide);
+      [&](const Entry& x, const Entry* local, Part& p, float* out) {
+        asm("" : "+v"(lane));
+        wide_part<T, D, kPlain>(a, x, local, p, stage, out, lane, wave);
+      });
 }
 
 template <class T, int D>
