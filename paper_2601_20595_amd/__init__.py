@@ -850,6 +850,7 @@ class PagedCache:
         self._table_bytes = 4 * batch * max_pages
 
     _append, _attn = "csg_cache_append", "csg_cache_attn"
+    _attn_workspace = staticmethod(csg_cache_attn_workspace)
 
     @staticmethod
     def _row_bytes(head_dim: int) -> int:
@@ -862,7 +863,7 @@ class PagedCache:
         """Bytes of the workspace that attn needs for up to that many new tokens and groups."""
         c = csg_cache_cfg.from_buffer_copy(self._cfg)
         c.tokens, c.n_groups, c.q_stride = tokens, n_groups, 0
-        return csg_cache_attn_workspace(c, self.device)
+        return self._attn_workspace(c, self.device)
 
     def _table(self, page_table) -> int:
         if type(page_table) is not int and page_table.shape[-1] != self._max_pages:
@@ -917,6 +918,7 @@ class PagedCache4(PagedCache):
     32)); everything else is as in PagedCache, dtype that of q, k, v and o."""
 
     _append, _attn = "csg_cache4_append", "csg_cache4_attn"
+    _attn_workspace = staticmethod(csg_cache4_attn_workspace)
 
     @staticmethod
     def _row_bytes(head_dim: int) -> int:

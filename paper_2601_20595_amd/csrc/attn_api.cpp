@@ -198,10 +198,15 @@ csg_status check_cache_attn(csg_cache_cfg* c) {
   return CSG_OK;
 }
 
-int64_t cache_workspace(const csg_cache_cfg& c, int32_t cus) {
+// Workgroups of attention on a CU.
+int32_t cu_groups(const csg_cache_cfg& c, bool four) {
+  return four && csg::cache4_few(c.tokens, c.n_heads, c.n_kv_heads, c.batch, c.n_groups) ? csg::kCache4Few : csg::kCacheGroups;
+}
+
+int64_t cache_workspace(const csg_cache_cfg& c, int32_t groups) {
   return csg::cache_plan_bytes() + csg::cache_part_bytes(c.head_dim) *
                                        csg::cache_max_parts(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups,
-                                                            csg::cache_head_workers(cus, c.n_kv_heads));
+                                                            csg::cache_head_workers(groups, c.n_kv_heads));
 }
 
 csg::CacheArgs cache_args(const csg_cache_cfg& c, const void* k_pages, const void* v_pages, const void* q, const int32_t* q_ptr,
@@ -270,8 +275,19 @@ csg_status cache_append(hipError_t (*launch)(const csg::AppendArgs&, bool, int, 
   return CSG_OK;
 }
 
+// The workspace of both caches' attention.
+csg_status attn_workspace(const csg_cache_cfg* cfg, bool four, int device, size_t* bytes) {
+  if (!cfg || !bytes) return fail(CSG_ERR_INVALID, "NULL argument");
+  csg_cache_cfg c = *cfg;
+  CSG_CHECK(check_cache_attn(&c));
+  int32_t cus = kDefaultCus;
+  if (device >= 0) CSG_CHECK(device_cus(device, &cus));
+  *bytes = static_cast<size_t>(cache_workspace(c, (four ? std::max(csg::kCache4Few, csg::kCacheGroups) : csg::kCacheGroups) * cus));
+  return CSG_OK;
+}
+
 // The same of both caches' attention.
-csg_status cache_attn(hipError_t (*launch)(const csg::CacheAttnArgs&, bool, int, hipStream_t), const csg_cache_cfg* cfg, const void* q, const void* k_pages, const void* v_pages,
+csg_status cache_attn(hipError_t (*launch)(const csg::CacheAttnArgs&, bool, int, hipStream_t), bool four, const csg_cache_cfg* cfg, const void* q, const void* k_pages, const void* v_pages,
                           const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table, const int32_t* group_ptr,
                           const int32_t* prefix, const float* slopes, void* o, void* lse, void* workspace,
                           size_t workspace_bytes, int32_t* status, int device, void* stream) {
@@ -285,9 +301,10 @@ csg_status cache_attn(hipError_t (*launch)(const csg::CacheAttnArgs&, bool, int,
   if (!all_aligned({q, k_pages, v_pages, o, workspace})) return fail(CSG_ERR_INVALID, "buffers must be 16-byte aligned");
   int32_t cus = 0;
   CSG_CHECK(device_cus(device, &cus));
-  if (static_cast<int64_t>(workspace_bytes) < cache_workspace(c, cus))
+  const int32_t groups = cu_groups(c, four) * cus;
+  if (static_cast<int64_t>(workspace_bytes) < cache_workspace(c, groups))
     return fail(CSG_ERR_INVALID, "the workspace holds %zu bytes; the call needs %lld", workspace_bytes,
-                static_cast<long long>(cache_workspace(c, cus)));
+                static_cast<long long>(cache_workspace(c, groups)));
   DeviceGuard g(device);
   if (g.err != hipSuccess) return hip_fail(g.err, "hipSetDevice");
   csg::CacheAttnArgs a{};
@@ -297,7 +314,7 @@ csg_status cache_attn(hipError_t (*launch)(const csg::CacheAttnArgs&, bool, int,
   a.group_ptr = group_ptr;
   a.prefix = prefix;
   a.n_groups = c.n_groups;
-  a.head_workers = csg::cache_head_workers(cus, c.n_kv_heads);
+  a.head_workers = csg::cache_head_workers(groups, c.n_kv_heads);
   a.dies = 8 / std::gcd(8, c.n_kv_heads);
   a.max_parts = csg::cache_max_parts(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups, a.head_workers);
   a.max_tiles = csg::cache_max_tiles(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups);
@@ -382,20 +399,14 @@ csg_status csg_cache_append(const csg_cache_cfg* cfg, void* k_pages, void* v_pag
 }
 
 csg_status csg_cache_attn_workspace(const csg_cache_cfg* cfg, int device, size_t* bytes) {
-  if (!cfg || !bytes) return fail(CSG_ERR_INVALID, "NULL argument");
-  csg_cache_cfg c = *cfg;
-  CSG_CHECK(check_cache_attn(&c));
-  int32_t cus = kDefaultCus;
-  if (device >= 0) CSG_CHECK(device_cus(device, &cus));
-  *bytes = static_cast<size_t>(cache_workspace(c, cus));
-  return CSG_OK;
+  return attn_workspace(cfg, false, device, bytes);
 }
 
 csg_status csg_cache_attn(const csg_cache_cfg* cfg, const void* q, const void* k_pages, const void* v_pages,
                           const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table, const int32_t* group_ptr,
                           const int32_t* prefix, const float* slopes, void* o, void* lse, void* workspace,
                           size_t workspace_bytes, int32_t* status, int device, void* stream) {
-  return cache_attn(csg::launch_cache_attn, cfg, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse,
+  return cache_attn(csg::launch_cache_attn, false, cfg, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse,
                     workspace, workspace_bytes, status, device, stream);
 }
 
@@ -436,13 +447,13 @@ csg_status csg_cache4_read(const csg_cache_cfg* cfg, const void* k_pages, const 
 }
 
 csg_status csg_cache4_attn_workspace(const csg_cache_cfg* cfg, int device, size_t* bytes) {
-  return csg_cache_attn_workspace(cfg, device, bytes);
+  return attn_workspace(cfg, true, device, bytes);
 }
 
 csg_status csg_cache4_attn(const csg_cache_cfg* cfg, const void* q, const void* k_pages, const void* v_pages,
                           const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table, const int32_t* group_ptr,
                           const int32_t* prefix, const float* slopes, void* o, void* lse, void* workspace,
                           size_t workspace_bytes, int32_t* status, int device, void* stream) {
-  return cache_attn(csg::launch_cache4_attn, cfg, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse,
+  return cache_attn(csg::launch_cache4_attn, true, cfg, q, k_pages, v_pages, q_ptr, lens, page_table, group_ptr, prefix, slopes, o, lse,
                     workspace, workspace_bytes, status, device, stream);
 }

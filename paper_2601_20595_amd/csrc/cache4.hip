@@ -439,14 +439,14 @@ struct Rows16 {
 // the queries follow); values through LDS, in 16 bits, where the transposing reads find them. The next
 // step's codes are asked for as soon as the last ones are converted.
 template <class T, int D, bool kPlain, int R, int kTiles>
-__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, const Part& p, unsigned char* stage,
+__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, const Part& p, int row0, unsigned char* stage,
                                             float (&s_ref)[4][32], float (&s_sum)[4][32], float* out, int lane, int wave) {
   using x8 = typename T::x8;
   constexpr int kStep = 16 * kTiles, kAtOnce = 64 / kTiles;
   constexpr int kParts = D / 32;  // products that a score sums
   const CacheArgs& c = a.c;
   const int l16 = lane & 15, g = lane >> 4;
-  unsigned char* mine = stage + wave * kStep * 2 * D;
+  unsigned char* mine = stage + wave * 32 * 2 * D;
   const int steps = (p.end - p.key0 + kStep - 1) / kStep;
   const int mine_n = steps > wave ? (steps - wave + 3) / 4 : 0;
   auto key_of = [&](int n) { return p.key0 + (wave + 4 * n) * kStep; };
@@ -471,7 +471,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     pr[i] = p;
-    locate_row(a, x, local, 16 * i + l16, pr[i]);
+    locate_row(a, x, local, row0 + 16 * i + l16, pr[i]);
     const uint16_t* q = c.Q + pr[i].token * c.q_stride + pr[i].h * D + (D / 4) * g;
 #pragma unroll
     for (int s = 0; s < kParts; ++s) {
@@ -547,27 +547,28 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
       }
     }
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      const int key = key_of(n) + 16 * t + l16;
-      const float scale = key >= p.lo && key < p.end ? scale_of(v[t].byte) : 0.0f;
+    for (int u = 0; u < kTiles / 2; ++u) {
 #pragma unroll
-      for (int s = 0; s < kParts; ++s)
-        *reinterpret_cast<u32x4_t*>(mine + 32 * D * t + (to ^ 16 * s)) = values<T>(v[t].codes[s], scale);
-    }
-    load(n + 1, c.v_pages, v);
-    asm volatile("" ::: "memory");  // (a wave's LDS accesses are done in order)
+      for (int t = 0; t < 2; ++t) {
+        const Rows16<D>& y = v[2 * u + t];
+        const int key = key_of(n) + 32 * u + 16 * t + l16;
+        const float scale = key >= p.lo && key < p.end ? scale_of(y.byte) : 0.0f;
 #pragma unroll
-    for (int u = 0; u < kTiles / 2; ++u)
+        for (int s = 0; s < kParts; ++s) *reinterpret_cast<u32x4_t*>(mine + 32 * D * t + (to ^ 16 * s)) = values<T>(y.codes[s], scale);
+      }
+      if (u == kTiles / 2 - 1) load(n + 1, c.v_pages, v);
+      asm volatile("" ::: "memory");  // (a wave's LDS accesses are done in order)
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) {
-        const lds_u8_t* at = (const lds_u8_t*)mine + 64 * D * u + (from ^ 32 * db);
+        const lds_u8_t* at = (const lds_u8_t*)mine + (from ^ 32 * db);
         const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)at);
         const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(at + 32 * D));
         const x8 vf = __builtin_bit_cast(x8, (i16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}));
 #pragma unroll
         for (int i = 0; i < R; ++i) acc[i][db] = Mfma16<T>::run(vf, pb[i][u], acc[i][db]);
       }
-    asm volatile("" ::: "memory");
+      asm volatile("" ::: "memory");
+    }
   }
 
   // the waves' results against their common reference, summed in the order of the waves; the
@@ -582,43 +583,45 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
     }
   }
   __syncthreads();  // (also: every wave has read its stage)
-  const int live = min(16 * R, x.rows);
   constexpr int kPieces = D / 4;
+  const int tid = wave * 64 + lane;
+  const int rows = x.rows - p.tile * kCacheTileRows - row0;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    const int r = 16 * i + l16;
-    if (r < live) {
+    const int live = min(16, rows - 16 * i);
+    if (i > 0) __syncthreads();
+    if (l16 < live) {
+      const int r = 16 * i + l16;
       const float top = fmaxf(fmaxf(s_ref[0][r], s_ref[1][r]), fmaxf(s_ref[2][r], s_ref[3][r]));
       const float f = factor(sm[i].m, top, cexp);
-      f32x4_t* at = reinterpret_cast<f32x4_t*>(stage) + (wave * 16 * R + r) * kPieces;
+      f32x4_t* at = reinterpret_cast<f32x4_t*>(stage) + (wave * 16 + l16) * kPieces;
 #pragma unroll
-      for (int db = 0; db < D / 16; ++db) at[(4 * db + g) ^ (r & 7)] = acc[i][db] * f;
+      for (int db = 0; db < D / 16; ++db) at[(4 * db + g) ^ (l16 & 7)] = acc[i][db] * f;
+    }
+    __syncthreads();
+    if (out) {
+      const f32x4_t* in = reinterpret_cast<const f32x4_t*>(stage);
+      for (int e = tid; e < live * kPieces; e += kThreads) {
+        const int r = e / kPieces, at = r * kPieces + ((e % kPieces) ^ (r & 7));
+        f32x4_t sum = in[at];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) sum += in[w * 16 * kPieces + at];
+        *reinterpret_cast<f32x4_t*>(out + (row0 + 16 * i) * D + 4 * e) = sum;
+      }
     }
   }
-  __syncthreads();
-  if (out) {
-    const f32x4_t* in = reinterpret_cast<const f32x4_t*>(stage);
-    const int tid = wave * 64 + lane;
-    for (int i = tid; i < live * kPieces; i += kThreads) {
-      const int r = i / kPieces, at = r * kPieces + ((i % kPieces) ^ (r & 7));
-      f32x4_t sum = in[at];
+  if (out && tid < min(16 * R, rows)) {
+    const float top = fmaxf(fmaxf(s_ref[0][tid], s_ref[1][tid]), fmaxf(s_ref[2][tid], s_ref[3][tid]));
+    float sum = 0.0f;
 #pragma unroll
-      for (int w = 1; w < 4; ++w) sum += in[w * 16 * R * kPieces + at];
-      *reinterpret_cast<f32x4_t*>(out + 4 * i) = sum;
-    }
-    if (tid < live) {
-      const float top = fmaxf(fmaxf(s_ref[0][tid], s_ref[1][tid]), fmaxf(s_ref[2][tid], s_ref[3][tid]));
-      float sum = 0.0f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) sum = fmaf(s_sum[w][tid], factor(s_ref[w][tid], top, cexp), sum);
-      out[32 * D + tid] = top;
-      out[32 * D + 32 + tid] = sum;
-    }
+    for (int w = 0; w < 4; ++w) sum = fmaf(s_sum[w][tid], factor(s_ref[w][tid], top, cexp), sum);
+    out[32 * D + row0 + tid] = top;
+    out[32 * D + 32 + row0 + tid] = sum;
   }
   __syncthreads();  // the stages are free again
 }
 
-// A part, whose waves share blocks of 64 keys: each brings 16 keys and values, in 16 bits into one of two
+// A wide part, whose waves share blocks of 64 keys: each brings 16 keys and values, in 16 bits into one of two
 // buffers.
 template <class T, int D, bool kPlain>
 __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, Part& p, unsigned char* stage, float* out, int lane,
@@ -692,27 +695,35 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
   __syncthreads();  // the buffers are free again
 }
 
-template <class T, int D, bool kPlain>
-__global__ __launch_bounds__(kThreads, 2) void cache4_attn(CacheAttnArgs a) {
-  __shared__ __attribute__((aligned(1024))) unsigned char stage[2 * 2 * kCacheWideBlock * 2 * D];
+// With few rows a sequence (few), the kernel has only the narrow parts of 16 rows, whose registers and LDS
+// let more workgroups onto a CU; an entry of more rows goes through its keys once for each 16 of them. Otherwise it has
+// parts for up to 16, up to 32 and up to 128 rows, that convert their keys once.
+template <class T, int D, bool kPlain, bool few>
+__global__ __launch_bounds__(kThreads, few ? kCache4Few : kCacheGroups) void cache4_attn(CacheAttnArgs a) {
+  __shared__ __attribute__((aligned(1024))) unsigned char stage[(few ? 2 : 4) * kCacheBlock * 4 * D];
   __shared__ float s_ref[4][32], s_sum[4][32];
   static_assert(sizeof(stage) >= kCacheGroupBytes, "the groups, before the buffers");
-  static_assert(sizeof(stage) >= 4 * 64 * 2 * D && sizeof(stage) >= 4 * 32 * D * 4, "the waves' values, and their results");
+  static_assert(few || sizeof(stage) == 2 * 2 * kCacheWideBlock * 2 * D, "a wide part's buffers");
+  static_assert(sizeof(stage) >= 4 * 32 * 2 * D && sizeof(stage) >= 4 * 16 * D * 4, "the narrow waves' values, and results of theirs");
   int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  cache_run<D>(
-      a, stage,
-      [&](const Entry& x, const Entry* local, Part& p, float* out) {
-        asm("" : "+v"(lane));  // (what the parts make of it is made again in each, and not kept through the others)
-        if (x.rows <= 16)
-          narrow_part<T, D, kPlain, 1, 4>(a, x, local, p, stage, s_ref, s_sum, out, lane, wave);
-        else
-          narrow_part<T, D, kPlain, 2, 2>(a, x, local, p, stage, s_ref, s_sum, out, lane, wave);
-      },
-      [&](const Entry& x, const Entry* local, Part& p, float* out) {
-        asm("" : "+v"(lane));
-        wide_part<T, D, kPlain>(a, x, local, p, stage, out, lane, wave);
-      });
+  cache_run(a, stage, [&](const Entry& x, const Entry* local, Part& p, int64_t place, bool wide) {
+    asm("" : "+v"(lane));  // (what a part makes of it is made again in each, and not kept through the others)
+    if constexpr (few) {
+      const int first = p.tile;
+      for (int r = first * kCacheTileRows; r < min(x.rows, first * kCacheTileRows + kCacheWideRows); r += 16) {
+        p.tile = r / kCacheTileRows;
+        narrow_part<T, D, kPlain, 1, 2>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, part_at<D>(a, place + p.tile - first), lane, wave);
+      }
+    } else if (wide) {
+      p.tile += wave;
+      wide_part<T, D, kPlain>(a, x, local, p, stage, part_at<D>(a, place + wave), lane, wave);
+    } else if (x.rows <= 16) {
+      narrow_part<T, D, kPlain, 1, 4>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+    } else {
+      narrow_part<T, D, kPlain, 2, 2>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+    }
+  });
 }
 
 template <class T, int D>
@@ -727,14 +738,19 @@ hipError_t read(const ReadArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <class T, int D>
+template <class T, int D, bool few>
 hipError_t attend(const CacheAttnArgs& a, hipStream_t s) {
   const dim3 grid(a.head_workers * a.c.Hkv);
   if (a.scoring.plain())
-    hipLaunchKernelGGL((cache4_attn<T, D, true>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((cache4_attn<T, D, true, few>), grid, dim3(kThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((cache4_attn<T, D, false>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((cache4_attn<T, D, false, few>), grid, dim3(kThreads), 0, s, a);
   return hipGetLastError();
+}
+
+template <class T, int D>
+hipError_t attend(const CacheAttnArgs& a, bool few, hipStream_t s) {
+  return few ? attend<T, D, true>(a, s) : attend<T, D, false>(a, s);
 }
 
 }  // namespace
@@ -750,8 +766,9 @@ hipError_t launch_cache4_read(const ReadArgs& a, bool f16, int head_dim, hipStre
 }
 
 hipError_t launch_cache4_attn(const CacheAttnArgs& a, bool f16, int head_dim, hipStream_t s) {
-  hipError_t e = head_dim == 128 ? (f16 ? attend<F16, 128>(a, s) : attend<Bf16, 128>(a, s))
-                                 : (f16 ? attend<F16, 64>(a, s) : attend<Bf16, 64>(a, s));
+  const bool few = cache4_few(a.c.tokens, a.c.H, a.c.Hkv, a.c.batch, a.n_groups);
+  hipError_t e = head_dim == 128 ? (f16 ? attend<F16, 128>(a, few, s) : attend<Bf16, 128>(a, few, s))
+                                 : (f16 ? attend<F16, 64>(a, few, s) : attend<Bf16, 64>(a, few, s));
   return e != hipSuccess ? e : launch_cache_merge(a, f16, head_dim, s);
 }
 

@@ -12,6 +12,13 @@ namespace csg {
 // A head's rows of a page: page size rows of D / 2 bytes, then page size times D / 32 scales.
 constexpr int cache4_row_bytes(int head_dim) { return head_dim / 2 + head_dim / 32; }
 
+// Attention's kernel for few rows has more workgroups on a CU than the other, whose number is the 16-bit cache's.
+constexpr int kCache4Few = 3;
+// Whether the sequences' rows (new tokens times heads of a key/value head) are few, on average; with groups, whose
+// sequences' rows go through the shared keys together, never.
+inline bool cache4_few(int64_t tokens, int32_t H, int32_t Hkv, int32_t batch, int32_t n_groups) {
+  return n_groups == 0 && tokens * (H / Hkv) <= int64_t{16} * batch;
+}
 constexpr int kReadRows = 32;  // rows of the outputs that a workgroup reads
 
 struct ReadArgs {

@@ -346,14 +346,14 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
   static_assert(sizeof(stage) >= 4 * 32 * D * 4, "and the waves' results");
   static_assert(sizeof(stage) >= kCacheGroupBytes, "and, before, the groups");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  cache_run<D>(
-      a, stage,
-      [&](const Entry& x, const Entry* local, Part& p, float* out) {
-        narrow_part<T, D, kPlain>(a, x, local, p, stage, s_ref, s_sum, out, lane, wave);
-      },
-      [&](const Entry& x, const Entry* local, Part& p, float* out) {
-        wide_part<T, D, kPlain>(a, x, local, p, stage, out, lane, wave);
-      });
+  cache_run(a, stage, [&](const Entry& x, const Entry* local, Part& p, int64_t place, bool wide) {
+    if (wide) {
+      p.tile += wave;
+      wide_part<T, D, kPlain>(a, x, local, p, stage, part_at<D>(a, place + wave), lane, wave);
+    } else {
+      narrow_part<T, D, kPlain>(a, x, local, p, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+    }
+  });
 }
 
 // One wave joins the parts of one row, as sum_w f_w acc_w / sum_w f_w l_w with f_w = e^(m_w - max m). A

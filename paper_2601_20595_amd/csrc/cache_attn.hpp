@@ -19,7 +19,7 @@ constexpr int kCacheWideBlock = 64;    // keys per inner step of a wide task
 constexpr int kCacheTaskCost = 4;
 constexpr int kCacheMinRun = 4;  // units a workgroup takes at least: a block for each wave
 constexpr int kMaxCacheEntries = 2048; // sequences and groups of one call
-constexpr int kCacheGroupBytes = (2 * kMaxCacheEntries + 1) * 4;  // LDS that holds a call's groups
+constexpr int kCacheGroupBytes = (kMaxCacheEntries + 1) * 4;  // LDS that holds a call's groups, no more than its sequences
 
 // status bits
 constexpr int kCacheBadPage = 1, kCacheBadLength = 2;
@@ -69,7 +69,8 @@ constexpr int64_t cache_plan_bytes() { return 256 + kMaxCacheEntries * 32; }
 constexpr int64_t cache_part_bytes(int head_dim) { return kCacheTileRows * (head_dim + 2) * 4; }
 // Workgroups for each key/value head, all of them as many as are on the device at once (two a
 // CU, by their registers and, for 128 elements a head, 64 KiB of LDS).
-constexpr int32_t cache_head_workers(int32_t cus, int32_t Hkv) { return 2 * cus > Hkv ? 2 * cus / Hkv : 1; }
+constexpr int kCacheGroups = 2;
+constexpr int32_t cache_head_workers(int32_t groups, int32_t Hkv) { return groups > Hkv ? groups / Hkv : 1; }
 // Tiles of a key/value head, at most: every token in its sequence and, maybe, its group.
 inline int64_t cache_max_tiles(int32_t H, int32_t Hkv, int64_t tokens, int32_t batch, int32_t n_groups) {
   return tokens * (H / Hkv) / kCacheTileRows * (n_groups > 0 ? 2 : 1) + batch + n_groups;

@@ -193,11 +193,17 @@ __device__ __forceinline__ void finish_scores(const CacheAttnArgs& a, const Part
   }
 }
 
-// A workgroup's run: its parts, one after the other, through narrow_part and wide_part, which all of its
-// threads call with the entry, the sequences' entries (locate_row), the part, and the place of its
-// results. `stage`: LDS that the parts use (and the groups, before them).
-template <int D, class Narrow, class Wide>
-__device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char* stage, Narrow narrow_part, Wide wide_part) {
+// Memory of a part's results in place `place`, null if there is none.
+template <int D>
+__device__ __forceinline__ float* part_at(const CacheAttnArgs& a, int64_t place) {
+  return place < a.max_parts ? reinterpret_cast<float*>(a.ws + cache_plan_bytes() + place * cache_part_bytes(D)) : nullptr;
+}
+
+// A workgroup's run: its parts, one after the other, through do_part, which all of its threads call with the
+// entry, the sequences' entries (locate_row), the part, whose tile is its task's first, that tile's place, and whether the
+// task is wide. `stage`: LDS that the parts use (and the groups, before them).
+template <class DoPart>
+__device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char* stage, DoPart do_part) {
   __shared__ uint32_t s_wave_units[4], s_wave_tiles[4];
   __shared__ int s_entry, s_first, s_tiles;
   __shared__ Entry s_entries[kThreads];
@@ -322,13 +328,8 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
       p.lo = x.lo;
       p.key0 = (x.block0 + first) * kCacheBlock;
       p.end = min(x.end, p.key0 + count * kCacheBlock);
-      p.tile = wide ? 4 * task + wave : 0;
-      const int64_t place = places + tiles_before + p.tile;
-      float* out = place < a.max_parts ? reinterpret_cast<float*>(a.ws + cache_plan_bytes() + place * cache_part_bytes(D)) : nullptr;
-      if (wide)
-        wide_part(x, sequences, p, out);
-      else
-        narrow_part(x, sequences, p, out);
+      p.tile = wide ? 4 * task : 0;
+      do_part(x, sequences, p, places + tiles_before + p.tile, wide);
     } else {
       in_entry = 0;
       tiles_before += x.tiles();

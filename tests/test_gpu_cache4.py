@@ -164,8 +164,17 @@ def test_bad_pages_and_other_rows_are_left():
         _same(got, want, "rows")
 
 
+# few rows on average, and some sequences with many
+MIXED = {
+    "one of many rows": ([40] + [1] * 20 + [0] * 10, [90] + [1 + 13 * i for i in range(20)] + [5] * 10, 8, 2, 128, 16, [], 0.0, False),
+    "of some rows": ([1, 5, 8, 1, 1, 1, 1, 1, 1, 1, 0, 0], [300, 77, 200, 64, 32, 31, 1, 2, 500, 129, 9, 0], 8, 2, 64, 32, [], 8.0, True),
+    "sixteen rows each": ([4] * 9, [4, 5, 63, 64, 65, 128, 129, 260, 1000], 4, 1, 128, 64, [], 0.0, False),
+    "seventeen heads": ([1, 1], [70, 1500], 17, 1, 128, 16, [], 0.0, False),
+}
+
+
 def _attn_case(name, dtype, sharp=1.0, stream=None):
-    new, lens, H, Hkv, D, page, groups, cap, bias = ATTN[name]
+    new, lens, H, Hkv, D, page, groups, cap, bias = MIXED[name] if name in MIXED else ATTN[name]
     rng = np.random.default_rng(7)
     n, tail = sum(new), 2
     table, pages = _table(rng, lens, page, shared=groups)
@@ -208,7 +217,7 @@ def _attn_case(name, dtype, sharp=1.0, stream=None):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
-@pytest.mark.parametrize("name", ATTN)
+@pytest.mark.parametrize("name", [*ATTN, *MIXED])
 def test_attention(name, dtype):
     _attn_case(name, dtype)
 
