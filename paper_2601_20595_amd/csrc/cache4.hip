@@ -408,18 +408,13 @@ __device__ __forceinline__ constexpr int swz16(int r) {
 }
 
 // Codes and scales of 16 rows of a head, as v_mfma_f32_16x16x32 takes the rows: lane l has quarter l / 16 of row
-// l % 16, D / 4 elements. Every row of a page may be read, so nothing is checked here: scores of keys that are not the part's
-// are masked, and their values get scale 0 (own). Where there is no page, all lanes read one place of page 0.
+// l % 16, D / 4 elements. `head`: where the head's rows of the page begin. Every row of a page may be read, so nothing is
+// checked here: scores of keys that are not the part's are masked, and their values get scale 0.
 template <int D>
 struct Rows16 {
   uint32_t codes[D / 32];
-  uint32_t byte;
-  __device__ __forceinline__ void load(const CacheArgs& c, const uint16_t* pages, int kvh, int page, int key, int lane) {
-    const int row0 = key & ((1 << c.page_shift) - 1);
-    const unsigned char* head = reinterpret_cast<const unsigned char*>(pages) + head_of<D>(c, max(page, 0), kvh);
-    const int row = lane & 15, quarter = lane >> 4;
-    const uint32_t at = page < 0 ? 0 : row * (D / 2) + quarter * (D / 8);
-    const uint32_t scale_at = page < 0 ? 0 : row * (D / 32) + quarter * (D / 32) / 4;
+  uint32_t scales;  // four of them: a byte would be widened at the end of the loop that loads it, which waits for it
+  __device__ __forceinline__ void load(const CacheArgs& c, const unsigned char* head, int row0, uint32_t at, uint32_t scale_at) {
     const unsigned char* from = head + row0 * (D / 2);
     if constexpr (D == 128) {
       const u32x4_t x = *reinterpret_cast<const u32x4_t*>(from + at);
@@ -430,41 +425,44 @@ struct Rows16 {
       codes[0] = x[0];
       codes[1] = x[1];
     }
-    byte = head[((D / 2) << c.page_shift) + row0 * (D / 32) + scale_at];
+    scales = *reinterpret_cast<const uint32_t*>(head + (((D / 2) << c.page_shift) + row0 * (D / 32)) + (scale_at & ~3u));
   }
+  __device__ __forceinline__ float scale(uint32_t scale_at) const { return scale_of(__builtin_amdgcn_ubfe(scales, 8 * (scale_at & 3u), 8)); }
 };
 
 // A narrow part: up to 16 R rows, whose four waves take every fourth step of 16 kTiles keys, each at its own pace. Keys go from
 // the loads' registers into the products (the elements of a head in the order in which the lanes have them, which
 // the queries follow); values through LDS, in 16 bits, where the transposing reads find them. The next
 // step's codes are asked for as soon as the last ones are converted.
-template <class T, int D, bool kPlain, int R, int kTiles>
-__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, const Part& p, int row0, unsigned char* stage,
+template <class T, int D, bool kPlain, int R, int kTiles, int kAhead>
+__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, const Part& p, int row0, unsigned char* stage,
                                             float (&s_ref)[4][32], float (&s_sum)[4][32], float* out, int lane, int wave) {
   using x8 = typename T::x8;
   constexpr int kStep = 16 * kTiles, kAtOnce = 64 / kTiles;
   constexpr int kParts = D / 32;  // products that a score sums
   const CacheArgs& c = a.c;
+  asm("" : "+v"(lane));  // (what a part makes of it is made again in each, and not kept through the others)
   const int l16 = lane & 15, g = lane >> 4;
   unsigned char* mine = stage + wave * 32 * 2 * D;
   const int steps = (p.end - p.key0 + kStep - 1) / kStep;
   const int mine_n = steps > wave ? (steps - wave + 3) / 4 : 0;
   auto key_of = [&](int n) { return p.key0 + (wave + 4 * n) * kStep; };
-  // lane n holds the page of the 16 keys n % kTiles of the wave's step n / kTiles (kAtOnce steps at a time); behind
-  // the part's end -1
-  auto page_at = [&](int n) { return page_of(c, p, key_of(n + lane / kTiles) + 16 * (lane % kTiles)); };
-  int pages = -1, next_pages = -1;
-  Rows16<D> k[kTiles], v[kTiles];
+  // lane n holds where the 16 keys n % kTiles of the wave's step n / kTiles have the head's rows of their page (kAtOnce steps
+  // at a time); page 0 where there is none
+  auto heads_at = [&](int n) { return head_of<D>(c, max(page_of(c, p, key_of(n + lane / kTiles) + 16 * (lane % kTiles)), 0), p.kvh); };
+  int64_t heads = 0, next_heads = 0;
+  const uint32_t code_at = l16 * (D / 2) + g * (D / 8), scale_at = l16 * (D / 32) + g * (D / 32) / 4;
+  Rows16<D> k_sets[kAhead][kTiles], v_sets[kAhead][kTiles];
   auto load = [&](int n, const uint16_t* from, Rows16<D> (&to)[kTiles]) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-      to[t].load(c, from, p.kvh, __builtin_amdgcn_readlane(pages, kTiles * (n % kAtOnce) + t), key_of(n) + 16 * t, lane);
+    for (int t = 0; t < kTiles; ++t) {
+      const int at = kTiles * (n % kAtOnce) + t;
+      const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(heads), at), hi = __builtin_amdgcn_readlane(static_cast<int>(heads >> 32), at);
+      to[t].load(c, reinterpret_cast<const unsigned char*>(from) + (static_cast<uint64_t>(hi) << 32 | lo),
+                 (key_of(n) + 16 * t) & ((1 << c.page_shift) - 1), code_at, scale_at);
+    }
   };
-  if (mine_n > 0) {
-    pages = page_at(0);
-    load(0, c.k_pages, k);
-    load(0, c.v_pages, v);
-  }
+  if (mine_n > 0) heads = heads_at(0);
   Part pr[R];
   x8 qf[R][kParts];
   float slope[R];
@@ -480,6 +478,18 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
     }
     slope[i] = kPlain ? 0.0f : slope_of(a.scoring, pr[i].h);
   }
+  if (mine_n > 0) {
+#pragma unroll
+    for (int n = 0; n < kAhead; ++n) {
+      load(n, c.k_pages, k_sets[n]);
+      load(n, c.v_pages, v_sets[n]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    arrived(qf[i]);
+    slope[i] = arrived(slope[i]);
+  }
   const float cexp = a.scoring.unit * kLog2e;
   // places in LDS: a lane's stores (piece (D / 32) g + s of row l16), its transposing reads (4 rows of the lane's
   // group, elements 16 db ..)
@@ -492,13 +502,13 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) acc[i][db] = f32x4_t{};
   QuarterSoftmax sm[R];
-  for (int n = 0; n < mine_n; ++n) {
-    if (n % kAtOnce == kAtOnce / 2) next_pages = page_at(n + kAtOnce / 2);
-    if (n % kAtOnce == kAtOnce - 1) pages = next_pages;
+  auto step = [&](int n, Rows16<D> (&k)[kTiles], Rows16<D> (&v)[kTiles]) {
+    if (n % kAtOnce == kAtOnce / 2) next_heads = heads_at(n + kAtOnce / 2);
+    if (n % kAtOnce == kAtOnce - kAhead) heads = next_heads;
     f32x4_t tile[R][kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const float scale = scale_of(k[t].byte);
+      const float scale = k[t].scale(scale_at);
 #pragma unroll
       for (int i = 0; i < R; ++i) tile[i][t] = f32x4_t{};
 #pragma unroll
@@ -508,7 +518,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
         for (int i = 0; i < R; ++i) tile[i][t] = Mfma16<T>::run(kf, qf[i][s], tile[i][t]);
       }
     }
-    load(n + 1, c.k_pages, k);
+    load(n + kAhead, c.k_pages, k);
     x8 pb[R][kTiles / 2];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -552,34 +562,45 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
       for (int t = 0; t < 2; ++t) {
         const Rows16<D>& y = v[2 * u + t];
         const int key = key_of(n) + 32 * u + 16 * t + l16;
-        const float scale = key >= p.lo && key < p.end ? scale_of(y.byte) : 0.0f;
+        const float scale = key >= p.lo && key < p.end ? y.scale(scale_at) : 0.0f;
 #pragma unroll
         for (int s = 0; s < kParts; ++s) *reinterpret_cast<u32x4_t*>(mine + 32 * D * t + (to ^ 16 * s)) = values<T>(y.codes[s], scale);
       }
-      if (u == kTiles / 2 - 1) load(n + 1, c.v_pages, v);
+      if (u == kTiles / 2 - 1) load(n + kAhead, c.v_pages, v);
       asm volatile("" ::: "memory");  // (a wave's LDS accesses are done in order)
+      x8 vf[D / 16];
 #pragma unroll
       for (int db = 0; db < D / 16; ++db) {
         const lds_u8_t* at = (const lds_u8_t*)mine + (from ^ 32 * db);
         const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)at);
         const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t*)(at + 32 * D));
-        const x8 vf = __builtin_bit_cast(x8, (i16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}));
-#pragma unroll
-        for (int i = 0; i < R; ++i) acc[i][db] = Mfma16<T>::run(vf, pb[i][u], acc[i][db]);
+        vf[db] = __builtin_bit_cast(x8, (i16x8_t{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}));
       }
+      __builtin_amdgcn_sched_barrier(0);  // (all of them are asked for before the first is waited for)
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+        for (int i = 0; i < R; ++i) acc[i][db] = Mfma16<T>::run(vf[db], pb[i][u], acc[i][db]);
       asm volatile("" ::: "memory");
     }
+  };
+  for (int n = 0; n < mine_n; n += kAhead) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (i == 0 || n + i < mine_n) step(n + i, k_sets[i], v_sets[i]);
   }
 
   // the waves' results against their common reference, summed in the order of the waves; the
   // 16-byte pieces of a row are turned by its number, against bank conflicts
+  asm("" : "+v"(lane));  // (these places are not made ahead of the loop, and kept through it)
+  const int r16 = lane & 15, quarter = lane >> 4;
   float l[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     l[i] = sum_quarters(sm[i].l);
-    if (g == 0) {
-      s_ref[wave][16 * i + l16] = sm[i].m;
-      s_sum[wave][16 * i + l16] = l[i];
+    if (quarter == 0) {
+      s_ref[wave][16 * i + r16] = sm[i].m;
+      s_sum[wave][16 * i + r16] = l[i];
     }
   }
   __syncthreads();  // (also: every wave has read its stage)
@@ -590,13 +611,13 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
   for (int i = 0; i < R; ++i) {
     const int live = min(16, rows - 16 * i);
     if (i > 0) __syncthreads();
-    if (l16 < live) {
-      const int r = 16 * i + l16;
+    if (r16 < live) {
+      const int r = 16 * i + r16;
       const float top = fmaxf(fmaxf(s_ref[0][r], s_ref[1][r]), fmaxf(s_ref[2][r], s_ref[3][r]));
       const float f = factor(sm[i].m, top, cexp);
-      f32x4_t* at = reinterpret_cast<f32x4_t*>(stage) + (wave * 16 + l16) * kPieces;
+      f32x4_t* at = reinterpret_cast<f32x4_t*>(stage) + (wave * 16 + r16) * kPieces;
 #pragma unroll
-      for (int db = 0; db < D / 16; ++db) at[(4 * db + g) ^ (l16 & 7)] = acc[i][db] * f;
+      for (int db = 0; db < D / 16; ++db) at[(4 * db + quarter) ^ (r16 & 7)] = acc[i][db] * f;
     }
     __syncthreads();
     if (out) {
@@ -624,10 +645,11 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 // A wide part, whose waves share blocks of 64 keys: each brings 16 keys and values, in 16 bits into one of two
 // buffers.
 template <class T, int D, bool kPlain>
-__device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, Part& p, unsigned char* stage, float* out, int lane,
+__device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, Part& p, unsigned char* stage, float* out, int lane,
                                           int wave) {
   constexpr int kTile = kCacheWideBlock * 2 * D;
   const CacheArgs& c = a.c;
+  asm("" : "+v"(lane));  // (as above)
   const int l32 = lane & 31, hlf = lane >> 5;
   const int nb = (p.end - p.key0 + kCacheWideBlock - 1) / kCacheWideBlock;
   // lane n holds the page of the wave's keys of block n (64 blocks at a time)
@@ -705,23 +727,22 @@ __global__ __launch_bounds__(kThreads, few ? kCache4Few : kCacheGroups) void cac
   static_assert(sizeof(stage) >= kCacheGroupBytes, "the groups, before the buffers");
   static_assert(few || sizeof(stage) == 2 * 2 * kCacheWideBlock * 2 * D, "a wide part's buffers");
   static_assert(sizeof(stage) >= 4 * 32 * 2 * D && sizeof(stage) >= 4 * 16 * D * 4, "the narrow waves' values, and results of theirs");
-  int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  cache_run(a, stage, [&](const Entry& x, const Entry* local, Part& p, int64_t place, bool wide) {
-    asm("" : "+v"(lane));  // (what a part makes of it is made again in each, and not kept through the others)
+  cache_run(a, stage, [&](const Entry& x, const KeptEntry* local, Part& p, int64_t place, bool wide) {
     if constexpr (few) {
       const int first = p.tile;
       for (int r = first * kCacheTileRows; r < min(x.rows, first * kCacheTileRows + kCacheWideRows); r += 16) {
         p.tile = r / kCacheTileRows;
-        narrow_part<T, D, kPlain, 1, 2>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, part_at<D>(a, place + p.tile - first), lane, wave);
+        narrow_part<T, D, kPlain, 1, 2, 1>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, part_at<D>(a, place + p.tile - first), lane, wave);
       }
     } else if (wide) {
       p.tile += wave;
       wide_part<T, D, kPlain>(a, x, local, p, stage, part_at<D>(a, place + wave), lane, wave);
     } else if (x.rows <= 16) {
-      narrow_part<T, D, kPlain, 1, 4>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+      narrow_part<T, D, kPlain, 1, 4, 1>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
     } else {
-      narrow_part<T, D, kPlain, 2, 2>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+      narrow_part<T, D, kPlain, 2, 2, 1>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
     }
   });
 }

@@ -151,7 +151,7 @@ __device__ __forceinline__ void load_16(const CacheArgs& c, const uint16_t* page
 // Two workgroups a CU keep 128 KiB in flight, and one streams while the other begins or ends
 // a part.
 template <class T, int D, bool kPlain>
-__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, Part& p, unsigned char* stage, float (&s_ref)[4][32],
+__device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, Part& p, unsigned char* stage, float (&s_ref)[4][32],
                                             float (&s_sum)[4][32], float* out, int lane, int wave) {
   constexpr int kTile = kCacheBlock * 2 * D, kLoads = kCacheBlock / kLoadRows<D>;
   const CacheArgs& c = a.c;
@@ -264,7 +264,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 
 // A wide part: blocks of 64 keys in two buffers, which all waves read.
 template <class T, int D, bool kPlain>
-__device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, const Entry* local, Part& p, unsigned char* stage, float* out, int lane,
+__device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, Part& p, unsigned char* stage, float* out, int lane,
                                           int wave) {
   constexpr int kTile = kCacheWideBlock * 2 * D;
   const CacheArgs& c = a.c;
@@ -346,7 +346,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
   static_assert(sizeof(stage) >= 4 * 32 * D * 4, "and the waves' results");
   static_assert(sizeof(stage) >= kCacheGroupBytes, "and, before, the groups");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  cache_run(a, stage, [&](const Entry& x, const Entry* local, Part& p, int64_t place, bool wide) {
+  cache_run(a, stage, [&](const Entry& x, const KeptEntry* local, Part& p, int64_t place, bool wide) {
     if (wide) {
       p.tile += wave;
       wide_part<T, D, kPlain>(a, x, local, p, stage, part_at<D>(a, place + wave), lane, wave);

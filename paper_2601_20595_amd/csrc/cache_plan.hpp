@@ -33,11 +33,20 @@ struct Entry {
   int own;             // the keys of one sequence, up to its end
   int group;           // its group, -1: none
   int block0, blocks;  // blocks of keys that hold them
+  __device__ __forceinline__ void count_blocks() {
+    block0 = lo / kCacheBlock;
+    blocks = end > lo && rows > 0 ? (end + kCacheBlock - 1) / kCacheBlock - block0 : 0;
+  }
   __device__ __forceinline__ int tiles() const { return (rows + kCacheTileRows - 1) / kCacheTileRows; }
   __device__ __forceinline__ bool wide() const { return rows > kCacheTileRows; }
   __device__ __forceinline__ int tasks() const { return wide() ? (rows + kCacheWideRows - 1) / kCacheWideRows : 1; }
   // a task's units of work: its blocks, behind what beginning and ending it costs
   __device__ __forceinline__ int span() const { return blocks > 0 ? kCacheTaskCost + blocks : 0; }
+};
+
+// What is kept of an entry in LDS.
+struct KeptEntry {
+  int token0, rows, b0, b1, lo, end;
 };
 
 // The groups of a call where they are given.
@@ -95,8 +104,7 @@ __device__ __forceinline__ Entry entry_of(const CacheAttnArgs& a, const Groups& 
   }
   x.token0 = first_token(c, x.b0);
   x.rows = x.b1 > x.b0 ? max(0, first_token(c, x.b1) - x.token0) * (c.H / c.Hkv) : 0;
-  x.block0 = x.lo / kCacheBlock;
-  x.blocks = x.end > x.lo && x.rows > 0 ? (x.end + kCacheBlock - 1) / kCacheBlock - x.block0 : 0;
+  x.count_blocks();
   return x;
 }
 
@@ -127,7 +135,7 @@ struct Part {
 };
 
 // `local`: the sequences' entries, where they are in LDS.
-__device__ __forceinline__ void locate_row(const CacheAttnArgs& a, const Entry& x, const Entry* local, int l32, Part& p) {
+__device__ __forceinline__ void locate_row(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, int l32, Part& p) {
   const CacheArgs& c = a.c;
   const int G = c.H / c.Hkv;
   const int r = p.tile * kCacheTileRows + l32;
@@ -206,7 +214,7 @@ template <class DoPart>
 __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char* stage, DoPart do_part) {
   __shared__ uint32_t s_wave_units[4], s_wave_tiles[4];
   __shared__ int s_entry, s_first, s_tiles;
-  __shared__ Entry s_entries[kThreads];
+  __shared__ KeptEntry s_entries[kThreads];
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_entries = a.n_groups + c.batch;
@@ -230,11 +238,13 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
   // has one entry, everyone finds it in LDS.
   const int per = (n_entries + kThreads - 1) / kThreads;
   uint32_t units = 0, tiles = 0;
+  Entry mine{};
   for (int i = 0; i < per; ++i) {
     const int e = tid * per + i;
     if (e >= n_entries) break;
     const Entry x = entry_of(a, local, e);
-    if (per == 1) s_entries[e] = x;
+    mine = x;
+    if (per == 1) s_entries[e] = {x.token0, x.rows, x.b0, x.b1, x.lo, x.end};
     units += x.tasks() * x.span();
     tiles += x.tiles();
   }
@@ -271,7 +281,7 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
     for (int i = 0; i < per; ++i) {
       const int e = tid * per + i;
       if (e >= n_entries) break;
-      const Entry x = per == 1 ? s_entries[e] : entry_of(a, local, e);
+      const Entry x = per == 1 ? mine : entry_of(a, local, e);
       const int n = x.tasks() * x.span();
       if (before <= begin && begin < before + n) {
         s_entry = e;
@@ -296,7 +306,7 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
   int e = __builtin_amdgcn_readfirstlane(s_entry), in_entry = __builtin_amdgcn_readfirstlane(s_first);
   int tiles_before = __builtin_amdgcn_readfirstlane(s_tiles);
   const int64_t places = static_cast<int64_t>(kvh) * (all_tiles + 4 * a.head_workers) + 4 * w;
-  const Entry* sequences = per == 1 ? s_entries + a.n_groups : nullptr;
+  const KeptEntry* sequences = per == 1 ? s_entries + a.n_groups : nullptr;
   while (left > 0) {
     Entry x;
     if (per == 1) {
@@ -307,9 +317,8 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
       x.b1 = __builtin_amdgcn_readfirstlane(s_entries[e].b1);
       x.lo = __builtin_amdgcn_readfirstlane(s_entries[e].lo);
       x.end = __builtin_amdgcn_readfirstlane(s_entries[e].end);
-      x.own = __builtin_amdgcn_readfirstlane(s_entries[e].own);
-      x.block0 = __builtin_amdgcn_readfirstlane(s_entries[e].block0);
-      x.blocks = __builtin_amdgcn_readfirstlane(s_entries[e].blocks);
+      x.own = e >= a.n_groups;
+      x.count_blocks();
     } else {
       x = entry_of(a, GlobalGroups{a}, e);
     }
