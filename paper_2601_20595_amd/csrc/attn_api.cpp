@@ -193,7 +193,7 @@ csg_status check_cache_attn(csg_cache_cfg* c) {
   const int64_t tiles = csg::cache_max_tiles(c->n_heads, c->n_kv_heads, c->tokens, c->batch, c->n_groups);
   const int64_t tasks = tiles / 4 + c->batch + c->n_groups;
   const int64_t blocks = static_cast<int64_t>(c->max_pages) * c->page_size / csg::kCacheBlock + 1;
-  if (tasks > 0 && blocks + csg::kCacheTaskCost > 0x7fffffff / tasks)
+  if (tasks > 0 && blocks + std::max(csg::kCacheTaskCost, csg::kCache4TaskCost) > 0x7fffffff / tasks)
     return fail(CSG_ERR_UNSUPPORTED, "max_pages pages for every sequence are too many keys for one launch");
   return CSG_OK;
 }
@@ -316,6 +316,7 @@ csg_status cache_attn(hipError_t (*launch)(const csg::CacheAttnArgs&, bool, int,
   a.n_groups = c.n_groups;
   a.head_workers = csg::cache_head_workers(groups, c.n_kv_heads);
   a.dies = 8 / std::gcd(8, c.n_kv_heads);
+  a.task_cost = four ? csg::kCache4TaskCost : csg::kCacheTaskCost;
   a.max_parts = csg::cache_max_parts(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups, a.head_workers);
   a.max_tiles = csg::cache_max_tiles(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups);
   a.ws = static_cast<unsigned char*>(workspace);

@@ -289,42 +289,6 @@ __global__ __launch_bounds__(kThreads) void cache4_read(ReadArgs a) {
 // Entries, tasks and runs are those of the cache in 16 bits (cache_plan.hpp), and so are the parts, which
 // its cache_merge joins.
 
-// Codes and scale of a lane's elements of 16 rows of a head: lane l has a quarter of row l / 4.
-template <int D>
-struct Quarter {
-  uint32_t codes[D / 32];
-  uint32_t byte;
-  // Rows key .. key + 15 of page (-1: none); those outside of the part's keys read zeros.
-  __device__ __forceinline__ void load(const CacheArgs& c, const uint16_t* pages, const Part& p, int page, int key, int lane) {
-    const int row = lane >> 2, quarter = lane & 3;
-    const unsigned char* head = reinterpret_cast<const unsigned char*>(pages) + head_of<D>(c, max(page, 0), p.kvh);
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(head, page < 0 ? 0 : static_cast<int>(head_bytes<D>(c)));
-    const int r = (key & ((1 << c.page_shift) - 1)) + row;
-    const bool in = key + row >= p.lo && key + row < p.end;
-    const int at = in ? r * (D / 2) + quarter * (D / 8) : 1 << 30;
-    const int scale_at = in ? ((D / 2) << c.page_shift) + r * (D / 32) + quarter * (D / 32) / 4 : 1 << 30;
-    if constexpr (D == 128) {
-      const u32x4_t x = __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) codes[i] = x[i];
-    } else {
-      const u32x2_t x = __builtin_amdgcn_raw_buffer_load_b64(rs, at, 0, 0);
-      codes[0] = x[0];
-      codes[1] = x[1];
-    }
-    byte = __builtin_amdgcn_raw_buffer_load_b8(rs, scale_at, 0, 0);
-  }
-  // Into a tile of 16-bit rows, the 16 rows beginning at `to`.
-  template <class T>
-  __device__ __forceinline__ void store(unsigned char* to, int lane) const {
-    const int row = lane >> 2, quarter = lane & 3;
-    const float scale = scale_of(byte);
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-      *reinterpret_cast<u32x4_t*>(to + row * 2 * D + 16 * ((quarter * (D / 32) + i) ^ swz<D>(row))) = values<T>(codes[i], scale);
-  }
-};
-
 // Combination of the four lanes of a row: lane ^ 16, then lane ^ 32, swapped as in max_halves.
 __device__ __forceinline__ float max_quarters(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -407,13 +371,15 @@ __device__ __forceinline__ constexpr int swz16(int r) {
   return D == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r >> 1 & 3) << 1 | (r >> 3 & 1);
 }
 
-// Codes and scales of 16 rows of a head, as v_mfma_f32_16x16x32 takes the rows: lane l has quarter l / 16 of row
-// l % 16, D / 4 elements. `head`: where the head's rows of the page begin. Every row of a page may be read, so nothing is
-// checked here: scores of keys that are not the part's are masked, and their values get scale 0.
+// A quarter of a row's codes, D / 4 elements, and its scale. `head`: where the head's rows of the page begin; the lane's
+// row and quarter are in `at` and `scale_at`, from row0 on. Every row of a page may be read, so nothing is checked here:
+// scores of keys that are not the part's are masked, and their values get scale 0.
 template <int D>
-struct Rows16 {
+struct Quarter {
   uint32_t codes[D / 32];
   uint32_t scales;  // four of them: a byte would be widened at the end of the loop that loads it, which waits for it
+  static __device__ __forceinline__ uint32_t code_place(int row, int quarter) { return row * (D / 2) + quarter * (D / 8); }
+  static __device__ __forceinline__ uint32_t scale_place(int row, int quarter) { return row * (D / 32) + quarter * (D / 32) / 4; }
   __device__ __forceinline__ void load(const CacheArgs& c, const unsigned char* head, int row0, uint32_t at, uint32_t scale_at) {
     const unsigned char* from = head + row0 * (D / 2);
     if constexpr (D == 128) {
@@ -429,6 +395,40 @@ struct Rows16 {
   }
   __device__ __forceinline__ float scale(uint32_t scale_at) const { return scale_of(__builtin_amdgcn_ubfe(scales, 8 * (scale_at & 3u), 8)); }
 };
+
+// Half a row's codes and all of its scales, of rows l32 of 32: the first 16 from row0 of head, the others from row1 of head1.
+template <int D>
+struct Half {
+  uint32_t codes[D / 16];
+  uint32_t scales;
+  __device__ __forceinline__ void load(const CacheArgs& c, const unsigned char* head, int row0, const unsigned char* head1, int row1, int l32,
+                                       int hlf) {
+    const bool second = l32 >= 16;
+    const unsigned char* from = second ? head1 : head;
+    const int row = (second ? row1 : row0) + (l32 & 15);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(from + row * (D / 2) + hlf * (D / 4) + 16 * i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) codes[4 * i + k] = x[k];
+    }
+    const uint32_t at = ((D / 2) << c.page_shift) + row * (D / 32);
+    if constexpr (D == 128)
+      scales = *reinterpret_cast<const uint32_t*>(from + at);
+    else
+      scales = *reinterpret_cast<const uint16_t*>(from + at);
+  }
+  // of codes[s]
+  __device__ __forceinline__ float scale(int s, int hlf) const {
+    return scale_of(__builtin_amdgcn_ubfe(scales, 8 * (hlf * (D / 64) + s / 4), 8));
+  }
+};
+
+// Where 16 keys' rows of the head begin, of those that lane `at` of `heads` knows.
+__device__ __forceinline__ const unsigned char* head_in(const uint16_t* pages, int64_t heads, int at) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(heads), at), hi = __builtin_amdgcn_readlane(static_cast<int>(heads >> 32), at);
+  return reinterpret_cast<const unsigned char*>(pages) + (static_cast<uint64_t>(hi) << 32 | lo);
+}
 
 // A narrow part: up to 16 R rows, whose four waves take every fourth step of 16 kTiles keys, each at its own pace. Keys go from
 // the loads' registers into the products (the elements of a head in the order in which the lanes have them, which
@@ -451,16 +451,12 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
   // at a time); page 0 where there is none
   auto heads_at = [&](int n) { return head_of<D>(c, max(page_of(c, p, key_of(n + lane / kTiles) + 16 * (lane % kTiles)), 0), p.kvh); };
   int64_t heads = 0, next_heads = 0;
-  const uint32_t code_at = l16 * (D / 2) + g * (D / 8), scale_at = l16 * (D / 32) + g * (D / 32) / 4;
-  Rows16<D> k_sets[kAhead][kTiles], v_sets[kAhead][kTiles];
-  auto load = [&](int n, const uint16_t* from, Rows16<D> (&to)[kTiles]) {
+  const uint32_t code_at = Quarter<D>::code_place(l16, g), scale_at = Quarter<D>::scale_place(l16, g);
+  Quarter<D> k_sets[kAhead][kTiles], v_sets[kAhead][kTiles];
+  auto load = [&](int n, const uint16_t* from, Quarter<D> (&to)[kTiles]) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      const int at = kTiles * (n % kAtOnce) + t;
-      const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(heads), at), hi = __builtin_amdgcn_readlane(static_cast<int>(heads >> 32), at);
-      to[t].load(c, reinterpret_cast<const unsigned char*>(from) + (static_cast<uint64_t>(hi) << 32 | lo),
-                 (key_of(n) + 16 * t) & ((1 << c.page_shift) - 1), code_at, scale_at);
-    }
+    for (int t = 0; t < kTiles; ++t)
+      to[t].load(c, head_in(from, heads, kTiles * (n % kAtOnce) + t), (key_of(n) + 16 * t) & ((1 << c.page_shift) - 1), code_at, scale_at);
   };
   if (mine_n > 0) heads = heads_at(0);
   Part pr[R];
@@ -502,7 +498,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) acc[i][db] = f32x4_t{};
   QuarterSoftmax sm[R];
-  auto step = [&](int n, Rows16<D> (&k)[kTiles], Rows16<D> (&v)[kTiles]) {
+  auto step = [&](int n, Quarter<D> (&k)[kTiles], Quarter<D> (&v)[kTiles]) {
     if (n % kAtOnce == kAtOnce / 2) next_heads = heads_at(n + kAtOnce / 2);
     if (n % kAtOnce == kAtOnce - kAhead) heads = next_heads;
     f32x4_t tile[R][kTiles];
@@ -560,7 +556,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
     for (int u = 0; u < kTiles / 2; ++u) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const Rows16<D>& y = v[2 * u + t];
+        const Quarter<D>& y = v[2 * u + t];
         const int key = key_of(n) + 32 * u + 16 * t + l16;
         const float scale = key >= p.lo && key < p.end ? y.scale(scale_at) : 0.0f;
 #pragma unroll
@@ -642,64 +638,88 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
   __syncthreads();  // the stages are free again
 }
 
-// A wide part, whose waves share blocks of 64 keys: each brings 16 keys and values, in 16 bits into one of two
-// buffers.
+// A wide part, whose waves share blocks of 64 keys. Each wave has 32 rows; it converts all of the keys for itself, from
+// registers (lane l has half l / 32 of the rows l % 32 and 32 + l % 32, which the queries follow), and 16 of the values
+// (a quarter of row l / 4) for all, through one of two buffers in LDS.
 template <class T, int D, bool kPlain>
 __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, Part& p, unsigned char* stage, float* out, int lane,
                                           int wave) {
+  using x8 = typename T::x8;
   constexpr int kTile = kCacheWideBlock * 2 * D;
   const CacheArgs& c = a.c;
   asm("" : "+v"(lane));  // (as above)
   const int l32 = lane & 31, hlf = lane >> 5;
+  const int row = lane >> 2, quarter = lane & 3;
   const int nb = (p.end - p.key0 + kCacheWideBlock - 1) / kCacheWideBlock;
-  // lane n holds the page of the wave's keys of block n (64 blocks at a time)
-  int pages = -1;
-  auto fetch = [&](int n) { pages = page_of(c, p, p.key0 + (n + lane) * kCacheWideBlock + 16 * wave); };
-  Quarter<D> k, v;
-  auto load = [&](int n) {
-    if (n > 0 && (n & 63) == 0) fetch(n);
-    const int page = __builtin_amdgcn_readlane(pages, n & 63), key = p.key0 + n * kCacheWideBlock + 16 * wave;
-    k.load(c, c.k_pages, p, page, key, lane);
-    v.load(c, c.v_pages, p, page, key, lane);
+  auto key_of = [&](int n) { return p.key0 + n * kCacheWideBlock; };
+  // lane n holds where the 16 keys n % 4 of block n / 4 have the head's rows of their page (16 blocks at a time)
+  auto heads_at = [&](int n) { return head_of<D>(c, max(page_of(c, p, key_of(n + lane / 4) + 16 * (lane % 4)), 0), p.kvh); };
+  int64_t heads = heads_at(0), next_heads = 0;
+  const int in_page = (1 << c.page_shift) - 1;
+  const uint32_t v_at = Quarter<D>::code_place(row, quarter), v_scale_at = Quarter<D>::scale_place(row, quarter);
+  Half<D> k[2];
+  Quarter<D> v;
+  auto load_k = [&](int n, int kb) {
+    // (the 32 keys may lie in two pages of 16)
+    const int at = 4 * (n & 15) + 2 * kb, key = key_of(n) + 32 * kb;
+    k[kb].load(c, head_in(c.k_pages, heads, at), key & in_page, head_in(c.k_pages, heads, at + 1), (key + 16) & in_page, l32, hlf);
   };
-  fetch(0);
-  load(0);
+  auto load_v = [&](int n) {
+    v.load(c, head_in(c.v_pages, heads, 4 * (n & 15) + wave), (key_of(n) + 16 * wave) & in_page, v_at, v_scale_at);
+  };
   locate_row(a, x, local, l32, p);
-  typename T::x8 qf[D / 16];
-  load_queries<T, D>(a, p, hlf, qf);
-  const float slope = kPlain ? 0.0f : slope_of(a.scoring, p.h);
+  x8 qf[D / 16];
+  const uint16_t* q = c.Q + p.token * c.q_stride + p.h * D + (D / 2) * hlf;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    const u32x4_t raw = p.ok ? *reinterpret_cast<const u32x4_t*>(q + 8 * s) : u32x4_t{0u, 0u, 0u, 0u};
+    qf[s] = __builtin_bit_cast(x8, raw);
+  }
+  float slope = kPlain ? 0.0f : slope_of(a.scoring, p.h);
+  load_v(0);
+  load_k(0, 0);
+  load_k(0, 1);
+  arrived(qf);
+  slope = arrived(slope);
   const float cexp = a.scoring.unit * kLog2e;
   const Frags<D> fr(lane);
   f32x16_t acc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) acc[db] = f32x16_t{};
   RowSoftmax sm;
-  const bool idle = p.tile * kCacheTileRows >= x.rows;  // no row in this wave
+  const int to = (16 * wave + row) * 2 * D + 16 * ((quarter * (D / 32)) ^ swz<D>(row));
   for (int n = 0; n < nb; ++n) {
-    unsigned char* kt = stage + (n & 1) * 2 * kTile;
-    k.template store<T>(kt + wave * 16 * 2 * D, lane);
-    v.template store<T>(kt + kTile + wave * 16 * 2 * D, lane);
-    if (n + 1 < nb) load(n + 1);
-    __syncthreads();  // block n is there, and everyone is done with block n - 1
-    if (idle) continue;
-    f32x16_t sc[2] = {f32x16_t{}, f32x16_t{}};
+    if ((n & 15) == 8) next_heads = heads_at(n + 8);
+    if ((n & 15) == 15) heads = next_heads;
+    unsigned char* vt = stage + (n & 1) * kTile;
+    const int key = key_of(n) + 16 * wave + row;
+    const float v_scale = key >= p.lo && key < p.end ? v.scale(v_scale_at) : 0.0f;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s)
+    for (int i = 0; i < D / 32; ++i) *reinterpret_cast<u32x4_t*>(vt + (to ^ 16 * i)) = values<T>(v.codes[i], v_scale);
+    load_v(n + 1);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) sc[kb] = T::mfma(row_frag<T, D>(kt, fr, s, 32 * kb), qf[s], sc[kb]);
-    finish_scores<2, kPlain>(a, p, slope, p.key0 + n * kCacheWideBlock, hlf, sc);
-    typename T::x8 pb[4];
-    bool moved;
-    const float alpha = sm.block<T, 2>(sc, cexp, pb, moved);
-    if (moved) {
+    for (int kb = 0; kb < 2; ++kb) {
+      f32x16_t sc[1] = {f32x16_t{}};
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
+      for (int s = 0; s < D / 16; ++s)
+        sc[0] = T::mfma(__builtin_bit_cast(x8, values<T>(k[kb].codes[s], k[kb].scale(s, hlf))), qf[s], sc[0]);
+      load_k(n + 1, kb);
+      finish_scores<1, kPlain>(a, p, slope, key_of(n) + 32 * kb, hlf, sc);
+      x8 pb[2];
+      bool moved;
+      const float alpha = sm.block<T, 1>(sc, cexp, pb, moved);
+      if (moved) {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
+      }
+      if (kb == 0) __syncthreads();  // block n's values are there, and everyone is done with those of block n - 1
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+          acc[db] = T::mfma(col_frag<T, D>((const lds_u8_t*)vt, fr, db, 32 * kb + 16 * t), pb[t], acc[db]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-        acc[db] = T::mfma(col_frag<T, D>((const lds_u8_t*)(kt + kTile), fr, db, 16 * t), pb[t], acc[db]);
   }
   const float l = sum_halves(sm.l);
   if (out && p.ok) {

@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void cache_append(AppendArgs a) {
 // task: the four waves take different blocks of 32 keys for the same rows, each at its own
 // pace. More rows make wide tasks of 128, 32 a wave, whose waves share the keys. Every key/value
 // head has the same number of workgroups. All tasks' blocks of 32 keys stand in one row (by
-// entry, task, block), each task's behind kCacheTaskCost empty ones, and the row is cut into equal
+// entry, task, block), each task's behind as many empty ones as it costs, and the row is cut into equal
 // runs, one a workgroup of the head: every workgroup has the same to do, whatever the lengths
 // are. What a workgroup has of a task is a
 // part: for each tile of 32 rows, its weights' sums and products against its own reference,
@@ -382,7 +382,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge(CacheAttnArgs a) {
     if (x.blocks == 0 || r < 0 || r >= x.rows) continue;
     const int tile = r / kCacheTileRows, in_tile = r % kCacheTileRows;
     // the first block's unit of its task
-    const int start = x.before + (x.rows > kCacheTileRows ? r / kCacheWideRows : 0) * (x.blocks + kCacheTaskCost) + kCacheTaskCost;
+    const int start = x.before + (x.rows > kCacheTileRows ? r / kCacheWideRows : 0) * (x.blocks + a.task_cost) + a.task_cost;
     const int w0 = start / plan.run, w1 = (start + x.blocks - 1) / plan.run;
     const int64_t first = static_cast<int64_t>(kvh) * (plan.tiles + 4 * a.head_workers) + x.tiles + tile + 4 * w0;
     const int parts = static_cast<int>(min<int64_t>(w1 - w0 + 1, (a.max_parts - first + 3) / 4));

@@ -41,7 +41,7 @@ struct Entry {
   __device__ __forceinline__ bool wide() const { return rows > kCacheTileRows; }
   __device__ __forceinline__ int tasks() const { return wide() ? (rows + kCacheWideRows - 1) / kCacheWideRows : 1; }
   // a task's units of work: its blocks, behind what beginning and ending it costs
-  __device__ __forceinline__ int span() const { return blocks > 0 ? kCacheTaskCost + blocks : 0; }
+  __device__ __forceinline__ int span(int cost) const { return blocks > 0 ? cost + blocks : 0; }
 };
 
 // What is kept of an entry in LDS.
@@ -245,7 +245,7 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
     const Entry x = entry_of(a, local, e);
     mine = x;
     if (per == 1) s_entries[e] = {x.token0, x.rows, x.b0, x.b1, x.lo, x.end};
-    units += x.tasks() * x.span();
+    units += x.tasks() * x.span(a.task_cost);
     tiles += x.tiles();
   }
   const uint32_t own_units = units, own_tiles = tiles;
@@ -282,7 +282,7 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
       const int e = tid * per + i;
       if (e >= n_entries) break;
       const Entry x = per == 1 ? mine : entry_of(a, local, e);
-      const int n = x.tasks() * x.span();
+      const int n = x.tasks() * x.span(a.task_cost);
       if (before <= begin && begin < before + n) {
         s_entry = e;
         s_first = begin - before;
@@ -322,14 +322,14 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
     } else {
       x = entry_of(a, GlobalGroups{a}, e);
     }
-    const int n = x.tasks() * x.span();
+    const int n = x.tasks() * x.span(a.task_cost);
     if (in_entry < n) {
       Part p;
       p.kvh = kvh;
       const bool wide = x.wide();
-      const int task = wide ? __builtin_amdgcn_readfirstlane(in_entry / x.span()) : 0;
-      const int from = in_entry - task * x.span(), take = min(x.span() - from, left);
-      const int first = max(0, from - kCacheTaskCost), count = from + take - kCacheTaskCost - first;
+      const int task = wide ? __builtin_amdgcn_readfirstlane(in_entry / x.span(a.task_cost)) : 0;
+      const int from = in_entry - task * x.span(a.task_cost), take = min(x.span(a.task_cost) - from, left);
+      const int first = max(0, from - a.task_cost), count = from + take - a.task_cost - first;
       left -= take;
       in_entry += take;
       if (count <= 0) continue;
