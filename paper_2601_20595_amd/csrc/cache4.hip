@@ -697,27 +697,38 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) *reinterpret_cast<u32x4_t*>(vt + (to ^ 16 * i)) = values<T>(v.codes[i], v_scale);
     load_v(n + 1);
+    f32x16_t sc[2] = {f32x16_t{}, f32x16_t{}};
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      f32x16_t sc[1] = {f32x16_t{}};
+    for (int s = 0; s < D / 16; ++s) {
 #pragma unroll
-      for (int s = 0; s < D / 16; ++s)
-        sc[0] = T::mfma(__builtin_bit_cast(x8, values<T>(k[kb].codes[s], k[kb].scale(s, hlf))), qf[s], sc[0]);
-      load_k(n + 1, kb);
-      finish_scores<1, kPlain>(a, p, slope, key_of(n) + 32 * kb, hlf, sc);
-      x8 pb[2];
-      bool moved;
-      const float alpha = sm.block<T, 1>(sc, cexp, pb, moved);
-      if (moved) {
+      for (int kb = 0; kb < 2; ++kb)
+        sc[kb] = T::mfma(__builtin_bit_cast(x8, values<T>(k[kb].codes[s], k[kb].scale(s, hlf))), qf[s], sc[kb]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(n + 1, 0);
+    load_k(n + 1, 1);
+    finish_scores<2, kPlain>(a, p, slope, key_of(n), hlf, sc);
+    x8 pb[4];
+    bool moved;
+    const float alpha = sm.block<T, 2>(sc, cexp, pb, moved);
+    if (moved) {
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
-      }
-      if (kb == 0) __syncthreads();  // block n's values are there, and everyone is done with those of block n - 1
+      for (int db = 0; db < D / 32; ++db) acc[db] *= alpha;
+    }
+    __syncthreads();  // block n's values are there, and everyone is done with those of block n - 1
+    // (a quarter of the values is on its way to the registers while the one before is multiplied)
+    x8 vf[2][D / 32];
+    auto read = [&](int t) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int db = 0; db < D / 32; ++db) vf[t & 1][db] = col_frag<T, D>((const lds_u8_t*)vt, fr, db, 16 * t);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    read(0);
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-          acc[db] = T::mfma(col_frag<T, D>((const lds_u8_t*)vt, fr, db, 32 * kb + 16 * t), pb[t], acc[db]);
+    for (int t = 0; t < 4; ++t) {
+      if (t < 3) read(t + 1);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) acc[db] = T::mfma(vf[t & 1][db], pb[t], acc[db]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
