@@ -443,6 +443,7 @@ csg_status csg_cache4_read(const csg_cache_cfg* cfg, const void* k_pages, const 
   a.V = static_cast<uint16_t*>(v);
   a.k_stride = c.k_stride;
   a.v_stride = c.v_stride;
+  a.heads = csg::cache4_read_heads(c.tokens, c.n_kv_heads, cus);
   CSG_HIP(csg::launch_cache4_read(a, c.dtype == CSG_F16, c.head_dim, static_cast<hipStream_t>(stream)));
   return CSG_OK;
 }

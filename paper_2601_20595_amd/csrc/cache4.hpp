@@ -23,12 +23,19 @@ inline bool cache4_few(int64_t tokens, int32_t H, int32_t Hkv, int32_t batch, in
   return n_groups == 0 && tokens * (H / Hkv) <= int64_t{16} * batch;
 }
 constexpr int kReadRows = 32;  // rows of the outputs that a workgroup reads
+// Heads that it reads: as many as leave four workgroups a CU, up to 8.
+inline int32_t cache4_read_heads(int64_t tokens, int32_t Hkv, int32_t cus) {
+  int32_t heads = 1;
+  while (heads < 8 && Hkv % (2 * heads) == 0 && (tokens / kReadRows + 1) * (Hkv / (2 * heads)) >= 4 * cus) heads *= 2;
+  return heads;
+}
 
 struct ReadArgs {
   CacheArgs c;      // q_ptr: first rows of the sequences; tokens: rows of the outputs
   uint16_t* K;      // rows of Hkv heads, k_stride elements apart
   uint16_t* V;
   int64_t k_stride, v_stride;
+  int32_t heads;    // that a workgroup reads, a divisor of Hkv
 };
 
 // The pages of these calls hold bytes (CacheArgs::k_pages and v_pages point at them).
