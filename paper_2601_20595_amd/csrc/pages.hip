@@ -112,8 +112,7 @@ __device__ __forceinline__ V sum_before(V x, V* total, V (&s_wave)[kThreads / 64
 
 // The workspace of extend and compact.
 struct Sums {
-  int64_t need;    // pages that are asked for
-  int64_t unused;
+  int32_t used, moving;  // compact: pages in use, and how many of them move
 };
 __device__ __forceinline__ Sums* sums_in(const PagesArgs& a) { return reinterpret_cast<Sums*>(a.ws); }
 __device__ __forceinline__ int32_t* counts_in(const PagesArgs& a) { return reinterpret_cast<int32_t*>(a.ws + 64); }
@@ -216,56 +215,80 @@ __global__ __launch_bounds__(kThreads) void extend_count(PagesArgs a) {
       splits_in(a)[b] = split;
     }
   }
-  if (tid == 0) {
-    sums_in(a)->need = need;
-    *a.n_moves = 0;
-  }
+  if (tid == 0) *a.n_moves = 0;
 }
 
-// The lowest free pages, as many as are asked for.
-__global__ __launch_bounds__(kThreads) void extend_list(PagesArgs a) {
-  __shared__ int s_wave[kThreads / 64];
-  const int c = blockIdx.x;
-  int used_all;
-  const int used = used_before(a, c, &used_all, s_wave);
-  const int free = c * kPageChunk - used;
-  const int64_t need = sums_in(a)->need;
-  if (free >= need) return;  // (the same in every thread)
-  uint32_t there;
-  const uint32_t bits = ~used_bits(a, c, &there) & there;
-  int all;
-  int at = free + sum_before(static_cast<int>(__popc(bits)), &all, s_wave);
-  for (int i = 0; i < kEach; ++i)
-    if (bits >> i & 1) {
-      if (at < need) list_in(a)[at] = c * kPageChunk + static_cast<int>(threadIdx.x) * kEach + i;
-      ++at;
+// Free pages before the chunks' (the workgroup's threads have one each of 256 at a time); *all: of all chunks.
+// If the page of rank q is in one of them, *chunk is it, and *before the free pages before it.
+__device__ __forceinline__ void find_free(const PagesArgs& a, int64_t q, int* all, int* chunk, int* before, int (&s_wave)[kThreads / 64],
+                                          int (&s_found)[2]) {
+  const int chunks = page_chunks(a.n_pages);
+  int sum = 0;
+  for (int c0 = 0; c0 < chunks; c0 += kThreads) {
+    const int c = c0 + static_cast<int>(threadIdx.x);
+    const int free = c < chunks ? min(kPageChunk, a.n_pages - c * kPageChunk) - counts_in(a)[c] : 0;
+    int total;
+    const int first = sum + sum_before(free, &total, s_wave);
+    if (first <= q && q < first + free) {
+      s_found[0] = c;
+      s_found[1] = first;
     }
+    sum += total;
+  }
+  __syncthreads();
+  *all = sum;
+  *chunk = s_found[0];
+  *before = s_found[1];
 }
 
+// The new rows. A workgroup finds the free pages that its entries get itself: usually they are in one chunk.
 __global__ __launch_bounds__(kThreads) void extend_rows(PagesArgs a, int across) {
-  __shared__ int s_wave[kThreads / 64];
+  __shared__ int s_wave[kThreads / 64], s_found[2];
+  __shared__ int s_new[kSlots + 1];
   const int b = blockIdx.x / across, s0 = blockIdx.x % across * kSlots, tid = threadIdx.x;
-  int used;
-  used_before(a, 0, &used, s_wave);
   Growth g = growth_of(a, b);
-  const int64_t first = first_in(a)[b];
-  const bool none = first + g.need > a.n_pages - used;
-  const bool granted = g.need == 0 ? g.fits : g.fits && !none;
-  if (s0 == 0 && tid == 0) {
-    if (g.before.bad || g.after.bad) tell(a.status, kCacheBadLength);
-    if (g.need > 0 && g.fits && none) tell(a.status, kPagesNone);
+  const int last = g.before.pages - 1;
+  const int64_t first = g.need > 0 ? first_in(a)[b] : 0;
+  bool granted = g.fits;
+  int64_t q0 = 0;
+  if (g.need > 0 && g.fits) {
+    // its requests: the copy's, if the entry is its own, then its new entries'
+    const bool copies = g.split && last >= s0 && last < s0 + kSlots;
+    const int from = max(s0, g.before.pages), count_new = max(0, min(s0 + kSlots, g.after.pages) - from);
+    q0 = copies ? first : first + g.split + (from - g.before.pages);
+    const int m = count_new + copies;
+    int all, chunk, before;
+    find_free(a, q0, &all, &chunk, &before, s_wave, s_found);
+    granted = first + g.need <= all;
+    if (granted) {
+      for (int64_t at = before; m > 0 && at < q0 + m && chunk < page_chunks(a.n_pages); ++chunk) {
+        uint32_t there;
+        const uint32_t bits = ~used_bits(a, chunk, &there) & there;
+        int total;
+        int64_t rank = at + sum_before(static_cast<int>(__popc(bits)), &total, s_wave);
+        for (int i = 0; i < kEach; ++i)
+          if (bits >> i & 1) {
+            if (rank >= q0 && rank < q0 + m) s_new[rank - q0] = chunk * kPageChunk + tid * kEach + i;
+            ++rank;
+          }
+        at += total;
+      }
+      __syncthreads();
+    } else if (s0 == 0 && tid == 0) {
+      tell(a.status, kPagesNone);
+    }
   }
+  if (s0 == 0 && tid == 0 && (g.before.bad || g.after.bad)) tell(a.status, kCacheBadLength);
   if (!granted) {
     g.after = g.before;
     g.split = false;
   }
   const int64_t row = static_cast<int64_t>(b) * a.max_pages;
-  const int last = g.before.pages - 1;
   for (int s = s0 + tid; s < min(s0 + kSlots, a.max_pages); s += kThreads) {
     const int old = s < g.before.pages ? a.table[row + s] : -1;
     int now = s < g.after.pages ? old : -1;
     if (s == last && g.split) {
-      now = list_in(a)[first];
+      now = s_new[first - q0];
       count(a, old, -1);
       count(a, now, 1);
       const int at = splits_in(a)[b];
@@ -273,7 +296,7 @@ __global__ __launch_bounds__(kThreads) void extend_rows(PagesArgs a, int across)
       a.moves[2 * at + 1] = now;
       atomicMax(a.n_moves, at + 1);
     } else if (s > last && s < g.after.pages) {
-      now = list_in(a)[first + g.split + (s - g.before.pages)];
+      now = s_new[first + g.split + (s - g.before.pages) - q0];
       count(a, now, 1);
     } else if (s < g.before.pages && s >= g.after.pages) {
       count(a, old, -1);
@@ -294,7 +317,7 @@ __global__ __launch_bounds__(kThreads) void compact_count(PagesArgs a) {
   if (threadIdx.x == 0) counts_in(a)[blockIdx.x] = all;
 }
 
-// The free pages before U by their rank, and the ranks of the pages in use among all in use.
+// The free pages before U by their rank, the ranks of the pages in use among all in use, and the sums.
 __global__ __launch_bounds__(kThreads) void compact_list(PagesArgs a) {
   __shared__ int s_wave[kThreads / 64];
   const int c = blockIdx.x;
@@ -304,9 +327,11 @@ __global__ __launch_bounds__(kThreads) void compact_list(PagesArgs a) {
   const uint32_t bits = used_bits(a, c, &there);
   int all;
   int used = before + sum_before(static_cast<int>(__popc(bits)), &all, s_wave);
+  if (c == 0 && threadIdx.x == 0) sums_in(a)->used = u;
   for (int i = 0; i < kEach; ++i) {
     const int p = c * kPageChunk + static_cast<int>(threadIdx.x) * kEach + i;
     if (p >= a.n_pages) break;
+    if (p == u - 1) sums_in(a)->moving = u - used - (bits >> i & 1);  // the free pages before U
     if (bits >> i & 1) {
       ranks_in(a)[p] = used++;
     } else if (p < u) {
@@ -317,51 +342,35 @@ __global__ __launch_bounds__(kThreads) void compact_list(PagesArgs a) {
 
 // Where a page in use lies afterwards. As many pages in use lie at U and beyond as are free before it, `moving`; the
 // one of rank r among all in use is number r - (U - moving) of them.
-__device__ __forceinline__ int place_of(const PagesArgs& a, int p, int u, int moving) {
-  return p < u ? p : list_in(a)[moving - (u - ranks_in(a)[p])];
+__device__ __forceinline__ int place_of(const PagesArgs& a, int p, const Sums& sums) {
+  return p < sums.used ? p : list_in(a)[sums.moving - (sums.used - ranks_in(a)[p])];
 }
 
-__global__ __launch_bounds__(kThreads) void compact_rows(PagesArgs a, int across) {
-  __shared__ int s_wave[kThreads / 64];
-  __shared__ int s_moving;
-  const int chunks = page_chunks(a.n_pages), tid = threadIdx.x;
-  int u;
-  used_before(a, 0, &u, s_wave);
-  // free pages before U: U less the pages in use there, which its chunk's are counted for
-  const int cu = u / kPageChunk;
-  int ignored;
-  const int low = used_before(a, cu, &ignored, s_wave);
-  int here = 0;
-  for (int p = cu * kPageChunk + tid; p < u; p += kThreads) here += a.refs[p] != 0;
-  int in_chunk;
-  sum_before(here, &in_chunk, s_wave);
-  if (tid == 0) s_moving = u - low - in_chunk;
-  __syncthreads();
-  const int moving = s_moving;
-  if (static_cast<int>(blockIdx.x) < chunks) {
-    if (blockIdx.x == 0 && tid == 0) *a.n_moves = moving;
-    for (int i = tid; i < kPageChunk; i += kThreads) {
-      const int p = blockIdx.x * kPageChunk + i;
-      if (p >= a.n_pages) break;
-      const int refs = a.refs[p];
-      if (refs == 0) {
-        a.renamed[p] = -1;
-        if (p >= u) a.refs_out[p] = 0;
-      } else {
-        const int to = place_of(a, p, u, moving);
-        a.renamed[p] = to;
-        a.refs_out[to] = refs;
-        if (p >= u) {
-          const int at = moving - (u - ranks_in(a)[p]);
-          a.refs_out[p] = 0;
-          a.moves[2 * at] = p;
-          a.moves[2 * at + 1] = to;
-        }
-      }
+__global__ __launch_bounds__(kThreads) void compact_rows(PagesArgs a, int page_blocks, int across) {
+  const int tid = threadIdx.x;
+  const Sums sums = {sums_in(a)->used, sums_in(a)->used > 0 ? sums_in(a)->moving : 0};
+  if (static_cast<int>(blockIdx.x) < page_blocks) {
+    if (blockIdx.x == 0 && tid == 0) *a.n_moves = sums.moving;
+    const int p = blockIdx.x * kThreads + tid;
+    if (p >= a.n_pages) return;
+    const int refs = a.refs[p];
+    if (refs == 0) {
+      a.renamed[p] = -1;
+      if (p >= sums.used) a.refs_out[p] = 0;
+      return;
+    }
+    const int to = place_of(a, p, sums);
+    a.renamed[p] = to;
+    a.refs_out[to] = refs;
+    if (p >= sums.used) {
+      const int at = sums.moving - (sums.used - ranks_in(a)[p]);
+      a.refs_out[p] = 0;
+      a.moves[2 * at] = p;
+      a.moves[2 * at + 1] = to;
     }
     return;
   }
-  const int item = blockIdx.x - chunks;
+  const int item = blockIdx.x - page_blocks;
   const int b = item / across, s0 = item % across * kSlots;
   const Held h = held(a, a.lens[b]);
   if (h.bad && s0 == 0 && tid == 0) tell(a.status, kCacheBadLength);
@@ -371,7 +380,7 @@ __global__ __launch_bounds__(kThreads) void compact_rows(PagesArgs a, int across
     if (s < h.pages) {
       const int p = a.table[row + s];
       if (names_page(a, p) && a.refs[p] != 0)
-        now = place_of(a, p, u, moving);
+        now = place_of(a, p, sums);
       else
         tell(a.status, kCacheBadPage);
     }
@@ -446,9 +455,6 @@ hipError_t launch_pages_extend(const PagesArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(extend_count, dim3(chunks + 1), dim3(kThreads), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || rows == 0) return e;
-  hipLaunchKernelGGL(extend_list, dim3(chunks), dim3(kThreads), 0, s, a);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
   hipLaunchKernelGGL(extend_rows, dim3(rows), dim3(kThreads), 0, s, a, across);
   return hipGetLastError();
 }
@@ -461,7 +467,8 @@ hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(compact_list, dim3(chunks), dim3(kThreads), 0, s, a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(compact_rows, dim3(chunks + rows), dim3(kThreads), 0, s, a, across);
+  const int page_blocks = (a.n_pages + kThreads - 1) / kThreads;
+  hipLaunchKernelGGL(compact_rows, dim3(page_blocks + rows), dim3(kThreads), 0, s, a, page_blocks, across);
   return hipGetLastError();
 }
 

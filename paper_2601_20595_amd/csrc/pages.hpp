@@ -7,8 +7,8 @@
 
 namespace csg {
 
-constexpr int kPageChunk = 4096;               // pages that a workgroup counts
-constexpr int32_t kMaxPoolPages = 1 << 24;     // as many chunks as a workgroup sums up in 16 turns
+constexpr int kPageChunk = 1024;               // pages that a workgroup counts
+constexpr int32_t kMaxPoolPages = 1 << 24;     // as many chunks as a workgroup sums up in 64 turns
 constexpr int32_t kMaxPoolBatch = 1 << 20;
 constexpr int kCopyBuffers = 64;               // buffers of one launch
 
@@ -41,7 +41,7 @@ struct CopyArgs {
 };
 
 constexpr int32_t page_chunks(int32_t n_pages) { return (n_pages + kPageChunk - 1) / kPageChunk; }
-// Workspace: two sums of 64 bits, counts of the chunks, two words a page, two of a sequence's places.
+// Workspace: sums, counts of the chunks, two words a page, and of a sequence the places of its requests and its copy.
 inline int64_t pages_workspace(int32_t n_pages, int32_t batch) {
   return 64 + int64_t{8} * (page_chunks(n_pages) / 2 + 1) + int64_t{8} * n_pages + int64_t{16} * batch;
 }
