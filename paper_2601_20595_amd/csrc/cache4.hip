@@ -374,12 +374,14 @@ struct Mfma16<F16> {
   static __device__ __forceinline__ f32x4_t run(f16x8_t a, f16x8_t b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
-// Where the 16-byte pieces of a row of a wave's values lie: piece p at p ^ swz16(row). A store puts one piece of 16 rows
-// (all at different places), a transposing read takes two neighbouring pieces of 8 rows at a time (the
-// same).
+// Where the 16-byte pieces of a row of a wave's values lie: piece p at p ^ swz16(row). A store puts one piece of 16 rows, a
+// transposing read takes two neighbouring pieces of 4 rows for each 16 lanes. With r0 .. r3 the row's bits, 8 rows in a
+// row have distinct places in 128 bytes for a store, 16 in 256, and the pairs of 4 rows, and of 8, likewise for a read:
+// neither has bank conflicts, with 32 or with 64 banks.
 template <int D>
 __device__ __forceinline__ constexpr int swz16(int r) {
-  return D == 128 ? (r & 7) << 1 | (r >> 3 & 1) : (r >> 1 & 3) << 1 | (r >> 3 & 1);
+  const int r0 = r & 1, r1 = r >> 1 & 1, r2 = r >> 2 & 1, r3 = r >> 3 & 1;
+  return D == 128 ? (r2 ^ r3) << 3 | r1 << 2 | r0 << 1 | r2 : r1 << 2 | (r0 ^ r2) << 1 | (r2 ^ r3);
 }
 
 // A quarter of a row's codes, D / 4 elements, and its scale. `head`: where the head's rows of the page begin; the lane's
@@ -651,7 +653,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 
 // A wide part, whose waves share blocks of 64 keys. Each wave has 32 rows; it converts all of the keys for itself, from
 // registers (lane l has half l / 32 of the rows l % 32 and 32 + l % 32, which the queries follow), and 16 of the values
-// (a quarter of row l / 4) for all, through one of two buffers in LDS.
+// (a quarter of row l % 16) for all, through one of two buffers in LDS.
 template <class T, int D, bool kPlain>
 __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, Part& p, unsigned char* stage, float* out, int lane,
                                           int wave) {
@@ -660,7 +662,7 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
   const CacheArgs& c = a.c;
   asm("" : "+v"(lane));  // (as above)
   const int l32 = lane & 31, hlf = lane >> 5;
-  const int row = lane >> 2, quarter = lane & 3;
+  const int row = lane & 15, quarter = lane >> 4;
   const int nb = (p.end - p.key0 + kCacheWideBlock - 1) / kCacheWideBlock;
   auto key_of = [&](int n) { return p.key0 + n * kCacheWideBlock; };
   // lane n holds where the 16 keys n % 4 of block n / 4 have the head's rows of their page (16 blocks at a time)
