@@ -173,8 +173,30 @@ MIXED = {
 }
 
 
+def _drawn(seed):
+    """A call of random shape: sequences, rows per key/value head from 1 to over 128, pages, groups, cap, bias."""
+    rng = np.random.default_rng(100 + seed)
+    batch = int(rng.choice([1, 2, 5, 17, 70]))
+    most = int(rng.choice([1, 1, 3, 20]))
+    new = [int(x) for x in rng.integers(0, most + 1, batch)]
+    lens = [int(x + rng.integers(0, rng.choice([3, 40, 300, 1500]))) for x in new]
+    page = int(rng.choice([16, 32, 64, 128, 256]))
+    groups = []
+    if batch > 2 and rng.random() < 0.5:
+        cuts = sorted(set(int(x) for x in rng.integers(0, batch + 1, 3)))
+        for b0, b1 in zip(cuts, cuts[1:]):
+            shared = page * int(rng.integers(1, 1 + max(1, 400 // page)))
+            for b in range(b0, b1):
+                lens[b] += shared
+            groups.append((b0, b1, shared))
+    hkv = int(rng.choice([1, 2, 3]))
+    return (new, lens, hkv * int(rng.choice([1, 2, 4, 7, 8, 16, 17, 33])), hkv, int(rng.choice([64, 128])), page, groups,
+            float(rng.choice([0.0, 0.0, 9.0])), bool(rng.random() < 0.3))
+
+
 def _attn_case(name, dtype, sharp=1.0, stream=None):
-    new, lens, H, Hkv, D, page, groups, cap, bias = MIXED[name] if name in MIXED else ATTN[name]
+    spec = _drawn(name) if isinstance(name, int) else MIXED[name] if name in MIXED else ATTN[name]
+    new, lens, H, Hkv, D, page, groups, cap, bias = spec
     rng = np.random.default_rng(7)
     n, tail = sum(new), 2
     table, pages = _table(rng, lens, page, shared=groups)
@@ -220,6 +242,38 @@ def _attn_case(name, dtype, sharp=1.0, stream=None):
 @pytest.mark.parametrize("name", [*ATTN, *MIXED])
 def test_attention(name, dtype):
     _attn_case(name, dtype)
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_attention_drawn(seed):
+    _attn_case(seed, "bf16" if seed % 3 else "f16", 1.0 + seed % 4)
+
+
+def test_two_streams_with_a_workspace_each():
+    """Calls of both kernels (few rows, many) at once, and the same one after the other."""
+    streams = [torch.cuda.Stream(device=DEV) for _ in range(2)]
+    rng = np.random.default_rng(9)
+    H, Hkv, D, page = 16, 4, 128, 32
+    jobs = []
+    for new, lens in (([1] * 20, [50 + 211 * i for i in range(20)]), ([30, 5], [2000, 1700])):
+        table, pages = _table(rng, lens, page)
+        c = csg.PagedCache4(H, Hkv, D, "bf16", pages, page, len(new), table.shape[1])
+        kp, vp = (pages4(s, pages, Hkv, page, D, "bf16")[0].to(DEV) for s in (1, 2))
+        q = normal(3, (sum(new), H, D), "bf16")[0].to(DEV)
+        ws = torch.zeros(c.workspace_bytes(sum(new)), dtype=torch.uint8, device=DEV)
+        jobs.append((c, (q, kp, vp, ints(pointers(new)), ints(lens), torch.tensor(table, device=DEV)), ws))
+    torch.cuda.synchronize()
+    out = []
+    for together in (False, True, True):
+        o = [torch.zeros_like(args[0]) for _, args, _ in jobs]
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for (c, args, ws), x, st in zip(jobs, o, streams):
+                c.attn(*args, x, None, ws, stream=st if together else None)
+        torch.cuda.synchronize()
+        out.append(o)
+    for o in out[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(o, out[0]))
 
 
 def test_sharp_scores_other_stream_same_bits():
