@@ -443,11 +443,12 @@ __device__ __forceinline__ const unsigned char* head_in(const uint16_t* pages, i
   return reinterpret_cast<const unsigned char*>(pages) + (static_cast<uint64_t>(hi) << 32 | lo);
 }
 
-// A narrow part: up to 16 R rows, whose four waves take every fourth step of 16 kTiles keys, each at its own pace. Keys go from
+// A narrow part: up to 16 R rows, whose four waves take every fourth step of 16 kTiles keys, each at its own pace, or
+// (alone) one wave all of them. Keys go from
 // the loads' registers into the products (the elements of a head in the order in which the lanes have them, which
 // the queries follow); values through LDS, in 16 bits, where the transposing reads find them. The next
 // step's codes are asked for as soon as the last ones are converted.
-template <class T, int D, bool kPlain, int R, int kTiles, int kAhead>
+template <class T, int D, bool kPlain, int R, int kTiles, int kAhead, bool alone>
 __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, const Part& p, int row0, unsigned char* stage,
                                             float (&s_ref)[4][32], float (&s_sum)[4][32], float* out, int lane, int wave) {
   using x8 = typename T::x8;
@@ -458,8 +459,9 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
   const int l16 = lane & 15, g = lane >> 4;
   unsigned char* mine = stage + wave * 32 * 2 * D;
   const int steps = (p.end - p.key0 + kStep - 1) / kStep;
-  const int mine_n = steps > wave ? (steps - wave + 3) / 4 : 0;
-  auto key_of = [&](int n) { return p.key0 + (wave + 4 * n) * kStep; };
+  const int mine_n = alone ? steps : steps > wave ? (steps - wave + 3) / 4 : 0;
+  const int stride = alone ? kStep : 4 * kStep, my_key0 = p.key0 + (alone ? 0 : wave * kStep);
+  auto key_of = [&](int n) { return my_key0 + n * stride; };
   // lane n holds where the 16 keys n % kTiles of the wave's step n / kTiles have the head's rows of their page (kAtOnce steps
   // at a time); page 0 where there is none
   auto heads_at = [&](int n) { return head_of<D>(c, max(page_of(c, p, key_of(n + lane / kTiles) + 16 * (lane % kTiles)), 0), p.kvh); };
@@ -603,10 +605,26 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
   // 16-byte pieces of a row are turned by its number, against bank conflicts
   asm("" : "+v"(lane));  // (these places are not made ahead of the loop, and kept through it)
   const int r16 = lane & 15, quarter = lane >> 4;
+  const int rows = x.rows - p.tile * kCacheTileRows - row0;
   float l[R];
 #pragma unroll
+  for (int i = 0; i < R; ++i) l[i] = sum_quarters(sm[i].l);
+  if constexpr (alone) {
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (!out || 16 * i + r16 >= rows) continue;
+      const int r = row0 + 16 * i + r16;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) *reinterpret_cast<f32x4_t*>(out + r * D + 16 * db + 4 * quarter) = acc[i][db];
+      if (quarter == 0) {
+        out[32 * D + r] = sm[i].m;
+        out[32 * D + 32 + r] = l[i];
+      }
+    }
+    return;
+  }
+#pragma unroll
   for (int i = 0; i < R; ++i) {
-    l[i] = sum_quarters(sm[i].l);
     if (quarter == 0) {
       s_ref[wave][16 * i + r16] = sm[i].m;
       s_sum[wave][16 * i + r16] = l[i];
@@ -615,7 +633,6 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
   __syncthreads();  // (also: every wave has read its stage)
   constexpr int kPieces = D / 4;
   const int tid = wave * 64 + lane;
-  const int rows = x.rows - p.tile * kCacheTileRows - row0;
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int live = min(16, rows - 16 * i);
@@ -763,8 +780,9 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
 
 // With few rows a sequence (few), the kernel has only the narrow parts of 16 rows, whose registers and LDS
 // let more workgroups onto a CU; an entry of more rows goes through its keys once for each 16 of them. Otherwise it has
-// parts for up to 16, up to 32 and up to 128 rows, that convert their keys once.
-template <class T, int D, bool kPlain, bool few>
+// parts for up to 16, up to 32 and up to 128 rows, that convert their keys once. With short_tasks, sequences are so many
+// that each wave may have runs of its own.
+template <class T, int D, bool kPlain, bool few, bool short_tasks>
 __global__ __launch_bounds__(kThreads, few ? kCache4Few : kCacheGroups) void cache4_attn(CacheAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char stage[(few ? 2 : 4) * kCacheBlock * 4 * D];
   __shared__ float s_ref[4][32], s_sum[4][32];
@@ -773,20 +791,24 @@ __global__ __launch_bounds__(kThreads, few ? kCache4Few : kCacheGroups) void cac
   static_assert(sizeof(stage) >= 4 * 32 * 2 * D && sizeof(stage) >= 4 * 16 * D * 4, "the narrow waves' values, and results of theirs");
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  cache_run(a, stage, [&](const Entry& x, const KeptEntry* local, Part& p, int64_t place, bool wide) {
+  cache_run<short_tasks ? kCache4AloneCost : 0, D == 128 ? kCache4AloneBlocks : 2 * kCache4AloneBlocks>(a, stage, [&](const Entry& x, const KeptEntry* local, Part& p, int64_t place, bool wide, bool alone) {
     if constexpr (few) {
       const int first = p.tile;
       for (int r = first * kCacheTileRows; r < min(x.rows, first * kCacheTileRows + kCacheWideRows); r += 16) {
         p.tile = r / kCacheTileRows;
-        narrow_part<T, D, kPlain, 1, 2, 1>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, part_at<D>(a, place + p.tile - first), lane, wave);
+        float* out = part_at<D>(a, place + p.tile - first);
+        if (short_tasks && alone)
+          narrow_part<T, D, kPlain, 1, 2, 1, true>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, out, lane, wave);
+        else
+          narrow_part<T, D, kPlain, 1, 2, 1, false>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, out, lane, wave);
       }
     } else if (wide) {
       p.tile += wave;
       wide_part<T, D, kPlain>(a, x, local, p, stage, part_at<D>(a, place + wave), lane, wave);
     } else if (x.rows <= 16) {
-      narrow_part<T, D, kPlain, 1, 4, 1>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+      narrow_part<T, D, kPlain, 1, 4, 1, false>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
     } else {
-      narrow_part<T, D, kPlain, 2, 2, 1>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+      narrow_part<T, D, kPlain, 2, 2, 1, false>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
     }
   });
 }
@@ -803,19 +825,20 @@ hipError_t read(const ReadArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <class T, int D, bool few>
+template <class T, int D, bool few, bool short_tasks>
 hipError_t attend(const CacheAttnArgs& a, hipStream_t s) {
   const dim3 grid(a.head_workers * a.c.Hkv);
   if (a.scoring.plain())
-    hipLaunchKernelGGL((cache4_attn<T, D, true, few>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((cache4_attn<T, D, true, few, short_tasks>), grid, dim3(kThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((cache4_attn<T, D, false, few>), grid, dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((cache4_attn<T, D, false, few, short_tasks>), grid, dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
 template <class T, int D>
 hipError_t attend(const CacheAttnArgs& a, bool few, hipStream_t s) {
-  return few ? attend<T, D, true>(a, s) : attend<T, D, false>(a, s);
+  if (!few) return attend<T, D, false, false>(a, s);
+  return enough_to_run_alone(a.c.batch, a.head_workers) ? attend<T, D, true, true>(a, s) : attend<T, D, true, false>(a, s);
 }
 
 }  // namespace

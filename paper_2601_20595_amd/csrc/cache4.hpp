@@ -17,6 +17,11 @@ constexpr int kCache4Few = 3;
 // kCacheTaskCost here, where a block is a quarter of the bytes: 64 unrelated sequences 41.2 us with 4, 39.4 with 8, 38.1 with
 // 12, 38.8 with 16; 64 on four shared prompts 44.5, 40.1, 42.5, 45.2.
 constexpr int kCache4TaskCost = 10;
+// Waves with runs of their own, four tasks of a workgroup at a time: 128 sequences of 20 to 300 keys 21.5 -> 18.1 us, 256 of 500 to
+// 2000 79.7 -> 78.6; but 64 of 100 to 8000, 58 blocks each, 38.9 -> 39.9 (heads of 64: 27.4 -> 26.6, so twice as many there). A
+// task's cost 2: 19.2 us (128 sequences), 4: 18.3, 8: 19.6.
+constexpr int kCache4AloneCost = 4;
+constexpr int kCache4AloneBlocks = 48;  // of 128 elements a head, on average; 64: twice as many
 // Whether the sequences' rows (new tokens times heads of a key/value head) are few, on average; with groups, whose
 // sequences' rows go through the shared keys together, never.
 inline bool cache4_few(int64_t tokens, int32_t H, int32_t Hkv, int32_t batch, int32_t n_groups) {

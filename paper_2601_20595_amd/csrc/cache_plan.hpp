@@ -114,9 +114,11 @@ struct PlanEntry {
   int32_t before, tiles, blocks, rows, token0, group, unused[2];
 };
 struct Plan {
-  int32_t run;    // units of a run
-  int32_t tiles;  // tiles of one key/value head
-  int32_t unused[6];
+  int32_t run;      // units of a run
+  int32_t tiles;    // tiles of one key/value head
+  int32_t shift;    // places from a tile's part in one run to that in the next, a task's tiles at most: 1 << shift
+  int32_t cost;     // units that beginning and ending a task costs
+  int32_t unused[4];
 };
 __device__ __forceinline__ Plan* plan_in(unsigned char* ws) { return reinterpret_cast<Plan*>(ws); }
 __device__ __forceinline__ PlanEntry* entries_in(unsigned char* ws) { return reinterpret_cast<PlanEntry*>(ws + sizeof(Plan)); }
@@ -207,13 +209,18 @@ __device__ __forceinline__ float* part_at(const CacheAttnArgs& a, int64_t place)
   return place < a.max_parts ? reinterpret_cast<float*>(a.ws + cache_plan_bytes() + place * cache_part_bytes(D)) : nullptr;
 }
 
+// Tasks of a head that are enough for waves with runs of their own.
+__host__ __device__ __forceinline__ bool enough_to_run_alone(int tasks, int workers) { return 2 * tasks >= workers; }
+
 // A workgroup's run: its parts, one after the other, through do_part, which all of its threads call with the
 // entry, the sequences' entries (locate_row), the part, whose tile is its task's first, that tile's place, and whether the
-// task is wide. `stage`: LDS that the parts use (and the groups, before them).
-template <class DoPart>
+// task is wide. With kAloneCost > 0 and many tasks (none of them wide) of up to kAloneBlocks blocks on average, every wave has
+// a run, and does its parts alone (the last argument): a task then costs kAloneCost units. `stage`: LDS that the parts
+// use (and the groups, before them).
+template <int kAloneCost, int kAloneBlocks, class DoPart>
 __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char* stage, DoPart do_part) {
-  __shared__ uint32_t s_wave_units[4], s_wave_tiles[4];
-  __shared__ int s_entry, s_first, s_tiles;
+  __shared__ uint32_t s_wave_blocks[4], s_wave_tasks[4], s_wave_tiles[4], s_wave_wide[4];
+  __shared__ int s_entry[4], s_first[4], s_tiles[4];
   __shared__ KeptEntry s_entries[kThreads];
   const CacheArgs& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -237,7 +244,8 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
   // Each thread counts some entries; units and tiles before each of them by a scan. Where a thread
   // has one entry, everyone finds it in LDS.
   const int per = (n_entries + kThreads - 1) / kThreads;
-  uint32_t units = 0, tiles = 0;
+  uint32_t blocks = 0, tasks = 0, tiles = 0;
+  bool wide_one = false;
   Entry mine{};
   for (int i = 0; i < per; ++i) {
     const int e = tid * per + i;
@@ -245,48 +253,80 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
     const Entry x = entry_of(a, local, e);
     mine = x;
     if (per == 1) s_entries[e] = {x.token0, x.rows, x.b0, x.b1, x.lo, x.end};
-    units += x.tasks() * x.span(a.task_cost);
+    if constexpr (kAloneCost > 0) {
+      if (x.blocks > 0) {
+        blocks += x.tasks() * x.blocks;
+        tasks += x.tasks();
+        wide_one |= x.wide();
+      }
+    } else {
+      blocks += x.tasks() * x.span(a.task_cost);  // (with what the tasks cost)
+    }
     tiles += x.tiles();
   }
-  const uint32_t own_units = units, own_tiles = tiles;
+  const uint32_t own_blocks = blocks, own_tasks = tasks, own_tiles = tiles;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const uint32_t uu = __shfl_up(units, d), ut = __shfl_up(tiles, d);
+    const uint32_t ub = __shfl_up(blocks, d), uk = kAloneCost > 0 ? __shfl_up(tasks, d) : 0, ut = __shfl_up(tiles, d);
     if (lane >= d) {
-      units += uu;
+      blocks += ub;
+      tasks += uk;
       tiles += ut;
     }
   }
+  const bool wide_any = kAloneCost > 0 && __builtin_amdgcn_ballot_w64(wide_one) != 0;
   if (lane == 63) {
-    s_wave_units[wave] = units;
+    s_wave_blocks[wave] = blocks;
     s_wave_tiles[wave] = tiles;
+    if constexpr (kAloneCost > 0) {
+      s_wave_tasks[wave] = tasks;
+      s_wave_wide[wave] = wide_any;
+    }
   }
   __syncthreads();
-  units -= own_units;
+  blocks -= own_blocks;
+  tasks -= own_tasks;
   tiles -= own_tiles;
   for (int i = 0; i < wave; ++i) {
-    units += s_wave_units[i];
+    blocks += s_wave_blocks[i];
+    if constexpr (kAloneCost > 0) tasks += s_wave_tasks[i];
     tiles += s_wave_tiles[i];
   }
   const int all_tiles = __builtin_amdgcn_readfirstlane(s_wave_tiles[0] + s_wave_tiles[1] + s_wave_tiles[2] + s_wave_tiles[3]);
   // Bounds that do not ascend may name rows several times, and with them more units than 32 bits count: then
   // there is nothing to do. (As many tiles as the host has reckoned with have no more units than it has.)
   const bool fits = static_cast<uint32_t>(all_tiles) <= a.max_tiles;
-  const int all = fits ? __builtin_amdgcn_readfirstlane(s_wave_units[0] + s_wave_units[1] + s_wave_units[2] + s_wave_units[3]) : 0;
-  const int run = max(kCacheMinRun, (all + a.head_workers - 1) / a.head_workers);
-  const int begin = w * run;
+  const int all_blocks = __builtin_amdgcn_readfirstlane(s_wave_blocks[0] + s_wave_blocks[1] + s_wave_blocks[2] + s_wave_blocks[3]);
+  bool alone = false;
+  int cost = a.task_cost, all = all_blocks, units = blocks, own_units = own_blocks;
+  if constexpr (kAloneCost > 0) {
+    const int all_tasks = __builtin_amdgcn_readfirstlane(s_wave_tasks[0] + s_wave_tasks[1] + s_wave_tasks[2] + s_wave_tasks[3]);
+    const int wide_task = __builtin_amdgcn_readfirstlane(s_wave_wide[0] | s_wave_wide[1] | s_wave_wide[2] | s_wave_wide[3]);
+    alone = !wide_task && enough_to_run_alone(all_tasks, a.head_workers) && all_blocks <= kAloneBlocks * all_tasks;
+    if (alone) cost = kAloneCost;
+    all += cost * all_tasks;
+    units += cost * tasks;
+    own_units += cost * own_tasks;
+  }
+  if (!fits) all = 0;
+  const int workers = alone ? 4 * a.head_workers : a.head_workers;
+  const int run = max(kCacheMinRun, (all + workers - 1) / workers);
+  const int first_begin = (alone ? 4 * w : w) * run;  // the workgroup's runs: one, or one a wave
   // for cache_merge, and the entry where the run begins
-  if (blockIdx.x == 0 || (static_cast<int>(units) <= begin && begin < static_cast<int>(units + own_units))) {
+  if (blockIdx.x == 0 || (units < first_begin + (alone ? 4 : 1) * run && first_begin < units + own_units)) {
     int before = units, tiles_before = tiles;
     for (int i = 0; i < per; ++i) {
       const int e = tid * per + i;
       if (e >= n_entries) break;
       const Entry x = per == 1 ? mine : entry_of(a, local, e);
-      const int n = x.tasks() * x.span(a.task_cost);
-      if (before <= begin && begin < before + n) {
-        s_entry = e;
-        s_first = begin - before;
-        s_tiles = tiles_before;
+      const int n = x.tasks() * x.span(cost);
+      for (int k = 0; k < (alone ? 4 : 1); ++k) {
+        const int begin = first_begin + k * run;
+        if (before <= begin && begin < before + n) {
+          s_entry[k] = e;
+          s_first[k] = begin - before;
+          s_tiles[k] = tiles_before;
+        }
       }
       if (blockIdx.x == 0) {
         entries_in(a.ws)[e] = {before, tiles_before, fits ? x.blocks : 0, x.rows, x.token0, x.group, {0, 0}};
@@ -296,16 +336,17 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
       tiles_before += x.tiles();
     }
     if (blockIdx.x == 0 && tid == 0) {
-      *plan_in(a.ws) = {run, all_tiles, {0, 0, 0, 0, 0, 0}};
+      *plan_in(a.ws) = {run, all_tiles, alone ? 0 : 2, cost, {0, 0, 0, 0}};
       if (!fits) tell(c, kCacheBadLength);
     }
   }
-  if (begin >= all) return;
+  if (first_begin >= all) return;
   __syncthreads();
-  int left = min(run, all - begin);
-  int e = __builtin_amdgcn_readfirstlane(s_entry), in_entry = __builtin_amdgcn_readfirstlane(s_first);
-  int tiles_before = __builtin_amdgcn_readfirstlane(s_tiles);
-  const int64_t places = static_cast<int64_t>(kvh) * (all_tiles + 4 * a.head_workers) + 4 * w;
+  const int mine_k = alone ? wave : 0, begin = first_begin + mine_k * run;
+  int left = min(run, all - begin);  // (not positive: the wave has no run)
+  int e = __builtin_amdgcn_readfirstlane(s_entry[mine_k]), in_entry = __builtin_amdgcn_readfirstlane(s_first[mine_k]);
+  int tiles_before = __builtin_amdgcn_readfirstlane(s_tiles[mine_k]);
+  const int64_t places = static_cast<int64_t>(kvh) * (all_tiles + 4 * a.head_workers) + 4 * w + mine_k;
   const KeptEntry* sequences = per == 1 ? s_entries + a.n_groups : nullptr;
   while (left > 0) {
     Entry x;
@@ -322,14 +363,14 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
     } else {
       x = entry_of(a, GlobalGroups{a}, e);
     }
-    const int n = x.tasks() * x.span(a.task_cost);
+    const int n = x.tasks() * x.span(cost);
     if (in_entry < n) {
       Part p;
       p.kvh = kvh;
       const bool wide = x.wide();
-      const int task = wide ? __builtin_amdgcn_readfirstlane(in_entry / x.span(a.task_cost)) : 0;
-      const int from = in_entry - task * x.span(a.task_cost), take = min(x.span(a.task_cost) - from, left);
-      const int first = max(0, from - a.task_cost), count = from + take - a.task_cost - first;
+      const int task = wide ? __builtin_amdgcn_readfirstlane(in_entry / x.span(cost)) : 0;
+      const int from = in_entry - task * x.span(cost), take = min(x.span(cost) - from, left);
+      const int first = max(0, from - cost), count = from + take - cost - first;
       left -= take;
       in_entry += take;
       if (count <= 0) continue;
@@ -338,7 +379,7 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
       p.key0 = (x.block0 + first) * kCacheBlock;
       p.end = min(x.end, p.key0 + count * kCacheBlock);
       p.tile = wide ? 4 * task : 0;
-      do_part(x, sequences, p, places + tiles_before + p.tile, wide);
+      do_part(x, sequences, p, places + tiles_before + p.tile, wide, alone);
     } else {
       in_entry = 0;
       tiles_before += x.tiles();

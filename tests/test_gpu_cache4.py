@@ -169,6 +169,8 @@ MIXED = {
     "one of many rows": ([40] + [1] * 20 + [0] * 10, [90] + [1 + 13 * i for i in range(20)] + [5] * 10, 8, 2, 128, 16, [], 0.0, False),
     "of some rows": ([1, 5, 8, 1, 1, 1, 1, 1, 1, 1, 0, 0], [300, 77, 200, 64, 32, 31, 1, 2, 500, 129, 9, 0], 8, 2, 64, 32, [], 8.0, True),
     "sixteen rows each": ([4] * 9, [4, 5, 63, 64, 65, 128, 129, 260, 1000], 4, 1, 128, 64, [], 0.0, False),
+    "a wave each": ([1, 1, 4, 0, 1] * 20, [(i * 37) % 190 + (4 if i % 5 == 2 else 1) for i in range(100)], 16, 2, 128, 32, [], 0.0, True),
+    "a wave each, over many runs": ([1] * 50, [3 + (i * i * 7) % 1400 for i in range(50)], 8, 8, 64, 16, [], 5.0, False),
     "seventeen heads": ([1, 1], [70, 1500], 17, 1, 128, 16, [], 0.0, False),
 }
 
