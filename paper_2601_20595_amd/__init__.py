@@ -954,53 +954,59 @@ class PagePool:
         self._cfg = csg_pages_cfg(n_pages=n_pages, page_size=page_size, batch=batch, max_pages=max_pages)
         self._workspace = csg_pages_workspace(self._cfg)  # (checks the configuration)
         self._table_bytes, self._batch_bytes, self._refs_bytes = 4 * batch * max_pages, 4 * batch, 4 * n_pages
-        self._batch, self._pages, self._max_pages = batch, n_pages, max_pages
+        self._pages, self._max_pages = n_pages, max_pages
 
     def workspace_bytes(self) -> int:
         """Bytes of the workspace that extend and compact need."""
         return self._workspace
 
-    def _table(self, t, what: str) -> int:
-        if type(t) is not int and t.shape[-1] != self._max_pages:
-            raise ValueError("%s must have %d pages a row" % (what, self._max_pages))
-        return _arg(t, self._table_bytes, _INT32, what, self.device)
-
-    def _lens(self, t, what: str) -> int:
-        return _arg(t, self._batch_bytes, _INT32, what, self.device)
-
-    def _refs(self, t, what: str) -> int:
-        return _arg(t, self._refs_bytes, _INT32, what, self.device)
+    def _words(self, tables, batches, pages, others=()):
+        """_arg of int32 tensors, (tensor, name) each: page tables, of a word a sequence, of a word a page, and others, (tensor,
+        bytes, name). (One loop: a step's tables take less time than calls for each.)"""
+        dev, known, width = self.device, _INT32.known, self._max_pages
+        got = []
+        for t, what in tables:
+            if type(t) is not int and t.shape[-1] != width:
+                raise ValueError("%s must have %d pages a row" % (what, width))
+        for need, group in ((self._table_bytes, tables), (self._batch_bytes, batches), (self._refs_bytes, pages)):
+            for t, what in group:
+                if type(t) is not int and t is not None and t.dtype in known and t.is_contiguous() and t.nbytes >= need and t.get_device() == dev:
+                    got.append(t.data_ptr())
+                else:
+                    got.append(_arg(t, need, _INT32, what, dev))
+        for t, need, what in others:
+            got.append(_arg(t, need, _INT32, what, dev))
+        return got
 
     def fork(self, page_table, lens, refs, parent, table_out, lens_out, refs_out, status=None, stream=None):
         """Sequence b becomes what sequence parent[b], int32 (batch), was; negative: none."""
-        dev = self.device
-        _check(_lib().csg_pages_fork(
-            self._cfg, self._table(page_table, "page_table"), self._lens(lens, "lens"), self._refs(refs, "refs"),
-            self._lens(parent, "parent"), self._table(table_out, "table_out"), self._lens(lens_out, "lens_out"),
-            self._refs(refs_out, "refs_out"), _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_pages_fork")
+        t, to, n, p, no, r, ro = self._words(((page_table, "page_table"), (table_out, "table_out")),
+                                             ((lens, "lens"), (parent, "parent"), (lens_out, "lens_out")),
+                                             ((refs, "refs"), (refs_out, "refs_out")))
+        _check(_lib().csg_pages_fork(self._cfg, t, n, r, p, to, no, ro, _arg(status, 4, _INT32, "status", self.device), self.device,
+                                     _stream(stream)), "csg_pages_fork")
 
     def extend(self, page_table, lens, refs, grow, table_out, lens_out, refs_out, moves, n_moves, workspace, status=None,
                stream=None):
         """Sequences grow by grow, int32 (batch), tokens, or shrink; moves (at least batch pairs) are
         to be copied before anything is appended."""
         dev = self.device
-        _check(_lib().csg_pages_extend(
-            self._cfg, self._table(page_table, "page_table"), self._lens(lens, "lens"), self._refs(refs, "refs"),
-            self._lens(grow, "grow"), self._table(table_out, "table_out"), self._lens(lens_out, "lens_out"),
-            self._refs(refs_out, "refs_out"), _arg(moves, 2 * self._batch_bytes, _INT32, "moves", dev), _arg(n_moves, 4, _INT32, "n_moves", dev),
-            _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes, _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)),
-               "csg_pages_extend")
+        t, to, n, g, no, r, ro, m, nm = self._words(
+            ((page_table, "page_table"), (table_out, "table_out")), ((lens, "lens"), (grow, "grow"), (lens_out, "lens_out")),
+            ((refs, "refs"), (refs_out, "refs_out")), ((moves, 2 * self._batch_bytes, "moves"), (n_moves, 4, "n_moves")))
+        _check(_lib().csg_pages_extend(self._cfg, t, n, r, g, to, no, ro, m, nm, _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes,
+                                       _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_pages_extend")
 
     def compact(self, page_table, lens, refs, table_out, refs_out, renamed, moves, n_moves, workspace, status=None, stream=None):
         """The pages in use get the lowest numbers: renamed, int32 (n_pages); moves has room for n_pages // 2
         pairs."""
         dev = self.device
-        _check(_lib().csg_pages_compact(
-            self._cfg, self._table(page_table, "page_table"), self._lens(lens, "lens"), self._refs(refs, "refs"),
-            self._table(table_out, "table_out"), self._refs(refs_out, "refs_out"), self._refs(renamed, "renamed"),
-            _arg(moves, 8 * (self._pages // 2), _INT32, "moves", dev), _arg(n_moves, 4, _INT32, "n_moves", dev),
-            _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes, _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)),
-               "csg_pages_compact")
+        t, to, n, r, ro, new, m, nm = self._words(
+            ((page_table, "page_table"), (table_out, "table_out")), ((lens, "lens"),),
+            ((refs, "refs"), (refs_out, "refs_out"), (renamed, "renamed")),
+            ((moves, 8 * (self._pages // 2), "moves"), (n_moves, 4, "n_moves")))
+        _check(_lib().csg_pages_compact(self._cfg, t, n, r, to, ro, new, m, nm, _arg(workspace, 1, 0, "workspace", dev), workspace.nbytes,
+                                        _arg(status, 4, _INT32, "status", dev), dev, _stream(stream)), "csg_pages_compact")
 
     def copy(self, buffers, moves, n_moves, status=None, stream=None):
         """Copies the pages of moves in every buffer (tensors whose first dimension is the pages, each

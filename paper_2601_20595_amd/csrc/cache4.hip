@@ -298,7 +298,14 @@ __global__ __launch_bounds__(kThreads) void cache4_read(ReadArgs a) {
 
 // ---- attention over the cache ---------------------------------------------------------------
 // Entries, tasks and runs are those of the cache in 16 bits (cache_plan.hpp), and so are the parts, which
-// its cache_merge joins.
+// its cache_merge joins. Codes become 16-bit numbers in registers, two an instruction, exactly: products and roundings are
+// those of attention over the same values in 16 bits.
+// With a quarter of the bytes, what is done for a key counts: a key of 4 rows costs its SIMD as much in products of 32 rows
+// as in those of 16 twice over, so that up to 16 rows are one tile here. Bound by the memory where keys are many: 2
+// sequences of over 100000, 244 MB in 51 us and the join 7, 4.8 TB/s (with 32-row products and every key through LDS 134);
+// 64 sequences of up to 8000, 129 MB, 34 and 5, of which the plan, the first loads and the last parts' ends are 8. With few
+// keys by a chain of latencies, 7.7 us for 900 keys. Where 16 sequences' rows share 8192 keys by the wide
+// parts' chain of products, weights and products, one wave a SIMD, and 21 MB of partial results (33 and 8).
 
 // Combination of the four lanes of a row: lane ^ 16, then lane ^ 32, swapped as in max_halves.
 __device__ __forceinline__ float max_quarters(float x) {
@@ -447,7 +454,8 @@ __device__ __forceinline__ const unsigned char* head_in(const uint16_t* pages, i
 // (alone) one wave all of them. Keys go from
 // the loads' registers into the products (the elements of a head in the order in which the lanes have them, which
 // the queries follow); values through LDS, in 16 bits, where the transposing reads find them. The next
-// step's codes are asked for as soon as the last ones are converted.
+// step's codes are asked for as soon as the last ones are converted, and waited for where they are; two steps ahead took
+// as long.
 template <class T, int D, bool kPlain, int R, int kTiles, int kAhead, bool alone>
 __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, const Part& p, int row0, unsigned char* stage,
                                             float (&s_ref)[4][32], float (&s_sum)[4][32], float* out, int lane, int wave) {
@@ -779,7 +787,8 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
 }
 
 // With few rows a sequence (few), the kernel has only the narrow parts of 16 rows, whose registers and LDS
-// let more workgroups onto a CU; an entry of more rows goes through its keys once for each 16 of them. Otherwise it has
+// let more workgroups onto a CU (64 sequences with two 41.2 us, three 38.9, four, which spill, 58); an entry of more rows
+// goes through its keys once for each 16 of them. Otherwise it has
 // parts for up to 16, up to 32 and up to 128 rows, that convert their keys once. With short_tasks, sequences are so many
 // that each wave may have runs of its own.
 template <class T, int D, bool kPlain, bool few, bool short_tasks>

@@ -200,9 +200,11 @@ def _attn_case(name, dtype, sharp=1.0, stream=None):
     spec = _drawn(name) if isinstance(name, int) else MIXED[name] if name in MIXED else ATTN[name]
     new, lens, H, Hkv, D, page, groups, cap, bias = spec
     rng = np.random.default_rng(7)
-    n, tail = sum(new), 2
+    # drawn calls: a part of a larger batch's rows, others before and behind
+    head, n, tail = name % 3 if isinstance(name, int) else 0, sum(new), 2
     table, pages = _table(rng, lens, page, shared=groups)
-    q, q64 = normal(1, (n + tail, H, D), dtype, sharp)
+    q, q64 = normal(1, (head + n + tail, H, D), dtype, sharp)
+    q64 = q64[head:]
     used = np.zeros((pages, page), dtype=bool)
     for b, x in enumerate(lens):
         i = np.arange(x)
@@ -219,9 +221,9 @@ def _attn_case(name, dtype, sharp=1.0, stream=None):
                             HALF_STEP[dtype], TINY[dtype])
         want[0][r], want[1][:, r], want[2][r], want[3][:, r] = got
     c = csg.PagedCache4(H, Hkv, D, dtype, pages, page, len(new), table.shape[1])
-    o = torch.full((n + tail, H, D), 17.0, dtype=TORCH[dtype], device=DEV)
-    lse = torch.full((H, n + tail), 17.0, device=DEV)
-    ws = torch.full((c.workspace_bytes(n + tail, len(groups)),), 255, dtype=torch.uint8, device=DEV)
+    o = torch.full((head + n + tail, H, D), 17.0, dtype=TORCH[dtype], device=DEV)
+    lse = torch.full((H, head + n + tail), 17.0, device=DEV)
+    ws = torch.full((c.workspace_bytes(head + n + tail, len(groups)),), 255, dtype=torch.uint8, device=DEV)
     st = torch.zeros(1, dtype=torch.int32, device=DEV)
     args = {"status": st, "softcap": cap, "stream": stream}
     if groups:
@@ -229,14 +231,15 @@ def _attn_case(name, dtype, sharp=1.0, stream=None):
         args["prefix"] = ints([g[2] for g in groups])
     if bias:
         args["slopes"] = torch.tensor(slopes, device=DEV)
-    dev = [q.to(DEV), kp.to(DEV), vp.to(DEV), ints(ptr), ints(lens), torch.tensor(table, device=DEV)]
+    dev = [q.to(DEV), kp.to(DEV), vp.to(DEV), ints(ptr + head), ints(lens), torch.tensor(table, device=DEV)]
     torch.cuda.synchronize()
     c.attn(*dev, o, lse, ws, **args)
     torch.cuda.synchronize()
     assert int(st) == 0
-    close(o[:n], want[0], want[2], "o")
-    close(lse[:, :n], want[1], want[3], "lse")
-    assert bool((o[n:] == 17.0).all()) and bool((lse[:, n:] == 17.0).all())
+    close(o[head:head + n], want[0], want[2], "o")
+    close(lse[:, head:head + n], want[1], want[3], "lse")
+    for x in (o.transpose(0, 1), lse):
+        assert bool((x[:, :head] == 17.0).all()) and bool((x[:, head + n:] == 17.0).all())
     return o, lse
 
 

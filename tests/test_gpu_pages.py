@@ -1,5 +1,8 @@
 """The management of a cache's pages on the GPU against the oracle, every number equal, and a run of
 it with the caches that it serves."""
+import os
+import re
+
 import numpy as np
 import pytest
 
@@ -318,3 +321,25 @@ def test_a_serving_run(bits):
                 want = oda.attention(x64[r, :H], k, v, oda.Scores(), 0, u, TINY[dtype])
                 close(o[r], want[0], want[2], "o")
                 close(lse[:, r], want[1], want[3], "lse")
+
+
+def test_readme_example():
+    """The serving example of README.md runs: both samples end with the prompt and two tokens, their first pages shared, and the
+    last step's attention is that of what their caches hold."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    blocks = re.findall(r"```py3\n(.*?)```", text, re.S)
+    assert len(blocks) == 1
+    x = {}
+    exec(compile(blocks[0], "README.md", "exec"), x)
+    torch.cuda.synchronize()
+    assert x["lens"].tolist() == [302, 302]
+    rows = x["table"].tolist()
+    assert rows[0][:4] == rows[1][:4] and rows[0][4] != rows[1][4] and rows[0][5:] == [-1] * 11
+    k, v = (torch.empty((604, 8, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    x["cache"].read(x["k_pages"], x["v_pages"], ints([0, 302, 604]), x["lens"], x["table"], k, v)
+    torch.cuda.synchronize()
+    for b in range(2):
+        s = slice(302 * b, 302 * b + 302)
+        want = oda.attention(f64(x["q"])[b:b + 1], f64(k)[s], f64(v)[s], oda.Scores(), 0, HALF_STEP["bf16"])
+        close(x["o"][b:b + 1], want[0], want[2], "o")
+    assert bool((k[:300] == k[302:602]).all()) and not bool((k[300:302] == k[602:604]).all())
