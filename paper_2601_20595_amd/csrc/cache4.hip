@@ -82,7 +82,8 @@ __device__ __forceinline__ int64_t head_of(const CacheArgs& c, int page, int kvh
 // once a token, 6 operations a pair and head), so that their rounding to T and from there to a
 // code, next to a border too, follows from the definition and not from the order of a kernel's operations. Eight
 // lanes (D = 64: four) have a head; its rotated elements go through LDS, since a block's elements come from
-// pairs of two places, and two lanes quantise a block.
+// pairs of two places, and two lanes quantise a block. 64 tokens of 32 query heads on 8 of 128 take 4.6 us, a chain of latencies;
+// 11322 of 64 on 8, 426 MB, 90 us, 4.7 TB/s (a large copy: 5.1).
 template <class T, int D>
 __global__ __launch_bounds__(kThreads) void cache4_append(AppendArgs a) {
   constexpr int kCols = D / 16, kHeads = kThreads / kCols;
@@ -305,7 +306,7 @@ __global__ __launch_bounds__(kThreads) void cache4_read(ReadArgs a) {
 // sequences of over 100000, 244 MB in 51 us and the join 7, 4.8 TB/s (with 32-row products and every key through LDS 134);
 // 64 sequences of up to 8000, 129 MB, 34 and 5, of which the plan, the first loads and the last parts' ends are 8. With few
 // keys by a chain of latencies, 7.7 us for 900 keys. Where 16 sequences' rows share 8192 keys by the wide
-// parts' chain of products, weights and products, one wave a SIMD, and 21 MB of partial results (33 and 8).
+// parts' chain of products, weights and products, one wave a SIMD, and 13 MB of partial results (33 and 8).
 
 // Combination of the four lanes of a row: lane ^ 16, then lane ^ 32, swapped as in max_halves.
 __device__ __forceinline__ float max_quarters(float x) {
@@ -456,7 +457,7 @@ __device__ __forceinline__ const unsigned char* head_in(const uint16_t* pages, i
 // the queries follow); values through LDS, in 16 bits, where the transposing reads find them. The next
 // step's codes are asked for as soon as the last ones are converted, and waited for where they are; two steps ahead took
 // as long.
-template <class T, int D, bool kPlain, int R, int kTiles, int kAhead, bool alone>
+template <class T, int D, bool kPlain, int R, int kTiles, bool alone>
 __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry& x, const KeptEntry* local, const Part& p, int row0, unsigned char* stage,
                                             float (&s_ref)[4][32], float (&s_sum)[4][32], float* out, int lane, int wave) {
   using x8 = typename T::x8;
@@ -475,7 +476,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
   auto heads_at = [&](int n) { return head_of<D>(c, max(page_of(c, p, key_of(n + lane / kTiles) + 16 * (lane % kTiles)), 0), p.kvh); };
   int64_t heads = 0, next_heads = 0;
   const uint32_t code_at = Quarter<D>::code_place(l16, g), scale_at = Quarter<D>::scale_place(l16, g);
-  Quarter<D> k_sets[kAhead][kTiles], v_sets[kAhead][kTiles];
+  Quarter<D> k[kTiles], v[kTiles];
   auto load = [&](int n, const uint16_t* from, Quarter<D> (&to)[kTiles]) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -498,11 +499,8 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
     slope[i] = kPlain ? 0.0f : slope_of(a.scoring, pr[i].h);
   }
   if (mine_n > 0) {
-#pragma unroll
-    for (int n = 0; n < kAhead; ++n) {
-      load(n, c.k_pages, k_sets[n]);
-      load(n, c.v_pages, v_sets[n]);
-    }
+    load(0, c.k_pages, k);
+    load(0, c.v_pages, v);
   }
 #pragma unroll
   for (int i = 0; i < R; ++i) {
@@ -521,9 +519,9 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) acc[i][db] = f32x4_t{};
   QuarterSoftmax sm[R];
-  auto step = [&](int n, Quarter<D> (&k)[kTiles], Quarter<D> (&v)[kTiles]) {
+  for (int n = 0; n < mine_n; ++n) {
     if (n % kAtOnce == kAtOnce / 2) next_heads = heads_at(n + kAtOnce / 2);
-    if (n % kAtOnce == kAtOnce - kAhead) heads = next_heads;
+    if (n % kAtOnce == kAtOnce - 1) heads = next_heads;
     f32x4_t tile[R][kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
@@ -537,7 +535,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
         for (int i = 0; i < R; ++i) tile[i][t] = Mfma16<T>::run(kf, qf[i][s], tile[i][t]);
       }
     }
-    load(n + kAhead, c.k_pages, k);
+    load(n + 1, c.k_pages, k);
     x8 pb[R][kTiles / 2];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -585,7 +583,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
 #pragma unroll
         for (int s = 0; s < kParts; ++s) *reinterpret_cast<u32x4_t*>(mine + 32 * D * t + (to ^ 16 * s)) = values<T>(y.codes[s], scale);
       }
-      if (u == kTiles / 2 - 1) load(n + kAhead, c.v_pages, v);
+      if (u == kTiles / 2 - 1) load(n + 1, c.v_pages, v);
       asm volatile("" ::: "memory");  // (a wave's LDS accesses are done in order)
       x8 vf[D / 16];
 #pragma unroll
@@ -602,11 +600,6 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
         for (int i = 0; i < R; ++i) acc[i][db] = Mfma16<T>::run(vf[db], pb[i][u], acc[i][db]);
       asm volatile("" ::: "memory");
     }
-  };
-  for (int n = 0; n < mine_n; n += kAhead) {
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-      if (i == 0 || n + i < mine_n) step(n + i, k_sets[i], v_sets[i]);
   }
 
   // the waves' results against their common reference, summed in the order of the waves; the
@@ -807,17 +800,17 @@ __global__ __launch_bounds__(kThreads, few ? kCache4Few : kCacheGroups) void cac
         p.tile = r / kCacheTileRows;
         float* out = part_at<D>(a, place + p.tile - first);
         if (short_tasks && alone)
-          narrow_part<T, D, kPlain, 1, 2, 1, true>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, out, lane, wave);
+          narrow_part<T, D, kPlain, 1, 2, true>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, out, lane, wave);
         else
-          narrow_part<T, D, kPlain, 1, 2, 1, false>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, out, lane, wave);
+          narrow_part<T, D, kPlain, 1, 2, false>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, out, lane, wave);
       }
     } else if (wide) {
       p.tile += wave;
       wide_part<T, D, kPlain>(a, x, local, p, stage, part_at<D>(a, place + wave), lane, wave);
     } else if (x.rows <= 16) {
-      narrow_part<T, D, kPlain, 1, 4, 1, false>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+      narrow_part<T, D, kPlain, 1, 4, false>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
     } else {
-      narrow_part<T, D, kPlain, 2, 2, 1, false>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+      narrow_part<T, D, kPlain, 2, 2, false>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
     }
   });
 }
