@@ -793,16 +793,15 @@ __global__ __launch_bounds__(kThreads, few ? kCache4Few : kCacheGroups) void cac
   static_assert(sizeof(stage) >= 4 * 32 * 2 * D && sizeof(stage) >= 4 * 16 * D * 4, "the narrow waves' values, and results of theirs");
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  cache_run<short_tasks ? kCache4AloneCost : 0, D == 128 ? kCache4AloneBlocks : 2 * kCache4AloneBlocks>(a, stage, [&](const Entry& x, const KeptEntry* local, Part& p, int64_t place, bool wide, bool alone) {
-    if constexpr (few) {
+  constexpr int kCost = short_tasks ? kCache4AloneCost : 0, kMost = D == 128 ? kCache4AloneBlocks : 2 * kCache4AloneBlocks;
+  cache_run<kCost, kMost, few ? 0 : kCache4OtherUnits>(a, stage, [&](const Entry& x, const KeptEntry* local, Part& p, int64_t place, bool wide, bool alone) {
+    if (short_tasks && alone) {
+      narrow_part<T, D, kPlain, 1, 2, true>(a, x, local, p, 0, stage, s_ref, s_sum, part_at<D>(a, place), lane, wave);
+    } else if constexpr (few) {
       const int first = p.tile;
       for (int r = first * kCacheTileRows; r < min(x.rows, first * kCacheTileRows + kCacheWideRows); r += 16) {
         p.tile = r / kCacheTileRows;
-        float* out = part_at<D>(a, place + p.tile - first);
-        if (short_tasks && alone)
-          narrow_part<T, D, kPlain, 1, 2, true>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, out, lane, wave);
-        else
-          narrow_part<T, D, kPlain, 1, 2, false>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, out, lane, wave);
+        narrow_part<T, D, kPlain, 1, 2, false>(a, x, local, p, r % kCacheTileRows, stage, s_ref, s_sum, part_at<D>(a, place + p.tile - first), lane, wave);
       }
     } else if (wide) {
       p.tile += wave;
@@ -839,8 +838,9 @@ hipError_t attend(const CacheAttnArgs& a, hipStream_t s) {
 
 template <class T, int D>
 hipError_t attend(const CacheAttnArgs& a, bool few, hipStream_t s) {
-  if (!few) return attend<T, D, false, false>(a, s);
-  return enough_to_run_alone(a.c.batch, a.head_workers) ? attend<T, D, true, true>(a, s) : attend<T, D, true, false>(a, s);
+  const bool many = enough_to_run_alone(a.c.batch, a.head_workers);
+  if (few) return many ? attend<T, D, true, true>(a, s) : attend<T, D, true, false>(a, s);
+  return many && a.n_groups > 0 ? attend<T, D, false, true>(a, s) : attend<T, D, false, false>(a, s);
 }
 
 }  // namespace

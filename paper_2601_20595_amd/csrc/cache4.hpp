@@ -22,6 +22,8 @@ constexpr int kCache4TaskCost = 10;
 // task's cost 2: 19.2 us (128 sequences), 4: 18.3, 8: 19.6.
 constexpr int kCache4AloneCost = 4;
 constexpr int kCache4AloneBlocks = 48;  // of 128 elements a head, on average; 64: twice as many
+// Units of a wave's run that a unit of another task counts for, where workgroups are divided between the two.
+constexpr int kCache4OtherUnits = 4;
 // Whether the sequences' rows (new tokens times heads of a key/value head) are few, on average; with groups, whose
 // sequences' rows go through the shared keys together, never.
 inline bool cache4_few(int64_t tokens, int32_t H, int32_t Hkv, int32_t batch, int32_t n_groups) {

@@ -346,7 +346,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attn(CacheAttnArgs a) {
   static_assert(sizeof(stage) >= 4 * 32 * D * 4, "and the waves' results");
   static_assert(sizeof(stage) >= kCacheGroupBytes, "and, before, the groups");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  cache_run<0, 0>(a, stage, [&](const Entry& x, const KeptEntry* local, Part& p, int64_t place, bool wide, bool) {
+  cache_run<0, 0, 0>(a, stage, [&](const Entry& x, const KeptEntry* local, Part& p, int64_t place, bool wide, bool) {
     if (wide) {
       p.tile += wave;
       wide_part<T, D, kPlain>(a, x, local, p, stage, part_at<D>(a, place + wave), lane, wave);
@@ -370,12 +370,15 @@ struct RowParts {
     if (x.blocks == 0 || r < 0 || r >= x.rows) return;
     const int tile = r / kCacheTileRows;
     in_tile = r % kCacheTileRows;
+    const bool wide = x.rows > kCacheTileRows;
+    const bool other = x.rows > kCacheAloneRows;
+    const int run = other ? plan.run[1] : plan.run[0], shift = other ? plan.shift[1] : plan.shift[0], cost = other ? plan.cost[1] : plan.cost[0];
     // the first block's unit of its task
-    const int start = x.before + (x.rows > kCacheTileRows ? r / kCacheWideRows : 0) * (x.blocks + plan.cost) + plan.cost;
-    const int w0 = start / plan.run, w1 = (start + x.blocks - 1) / plan.run;
-    const int64_t first = static_cast<int64_t>(kvh) * (plan.tiles + 4 * a.head_workers) + x.tiles + tile + (w0 << plan.shift);
-    count = static_cast<int>(min<int64_t>(w1 - w0 + 1, (a.max_parts - first + (1 << plan.shift) - 1) >> plan.shift));
-    step = cache_part_bytes(D) << plan.shift;
+    const int start = x.before + (wide ? r / kCacheWideRows : 0) * (x.blocks + cost) + cost;
+    const int w0 = start / run, w1 = (start + x.blocks - 1) / run;
+    const int64_t first = static_cast<int64_t>(kvh) * (plan.tiles + 4 * a.head_workers) + x.tiles + tile + (w0 << shift);
+    count = static_cast<int>(min<int64_t>(w1 - w0 + 1, (a.max_parts - first + (1 << shift) - 1) >> shift));
+    step = cache_part_bytes(D) << shift;
     base = a.ws + cache_plan_bytes() + first * cache_part_bytes(D);
   }
   // (behind the end of p0 .. p0 + n - 1 the last one again, which weighs 0 there)

@@ -11,6 +11,7 @@ namespace csg {
 
 constexpr int kCacheTileRows = 32;     // (token, head) rows of a tile, one wave's
 constexpr int kCacheWideRows = 128;    // rows of a wide task: a tile for each of four waves
+constexpr int kCacheAloneRows = 16;    // rows of a task that a wave can do alone, at most
 constexpr int kCacheBlock = 32;        // keys per inner step of a wave, and unit of work
 constexpr int kCacheWideBlock = 64;    // keys per inner step of a wide task
 // What beginning and ending a task costs, in blocks. 64 sequences on four shared prompts 47.9 us with 3,

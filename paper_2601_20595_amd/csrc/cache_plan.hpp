@@ -39,6 +39,7 @@ struct Entry {
   }
   __device__ __forceinline__ int tiles() const { return (rows + kCacheTileRows - 1) / kCacheTileRows; }
   __device__ __forceinline__ bool wide() const { return rows > kCacheTileRows; }
+  __device__ __forceinline__ bool small() const { return rows <= kCacheAloneRows; }
   __device__ __forceinline__ int tasks() const { return wide() ? (rows + kCacheWideRows - 1) / kCacheWideRows : 1; }
   // a task's units of work: its blocks, behind what beginning and ending it costs
   __device__ __forceinline__ int span(int cost) const { return blocks > 0 ? cost + blocks : 0; }
@@ -108,17 +109,19 @@ __device__ __forceinline__ Entry entry_of(const CacheAttnArgs& a, const Groups& 
   return x;
 }
 
-// The plan of a call in the workspace, for cache_merge: an entry's units and tiles before it,
+// The plan of a call in the workspace, for cache_merge: an entry's units and tiles before it (of its kind, where
+// small and other tasks have runs of their own; the tiles with where the kind's places begin),
 // its own blocks, rows and first token; of a sequence, its group's entry too (-1: none).
 struct PlanEntry {
   int32_t before, tiles, blocks, rows, token0, group, unused[2];
 };
 struct Plan {
-  int32_t run;      // units of a run
   int32_t tiles;    // tiles of one key/value head
-  int32_t shift;    // places from a tile's part in one run to that in the next, a task's tiles at most: 1 << shift
-  int32_t cost;     // units that beginning and ending a task costs
-  int32_t unused[4];
+  // of entries of up to kCacheAloneRows rows, and of more:
+  int32_t run[2];    // units of a run
+  int32_t shift[2];  // places from a tile's part in one run to that in the next, a task's tiles at most: 1 << shift
+  int32_t cost[2];   // units that beginning and ending a task costs
+  int32_t unused;
 };
 __device__ __forceinline__ Plan* plan_in(unsigned char* ws) { return reinterpret_cast<Plan*>(ws); }
 __device__ __forceinline__ PlanEntry* entries_in(unsigned char* ws) { return reinterpret_cast<PlanEntry*>(ws + sizeof(Plan)); }
@@ -214,12 +217,13 @@ __host__ __device__ __forceinline__ bool enough_to_run_alone(int tasks, int work
 
 // A workgroup's run: its parts, one after the other, through do_part, which all of its threads call with the
 // entry, the sequences' entries (locate_row), the part, whose tile is its task's first, that tile's place, and whether the
-// task is wide. With kAloneCost > 0 and many tasks (none of them wide) of up to kAloneBlocks blocks on average, every wave has
-// a run, and does its parts alone (the last argument): a task then costs kAloneCost units. `stage`: LDS that the parts
-// use (and the groups, before them).
-template <int kAloneCost, int kAloneBlocks, class DoPart>
+// task is wide. With kAloneCost > 0 and many tasks of small entries, of up to kAloneBlocks blocks on average, every wave has a run
+// of those, and does its parts alone (the last argument): a task then costs kAloneCost units. With other tasks beside
+// them the workgroups are divided, another task's unit counting kOtherUnits of a wave's (0: that is not done).
+// `stage`: LDS that the parts use (and the groups, before them).
+template <int kAloneCost, int kAloneBlocks, int kOtherUnits, class DoPart>
 __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char* stage, DoPart do_part) {
-  __shared__ uint32_t s_wave_blocks[4], s_wave_tasks[4], s_wave_tiles[4], s_wave_wide[4];
+  __shared__ uint32_t s_wave_units[4], s_wave_tiles[4], s_wave_blocks[4], s_wave_tasks[4];
   __shared__ int s_entry[4], s_first[4], s_tiles[4];
   __shared__ KeptEntry s_entries[kThreads];
   const CacheArgs& c = a.c;
@@ -244,8 +248,8 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
   // Each thread counts some entries; units and tiles before each of them by a scan. Where a thread
   // has one entry, everyone finds it in LDS.
   const int per = (n_entries + kThreads - 1) / kThreads;
-  uint32_t blocks = 0, tasks = 0, tiles = 0;
-  bool wide_one = false;
+  // (With kAloneCost, small entries are counted by themselves: blocks, and tasks and tiles in the halves of a word.)
+  uint32_t units = 0, tiles = 0, blocks = 0, tasks = 0;
   Entry mine{};
   for (int i = 0; i < per; ++i) {
     const int e = tid * per + i;
@@ -253,100 +257,142 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
     const Entry x = entry_of(a, local, e);
     mine = x;
     if (per == 1) s_entries[e] = {x.token0, x.rows, x.b0, x.b1, x.lo, x.end};
-    if constexpr (kAloneCost > 0) {
-      if (x.blocks > 0) {
-        blocks += x.tasks() * x.blocks;
-        tasks += x.tasks();
-        wide_one |= x.wide();
-      }
+    if (kAloneCost > 0 && x.small()) {
+      blocks += x.blocks;
+      tasks += (x.blocks > 0 ? 1 : 0) + (x.tiles() << 16);
     } else {
-      blocks += x.tasks() * x.span(a.task_cost);  // (with what the tasks cost)
+      units += x.tasks() * x.span(a.task_cost);
+      tiles += x.tiles();
     }
-    tiles += x.tiles();
   }
-  const uint32_t own_blocks = blocks, own_tasks = tasks, own_tiles = tiles;
+  uint32_t own_units = units, own_blocks = blocks, own_tasks = tasks;
+  const uint32_t own_tiles = tiles;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const uint32_t ub = __shfl_up(blocks, d), uk = kAloneCost > 0 ? __shfl_up(tasks, d) : 0, ut = __shfl_up(tiles, d);
+    const uint32_t uu = __shfl_up(units, d), ut = __shfl_up(tiles, d);
+    const uint32_t ub = kAloneCost > 0 ? __shfl_up(blocks, d) : 0, uk = kAloneCost > 0 ? __shfl_up(tasks, d) : 0;
     if (lane >= d) {
+      units += uu;
+      tiles += ut;
       blocks += ub;
       tasks += uk;
-      tiles += ut;
     }
   }
-  const bool wide_any = kAloneCost > 0 && __builtin_amdgcn_ballot_w64(wide_one) != 0;
   if (lane == 63) {
-    s_wave_blocks[wave] = blocks;
+    s_wave_units[wave] = units;
     s_wave_tiles[wave] = tiles;
     if constexpr (kAloneCost > 0) {
+      s_wave_blocks[wave] = blocks;
       s_wave_tasks[wave] = tasks;
-      s_wave_wide[wave] = wide_any;
     }
   }
   __syncthreads();
+  units -= own_units;
+  tiles -= own_tiles;
   blocks -= own_blocks;
   tasks -= own_tasks;
-  tiles -= own_tiles;
   for (int i = 0; i < wave; ++i) {
-    blocks += s_wave_blocks[i];
-    if constexpr (kAloneCost > 0) tasks += s_wave_tasks[i];
+    units += s_wave_units[i];
     tiles += s_wave_tiles[i];
+    if constexpr (kAloneCost > 0) {
+      blocks += s_wave_blocks[i];
+      tasks += s_wave_tasks[i];
+    }
   }
-  const int all_tiles = __builtin_amdgcn_readfirstlane(s_wave_tiles[0] + s_wave_tiles[1] + s_wave_tiles[2] + s_wave_tiles[3]);
+  auto sum = [](const uint32_t (&of)[4]) { return __builtin_amdgcn_readfirstlane(of[0] + of[1] + of[2] + of[3]); };
+  int all_tiles = sum(s_wave_tiles), all_units = sum(s_wave_units);
+  // the first `alone` workgroups have runs of small tasks for each wave, the others those of all other tasks
+  int alone = 0, all_small = 0, small_tiles = 0;
+  if constexpr (kAloneCost > 0) {
+    const int all_blocks = sum(s_wave_blocks), all_tasks = sum(s_wave_tasks);
+    const int n_tasks = all_tasks & 0xffff;
+    small_tiles = all_tasks >> 16;
+    const bool pure = kOtherUnits > 0 ? all_units == 0 : all_tiles == 0;
+    all_tiles += small_tiles;
+    if (enough_to_run_alone(n_tasks, a.head_workers) && all_blocks <= kAloneBlocks * n_tasks &&
+        (pure || (kOtherUnits > 0 && a.head_workers > 1))) {
+      all_small = all_blocks + kAloneCost * n_tasks;
+      alone = a.head_workers;
+      if (!pure) {
+        const float part = all_small * __builtin_amdgcn_rcpf(static_cast<float>(all_small) + kOtherUnits * static_cast<float>(all_units));
+        alone = __builtin_amdgcn_readfirstlane(clamped(static_cast<int>(part * a.head_workers + 0.5f), 1, a.head_workers - 1));
+      }
+    } else {
+      all_units += all_blocks + a.task_cost * n_tasks;
+      units += blocks + a.task_cost * (tasks & 0xffff);
+      own_units += own_blocks + a.task_cost * (own_tasks & 0xffff);
+      tiles += tasks >> 16;
+      small_tiles = 0;
+    }
+  }
   // Bounds that do not ascend may name rows several times, and with them more units than 32 bits count: then
   // there is nothing to do. (As many tiles as the host has reckoned with have no more units than it has.)
   const bool fits = static_cast<uint32_t>(all_tiles) <= a.max_tiles;
-  const int all_blocks = __builtin_amdgcn_readfirstlane(s_wave_blocks[0] + s_wave_blocks[1] + s_wave_blocks[2] + s_wave_blocks[3]);
-  bool alone = false;
-  int cost = a.task_cost, all = all_blocks, units = blocks, own_units = own_blocks;
+  const int others = a.head_workers - alone;
+  const bool small = kOtherUnits > 0 ? w < alone : alone > 0;  // (the workgroup's kind of tasks)
+  auto run_of = [&](bool is_small) {
+    const int all = is_small ? all_small : all_units, runs = is_small ? 4 * alone : others;
+    return max(kCacheMinRun, (all + runs - 1) / max(1, runs));
+  };
+  const int all = fits ? (small ? all_small : all_units) : 0;
+  const int run = run_of(small);
+  const int first_begin = (small ? 4 * w : w - alone) * run;  // the workgroup's runs: one, or one a wave
+  const int other_places = 4 * alone + small_tiles;
+  int before = units, own = own_units;
   if constexpr (kAloneCost > 0) {
-    const int all_tasks = __builtin_amdgcn_readfirstlane(s_wave_tasks[0] + s_wave_tasks[1] + s_wave_tasks[2] + s_wave_tasks[3]);
-    const int wide_task = __builtin_amdgcn_readfirstlane(s_wave_wide[0] | s_wave_wide[1] | s_wave_wide[2] | s_wave_wide[3]);
-    alone = !wide_task && enough_to_run_alone(all_tasks, a.head_workers) && all_blocks <= kAloneBlocks * all_tasks;
-    if (alone) cost = kAloneCost;
-    all += cost * all_tasks;
-    units += cost * tasks;
-    own_units += cost * own_tasks;
+    if (small) {
+      before = blocks + kAloneCost * (tasks & 0xffff);
+      own = own_blocks + kAloneCost * (own_tasks & 0xffff);
+    }
   }
-  if (!fits) all = 0;
-  const int workers = alone ? 4 * a.head_workers : a.head_workers;
-  const int run = max(kCacheMinRun, (all + workers - 1) / workers);
-  const int first_begin = (alone ? 4 * w : w) * run;  // the workgroup's runs: one, or one a wave
   // for cache_merge, and the entry where the run begins
-  if (blockIdx.x == 0 || (units < first_begin + (alone ? 4 : 1) * run && first_begin < units + own_units)) {
-    int before = units, tiles_before = tiles;
+  if (blockIdx.x == 0 || (before < first_begin + (small ? 4 : 1) * run && first_begin < before + own)) {
+    int units_before = units, tiles_before = tiles;
+    int small_before = blocks + kAloneCost * (tasks & 0xffff), small_tiles_before = tasks >> 16;
     for (int i = 0; i < per; ++i) {
       const int e = tid * per + i;
       if (e >= n_entries) break;
       const Entry x = per == 1 ? mine : entry_of(a, local, e);
-      const int n = x.tasks() * x.span(cost);
-      for (int k = 0; k < (alone ? 4 : 1); ++k) {
-        const int begin = first_begin + k * run;
-        if (before <= begin && begin < before + n) {
-          s_entry[k] = e;
-          s_first[k] = begin - before;
-          s_tiles[k] = tiles_before;
+      const bool is_small = kOtherUnits > 0 ? alone > 0 && x.small() : small;
+      const int n = x.tasks() * x.span(is_small ? kAloneCost : a.task_cost);
+      const int x_before = is_small ? small_before : units_before, x_tiles = is_small ? small_tiles_before : tiles_before;
+      if (is_small == small) {
+        for (int k = 0; k < (small ? 4 : 1); ++k) {
+          const int begin = first_begin + k * run;
+          if (x_before <= begin && begin < x_before + n) {
+            s_entry[k] = e;
+            s_first[k] = begin - x_before;
+            s_tiles[k] = x_tiles;
+          }
         }
       }
       if (blockIdx.x == 0) {
-        entries_in(a.ws)[e] = {before, tiles_before, fits ? x.blocks : 0, x.rows, x.token0, x.group, {0, 0}};
+        entries_in(a.ws)[e] = {x_before, x_tiles + (is_small ? 0 : other_places), fits ? x.blocks : 0, x.rows, x.token0, x.group, {0, 0}};
         if (x.own && (x.end != c.lens[x.b0] || x.rows / (c.H / c.Hkv) > x.end)) tell(c, kCacheBadLength);
       }
-      before += n;
-      tiles_before += x.tiles();
+      if (is_small) {
+        small_before += n;
+        small_tiles_before += x.tiles();
+      } else {
+        units_before += n;
+        tiles_before += x.tiles();
+      }
     }
     if (blockIdx.x == 0 && tid == 0) {
-      *plan_in(a.ws) = {run, all_tiles, alone ? 0 : 2, cost, {0, 0, 0, 0}};
+      const int small_run = kOtherUnits > 0 && alone ? run_of(true) : run, other_run = kOtherUnits > 0 ? run_of(false) : run;
+      *plan_in(a.ws) = {all_tiles, {small_run, other_run}, {alone ? 0 : 2, 2},
+                        {alone ? kAloneCost : a.task_cost, a.task_cost}, 0};
       if (!fits) tell(c, kCacheBadLength);
     }
   }
   if (first_begin >= all) return;
   __syncthreads();
-  const int mine_k = alone ? wave : 0, begin = first_begin + mine_k * run;
+  const int mine_k = small ? wave : 0, begin = first_begin + mine_k * run;
   int left = min(run, all - begin);  // (not positive: the wave has no run)
   int e = __builtin_amdgcn_readfirstlane(s_entry[mine_k]), in_entry = __builtin_amdgcn_readfirstlane(s_first[mine_k]);
   int tiles_before = __builtin_amdgcn_readfirstlane(s_tiles[mine_k]);
-  const int64_t places = static_cast<int64_t>(kvh) * (all_tiles + 4 * a.head_workers) + 4 * w + mine_k;
+  const int cost = small ? kAloneCost : a.task_cost;
+  const int64_t places = static_cast<int64_t>(kvh) * (all_tiles + 4 * a.head_workers) + 4 * w + mine_k + (small ? 0 : small_tiles);
   const KeptEntry* sequences = per == 1 ? s_entries + a.n_groups : nullptr;
   while (left > 0) {
     Entry x;
@@ -363,7 +409,8 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
     } else {
       x = entry_of(a, GlobalGroups{a}, e);
     }
-    const int n = x.tasks() * x.span(cost);
+    const bool other = kOtherUnits > 0 && alone > 0 && x.small() != small;  // (it is of the other workgroups')
+    const int n = other ? 0 : x.tasks() * x.span(cost);
     if (in_entry < n) {
       Part p;
       p.kvh = kvh;
@@ -379,10 +426,10 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
       p.key0 = (x.block0 + first) * kCacheBlock;
       p.end = min(x.end, p.key0 + count * kCacheBlock);
       p.tile = wide ? 4 * task : 0;
-      do_part(x, sequences, p, places + tiles_before + p.tile, wide, alone);
+      do_part(x, sequences, p, places + tiles_before + p.tile, wide, small);
     } else {
       in_entry = 0;
-      tiles_before += x.tiles();
+      if (!other) tiles_before += x.tiles();
       ++e;
     }
   }

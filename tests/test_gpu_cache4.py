@@ -171,6 +171,10 @@ MIXED = {
     "sixteen rows each": ([4] * 9, [4, 5, 63, 64, 65, 128, 129, 260, 1000], 4, 1, 128, 64, [], 0.0, False),
     "a wave each": ([1, 1, 4, 0, 1] * 20, [(i * 37) % 190 + (4 if i % 5 == 2 else 1) for i in range(100)], 16, 2, 128, 32, [], 0.0, True),
     "a wave each, over many runs": ([1] * 50, [3 + (i * i * 7) % 1400 for i in range(50)], 8, 8, 64, 16, [], 5.0, False),
+    "a wave each, beside groups": ([1] * 60 + [0, 3, 9, 1] * 3, [160 + (i * 37) % 300 for i in range(30)] + [70 + (i * 53) % 200 for i in range(30)] +
+                                   [1, 3, 9, 40] * 3, 32, 8, 64, 16, [(0, 25, 128), (25, 30, 96), (30, 60, 64)], 0.0, False),
+    "a wave each, beside groups, with a cap": ([1, 2] * 40, [800 + (i * 91) % 700 for i in range(40)] + [5 + (i * 29) % 90 for i in range(40)],
+                                               16, 4, 128, 32, [(0, 5, 640), (5, 40, 800)], 5.0, True),
     "seventeen heads": ([1, 1], [70, 1500], 17, 1, 128, 16, [], 0.0, False),
 }
 
