@@ -317,6 +317,7 @@ csg_status cache_attn(hipError_t (*launch)(const csg::CacheAttnArgs&, bool, int,
   a.head_workers = csg::cache_head_workers(groups, c.n_kv_heads);
   a.dies = 8 / std::gcd(8, c.n_kv_heads);
   a.task_cost = four ? csg::kCache4TaskCost : csg::kCacheTaskCost;
+  a.min_run = four ? csg::cache4_min_run(c.tokens, c.n_heads, c.n_kv_heads, c.batch, c.n_groups) : csg::kCacheMinRun;
   a.max_parts = csg::cache_max_parts(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups, a.head_workers);
   a.max_tiles = csg::cache_max_tiles(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups);
   a.ws = static_cast<unsigned char*>(workspace);

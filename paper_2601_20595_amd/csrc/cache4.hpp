@@ -29,6 +29,11 @@ constexpr int kCache4OtherUnits = 4;
 inline bool cache4_few(int64_t tokens, int32_t H, int32_t Hkv, int32_t batch, int32_t n_groups) {
   return n_groups == 0 && tokens * (H / Hkv) <= int64_t{16} * batch;
 }
+// Units of a run, at least.
+constexpr int kCache4WideRun = 8;
+inline int32_t cache4_min_run(int64_t tokens, int32_t H, int32_t Hkv, int32_t batch, int32_t n_groups) {
+  return tokens * (H / Hkv) > int64_t{kCacheTileRows} * n_groups && n_groups > 0 ? kCache4WideRun : kCacheMinRun;
+}
 constexpr int kReadRows = 32;  // rows of the outputs that a workgroup reads
 // Heads that it reads: as many as leave four workgroups a CU, up to 8.
 inline int32_t cache4_read_heads(int64_t tokens, int32_t Hkv, int32_t cus) {

@@ -60,6 +60,7 @@ struct CacheAttnArgs {
   int32_t head_workers;  // workgroups that share the blocks of keys of a key/value head
   int32_t dies;          // dies that its workgroups are on
   int32_t task_cost;     // what beginning and ending a task costs, in blocks
+  int32_t min_run;       // units that a workgroup takes at least
   int64_t max_parts;     // places of partial results in the workspace
   int64_t max_tiles;     // tiles of a key/value head, if the bounds ascend
   unsigned char* ws;

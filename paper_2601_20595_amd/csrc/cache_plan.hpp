@@ -332,7 +332,8 @@ __device__ __forceinline__ void cache_run(const CacheAttnArgs& a, unsigned char*
   const bool small = kOtherUnits > 0 ? w < alone : alone > 0;  // (the workgroup's kind of tasks)
   auto run_of = [&](bool is_small) {
     const int all = is_small ? all_small : all_units, runs = is_small ? 4 * alone : others;
-    return max(kCacheMinRun, (all + runs - 1) / max(1, runs));
+    const int units = max(is_small ? kCacheMinRun : a.min_run, (all + runs - 1) / max(1, runs));
+    return is_small || kOtherUnits == 0 ? units : units + (units & 1);  // (a wide block is two)
   };
   const int all = fits ? (small ? all_small : all_units) : 0;
   const int run = run_of(small);
