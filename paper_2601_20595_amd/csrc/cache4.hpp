@@ -22,17 +22,22 @@ constexpr int kCache4TaskCost = 10;
 // task's cost 2: 19.2 us (128 sequences), 4: 18.3, 8: 19.6.
 constexpr int kCache4AloneCost = 4;
 constexpr int kCache4AloneBlocks = 48;  // of 128 elements a head, on average; 64: twice as many
-// Units of a wave's run that a unit of another task counts for, where workgroups are divided between the two.
+// Units of a wave's run that a unit of another task counts for, where workgroups are divided between the two (undivided; 2, 4, 6,
+// 8): 64 sequences of 20 to 1000 keys on four prompts 39.2 us; 42.7, 38.5, 39.0, 41.9; 256 of 300 to 2000 130; 106, 88.7, 90.1,
+// 92.0; 96 of up to 400 on three (heads of 64) 30.1; 23.6, 24.9, 23.2, 23.9. With fewer than half as many small tasks as workgroups
+// it gains nothing (24 sequences on two prompts 24.1, divided 24.4).
 constexpr int kCache4OtherUnits = 4;
 // Whether the sequences' rows (new tokens times heads of a key/value head) are few, on average; with groups, whose
 // sequences' rows go through the shared keys together, never.
 inline bool cache4_few(int64_t tokens, int32_t H, int32_t Hkv, int32_t batch, int32_t n_groups) {
   return n_groups == 0 && tokens * (H / Hkv) <= int64_t{16} * batch;
 }
-// Units of a run, at least.
+// Units of a run, at least. A part of a wide task writes 66 KB: 16 sequences on a prompt of 8192 take 32.4 us with runs of 4, 27.7
+// with 8, 28.6 with 16; 64 of up to 100 keys on one of 2000 26.0, 24.3, 27.9. Without groups shorter ones end sooner (16 rows of
+// a head on 500 keys, two sequences: 14.3, 16.5, 16.6).
 constexpr int kCache4WideRun = 8;
 inline int32_t cache4_min_run(int64_t tokens, int32_t H, int32_t Hkv, int32_t batch, int32_t n_groups) {
-  return tokens * (H / Hkv) > int64_t{kCacheTileRows} * n_groups && n_groups > 0 ? kCache4WideRun : kCacheMinRun;
+  return n_groups > 0 && tokens * (H / Hkv) > int64_t{kCacheTileRows} * n_groups ? kCache4WideRun : kCacheMinRun;
 }
 constexpr int kReadRows = 32;  // rows of the outputs that a workgroup reads
 // Heads that it reads: as many as leave four workgroups a CU, up to 8.

@@ -7,11 +7,12 @@ import paper_2601_20595_amd as csg
 from oracle import cache4
 from oracle import doc_attention as oda
 
+from test_gpu_cache import APPEND, ATTN, _table
+
 torch = pytest.importorskip("torch")
 if torch.cuda.is_available():
     from attn_util import DEV, HALF_STEP, TINY, TORCH, close, f64, ints, normal, pointers
     from cache4_util import pages4, values4
-    from test_gpu_cache import APPEND, ATTN, _table
 
 pytestmark = pytest.mark.gpu
 BITS = {"bf16": 0x7F80, "f16": 0x7C00}  # infinity
@@ -179,6 +180,23 @@ MIXED = {
 }
 
 
+def _drawn_many(seed):
+    """Many sequences, most of them in groups, on 8 key/value heads: short ones beside the shared keys' rows."""
+    rng = np.random.default_rng(900 + seed)
+    batch = int(rng.choice([34, 70, 130, 300]))
+    new = [int(x) for x in rng.integers(0, rng.choice([2, 2, 5]), batch)]
+    lens = [int(x + rng.integers(0, rng.choice([3, 40, 200]))) for x in new]
+    page = int(rng.choice([16, 32, 64]))
+    groups, cuts = [], sorted(set(int(x) for x in rng.integers(0, batch + 1, int(rng.integers(2, 7)))))
+    for b0, b1 in zip(cuts, cuts[1:]):
+        shared = page * int(rng.integers(1, 1 + 320 // page))
+        for b in range(b0, b1):
+            lens[b] += shared
+        groups.append((b0, b1, shared))
+    return (new, lens, 8 * int(rng.choice([1, 2, 3, 5])), 8, int(rng.choice([64, 128])), page, groups,
+            float(rng.choice([0.0, 0.0, 9.0])), bool(rng.random() < 0.3))
+
+
 def _drawn(seed):
     """A call of random shape: sequences, rows per key/value head from 1 to over 128, pages, groups, cap, bias."""
     rng = np.random.default_rng(100 + seed)
@@ -200,8 +218,8 @@ def _drawn(seed):
             float(rng.choice([0.0, 0.0, 9.0])), bool(rng.random() < 0.3))
 
 
-def _attn_case(name, dtype, sharp=1.0, stream=None):
-    spec = _drawn(name) if isinstance(name, int) else MIXED[name] if name in MIXED else ATTN[name]
+def _attn_case(name, dtype, sharp=1.0, stream=None, many=False):
+    spec = (_drawn_many if many else _drawn)(name) if isinstance(name, int) else MIXED[name] if name in MIXED else ATTN[name]
     new, lens, H, Hkv, D, page, groups, cap, bias = spec
     rng = np.random.default_rng(7)
     # drawn calls: a part of a larger batch's rows, others before and behind
@@ -256,6 +274,11 @@ def test_attention(name, dtype):
 @pytest.mark.parametrize("seed", range(40))
 def test_attention_drawn(seed):
     _attn_case(seed, "bf16" if seed % 3 else "f16", 1.0 + seed % 4)
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_attention_drawn_beside_groups(seed):
+    _attn_case(seed, "f16" if seed % 3 else "bf16", 1.0 + seed % 4, many=True)
 
 
 def test_two_streams_with_a_workspace_each():
