@@ -176,6 +176,8 @@ MIXED = {
                                    [1, 3, 9, 40] * 3, 32, 8, 64, 16, [(0, 25, 128), (25, 30, 96), (30, 60, 64)], 0.0, False),
     "a wave each, beside groups, with a cap": ([1, 2] * 40, [800 + (i * 91) % 700 for i in range(40)] + [5 + (i * 29) % 90 for i in range(40)],
                                                16, 4, 128, 32, [(0, 5, 640), (5, 40, 800)], 5.0, True),
+    "two workgroups a head, beside a group": ([1] * 4, [49, 70, 53, 9], 9 * 256, 256, 64, 16, [(0, 3, 48)], 0.0, False),
+    "one workgroup a head, beside a group": ([1] * 4, [33, 40, 36, 20], 9 * 512, 512, 64, 16, [(0, 3, 32)], 0.0, False),
     "seventeen heads": ([1, 1], [70, 1500], 17, 1, 128, 16, [], 0.0, False),
 }
 
