@@ -394,7 +394,8 @@ __device__ __forceinline__ constexpr int swz16(int r) {
 
 // A quarter of a row's codes, D / 4 elements, and its scale. `head`: where the head's rows of the page begin; the lane's
 // row and quarter are in `at` and `scale_at`, from row0 on. Every row of a page may be read, so nothing is checked here:
-// scores of keys that are not the part's are masked, and their values get scale 0.
+// scores of keys that are not the part's are masked, and their values get scale 0 (which the
+// conversions take for 2^-127: a weight of 0 makes zeros of them, and codes of 0 of keys without a page).
 template <int D>
 struct Quarter {
   uint32_t codes[D / 32];
@@ -413,6 +414,11 @@ struct Quarter {
       codes[1] = x[1];
     }
     scales = *reinterpret_cast<const uint32_t*>(head + (((D / 2) << c.page_shift) + row0 * (D / 32)) + (scale_at & ~3u));
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (uint32_t& x : codes) x = 0;
+    scales = 0;
   }
   __device__ __forceinline__ float scale(uint32_t scale_at) const { return scale_of(__builtin_amdgcn_ubfe(scales, 8 * (scale_at & 3u), 8)); }
 };
@@ -439,11 +445,25 @@ struct Half {
     else
       scales = *reinterpret_cast<const uint16_t*>(from + at);
   }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (uint32_t& x : codes) x = 0;
+    scales = 0;
+  }
   // of codes[s]
   __device__ __forceinline__ float scale(int s, int hlf) const {
     return scale_of(__builtin_amdgcn_ubfe(scales, 8 * (hlf * (D / 64) + s / 4), 8));
   }
 };
+
+// Where the head's rows of the page of keys key .. key + 15 begin, of page 0 if they have none; without: the lanes whose
+// keys are the part's and have none.
+template <int D>
+__device__ __forceinline__ int64_t head_at(const CacheArgs& c, const Part& p, int key, uint64_t& without) {
+  const int page = page_of(c, p, key);
+  without = __builtin_amdgcn_ballot_w64(page < 0 && key < p.end && key + 16 > p.lo);
+  return head_of<D>(c, max(page, 0), p.kvh);
+}
 
 // Where 16 keys' rows of the head begin, of those that lane `at` of `heads` knows.
 __device__ __forceinline__ const unsigned char* head_in(const uint16_t* pages, int64_t heads, int at) {
@@ -472,9 +492,10 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
   const int stride = alone ? kStep : 4 * kStep, my_key0 = p.key0 + (alone ? 0 : wave * kStep);
   auto key_of = [&](int n) { return my_key0 + n * stride; };
   // lane n holds where the 16 keys n % kTiles of the wave's step n / kTiles have the head's rows of their page (kAtOnce steps
-  // at a time); page 0 where there is none
-  auto heads_at = [&](int n) { return head_of<D>(c, max(page_of(c, p, key_of(n + lane / kTiles) + 16 * (lane % kTiles)), 0), p.kvh); };
+  // at a time); where there is none, those of page 0 are read, and zeros put in their place if bit n of `without` says so
+  auto heads_at = [&](int n, uint64_t& without) { return head_at<D>(c, p, key_of(n + lane / kTiles) + 16 * (lane % kTiles), without); };
   int64_t heads = 0, next_heads = 0;
+  uint64_t without = 0, next_without = 0;
   const uint32_t code_at = Quarter<D>::code_place(l16, g), scale_at = Quarter<D>::scale_place(l16, g);
   Quarter<D> k[kTiles], v[kTiles];
   auto load = [&](int n, const uint16_t* from, Quarter<D> (&to)[kTiles]) {
@@ -482,7 +503,7 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
     for (int t = 0; t < kTiles; ++t)
       to[t].load(c, head_in(from, heads, kTiles * (n % kAtOnce) + t), (key_of(n) + 16 * t) & ((1 << c.page_shift) - 1), code_at, scale_at);
   };
-  if (mine_n > 0) heads = heads_at(0);
+  if (mine_n > 0) heads = heads_at(0, without);
   Part pr[R];
   x8 qf[R][kParts];
   float slope[R];
@@ -520,8 +541,21 @@ __device__ __forceinline__ void narrow_part(const CacheAttnArgs& a, const Entry&
     for (int db = 0; db < D / 16; ++db) acc[i][db] = f32x4_t{};
   QuarterSoftmax sm[R];
   for (int n = 0; n < mine_n; ++n) {
-    if (n % kAtOnce == kAtOnce / 2) next_heads = heads_at(n + kAtOnce / 2);
-    if (n % kAtOnce == kAtOnce - 1) heads = next_heads;
+    const uint32_t zeros = static_cast<uint32_t>(without >> kTiles * (n % kAtOnce));
+    if (n % kAtOnce == kAtOnce / 2) next_heads = heads_at(n + kAtOnce / 2, next_without);
+    if (n % kAtOnce == kAtOnce - 1) {
+      heads = next_heads;
+      without = next_without;
+    }
+    if (zeros & ((1u << kTiles) - 1)) {
+      asm volatile("");  // (a branch: as selections, this would wait for the values here)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+        if (zeros >> t & 1) {
+          k[t].clear();
+          v[t].clear();
+        }
+    }
     f32x4_t tile[R][kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
@@ -683,9 +717,11 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
   const int row = lane & 15, quarter = lane >> 4;
   const int nb = (p.end - p.key0 + kCacheWideBlock - 1) / kCacheWideBlock;
   auto key_of = [&](int n) { return p.key0 + n * kCacheWideBlock; };
-  // lane n holds where the 16 keys n % 4 of block n / 4 have the head's rows of their page (16 blocks at a time)
-  auto heads_at = [&](int n) { return head_of<D>(c, max(page_of(c, p, key_of(n + lane / 4) + 16 * (lane % 4)), 0), p.kvh); };
-  int64_t heads = heads_at(0), next_heads = 0;
+  // lane n holds where the 16 keys n % 4 of block n / 4 have the head's rows of their page (16 blocks at a time; `without` as
+  // above)
+  auto heads_at = [&](int n, uint64_t& without) { return head_at<D>(c, p, key_of(n + lane / 4) + 16 * (lane % 4), without); };
+  uint64_t without, next_without = 0;
+  int64_t heads = heads_at(0, without), next_heads = 0;
   const int in_page = (1 << c.page_shift) - 1;
   const uint32_t v_at = Quarter<D>::code_place(row, quarter), v_scale_at = Quarter<D>::scale_place(row, quarter);
   Half<D> k[2];
@@ -720,8 +756,19 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
   RowSoftmax sm;
   const int to = (16 * wave + row) * 2 * D + 16 * ((quarter * (D / 32)) ^ swz<D>(row));
   for (int n = 0; n < nb; ++n) {
-    if ((n & 15) == 8) next_heads = heads_at(n + 8);
-    if ((n & 15) == 15) heads = next_heads;
+    const uint32_t zeros = static_cast<uint32_t>(without >> 4 * (n & 15));
+    if ((n & 15) == 8) next_heads = heads_at(n + 8, next_without);
+    if ((n & 15) == 15) {
+      heads = next_heads;
+      without = next_without;
+    }
+    if (zeros & 15) {
+      asm volatile("");  // (as above)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+        if (zeros >> (2 * kb + (l32 >> 4)) & 1) k[kb].clear();
+      if (zeros >> wave & 1) v.clear();
+    }
     unsigned char* vt = stage + (n & 1) * kTile;
     const int key = key_of(n) + 16 * wave + row;
     const float v_scale = key >= p.lo && key < p.end ? v.scale(v_scale_at) : 0.0f;
