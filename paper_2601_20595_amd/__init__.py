@@ -842,7 +842,7 @@ class PagedCache:
         self._cfg = csg_cache_cfg(n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
                                   dtype=DTYPES[dtype] if isinstance(dtype, str) else int(dtype), n_pages=n_pages,
                                   page_size=page_size, batch=batch, max_pages=max_pages)
-        csg_cache_attn_workspace(self._cfg, -1)  # checks the configuration
+        self._attn_workspace(self._cfg, -1)  # checks the configuration
         self._shape = n_heads, n_kv_heads, head_dim, _HEAD_TYPES[self._cfg.dtype]
         self._batch = batch
         self._pages = n_pages * n_kv_heads * page_size * self._row_bytes(head_dim), self._page_type()

@@ -181,7 +181,9 @@ csg_status check_cache(csg_cache_cfg* c) {
   return CSG_OK;
 }
 
-csg_status check_cache_attn(csg_cache_cfg* c) {
+int32_t task_cost(bool four) { return four ? csg::kCache4TaskCost : csg::kCacheTaskCost; }
+
+csg_status check_cache_attn(csg_cache_cfg* c, bool four) {
   CSG_CHECK(check_cache(c));
   CSG_CHECK(check_scores(&c->scale, c->softcap, c->head_dim));
   if (c->n_groups > c->batch) return fail(CSG_ERR_INVALID, "more groups than sequences");
@@ -193,7 +195,7 @@ csg_status check_cache_attn(csg_cache_cfg* c) {
   const int64_t tiles = csg::cache_max_tiles(c->n_heads, c->n_kv_heads, c->tokens, c->batch, c->n_groups);
   const int64_t tasks = tiles / 4 + c->batch + c->n_groups;
   const int64_t blocks = static_cast<int64_t>(c->max_pages) * c->page_size / csg::kCacheBlock + 1;
-  if (tasks > 0 && blocks + std::max(csg::kCacheTaskCost, csg::kCache4TaskCost) > 0x7fffffff / tasks)
+  if (tasks > 0 && blocks + task_cost(four) > 0x7fffffff / tasks)
     return fail(CSG_ERR_UNSUPPORTED, "max_pages pages for every sequence are too many keys for one launch");
   return CSG_OK;
 }
@@ -279,7 +281,7 @@ csg_status cache_append(hipError_t (*launch)(const csg::AppendArgs&, bool, int, 
 csg_status attn_workspace(const csg_cache_cfg* cfg, bool four, int device, size_t* bytes) {
   if (!cfg || !bytes) return fail(CSG_ERR_INVALID, "NULL argument");
   csg_cache_cfg c = *cfg;
-  CSG_CHECK(check_cache_attn(&c));
+  CSG_CHECK(check_cache_attn(&c, four));
   int32_t cus = kDefaultCus;
   if (device >= 0) CSG_CHECK(device_cus(device, &cus));
   *bytes = static_cast<size_t>(cache_workspace(c, (four ? std::max(csg::kCache4Few, csg::kCacheGroups) : csg::kCacheGroups) * cus));
@@ -293,7 +295,7 @@ csg_status cache_attn(hipError_t (*launch)(const csg::CacheAttnArgs&, bool, int,
                           size_t workspace_bytes, int32_t* status, int device, void* stream) {
   if (!cfg) return fail(CSG_ERR_INVALID, "cfg is NULL");
   csg_cache_cfg c = *cfg;
-  CSG_CHECK(check_cache_attn(&c));
+  CSG_CHECK(check_cache_attn(&c, four));
   if (c.tokens == 0 || c.batch == 0) return CSG_OK;
   if (!q || !k_pages || !v_pages || !q_ptr || !lens || !page_table || !o || !workspace ||
       (c.n_groups > 0 && (!group_ptr || !prefix)))
@@ -316,7 +318,7 @@ csg_status cache_attn(hipError_t (*launch)(const csg::CacheAttnArgs&, bool, int,
   a.n_groups = c.n_groups;
   a.head_workers = csg::cache_head_workers(groups, c.n_kv_heads);
   a.dies = 8 / std::gcd(8, c.n_kv_heads);
-  a.task_cost = four ? csg::kCache4TaskCost : csg::kCacheTaskCost;
+  a.task_cost = task_cost(four);
   a.min_run = four ? csg::cache4_min_run(c.tokens, c.n_heads, c.n_kv_heads, c.batch, c.n_groups) : csg::kCacheMinRun;
   a.max_parts = csg::cache_max_parts(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups, a.head_workers);
   a.max_tiles = csg::cache_max_tiles(c.n_heads, c.n_kv_heads, c.tokens, c.batch, c.n_groups);
