@@ -80,6 +80,7 @@ __global__ __launch_bounds__(kThreads) void fork_counts(PagesArgs a, int across)
   const Held now = parent_of(a, b, &parent);
   if (parent == b) return;
   const Held old = held(a, a.lens[b]);
+  if (old.bad && s0 == 0 && threadIdx.x == 0) tell(a.status, kCacheBadLength);  // (fork_rows looks at lengths that are kept)
   const int64_t row = static_cast<int64_t>(b) * a.max_pages;
   for (int s = s0 + static_cast<int>(threadIdx.x); s < min(s0 + kSlots, max(old.pages, now.pages)); s += kThreads) {
     if (s < old.pages) count(a, a.table[row + s], -1);

@@ -1,0 +1,66 @@
+"""The status bits of the page calls: every length, of sequences that stay, end, are taken over, grow and shrink alike."""
+import pytest
+
+from oracle import pages as op
+from test_gpu_pages import _moves, _Pool
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+N, PAGE, BATCH, WIDTH = 20, 16, 4, 3
+TABLE = [[0, 1, 2], [3, 4, 5], [6, 7, 8], [9, 10, 11]]
+LENS = [40, 33, 16, 0]  # entries held: 3, 3, 1, 0
+REFS = [1] * 7 + [0] * 13
+# (sequence, entry, page) that are put into the table, lengths that replace others, the bits of both
+TABLES = {
+    "as they should be": ([], {}, 0),
+    "behind the ends": ([(2, 1, 99), (2, 2, -5), (3, 0, 20)], {}, 0),
+    "too long": ([], {1: WIDTH * PAGE + 1}, 2),
+    "below zero": ([], {2: -1}, 2),
+}
+PARENTS = {"all stay": [0, 1, 2, 3], "all end": [-1, -1, -1, -1], "one ends": [0, -1, 2, 3], "another ends": [0, 1, -1, 3],
+           "taken over": [1, 1, 2, 2], "exchanged": [1, 2, 0, 3]}
+GROWTH = {"nothing": [0, 0, 0, 0], "a token": [1, 1, 1, 1], "fewer": [-3, -17, -1, 0], "all of it": [-40, -33, -16, 0],
+          "no room": [8, 15, 32, 48]}
+
+
+def _state(name):
+    changes, lens, bits = TABLES[name]
+    table = [list(r) for r in TABLE]
+    for b, s, p in changes:
+        table[b][s] = p
+    lens = [lens.get(b, x) for b, x in enumerate(LENS)]
+    rows, cut, _ = op.rows_of(table, lens, PAGE)
+    return table, lens, rows, cut, bits
+
+
+@pytest.mark.parametrize("parent", PARENTS)
+@pytest.mark.parametrize("name", TABLES)
+def test_fork(name, parent):
+    table, lens, rows, cut, bits = _state(name)
+    new, l1, r1, pages = op.fork(rows, cut, REFS, PARENTS[parent])
+    assert pages == bits & 1  # (of every sequence, whatever becomes of it)
+    got = _Pool(N, PAGE, BATCH, WIDTH).fork(table, lens, REFS, PARENTS[parent])
+    assert got == [op.table_of(new, WIDTH), l1, r1, bits]
+
+
+@pytest.mark.parametrize("free", [13, 1, 0])
+@pytest.mark.parametrize("grow", GROWTH)
+@pytest.mark.parametrize("name", TABLES)
+def test_extend(name, grow, free):
+    table, lens, rows, cut, bits = _state(name)
+    refs = REFS[:7] + [1] * (13 - free) + [0] * free
+    new, l1, r1, moves, more = op.extend(rows, cut, refs, GROWTH[grow], PAGE, WIDTH)
+    assert more & 1 == bits & 1
+    got = _Pool(N, PAGE, BATCH, WIDTH).extend(table, lens, refs, GROWTH[grow])
+    assert got == [op.table_of(new, WIDTH), l1, r1, _moves(moves, BATCH), [len(moves)], bits | more]
+
+
+@pytest.mark.parametrize("name", TABLES)
+def test_compact(name):
+    table, lens, rows, cut, bits = _state(name)
+    refs = REFS[:9] + [1] + REFS[10:]  # (page 9 moves)
+    new, r1, renamed, moves, pages = op.compact(rows, refs)
+    assert pages == bits & 1
+    got = _Pool(N, PAGE, BATCH, WIDTH).compact(table, lens, refs)
+    assert got == [op.table_of(new, WIDTH), r1, renamed, _moves(moves, N // 2), [len(moves)], bits | pages]
