@@ -19,17 +19,18 @@ def table_of(rows, width: int):
     return [list(r) + [-1] * (width - len(r)) for r in rows]
 
 
+def _bad_pages(rows, n):
+    return int(any(not 0 <= p < n for r in rows for p in r))
+
+
 def fork(rows, lens, refs, parent):
-    refs, status, n = list(refs), 0, len(refs)
+    refs, n = list(refs), len(refs)
+    status = _bad_pages(rows, n)
 
     def count(row, by):
-        bits = 0
         for p in row:
             if 0 <= p < n:
                 refs[p] += by
-            else:
-                bits = 1
-        return bits
 
     new, new_lens = [], []
     for b, p in enumerate(parent):
@@ -39,13 +40,14 @@ def fork(rows, lens, refs, parent):
         new.append(list(rows[p]) if p >= 0 else [])
         new_lens.append(lens[p] if p >= 0 else 0)
         if p != b:
-            status |= count(rows[b], -1) | count(new[b], 1)
+            count(rows[b], -1)
+            count(new[b], 1)
     return new, new_lens, refs, status
 
 
 def extend(rows, lens, refs, grow, page: int, width: int):
     free = [p for p, r in enumerate(refs) if r == 0]
-    after, moves, taken, status, out = list(refs), [], 0, 0, []
+    after, moves, taken, status, out = list(refs), [], 0, _bad_pages(rows, len(refs)), []
     lens = list(lens)
     for b, row in enumerate(rows):
         row = list(row)
@@ -75,8 +77,6 @@ def extend(rows, lens, refs, grow, page: int, width: int):
             for p in row[pages:]:
                 if 0 <= p < len(refs):
                     after[p] -= 1
-                else:
-                    status |= 1
             row = row[:pages] + mine[split:]
         out.append(row)
     return out, lens, after, moves, status

@@ -36,10 +36,7 @@ __device__ __forceinline__ Held held(const PagesArgs& a, int tokens) {
 
 __device__ __forceinline__ bool names_page(const PagesArgs& a, int p) { return p >= 0 && p < a.n_pages; }
 __device__ __forceinline__ void count(const PagesArgs& a, int p, int by) {
-  if (names_page(a, p))
-    atomicAdd(a.refs_out + p, by);
-  else
-    tell(a.status, kCacheBadPage);
+  if (names_page(a, p)) atomicAdd(a.refs_out + p, by);
 }
 
 // ---- fork ------------------------------------------------------------------------------------
@@ -66,7 +63,11 @@ __global__ __launch_bounds__(kThreads) void fork_rows(PagesArgs a, int row_block
   const Held h = parent_of(a, b, &parent);
   const int32_t* from = a.table + static_cast<int64_t>(max(parent, 0)) * a.max_pages;
   int32_t* to = a.table_out + static_cast<int64_t>(b) * a.max_pages;
-  for (int s = s0 + tid; s < min(s0 + kSlots, a.max_pages); s += kThreads) to[s] = s < h.pages ? from[s] : -1;
+  for (int s = s0 + tid; s < min(s0 + kSlots, a.max_pages); s += kThreads) {
+    const int p = s < h.pages ? from[s] : -1;
+    if (s < h.pages && !names_page(a, p)) tell(a.status, kCacheBadPage);
+    to[s] = p;
+  }
   if (s0 == 0 && tid == 0) {
     a.lens_out[b] = h.tokens;
     if (h.bad) tell(a.status, kCacheBadLength);
@@ -83,7 +84,11 @@ __global__ __launch_bounds__(kThreads) void fork_counts(PagesArgs a, int across)
   if (old.bad && s0 == 0 && threadIdx.x == 0) tell(a.status, kCacheBadLength);  // (fork_rows looks at lengths that are kept)
   const int64_t row = static_cast<int64_t>(b) * a.max_pages;
   for (int s = s0 + static_cast<int>(threadIdx.x); s < min(s0 + kSlots, max(old.pages, now.pages)); s += kThreads) {
-    if (s < old.pages) count(a, a.table[row + s], -1);
+    if (s < old.pages) {
+      const int p = a.table[row + s];
+      if (!names_page(a, p)) tell(a.status, kCacheBadPage);
+      count(a, p, -1);
+    }
     if (s < now.pages) count(a, a.table_out[row + s], 1);
   }
 }
@@ -288,6 +293,7 @@ __global__ __launch_bounds__(kThreads) void extend_rows(PagesArgs a, int across)
   const int64_t row = static_cast<int64_t>(b) * a.max_pages;
   for (int s = s0 + tid; s < min(s0 + kSlots, a.max_pages); s += kThreads) {
     const int old = s < g.before.pages ? a.table[row + s] : -1;
+    if (s < g.before.pages && !names_page(a, old)) tell(a.status, kCacheBadPage);
     int now = s < g.after.pages ? old : -1;
     if (s == last && g.split) {
       now = s_new[first - q0];

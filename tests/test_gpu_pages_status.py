@@ -1,4 +1,6 @@
-"""The status bits of the page calls: every length, of sequences that stay, end, are taken over, grow and shrink alike."""
+"""The status bits of the page calls: every entry that a sequence holds and every length, of sequences that stay, end,
+are taken over, grow and shrink alike."""
+import numpy as np
 import pytest
 
 from oracle import pages as op
@@ -15,7 +17,12 @@ REFS = [1] * 7 + [0] * 13
 TABLES = {
     "as they should be": ([], {}, 0),
     "behind the ends": ([(2, 1, 99), (2, 2, -5), (3, 0, 20)], {}, 0),
+    "the first entry": ([(0, 0, -1)], {}, 1),
+    "one in the middle": ([(1, 1, N)], {}, 1),
+    "the last, partly filled": ([(1, 2, 1 << 30)], {}, 1),
+    "the only one": ([(2, 0, -(1 << 31))], {}, 1),
     "too long": ([], {1: WIDTH * PAGE + 1}, 2),
+    "too long, and not its pages": ([(1, 0, 20)], {1: 1 << 30}, 3),
     "below zero": ([], {2: -1}, 2),
 }
 PARENTS = {"all stay": [0, 1, 2, 3], "all end": [-1, -1, -1, -1], "one ends": [0, -1, 2, 3], "another ends": [0, 1, -1, 3],
@@ -64,3 +71,18 @@ def test_compact(name):
     assert pages == bits & 1
     got = _Pool(N, PAGE, BATCH, WIDTH).compact(table, lens, refs)
     assert got == [op.table_of(new, WIDTH), r1, renamed, _moves(moves, N // 2), [len(moves)], bits | pages]
+
+
+@pytest.mark.parametrize("at", [0, 1023, 1024, 2000, 2499])
+def test_an_entry_far_in_a_row(at):
+    n, width = 3000, 2500
+    table = np.arange(width)[None].repeat(2, axis=0)
+    table[1, at] = n
+    lens, refs = [0, width * 16], [1] * width + [0] * 500
+    refs[at] = 0
+    pool = _Pool(n, 16, 2, width)
+    rows = op.rows_of(table.tolist(), lens, 16)[0]
+    new, l1, r1, bits = op.fork(rows, lens, refs, [0, 1])
+    assert pool.fork(table, lens, refs, [0, 1]) == [op.table_of(new, width), l1, r1, bits] and bits == 1
+    new, l1, r1, moves, bits = op.extend(rows, lens, refs, [0, 0], 16, width)
+    assert pool.extend(table, lens, refs, [0, 0]) == [op.table_of(new, width), l1, r1, _moves(moves, 2), [0], bits] and bits == 1
