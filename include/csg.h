@@ -634,7 +634,8 @@ csg_status csg_cache4_append(const csg_cache_cfg* cfg, void* k_pages, void* v_pa
  * [head_dim] of dtype, strides k_stride and v_stride): sequence b's last k_ptr[b+1] - k_ptr[b] tokens (int32
  * [batch + 1], ascending; with lens summed up, all of it) into rows k_ptr[b] .. k_ptr[b+1] - 1, as csg_doc_attn takes
  * them. Tokens without a page read zeros and set status; rows of no sequence are left as they are. k and v
- * may be parts of one tensor, and may not overlap each other or the pages. */
+ * may be parts of one tensor, and may not overlap each other or the pages (CSG_ERR_INVALID; of k and v with different
+ * strides only what meets the other's first row is found). */
 csg_status csg_cache4_read(const csg_cache_cfg* cfg, const void* k_pages, const void* v_pages,
                            const int32_t* k_ptr, const int32_t* lens, const int32_t* page_table, void* k,
                            void* v, int32_t* status, int device, void* stream);

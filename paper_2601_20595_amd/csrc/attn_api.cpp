@@ -238,6 +238,13 @@ bool all_aligned(std::initializer_list<const void*> list) {
   return true;
 }
 
+// Whether one of n rows of `row` bytes, `stride` bytes apart, has some of the `size` bytes at `other`.
+bool rows_meet(const void* rows, int64_t row, int64_t stride, int64_t n, const void* other, int64_t size) {
+  const int64_t at = static_cast<int64_t>(reinterpret_cast<uintptr_t>(other) - reinterpret_cast<uintptr_t>(rows));
+  const int64_t i = at < row ? 0 : (at - row) / stride + 1;  // the first row that does not end before it
+  return i < n && i * stride < at + size;
+}
+
 // The checks and the launch of both caches' append.
 csg_status cache_append(hipError_t (*launch)(const csg::AppendArgs&, bool, int, hipStream_t), const csg_cache_cfg* cfg, void* k_pages, void* v_pages, const void* k, const void* v, const void* q,
                             void* q_out, const int32_t* q_ptr, const int32_t* lens, const int32_t* page_table,
@@ -436,6 +443,14 @@ csg_status csg_cache4_read(const csg_cache_cfg* cfg, const void* k_pages, const 
   if (c.tokens == 0 || c.batch == 0) return CSG_OK;
   if (!k_pages || !v_pages || !k_ptr || !lens || !page_table || !k || !v) return fail(CSG_ERR_INVALID, "NULL buffer");
   if (!all_aligned({k_pages, v_pages, k, v})) return fail(CSG_ERR_INVALID, "buffers must be 16-byte aligned");
+  // (of rows with the same stride, two meet if any meets the other's first one; with different strides the first ones are looked at)
+  const int64_t row = 2 * k_row, ks = 2 * c.k_stride, vs = 2 * c.v_stride;
+  if (rows_meet(k, row, ks, c.tokens, v, row) || rows_meet(v, row, vs, c.tokens, k, row))
+    return fail(CSG_ERR_INVALID, "k and v may not overlap");
+  const int64_t pages = static_cast<int64_t>(c.n_pages) * c.n_kv_heads * c.page_size * csg::cache4_row_bytes(c.head_dim);
+  for (const void* p : {k_pages, v_pages})
+    if (rows_meet(k, row, ks, c.tokens, p, pages) || rows_meet(v, row, vs, c.tokens, p, pages))
+      return fail(CSG_ERR_INVALID, "k and v may not overlap the pages");
   int32_t cus = 0;
   CSG_CHECK(device_cus(device, &cus));
   DeviceGuard g(device);
