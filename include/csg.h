@@ -624,7 +624,8 @@ csg_status csg_cache_attn(const csg_cache_cfg* cfg, const void* q, const void* k
  * Arguments, layouts, errors, and what may be captured are those of the cache in 16 bits; q, k, v
  * and o are of dtype. */
 
-/* As csg_cache_append. Keys are rotated in 64 bits, rounded to dtype, then to 4 bits. */
+/* As csg_cache_append. Keys are rotated in 64 bits; what comes out is rounded to 32 bits, from there to dtype, and from
+ * there to 4 bits. */
 csg_status csg_cache4_append(const csg_cache_cfg* cfg, void* k_pages, void* v_pages, const void* k,
                              const void* v, const void* q, void* q_out, const int32_t* q_ptr,
                              const int32_t* lens, const int32_t* page_table, const double* inv_freq,

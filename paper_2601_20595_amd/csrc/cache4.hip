@@ -79,8 +79,10 @@ __device__ __forceinline__ int64_t head_of(const CacheArgs& c, int page, int kvh
 
 // ---- new tokens into the cache --------------------------------------------------------------
 // A workgroup per token, as in the cache of 16 bits; but keys are rotated in 64 bits (sines and cosines
-// once a token, 6 operations a pair and head), so that their rounding to T and from there to a
-// code, next to a border too, follows from the definition and not from the order of a kernel's operations. Eight
+// once a token, 6 operations a pair and head), so that what they are rounded to, next to a border too, does not depend on
+// the order of a kernel's operations: to 32 bits (which the conversions to T take), from there to T, and to a code. The
+// step through 32 bits is part of the definition: where it ends halfway between two numbers of T (one result in 2^16, f16:
+// 2^13), a single rounding may take the other one. Eight
 // lanes (D = 64: four) have a head; its rotated elements go through LDS, since a block's elements come from
 // pairs of two places, and two lanes quantise a block. 64 tokens of 32 query heads on 8 of 128 take 4.6 us, a chain of latencies;
 // 11322 of 64 on 8, 426 MB, 90 us, 4.7 TB/s (a large copy: 5.1).
