@@ -684,12 +684,13 @@ csg_status csg_pages_fork(const csg_pages_cfg* cfg, const int32_t* page_table, c
                           int32_t* status, int device, void* stream);
 
 /* Sequence b grows by grow[b] tokens (int32[batch]), or gives its last -grow[b] back. Where tokens are added behind a
- * last page that is partly filled and counted more than once, that page is replaced by a
- * free one and the pair (page, its copy) appended to moves (int32[batch][2], by sequence; *n_moves of them, int32; entries
- * behind are left as they were). Each page asked for, a sequence's copy before its new pages, sequences in
+ * last page that is partly filled and counted more than once (before the call: where all of its holders grow, each of them
+ * gets a copy), that page is replaced by a free one and the pair (page, its copy) appended to moves (int32[batch][2], by sequence;
+ * *n_moves of them, int32; entries behind are left as they were). Each page asked for, a sequence's copy before its new pages, sequences in
  * order, is the next lowest free one; pages given back in the same call are not free yet. The first sequence for which
  * there are not enough, and every later one that asks for pages, is left as it was (bit 2), as is one that would
- * outgrow its row (bit 1; what it asked for stays free). One that gives back more than it has is empty then (bit 1). */
+ * outgrow its row (bit 1; the pages that it asked for stay free, and no later one gets them in this call). One that gives
+ * back more than it has is empty then (bit 1). */
 csg_status csg_pages_extend(const csg_pages_cfg* cfg, const int32_t* page_table, const int32_t* lens, const int32_t* refs,
                             const int32_t* grow, int32_t* table_out, int32_t* lens_out, int32_t* refs_out, int32_t* moves,
                             int32_t* n_moves, void* workspace, size_t workspace_bytes, int32_t* status, int device,

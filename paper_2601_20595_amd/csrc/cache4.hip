@@ -308,7 +308,7 @@ __global__ __launch_bounds__(kThreads) void cache4_read(ReadArgs a) {
 // sequences of over 100000, 244 MB in 51 us and the join 7, 4.8 TB/s (with 32-row products and every key through LDS 134);
 // 64 sequences of up to 8000, 129 MB, 34 and 5, of which the plan, the first loads and the last parts' ends are 8. With few
 // keys by a chain of latencies, 7.7 us for 900 keys. Where 16 sequences' rows share up to 8192 keys by the beginnings and ends of
-// wide parts and their 26 MB of partial results (31 and 9); a wide block of 64 keys takes 2.3 us beside another workgroup's, 0.93 PFLOP/s.
+// wide parts and their 26 MB of partial results (30 and 9); a wide block of 64 keys takes 2.3 us beside another workgroup's, 0.93 PFLOP/s.
 
 // Combination of the four lanes of a row: lane ^ 16, then lane ^ 32, swapped as in max_halves.
 __device__ __forceinline__ float max_quarters(float x) {
@@ -320,7 +320,9 @@ __device__ __forceinline__ float sum_quarters(float x) {
   return sum_halves(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-// RowSoftmax for rows of four lanes, N / 4 tiles of 16 keys at a time. The reference moves where one of the row's lanes finds
+// RowSoftmax for rows of four lanes, N / 4 tiles of 16 keys at a time. Weights are rounded to T, which the products with the values take; their
+// sum is of 32 bits, before that rounding, so that the log-sum-exp has none of it (outputs of 64 sequences are off by 0.0021 of their
+// size in bf16, with weights of 32 bits by 0.0017). The reference moves where one of the row's lanes finds
 // its weights' sum beyond the limit: until then the lanes need not know each other's.
 struct QuarterSoftmax {
   float m = -__builtin_inff();
@@ -829,11 +831,12 @@ __device__ __forceinline__ void wide_part(const CacheAttnArgs& a, const Entry& x
 }
 
 // With few rows a sequence (few), the kernel has only the narrow parts of 16 rows, whose registers and LDS
-// let more workgroups onto a CU (64 sequences with two 41.2 us, three 38.9, four, which spill, 58); an entry of more rows
-// goes through its keys once for each 16 of them. Otherwise it has
+// let more workgroups onto a CU (64 sequences with two 41.6 us, three 39.7; four, which spilled when it was tried, 58); an entry of
+// more rows goes through its keys once for each 16 of them, which the runs' units do not count: one sequence of many rows among many of
+// few makes its workgroups the last (127 of 2000 keys and a part of 300 tokens on 8000 296 us, as two calls 69 and 71). Otherwise it has
 // parts for up to 16, up to 32 and up to 128 rows, that convert their keys once. With short_tasks, sequences are so many
-// that each wave may have runs of its own: of all tasks (few), or, beside groups, of the small ones (without groups calls of more rows
-// have no more than some).
+// that each wave may have runs of its own: of all tasks (few, if all of them are small), or, beside groups, of the small ones. A call of
+// more rows without groups has none.
 template <class T, int D, bool kPlain, bool few, bool short_tasks>
 __global__ __launch_bounds__(kThreads, few ? kCache4Few : kCacheGroups) void cache4_attn(CacheAttnArgs a) {
   __shared__ __attribute__((aligned(1024))) unsigned char stage[(few ? 2 : 4) * kCacheBlock * 4 * D];
